@@ -72,7 +72,10 @@ typedef enum {
 typedef enum {
   TGRAD_C64 = 0,   /* interleaved 2 x fp32 */
   TGRAD_C32H = 1,  /* interleaved 2 x IEEE fp16 */
-  TGRAD_C32B = 2   /* interleaved 2 x bfloat16 (general kernels only: no fp16 tensor-core fast path) */
+  TGRAD_C32B = 2,  /* interleaved 2 x bfloat16 (general kernels only: no fp16 tensor-core fast path) */
+  TGRAD_R32 = 3,   /* fp32; the real types are for the dense tensors and logits of the calls at the end of this file, */
+  TGRAD_R16H = 4,  /* IEEE fp16                                            not for the weight of a tgrad_state        */
+  TGRAD_R16B = 5   /* bfloat16 */
 } tgrad_dtype;
 
 #define TGRAD_MAX_NDIM 8
@@ -177,6 +180,14 @@ tgrad_status tgrad_init_state(const tgrad_config* cfg, void* d_persistent, size_
  * is 0. */
 tgrad_status tgrad_step(tgrad_state* st, void* d_weight, void* d_grad, void* cuda_stream);
 
+/* tgrad_step with the gradient multiplied by the device scalar *d_scale (NULL: 1), which the call's kernels read when
+ * they run: a clipping coefficient that an earlier call on the stream computes (tgrad_grad_norm) is applied without a
+ * pass over the gradient and without the host knowing it.  The compression is linear, so the factor is applied to the
+ * Tucker core and to the sparse values where Adam reads them; the selection of Omega and the factor matrices do not
+ * depend on a positive factor and are taken from the gradient as it is.  tgrad_export_state's CORE is that of the
+ * gradient as it is. */
+tgrad_status tgrad_step_scaled(tgrad_state* st, void* d_weight, void* d_grad, const float* d_scale, void* cuda_stream);
+
 /* The `t mod T = 0` branch of Algorithm 1 on the supplied gradient:
  * Omega <- magnitude top-k of grad (key = fp32 re*re + im*im without fused
  * multiply-add, ties to the lower flat index, stored ascending);
@@ -206,6 +217,9 @@ tgrad_status tgrad_refresh_subspace(tgrad_state* st, void* d_grad, void* cuda_st
  * and d_weights / d_grads must not overlap between tensors. */
 tgrad_status tgrad_step_batched(tgrad_state* const* states, void* const* d_weights, void* const* d_grads,
                                 int32_t n_tensors, void* cuda_stream);
+/* the same with one scale for all gradients, as in tgrad_step_scaled */
+tgrad_status tgrad_step_batched_scaled(tgrad_state* const* states, void* const* d_weights, void* const* d_grads,
+                                       int32_t n_tensors, const float* d_scale, void* cuda_stream);
 tgrad_status tgrad_refresh_subspace_batched(tgrad_state* const* states, void* const* d_grads, int32_t n_tensors,
                                             void* cuda_stream);
 
@@ -294,6 +308,132 @@ int64_t tgrad_launch_count(void);
 #define TGRAD_NUM_STAGES 5
 tgrad_status tgrad_set_stage_timing(tgrad_state* st, int32_t enable);
 tgrad_status tgrad_get_stage_times(tgrad_state* st, void* cuda_stream, float* ms_sum, int32_t* n_steps);
+
+/* ---------------------------------------------------------------------------
+ * What a training loop computes between a model's logits and the step above.
+ *
+ * The calls below keep nothing between calls and hold no state: lists of
+ * tensors are HOST arrays that travel with the launch, results and workspaces
+ * are device memory of the caller (256-byte aligned workspaces, whose contents
+ * need not survive and which two calls that may overlap must not share).
+ * Everything is enqueued on the stream, nothing synchronises, every sum has a
+ * fixed order (the same inputs give the same bits), and all arithmetic is in
+ * fp32 or wider with one rounding to the storage type at the end.
+ * Pointers need the alignment of their element type only. */
+
+typedef struct {
+  void* d_data;        /* numel entries, contiguous in memory (in any order of the dimensions) */
+  int64_t numel;       /* entries (complex ones for the complex types); 0 is allowed            */
+  int32_t dtype;       /* tgrad_dtype, complex or real                                          */
+  int32_t reserved;
+} tgrad_tensor;
+
+/* Gradient norm over a list of tensors: d_out[2 + i] = n_i = sqrt(sum |g|^2) of tensor i, d_out[0] = sqrt(sum n_i^2),
+ * d_out[1] = min(1, max_norm / (d_out[0] + 1e-6)), the coefficient that brings the global norm down to max_norm (1 for
+ * max_norm = infinity).  d_out holds 2 + n floats.  Magnitudes far from 1 are summed without overflow or underflow.
+ * A NaN or infinity in the list gives a norm of NaN or infinity and the coefficient that follows from the formula (NaN
+ * or 0); the caller that wants to skip such a step reads d_out[0]. */
+tgrad_status tgrad_grad_norm_bytes(int32_t n, size_t* workspace_bytes);
+tgrad_status tgrad_grad_norm(const tgrad_tensor* grads, int32_t n, float max_norm, float* d_out, void* d_workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+/* The same, and every gradient multiplied by d_out[1] in place.  Tensors of the list must not overlap. */
+tgrad_status tgrad_clip_grads(const tgrad_tensor* grads, int32_t n, float max_norm, float* d_out, void* d_workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
+/* AdamW on a list of dense tensors (those without a Tucker structure: biases, norms, embeddings): with the gradient g
+ * multiplied by *d_grad_scale first,
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) |g|^2,
+ *   w <- (1 - lr weight_decay) w - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * dtype: TGRAD_R32, TGRAD_R16H, TGRAD_R16B or TGRAD_C64, of weight and gradient.  m is fp32 (complex64 for TGRAD_C64), v
+ * fp32 with one entry per weight: for complex weights |g|^2 is the squared modulus, as in Algorithm 1.  16-bit weights
+ * may have fp32 master weights, which are then what is updated; the 16-bit ones receive their rounded values. */
+typedef struct {
+  void* d_weight;
+  const void* d_grad;
+  void* d_exp_avg;       /* m */
+  float* d_exp_avg_sq;   /* v */
+  float* d_master;       /* fp32 weights, or NULL */
+  int64_t numel;
+  int32_t dtype;
+  int32_t reserved;
+} tgrad_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;               /* counts from 1 */
+  const float* d_grad_scale;  /* device scalar, or NULL (1) */
+} tgrad_adamw_config;
+tgrad_status tgrad_adamw_step(const tgrad_adamw_tensor* list, int32_t n, const tgrad_adamw_config* config, void* cuda_stream);
+
+/* Rows of logits with one target each.  With z = logits / temperature of a row, p = softmax(z):
+ *   lse = log sum exp z,  logp = z[target] - lse,  entropy = -sum p log p.
+ * A row whose target is negative is ignored: its logits are not read, its outputs and its gradient are 0.  A target
+ * >= vocab gives NaN.  Logits of -infinity have p = 0 and gradient 0; a row of nothing else has no distribution (NaN).
+ * rows < 2^28 and vocab <= 2^30. */
+typedef struct {
+  const void* d_logits;
+  int64_t rows, vocab;
+  int64_t row_stride;        /* entries from one row to the next, >= vocab */
+  const int64_t* d_targets;  /* rows */
+  int32_t dtype;             /* TGRAD_R32, TGRAD_R16H or TGRAD_R16B */
+  float temperature;         /* > 0 */
+} tgrad_logits;
+
+/* Each output (rows fp32) may be NULL. */
+tgrad_status tgrad_token_logprob(const tgrad_logits* logits, float* d_logp, float* d_lse, float* d_entropy, void* cuda_stream);
+/* d_dlogits (dtype of the logits) = gradient of sum(grad_logp logp + grad_entropy entropy) with respect to the logits.
+ * d_lse and d_entropy are those of the forward call; d_grad_entropy may be NULL (and d_entropy with it).
+ * Here and below d_dlogits may be d_logits itself, with the same stride. */
+tgrad_status tgrad_token_logprob_backward(const tgrad_logits* logits, const float* d_lse, const float* d_entropy,
+                                          const float* d_grad_logp, const float* d_grad_entropy, void* d_dlogits,
+                                          int64_t dlogits_stride, void* cuda_stream);
+
+/* Clipped policy loss, forward and backward.  With r = exp(logp - old_logp) and A the advantage of a row's token,
+ *   policy  = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *   kl      = exp(ref_logp - logp) - (ref_logp - logp) - 1      (0 without ref_logp)
+ *   loss    = sum over the rows of weight (policy + kl_coef kl - entropy_coef entropy).
+ * The weights carry the mask and the normalisation (1 / tokens for a mean).  Where the clipped term is the smaller one
+ * no gradient flows through the ratio; at a tie it does.
+ * d_stats[5] = loss and the weighted sums of policy, kl, entropy and of the rows that were clipped.
+ * d_dlogits = grad_scale * d loss / d logits; NULL: forward only.  d_logp and d_entropy (rows) may be NULL. */
+typedef struct {
+  const float* d_old_logp;
+  const float* d_ref_logp;     /* or NULL */
+  const float* d_advantages;
+  const float* d_weights;
+  float clip_low, clip_high, kl_coef, entropy_coef;
+  float grad_scale;            /* factor of the gradient (loss scaling) */
+  float reserved;
+  float* d_stats;
+  float* d_logp;
+  float* d_entropy;
+  void* d_dlogits;
+  int64_t dlogits_stride;
+} tgrad_policy_args;
+tgrad_status tgrad_policy_loss_bytes(int64_t rows, size_t* workspace_bytes);
+tgrad_status tgrad_policy_loss(const tgrad_logits* logits, const tgrad_policy_args* args, void* d_workspace,
+                               size_t workspace_bytes, void* cuda_stream);
+
+/* Loss on pairs of answers, forward and backward.  Answer s has the rows [starts[s], starts[s + 1]), answers 2 b and
+ * 2 b + 1 are the chosen and the rejected one of pair b (rows of prompts have a negative target):
+ *   rewards[s] = beta * sum over its rows of (logp - ref_logp),  h = rewards[2 b] - rewards[2 b + 1],
+ *   loss = mean over the pairs of -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h).
+ * starts is read on the device; rows outside every answer take no part.  An answer may be empty, and no pairs give a
+ * loss of 0.  d_dlogits as above, NULL: forward only. */
+typedef struct {
+  const int32_t* d_starts;     /* 2 * pairs + 1, not decreasing */
+  const float* d_ref_logp;     /* rows */
+  int32_t pairs;
+  float beta, label_smoothing;
+  float grad_scale;
+  float* d_loss;
+  float* d_rewards;            /* 2 * pairs */
+  float* d_logp;               /* rows */
+  void* d_dlogits;
+  int64_t dlogits_stride;
+} tgrad_preference_args;
+tgrad_status tgrad_preference_loss_bytes(int64_t rows, int32_t pairs, size_t* workspace_bytes);
+tgrad_status tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference_args* args, void* d_workspace,
+                                   size_t workspace_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

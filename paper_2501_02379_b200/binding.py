@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -22,7 +22,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_BUFFER_TOO_SMALL, ERR_CUDA, ERR_NO_CON
 ERR_TOO_LARGE = 8
 NOALLOC_MAX_NUMEL = 1 << 26
 FLAG_NO_CONVERGE, FLAG_NONFINITE, FLAG_COPY_TIMEOUT = 1, 2, 4
-C64, C32H, C32B = 0, 1, 2
+C64, C32H, C32B, R32, R16H, R16B = range(6)
 COMPOSITIONS = {"us_lr": 0, "lr_us": 1, "sum": 2}
 STRATEGIES = {"topk": 0, "randk": 1, "probk": 2}
 WHAT_OMEGA, WHAT_M_L, WHAT_V_L, WHAT_M_S, WHAT_V_S, WHAT_CORE, WHAT_N_L, WHAT_N_S = 1, 2, 3, 4, 5, 6, 7, 8
@@ -51,6 +51,38 @@ class TgradConfig(C.Structure):
     ]
 
 
+class TgradTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("numel", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class TgradAdamwTensor(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("master", C.c_void_p), ("numel", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class TgradAdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("grad_scale", C.c_void_p)]
+
+
+class TgradLogits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64),
+                ("targets", C.c_void_p), ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class TgradPolicyArgs(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("ref_logp", C.c_void_p), ("advantages", C.c_void_p), ("weights", C.c_void_p),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("entropy_coef", C.c_float),
+                ("grad_scale", C.c_float), ("reserved", C.c_float), ("stats", C.c_void_p), ("logp", C.c_void_p),
+                ("entropy", C.c_void_p), ("dlogits", C.c_void_p), ("dlogits_stride", C.c_int64)]
+
+
+class TgradPreferenceArgs(C.Structure):
+    _fields_ = [("starts", C.c_void_p), ("ref_logp", C.c_void_p), ("pairs", C.c_int32), ("beta", C.c_float),
+                ("label_smoothing", C.c_float), ("grad_scale", C.c_float), ("loss", C.c_void_p), ("rewards", C.c_void_p),
+                ("logp", C.c_void_p), ("dlogits", C.c_void_p), ("dlogits_stride", C.c_int64)]
+
+
 class TgradError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -64,6 +96,9 @@ EXPORTS = [
     "tgrad_refresh_subspace_batched", "tgrad_query_status", "tgrad_export_state", "tgrad_import_state",
     "tgrad_set_step", "tgrad_destroy_state", "tgrad_status_string", "tgrad_launch_count",
     "tgrad_set_stage_timing", "tgrad_get_stage_times", "tgrad_select_topk_noalloc", "tgrad_diagnostics",
+    "tgrad_step_scaled", "tgrad_step_batched_scaled", "tgrad_grad_norm_bytes", "tgrad_grad_norm", "tgrad_clip_grads",
+    "tgrad_adamw_step", "tgrad_token_logprob", "tgrad_token_logprob_backward", "tgrad_policy_loss_bytes",
+    "tgrad_policy_loss", "tgrad_preference_loss_bytes", "tgrad_preference_loss",
 ]
 
 
@@ -96,6 +131,18 @@ def lib() -> C.CDLL:
         l.tgrad_get_stage_times.argtypes = [vp, vp, C.POINTER(C.c_float), C.POINTER(C.c_int32)]
         l.tgrad_select_topk_noalloc.argtypes = [vp, C.c_int64, C.c_int64, C.c_int32, vp, vp, vp]
         l.tgrad_diagnostics.argtypes = [vp, vp, vp, C.POINTER(C.c_double)]
+        l.tgrad_step_scaled.argtypes = [vp, vp, vp, vp, vp]
+        l.tgrad_step_batched_scaled.argtypes = [C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.c_int32, vp, vp]
+        l.tgrad_grad_norm_bytes.argtypes = [C.c_int32, C.POINTER(sz)]
+        l.tgrad_grad_norm.argtypes = [vp, C.c_int32, C.c_float, vp, vp, sz, vp]
+        l.tgrad_clip_grads.argtypes = [vp, C.c_int32, C.c_float, vp, vp, sz, vp]
+        l.tgrad_adamw_step.argtypes = [vp, C.c_int32, vp, vp]
+        l.tgrad_token_logprob.argtypes = [vp, vp, vp, vp, vp]
+        l.tgrad_token_logprob_backward.argtypes = [vp, vp, vp, vp, vp, vp, C.c_int64, vp]
+        l.tgrad_policy_loss_bytes.argtypes = [C.c_int64, C.POINTER(sz)]
+        l.tgrad_policy_loss.argtypes = [vp, vp, vp, sz, vp]
+        l.tgrad_preference_loss_bytes.argtypes = [C.c_int64, C.c_int32, C.POINTER(sz)]
+        l.tgrad_preference_loss.argtypes = [vp, vp, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("tgrad_status_string", "tgrad_launch_count"):
                 getattr(l, name).restype = C.c_int
@@ -160,6 +207,15 @@ def _stream_ptr(stream) -> Optional[int]:
     return int(stream)
 
 
+def _scalar_ptr(scale) -> Optional[int]:
+    if scale is None:
+        return None
+    import torch
+    if scale.dtype != torch.float32 or scale.numel() != 1 or not scale.is_cuda:
+        raise ValueError("a scale is an fp32 CUDA tensor of one entry")
+    return scale.data_ptr()
+
+
 class TgradState:
     """One optimizer state (one weight tensor).  Device blocks are torch uint8
     tensors owned by this object; the library only borrows them."""
@@ -193,6 +249,12 @@ class TgradState:
     # --- the hot path -------------------------------------------------------------
     def step(self, weight, grad, stream=None):
         _check(lib().tgrad_step(self.handle, weight.data_ptr(), grad.data_ptr(), _stream_ptr(stream)), "tgrad_step")
+
+    def step_scaled(self, weight, grad, scale, stream=None):
+        """step() with the gradient multiplied by the device scalar `scale` (an fp32 tensor of one entry, such as the
+        clipping coefficient grad_norm(...)[1:2]); costs no pass over the gradient."""
+        _check(lib().tgrad_step_scaled(self.handle, weight.data_ptr(), grad.data_ptr(), _scalar_ptr(scale), _stream_ptr(stream)),
+               "tgrad_step_scaled")
 
     def refresh_subspace(self, grad, stream=None):
         _check(lib().tgrad_refresh_subspace(self.handle, grad.data_ptr(), _stream_ptr(stream)),
@@ -263,11 +325,15 @@ class TgradState:
         return [float(ms[i]) for i in range(NUM_STAGES)], int(n.value)
 
 
-def step_batched(states: Sequence[TgradState], weights, grads, stream=None):
+def step_batched(states: Sequence[TgradState], weights, grads, stream=None, scale=None):
+    """`scale`: device scalar that multiplies every gradient, as in TgradState.step_scaled."""
     n = len(states)
     hs = (C.c_void_p * n)(*[s.handle for s in states])
     ws = (C.c_void_p * n)(*[w.data_ptr() for w in weights])
     gs = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
+    if scale is not None:
+        _check(lib().tgrad_step_batched_scaled(hs, ws, gs, n, _scalar_ptr(scale), _stream_ptr(stream)), "tgrad_step_batched_scaled")
+        return
     _check(lib().tgrad_step_batched(hs, ws, gs, n, _stream_ptr(stream)), "tgrad_step_batched")
 
 
@@ -287,3 +353,284 @@ def select_topk_noalloc(grad, numel: int, k: int, omega_out, values_out, half_st
     _check(lib().tgrad_select_topk_noalloc(grad.data_ptr(), int(numel), int(k), C32H if half_storage else C64,
                                            omega_out.data_ptr() if k else None, values_out.data_ptr() if k else None,
                                            _stream_ptr(stream)), "tgrad_select_topk_noalloc")
+
+
+# --- around the step: gradient norm and clipping, AdamW, losses on logits ------------------------------------------
+#
+# Everything below runs on the current stream of the tensors' device, or on `stream` (a torch stream or its address).
+# Results and workspaces that a call allocates belong to that stream.
+
+def _dtype_of(t) -> int:
+    import torch
+    d = {torch.float32: R32, torch.float16: R16H, torch.bfloat16: R16B, torch.complex64: C64}.get(t.dtype)
+    if d is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return d
+
+
+def _dense(t) -> bool:
+    """Every entry of the storage range belongs to the tensor once: contiguous in some order of the dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+class _on_stream:
+    """Context: allocations and calls on `stream` of the tensors' device; enters as the stream's address."""
+
+    def __init__(self, device, stream):
+        import torch
+        self._ctx = []
+        if device.index != torch.cuda.current_device():
+            self._ctx.append(torch.cuda.device(device))
+        if stream is not None:
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            self._ctx.append(torch.cuda.stream(stream))
+        self._device = device.index
+
+    def __enter__(self):
+        import torch
+        for c in self._ctx:
+            c.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self._device)
+
+    def __exit__(self, *exc):
+        for c in reversed(self._ctx):
+            c.__exit__(*exc)
+
+
+class TensorList:
+    """A list of CUDA tensors as the list calls take it, laid out once for tensors that stay where they are (it keeps
+    them alive).  Every call that takes one also takes a plain sequence of tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        for t in self.tensors:
+            if not t.is_cuda or t.device != self.tensors[0].device:
+                raise ValueError("the tensors of a list live on one CUDA device")
+            if t.is_conj() or t.is_neg():
+                raise ValueError("resolve lazy conjugations first")
+            if not _dense(t):
+                raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not dense in memory")
+        n = len(self.tensors)
+        self.array = (TgradTensor * max(n, 1))()
+        for a, t in zip(self.array, self.tensors):
+            a.data, a.numel, a.dtype = t.data_ptr(), t.numel(), _dtype_of(t)
+        b = C.c_size_t(0)
+        _check(lib().tgrad_grad_norm_bytes(n, C.byref(b)), "tgrad_grad_norm_bytes")
+        self.workspace_bytes = int(b.value)
+        self._adamw = None
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def device(self):
+        import torch
+        return self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
+
+
+def _as_list(x) -> TensorList:
+    return x if isinstance(x, TensorList) else TensorList(x)
+
+
+def _norm_call(name, grads, max_norm, stream):
+    import torch
+    grads = _as_list(grads)
+    device = grads.device()
+    with _on_stream(device, stream) as st:
+        out = torch.empty(2 + len(grads), dtype=torch.float32, device=device)
+        ws = torch.empty(grads.workspace_bytes, dtype=torch.uint8, device=device)
+        _check(getattr(lib(), name)(C.addressof(grads.array), len(grads), max_norm, out.data_ptr(), ws.data_ptr(), grads.workspace_bytes, st), name)
+    return out
+
+
+def grad_norm(grads, max_norm: float = float("inf"), stream=None):
+    """Gradient norm over a list of tensors (fp32, fp16, bfloat16, complex64): an fp32 tensor [global norm, clipping
+    coefficient min(1, max_norm / (norm + 1e-6)), norm of each tensor...] on the device.  Entry 1 as [1:2] is what
+    step_scaled, step_batched and adamw_step take as a scale."""
+    return _norm_call("tgrad_grad_norm", grads, max_norm, stream)
+
+
+def clip_grads(grads, max_norm: float, stream=None):
+    """grad_norm, and every gradient multiplied by the coefficient in place."""
+    return _norm_call("tgrad_clip_grads", grads, max_norm, stream)
+
+
+def _adamw_array(params, grads, exp_avgs, exp_avg_sqs, masters):
+    import torch
+    lists = [params, grads, exp_avgs, exp_avg_sqs] + ([masters] if masters is not None else [])
+    if len({len(x) for x in lists}) != 1:
+        raise ValueError("the lists differ in length")
+    if any(x.device() != params.device() for x in lists):
+        raise ValueError("the lists live on one device")
+    array = (TgradAdamwTensor * max(len(params), 1))()
+    for i, a in enumerate(array[:len(params)]):
+        p, g, m, v = (x.tensors[i] for x in (params, grads, exp_avgs, exp_avg_sqs))
+        w = masters.tensors[i] if masters is not None else None
+        if g.dtype != p.dtype or v.dtype != torch.float32 or m.dtype != (torch.complex64 if p.is_complex() else torch.float32):
+            raise ValueError("gradients have the weights' dtype, moments are fp32 (the first one complex64 for complex weights)")
+        if w is not None and (w.dtype != torch.float32 or p.dtype not in (torch.float16, torch.bfloat16)):
+            raise ValueError("master weights are the fp32 weights of 16-bit ones")
+        for x in (g, m, v) + ((w,) if w is not None else ()):
+            if x.shape != p.shape or x.stride() != p.stride():
+                raise ValueError("weight, gradient and moments have the same shape and strides")
+    for i in range(len(params)):
+        a, p = array[i], params.tensors[i]
+        a.weight, a.grad, a.exp_avg, a.exp_avg_sq = (x.tensors[i].data_ptr() for x in (params, grads, exp_avgs, exp_avg_sqs))
+        a.master = masters.tensors[i].data_ptr() if masters is not None else None
+        a.numel, a.dtype = p.numel(), _dtype_of(p)
+    return array
+
+
+def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+               eps: float = 1e-8, weight_decay: float = 0.0, grad_scale=None, masters=None, stream=None):
+    """One AdamW step in place on a list of dense tensors (fp32, fp16, bfloat16 or complex64 weights; gradients of the
+    same dtype; fp32 moments).  `step` counts from 1.  `grad_scale`: device scalar that multiplies the gradients.
+    `masters`: fp32 weights of 16-bit ones, which are then what is updated.  For complex weights the second moment is
+    real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once."""
+    lists = [_as_list(params), _as_list(grads), _as_list(exp_avgs), _as_list(exp_avg_sqs), _as_list(masters) if masters is not None else None]
+    kept = lists[0]._adamw
+    if kept is None or any(a is not b for a, b in zip(kept[0], lists[1:])):
+        kept = lists[0]._adamw = (lists[1:], _adamw_array(*lists))
+    cfg = TgradAdamwConfig(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale))
+    with _on_stream(lists[0].device(), stream) as st:
+        _check(lib().tgrad_adamw_step(C.addressof(kept[1]), len(lists[0]), C.addressof(cfg), st), "tgrad_adamw_step")
+
+
+def _logits(logits, targets, temperature):
+    """The logits' description for the library; checks what the library cannot see."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits are a CUDA tensor [rows, vocabulary]")
+    rows, vocab = logits.shape
+    d = _dtype_of(logits)
+    if d == C64:
+        raise ValueError("logits are real")
+    if vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("the entries of a row of logits are adjacent")
+    if targets.dtype != torch.int64 or targets.shape != (rows,) or targets.device != logits.device or not targets.is_contiguous():
+        raise ValueError("targets are a contiguous int64 tensor [rows] on the logits' device")
+    stride = logits.stride(0) if rows > 1 else vocab
+    return TgradLogits(logits.data_ptr(), rows, vocab, stride, targets.data_ptr(), d, temperature)
+
+
+def _rows_f32(logits, **tensors):
+    import torch
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.float32 or t.shape != logits.shape[:1] or t.device != logits.device or not t.is_contiguous()):
+            raise ValueError(f"{name} is a contiguous fp32 tensor [rows] on the logits' device")
+
+
+def _dlogits(logits, out):
+    """The gradient's tensor: `out` after a check, or a new one whose rows lie like those of the logits, so that both
+    are accessed 16 bytes at a time."""
+    import torch
+    rows, vocab = logits.shape
+    if out is None:
+        stride = logits.stride(0) if rows > 1 else vocab
+        if not vocab <= stride <= vocab + 128:
+            stride = vocab
+        lead = (logits.data_ptr() & 15) // logits.element_size()
+        out = torch.empty(rows * stride + lead, dtype=logits.dtype, device=logits.device)
+        return out.as_strided((rows, vocab), (stride, 1), lead), stride
+    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (vocab > 1 and out.stride(1) != 1):
+        raise ValueError("dlogits has the logits' shape, dtype and device, and the entries of a row are adjacent")
+    return out, out.stride(0) if rows > 1 else vocab
+
+
+def token_logprob(logits, targets, temperature: float = 1.0, stream=None):
+    """(logp, lse, entropy), each fp32 [rows], of softmax(logits / temperature): log-probability of the row's target,
+    log-sum-exp and entropy.  Rows with a negative target are ignored (0, and their logits are not read)."""
+    import torch
+    desc = _logits(logits, targets, temperature)
+    with _on_stream(logits.device, stream) as st:
+        out = torch.empty(3, logits.shape[0], dtype=torch.float32, device=logits.device)
+        logp, lse, entropy = out.unbind(0)
+        _check(lib().tgrad_token_logprob(C.addressof(desc), logp.data_ptr(), lse.data_ptr(), entropy.data_ptr(), st), "tgrad_token_logprob")
+    return logp, lse, entropy
+
+
+def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_entropy=None, temperature: float = 1.0, dlogits=None, stream=None):
+    """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits.  `dlogits` may be the
+    logits themselves."""
+    desc = _logits(logits, targets, temperature)
+    if grad_entropy is not None and entropy is None:
+        raise ValueError("grad_entropy needs the entropy of the forward call")
+    _rows_f32(logits, lse=lse, grad_logp=grad_logp, entropy=entropy, grad_entropy=grad_entropy)
+    with _on_stream(logits.device, stream) as st:
+        out, stride = _dlogits(logits, dlogits)
+        _check(lib().tgrad_token_logprob_backward(C.addressof(desc), lse.data_ptr(), entropy.data_ptr() if grad_entropy is not None else None,
+                                                  grad_logp.data_ptr(), grad_entropy.data_ptr() if grad_entropy is not None else None,
+                                                  out.data_ptr(), stride, st), "tgrad_token_logprob_backward")
+    return out
+
+
+class PolicyLoss(NamedTuple):
+    stats: "torch.Tensor"       # loss, and the weighted sums of the policy term, KL, entropy and clipped rows
+    logp: "torch.Tensor"
+    entropy: "torch.Tensor"
+    dlogits: Optional["torch.Tensor"]
+
+
+class PreferenceLoss(NamedTuple):
+    loss: "torch.Tensor"        # scalar
+    rewards: "torch.Tensor"     # beta * sum (logp - ref_logp) of each answer
+    logp: "torch.Tensor"
+    dlogits: Optional["torch.Tensor"]
+
+
+def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2,
+                kl_coef: float = 0.0, entropy_coef: float = 0.0, temperature: float = 1.0, grad_scale: float = 1.0,
+                dlogits=None, forward_only: bool = False, stream=None) -> PolicyLoss:
+    """Clipped policy loss with a KL term and an entropy bonus, and its gradient with respect to the logits in the same
+    pass: loss = sum_i weights_i (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(u) - u - 1)
+    - entropy_coef H), r = exp(logp - old_logp), u = ref_logp - logp.  The weights carry mask and normalisation; rows
+    with a negative target are ignored.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
+    `dlogits` may be the logits themselves."""
+    import torch
+    desc = _logits(logits, targets, temperature)
+    _rows_f32(logits, old_logp=old_logp, advantages=advantages, weights=weights, ref_logp=ref_logp)
+    rows = logits.shape[0]
+    b = C.c_size_t(0)
+    _check(lib().tgrad_policy_loss_bytes(rows, C.byref(b)), "tgrad_policy_loss_bytes")
+    with _on_stream(logits.device, stream) as st:
+        grad, stride = (None, 0) if forward_only else _dlogits(logits, dlogits)
+        out = torch.empty(8 + 2 * rows, dtype=torch.float32, device=logits.device)
+        ws = torch.empty(b.value, dtype=torch.uint8, device=logits.device)
+        base = out.data_ptr()
+        args = TgradPolicyArgs(old_logp.data_ptr(), ref_logp.data_ptr() if ref_logp is not None else None, advantages.data_ptr(),
+                               weights.data_ptr(), clip_low, clip_high, kl_coef, entropy_coef, grad_scale, 0.0, base, base + 32,
+                               base + 32 + 4 * rows, grad.data_ptr() if grad is not None else None, stride)
+        _check(lib().tgrad_policy_loss(C.addressof(desc), C.addressof(args), ws.data_ptr(), b.value, st), "tgrad_policy_loss")
+    return PolicyLoss(out[:5], out[8:8 + rows], out[8 + rows:], grad)
+
+
+def preference_loss(logits, targets, starts, ref_logp, beta: float = 0.1, label_smoothing: float = 0.0, temperature: float = 1.0,
+                    grad_scale: float = 1.0, dlogits=None, forward_only: bool = False, stream=None) -> PreferenceLoss:
+    """Loss on pairs of answers and its gradient with respect to the logits.  `starts`: int32 device tensor of
+    2 * pairs + 1 row numbers, answers 2 b and 2 b + 1 are the chosen and the rejected one of pair b; rows of prompts
+    have a negative target.  rewards_s = beta * sum (logp - ref_logp), h = rewards_chosen - rewards_rejected, loss = mean of
+    -(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h)."""
+    import torch
+    desc = _logits(logits, targets, temperature)
+    _rows_f32(logits, ref_logp=ref_logp)
+    if starts.dtype != torch.int32 or starts.dim() != 1 or starts.numel() % 2 != 1 or starts.device != logits.device or not starts.is_contiguous():
+        raise ValueError("starts is a contiguous int32 tensor of 2 * pairs + 1 entries on the logits' device")
+    rows, pairs = logits.shape[0], starts.numel() // 2
+    b = C.c_size_t(0)
+    _check(lib().tgrad_preference_loss_bytes(rows, pairs, C.byref(b)), "tgrad_preference_loss_bytes")
+    with _on_stream(logits.device, stream) as st:
+        grad, stride = (None, 0) if forward_only else _dlogits(logits, dlogits)
+        out = torch.empty(4 + rows + 2 * pairs, dtype=torch.float32, device=logits.device)
+        ws = torch.empty(b.value, dtype=torch.uint8, device=logits.device)
+        base = out.data_ptr()
+        args = TgradPreferenceArgs(starts.data_ptr(), ref_logp.data_ptr(), pairs, beta, label_smoothing, grad_scale, base,
+                                   base + 16 + 4 * rows, base + 16, grad.data_ptr() if grad is not None else None, stride)
+        _check(lib().tgrad_preference_loss(C.addressof(desc), C.addressof(args), ws.data_ptr(), b.value, st), "tgrad_preference_loss")
+    return PreferenceLoss(out[0], out[4 + rows:], out[4:4 + rows], grad)

@@ -22,11 +22,14 @@ struct AdamScalars {
   float beta1, beta2, omb1, omb2;   // decay rates and (1 - beta)
   float inv_c1, inv_c2;             // 1 / (1 - beta^(t+1))
   float eps;
+  const float* gscale;              // device scalar the compressed gradient is multiplied by, or null (1)
 };
 
 // One Adam update in the compressed space (AdamUpdate of Algorithm 1; |x conj(x)|
-// for the second moment).  Returns the normalised update N.
+// for the second moment).  Returns the normalised update N.  The compression is linear, so scaling the compressed
+// values (gradient clipping) is scaling the gradient, without a pass over it.
 __device__ __forceinline__ cf adam_apply(cf x, cf& m, float& v, const AdamScalars& a) {
+  if (a.gscale) { const float c = *a.gscale; x.x *= c; x.y *= c; }
   m.x = a.beta1 * m.x + a.omb1 * x.x;
   m.y = a.beta1 * m.y + a.omb1 * x.y;
   v = a.beta2 * v + a.omb2 * (x.x * x.x + x.y * x.y);

@@ -13,6 +13,7 @@
 #include "gram.cuh"
 #include "gram_tc.cuh"
 #include "jacobi.cuh"
+#include "launch.cuh"
 #include "modeprod.cuh"
 #include "select.cuh"
 #include "subspace.cuh"
@@ -22,9 +23,9 @@
 
 using namespace tg;
 
-namespace {
+namespace tg { std::atomic<int64_t> g_launches{0}; }
 
-std::atomic<int64_t> g_launches{0};
+namespace {
 
 constexpr int kStages = 5;   // proj_tail, proj_chain, adam_core, back_chain, back_tail
 constexpr int kTimingRing = 64;
@@ -293,24 +294,6 @@ struct tgrad_state {
 
 namespace {
 
-#define TG_LAUNCH_CHECK()                                  \
-  do {                                                     \
-    g_launches.fetch_add(1, std::memory_order_relaxed);    \
-    if (cudaPeekAtLastError() != cudaSuccess) return TGRAD_ERR_CUDA; \
-  } while (0)
-
-// Launch of a kernel of the step: programmatic dependent launch, so that its blocks are scheduled while the
-// previous kernel of the stream drains (every such kernel begins with griddep_chain()).
-template <typename... KA, typename... AA>
-inline void launch_chained(void (*kern)(KA...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, AA&&... args) {
-  cudaLaunchConfig_t lc; memset(&lc, 0, sizeof(lc));
-  lc.gridDim = grid; lc.blockDim = block; lc.dynamicSmemBytes = smem; lc.stream = st;
-  cudaLaunchAttribute at; memset(&at, 0, sizeof(at));
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization; at.val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = &at; lc.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&lc, kern, static_cast<KA>(args)...);     // an error stays pending for TG_LAUNCH_CHECK
-}
-
 // op: 0 = set attributes, 1 = proj, 2 = back
 template <class S>
 tgrad_status tail_dispatch(int op, const TailPlan& tp, void* ptr, const TailParams& p, cudaStream_t st) {
@@ -503,6 +486,7 @@ AdamScalars adam_scalars(const tgrad_config& c, int64_t t) {
   float c2 = (float)(1.0 - std::pow((double)c.beta2, (double)(t + 1)));
   a.inv_c1 = 1.0f / c1; a.inv_c2 = 1.0f / c2;
   a.eps = c.eps;
+  a.gscale = nullptr;
   return a;
 }
 
@@ -1124,7 +1108,7 @@ tgrad_status mode_product(bool conj_t, const cf* in, cf* out, const cf* U, uint6
 
 #define TG_MARK(i) do { if (evs) cudaEventRecord(evs[i], st); } while (0)
 
-tgrad_status do_step(tgrad_state* s, void* d_weight, void* d_grad, cudaStream_t st) {
+tgrad_status do_step(tgrad_state* s, void* d_weight, void* d_grad, const float* d_scale, cudaStream_t st) {
   const tgrad_config& c = s->cfg;
   const Layout& L = s->L;
   const int N = c.ndim;
@@ -1134,6 +1118,7 @@ tgrad_status do_step(tgrad_state* s, void* d_weight, void* d_grad, cudaStream_t 
 
   TailParams p = tail_params(s);
   p.adam = adam_scalars(c, s->t);
+  p.adam.gscale = d_scale;
   p.keep = c.composition != 0;          // only Algorithm 1's order feeds the low-rank part with the sparse part's residual
   cf* bufa = reinterpret_cast<cf*>(s->dw + L.w_bufa);
   cf* core = reinterpret_cast<cf*>(s->dw + L.w_core);
@@ -1306,9 +1291,13 @@ tgrad_status tgrad_init_state(const tgrad_config* cfg, void* d_persistent, size_
 }
 
 tgrad_status tgrad_step(tgrad_state* st, void* d_weight, void* d_grad, void* cuda_stream) {
+  return tgrad_step_scaled(st, d_weight, d_grad, nullptr, cuda_stream);
+}
+
+tgrad_status tgrad_step_scaled(tgrad_state* st, void* d_weight, void* d_grad, const float* d_scale, void* cuda_stream) {
   if (!st || !d_weight || !d_grad) return TGRAD_ERR_INVALID_ARG;
-  if (!aligned16(d_weight) || !aligned16(d_grad)) return TGRAD_ERR_INVALID_ARG;
-  return do_step(st, d_weight, d_grad, static_cast<cudaStream_t>(cuda_stream));
+  if (!aligned16(d_weight) || !aligned16(d_grad) || (reinterpret_cast<uintptr_t>(d_scale) & 3)) return TGRAD_ERR_INVALID_ARG;
+  return do_step(st, d_weight, d_grad, d_scale, static_cast<cudaStream_t>(cuda_stream));
 }
 
 tgrad_status tgrad_refresh_subspace(tgrad_state* st, void* d_grad, void* cuda_stream) {
@@ -1319,6 +1308,12 @@ tgrad_status tgrad_refresh_subspace(tgrad_state* st, void* d_grad, void* cuda_st
 
 tgrad_status tgrad_step_batched(tgrad_state* const* states, void* const* d_weights, void* const* d_grads,
                                 int32_t n_tensors, void* cuda_stream) {
+  return tgrad_step_batched_scaled(states, d_weights, d_grads, n_tensors, nullptr, cuda_stream);
+}
+
+tgrad_status tgrad_step_batched_scaled(tgrad_state* const* states, void* const* d_weights, void* const* d_grads,
+                                       int32_t n_tensors, const float* d_scale, void* cuda_stream) {
+  if (reinterpret_cast<uintptr_t>(d_scale) & 3) return TGRAD_ERR_INVALID_ARG;
   if (n_tensors < 0 || (n_tensors > 0 && (!states || !d_weights || !d_grads))) return TGRAD_ERR_INVALID_ARG;
   for (int i = 0; i < n_tensors; ++i) {
     if (!states[i] || !d_weights[i] || !d_grads[i]) return TGRAD_ERR_INVALID_ARG;
@@ -1332,7 +1327,7 @@ tgrad_status tgrad_step_batched(tgrad_state* const* states, void* const* d_weigh
   // enqueued on the caller's stream before this call happens before all of it, work enqueued after it happens after.
   BatchStreams* bs = (n_tensors > 1) ? batch_streams() : nullptr;
   if (!bs) {
-    for (int i = 0; i < n_tensors; ++i) TG_TRY(do_step(states[i], d_weights[i], d_grads[i], user));
+    for (int i = 0; i < n_tensors; ++i) TG_TRY(do_step(states[i], d_weights[i], d_grads[i], d_scale, user));
     return TGRAD_OK;
   }
   std::lock_guard<std::mutex> lock(bs->mu);
@@ -1341,7 +1336,7 @@ tgrad_status tgrad_step_batched(tgrad_state* const* states, void* const* d_weigh
   for (int j = 0; j < lanes; ++j)
     if (cudaStreamWaitEvent(bs->side[j], bs->fork, 0) != cudaSuccess) return TGRAD_ERR_CUDA;
   tgrad_status result = TGRAD_OK;
-  for (int i = 0; i < n_tensors && result == TGRAD_OK; ++i) result = do_step(states[i], d_weights[i], d_grads[i], bs->side[i % lanes]);
+  for (int i = 0; i < n_tensors && result == TGRAD_OK; ++i) result = do_step(states[i], d_weights[i], d_grads[i], d_scale, bs->side[i % lanes]);
   for (int j = 0; j < lanes; ++j) {           // join even after an error, so that nothing is left running unordered
     if (cudaEventRecord(bs->join[j], bs->side[j]) != cudaSuccess || cudaStreamWaitEvent(user, bs->join[j], 0) != cudaSuccess)
       return TGRAD_ERR_CUDA;

@@ -1,0 +1,563 @@
+// Kernels over rows of logits: log-probability of one token per row, its entropy and gradients; a clipped policy loss
+// and a loss on pairs of answers, each with its gradient with respect to the logits.
+//
+// With z = logits / tau, M the row's largest logit, k = log2(e) / tau and d_j = (logit_j - M) k (so p_j = 2^d_j / S):
+//   S = sum 2^d_j,  T = sum 2^d_j d_j;   lse = M / tau + ln S,   log p_j = ln2 (d_j - log2 S),
+//   H = -sum p ln p = ln2 (log2 S - T / S),
+//   d(g log p_y + h H) / d logit_j = (g 1[j = y] - p_j (g + h H + h ln p_j)) / tau.
+// All three sums are held as (M, S, T) triples that combine associatively, so a row is read once, in any split.
+// d_j is formed from the difference, not as logit k - M k: the difference of 16-bit values is exact or nearly so, and
+// nothing overflows on rows whose entries are all the type's lowest value.
+//
+// Rows whose target is negative are ignored: their logits are not read (they may hold anything) and their gradient is
+// zero.  A target beyond the vocabulary gives NaN.
+#pragma once
+#include "lists.cuh"
+
+namespace tg {
+
+struct TokenArgs {
+  const char* z;         // logits
+  char* dz;              // gradient, or null
+  int64_t ldz, lddz;     // entries between rows
+  const long long* y;    // targets
+  int V;
+  float k, inv_tau;      // log2(e) / tau, 1 / tau
+};
+
+constexpr float TK_LN2 = 0.6931471805599453f;
+constexpr float TK_LOWEST = -3.402823466e38f;
+
+// ---- packed pairs of fp32 (one instruction per two lanes on this architecture) ----
+__device__ __forceinline__ uint64_t pk2(float a, float b) {
+  uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r;
+}
+__device__ __forceinline__ float2 upk2(uint64_t v) {
+  float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+
+// ---- granules: the 16 bytes of storage that a thread handles at a time ----
+template <int KIND> struct Gran { static constexpr int E = KIND == LS_F32 ? 4 : 8, B = KIND == LS_F32 ? 4 : 2; };
+template <int KIND> __device__ __forceinline__ uint32_t neg_inf_word() {
+  return KIND == LS_F32 ? 0xff800000u : (KIND == LS_F16 ? 0xfc00fc00u : 0xff80ff80u);
+}
+// the pair q of a granule's entries (16-bit storage: q = 0..3, fp32: q = 0..1)
+template <int KIND>
+__device__ __forceinline__ float2 gpair(const uint4& v, int q) {
+  if (KIND == LS_F32) return q == 0 ? make_float2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+  return widen2<KIND>(q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w);
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {     // larger entries of two words; a NaN loses
+  if (KIND == LS_F32) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  if (KIND == LS_F16) { const __half2 r = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b)); return *reinterpret_cast<const uint32_t*>(&r); }
+  const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <int KIND>
+__device__ __forceinline__ float max_of_word(uint32_t a) {
+  if (KIND == LS_F32) return __uint_as_float(a);
+  const float2 x = widen2<KIND>(a);
+  return fmaxf(x.x, x.y);
+}
+
+// A row seen as granules: `mis` entries lie before it in its first granule.
+template <int KIND>
+struct Row {
+  const char* base;      // 16-byte aligned address of the first granule
+  int mis, V;
+  __device__ __forceinline__ Row(const char* p, int V_) {
+    const uint32_t o = (uint32_t)((uintptr_t)p & 15);
+    base = p - o; mis = (int)(o / Gran<KIND>::B); V = V_;
+  }
+  __device__ __forceinline__ int granules() const { return (mis + V + Gran<KIND>::E - 1) / Gran<KIND>::E; }
+  __device__ __forceinline__ bool whole(int g) const {          // all of granule g belongs to the row
+    return (g > 0 || mis == 0) && (g + 1) * Gran<KIND>::E <= mis + V;
+  }
+  // an outer granule: entries outside the row read as -inf
+  __device__ __noinline__ uint4 partial(int g) const {
+    uint32_t w[4];
+    for (int q = 0; q < 4; ++q) w[q] = neg_inf_word<KIND>();
+    for (int i = 0; i < Gran<KIND>::E; ++i) {
+      const int j = g * Gran<KIND>::E + i - mis;
+      if (j < 0 || j >= V) continue;
+      const char* p = base + ((int64_t)j + mis) * Gran<KIND>::B;
+      if (KIND == LS_F32) w[i] = *reinterpret_cast<const uint32_t*>(p);
+      else {
+        const uint32_t h = *reinterpret_cast<const unsigned short*>(p);
+        w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xffffu) | (h << 16) : (w[i >> 1] & 0xffff0000u) | h;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ uint4 load(int g) const {
+    if (whole(g)) return ld_stream(reinterpret_cast<const uint4*>(base) + g);
+    return partial(g);
+  }
+};
+
+// ---- (M, S, T) ----
+struct Triple { float m, s, t; };
+// Moves a triple to a larger maximum.  A part that has seen nothing but -inf has m = lowest, s = t = 0 and stays so.
+__device__ __forceinline__ void rebase(Triple& a, float m, float k) {
+  const float d = fmaxf((a.m - m) * k, -1e30f);
+  const float f = ex2(d);
+  a.t = f * fmaf(a.s, d, a.t);
+  a.s *= f;
+  a.m = m;
+}
+// adds a batch of granules whose maximum is not above a.m
+template <int KIND, int NV>
+__device__ __forceinline__ void accumulate(Triple& a, const uint4 (&v)[NV], float k) {
+  const uint64_t nm = pk2(-a.m, -a.m), kk = pk2(k, k);
+  uint64_t s2 = pk2(0.f, 0.f), t2 = s2;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int q = 0; q < Gran<KIND>::E / 2; ++q) {
+      const float2 x = gpair<KIND>(v[i], q);
+      const float2 d = upk2(mul2(add2(pk2(x.x, x.y), nm), kk));
+      const uint64_t e = pk2(ex2(d.x), ex2(d.y));
+      s2 = add2(s2, e);
+      t2 = fma2(e, pk2(max_nan(d.x, -200.f), max_nan(d.y, -200.f)), t2);   // 0 * -inf is not wanted
+    }
+  const float2 s = upk2(s2), t = upk2(t2);
+  a.s += s.x + s.y;
+  a.t += t.x + t.y;
+}
+template <int KIND, int NV>
+__device__ __forceinline__ float batch_max(const uint4 (&v)[NV]) {
+  uint32_t m = v[0].x;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    m = max_word<KIND>(m, v[i].x); m = max_word<KIND>(m, v[i].y);
+    m = max_word<KIND>(m, v[i].z); m = max_word<KIND>(m, v[i].w);
+  }
+  return fmaxf(max_of_word<KIND>(m), TK_LOWEST);      // also for a batch of NaN
+}
+__device__ __forceinline__ void warp_combine(Triple& a, float k) {
+  float m = a.m;
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  rebase(a, m, k);
+  for (int o = 16; o; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+  }
+}
+
+// ---- cluster of blocks that share a row ----
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_map(const void* smem, uint32_t rank) {
+  uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(smem)), "r"(rank)); return r;
+}
+__device__ __forceinline__ void cluster_st4(uint32_t addr, float a, float b, float c, float d) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
+
+constexpr int TK_MAX_CLUSTER = 8;
+
+// Combines the triples of all threads of the C blocks that share a row; the result is in every thread.  Each warp
+// leaves its triple in the shared memory of each block, one barrier (over the cluster) follows, and each warp combines
+// all of them, so that no second exchange is needed.  The caller has passed the cluster's start (cluster_wait after
+// cluster_arrive_relaxed) where C > 1; nobody touches another block's memory after the barrier.
+template <int THREADS>
+__device__ __forceinline__ void row_combine(Triple& a, float k, int C, float4* sh) {
+  constexpr int W = THREADS / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  warp_combine(a, k);
+  if (C == 1) {
+    if (W == 1) return;
+    if (lane == 0) sh[warp] = make_float4(a.m, a.s, a.t, 0.f);
+    __syncthreads();
+  } else {
+    const int slot = (int)cluster_rank() * W + warp;
+    if (lane < C) cluster_st4(cluster_map(sh + slot, (uint32_t)lane), a.m, a.s, a.t, 0.f);
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
+  a.m = TK_LOWEST; a.s = a.t = 0.f;
+  for (int i = lane; i < C * W; i += 32) {
+    const float4 o = sh[i];
+    Triple b; b.m = o.x; b.s = o.y; b.t = o.z;
+    const float m = fmaxf(a.m, b.m);
+    rebase(a, m, k); rebase(b, m, k);
+    a.s += b.s; a.t += b.t;
+  }
+  warp_combine(a, k);
+}
+
+// What the sums say about one row.
+struct RowStat { float M, ls2, lse, logp, H; };
+__device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, float inv_tau) {
+  RowStat r;
+  r.M = a.m;
+  const float ls = logf(a.s);
+  r.ls2 = ls * 1.4426950408889634f;
+  r.lse = fmaf(a.m, inv_tau, ls);
+  r.logp = fmaf(zy - a.m, inv_tau, -ls);
+  r.H = fmaf(-TK_LN2, a.t / a.s, ls);
+  return r;
+}
+template <int KIND>
+__device__ __forceinline__ float target_logit(const TokenArgs& p, int64_t row, long long y) {
+  if (y >= p.V) return __int_as_float(0x7fc00000);      // NaN: reported, not read
+  return ld_real<KIND>(p.z + (row * p.ldz + y) * Gran<KIND>::B);
+}
+
+// ---- gradient ----
+// p_j (c0 + c1 L_j) with L_j = log2 p_j: c0 = -(g + h H) / tau, c1 = -h ln2 / tau, all times the loss scale.
+struct GradCoef { float M, k, ls2, c0, c1; };
+template <int KIND, bool ENT>
+__device__ __forceinline__ uint4 grad_granule(const uint4& v, const GradCoef& gc) {
+  const uint64_t nm = pk2(-gc.M, -gc.M), kk = pk2(gc.k, gc.k), nl = pk2(-gc.ls2, -gc.ls2), c0 = pk2(gc.c0, gc.c0), c1 = pk2(gc.c1, gc.c1);
+  uint32_t w[4];
+#pragma unroll
+  for (int q = 0; q < Gran<KIND>::E / 2; ++q) {
+    const float2 x = gpair<KIND>(v, q);
+    const uint64_t L = fma2(add2(pk2(x.x, x.y), nm), kk, nl);
+    const float2 l = upk2(L);
+    uint64_t c = c0;
+    if (ENT) c = fma2(pk2(max_nan(l.x, -200.f), max_nan(l.y, -200.f)), c1, c0);
+    const float2 d = upk2(mul2(pk2(ex2(l.x), ex2(l.y)), c));
+    if (KIND == LS_F32) { w[2 * q] = __float_as_uint(d.x); w[2 * q + 1] = __float_as_uint(d.y); }
+    else w[q] = narrow2<KIND>(d.x, d.y);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int KIND, bool ENT>
+__device__ __forceinline__ float grad_target(float zy, const GradCoef& gc, float g) {
+  const float l = fmaf(zy - gc.M, gc.k, -gc.ls2);
+  const float c = ENT ? fmaf(max_nan(l, -200.f), gc.c1, gc.c0) : gc.c0;
+  return fmaf(ex2(l), c, g);
+}
+// entry i of a granule
+template <int KIND>
+__device__ __forceinline__ void st_entry(char* p, const uint4& v, int i) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (KIND == LS_F32) *reinterpret_cast<uint32_t*>(p) = w[i];
+  else *reinterpret_cast<unsigned short*>(p) = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
+}
+// Stores granule g of the row's gradient.  `same`: gradient row and logits row lie alike relative to 16 bytes.
+template <int KIND>
+__device__ __noinline__ void store_entries(char* drow, int mis, int V, int g, uint4 v) {
+#pragma unroll
+  for (int i = 0; i < Gran<KIND>::E; ++i) {
+    const int j = g * Gran<KIND>::E + i - mis;
+    if (j >= 0 && j < V) st_entry<KIND>(drow + (int64_t)j * Gran<KIND>::B, v, i);
+  }
+}
+template <int KIND>
+__device__ __forceinline__ void store_granule(const Row<KIND>& r, char* drow, bool same, int g, const uint4& v) {
+  if (same && r.whole(g)) st_stream(reinterpret_cast<uint4*>(drow - r.mis * Gran<KIND>::B) + g, v);
+  else store_entries<KIND>(drow, r.mis, r.V, g, v);
+}
+template <int KIND>
+__device__ __forceinline__ bool same_alignment(const Row<KIND>& r, const char* drow) {
+  return (int)((uintptr_t)drow & 15) == r.mis * Gran<KIND>::B;
+}
+
+// ---- clipped policy loss of one token ----
+struct PolicyArgs {
+  const float* old_logp; const float* ref_logp; const float* adv; const float* weight;   // ref_logp may be null
+  float low, high;           // bounds of the ratio
+  float kl_coef, ent_coef, grad_scale;
+  float* logp; float* entropy;             // out, may be null
+  float4* terms;                           // out: weighted policy, KL, entropy and clipping terms of each row
+};
+struct PolicyToken { float g, h; float4 terms; };
+// r = exp(logp - old); the loss -min(r A, clip(r) A) has gradient -r A where the unclipped term is the smaller one or
+// they are equal, and none elsewhere; kl = exp(u) - u - 1 with u = ref - logp has gradient 1 - exp(u).
+__device__ __forceinline__ PolicyToken policy_token(float logp, float H, float old, float ref, bool has_ref, float A, float w, const PolicyArgs& q) {
+  PolicyToken o;
+  const float r = expf(logp - old);
+  const float free = r * A, bound = fminf(fmaxf(r, q.low), q.high) * A;
+  const bool cut = free > bound;
+  const float pg = cut ? -bound : -free;
+  float kl = 0.f, dkl = 0.f;
+  if (has_ref) { const float u = ref - logp, em = expm1f(u); kl = em - u; dkl = -em; }
+  o.g = w * ((cut ? 0.f : -free) + q.kl_coef * dkl);
+  o.h = -q.ent_coef * w;
+  o.terms = make_float4(w * pg, w * kl, w * H, cut ? w : 0.f);
+  return o;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Policy loss, forward and backward in one pass: the row stays in the registers of the C blocks that share it (16-byte
+// granules, NV per thread), so the logits are read once and the gradient written once.
+template <int KIND, int THREADS, bool ENT>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int C) {
+  constexpr int NV = 8;
+  __shared__ float4 sh[TK_MAX_CLUSTER * (THREADS / 32)];
+  if (C > 1) cluster_arrive_relaxed();
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t row = blockIdx.x / C;
+  const int rank = C > 1 ? (int)cluster_rank() : 0;
+  const long long y = p.y[row];
+  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
+  char* drow = p.dz + row * p.lddz * Gran<KIND>::B;
+  const bool same = same_alignment(r, drow);
+  const int G = r.granules(), per = (G + C - 1) / C, g0 = rank * per, g1 = min(G, g0 + per);
+  if (C > 1) cluster_wait();
+  if (y < 0) {
+    for (int g = g0 + threadIdx.x; g < g1; g += THREADS) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+    if (rank == 0 && threadIdx.x == 0) {
+      if (q.logp) q.logp[row] = 0.f;
+      if (q.entropy) q.entropy[row] = 0.f;
+      q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    return;
+  }
+  uint4 v[NV];
+  const uint32_t ni = neg_inf_word<KIND>();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int g = g0 + (int)threadIdx.x + i * THREADS;
+    v[i] = make_uint4(ni, ni, ni, ni);
+    if (g < g1) v[i] = r.load(g);
+  }
+  const float zy = target_logit<KIND>(p, row, y);
+  const float old = q.old_logp[row], A = q.adv[row], w = q.weight[row], ref = q.ref_logp ? q.ref_logp[row] : 0.f;
+  Triple a;
+  a.m = batch_max<KIND, NV>(v); a.s = a.t = 0.f;
+  accumulate<KIND, NV>(a, v, p.k);
+  row_combine<THREADS>(a, p.k, C, sh);
+  const RowStat st = row_stat(a, zy, p.inv_tau);
+  const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, A, w, q);
+  if (rank == 0 && threadIdx.x == 0) {
+    if (q.logp) q.logp[row] = st.logp;
+    if (q.entropy) q.entropy[row] = st.H;
+    q.terms[row] = o.terms;
+  }
+  const float sc = q.grad_scale * p.inv_tau;
+  GradCoef gc; gc.M = st.M; gc.k = p.k; gc.ls2 = st.ls2;
+  gc.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; gc.c1 = -o.h * TK_LN2 * sc;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int g = g0 + (int)threadIdx.x + i * THREADS;
+    if (g < g1) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+  }
+  // the target's entry once more, by the thread that wrote its granule
+  const int gy = y < p.V ? (r.mis + (int)y) / Gran<KIND>::E : -1;
+  if (gy >= g0 && gy < g1 && (gy - g0) % THREADS == (int)threadIdx.x)
+    st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
+}
+
+// Deterministic sum of the rows' terms by one block: stats = loss, policy, KL, entropy, clipped weight.
+__global__ void __launch_bounds__(1024) policy_sum_kernel(const float4* __restrict__ terms, int64_t rows, float kl_coef, float ent_coef, float* __restrict__ stats) {
+  __shared__ double sh[4][32];
+  griddep_wait();
+  griddep_launch_dependents();
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int64_t i = threadIdx.x; i < rows; i += 4096) {
+    float4 t[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) t[u] = i + 1024 * u < rows ? terms[i + 1024 * u] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) { s[0] += t[u].x; s[1] += t[u].y; s[2] += t[u].z; s[3] += t[u].w; }
+  }
+  for (int c = 0; c < 4; ++c) {
+    for (int o = 16; o; o >>= 1) s[c] += __shfl_xor_sync(0xffffffffu, s[c], o);
+    if ((threadIdx.x & 31) == 0) sh[c][threadIdx.x >> 5] = s[c];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double t[4];
+    for (int c = 0; c < 4; ++c) { t[c] = 0.0; for (int w = 0; w < 32; ++w) t[c] += sh[c][w]; }
+    stats[0] = (float)(t[0] + (double)kl_coef * t[1] - (double)ent_coef * t[2]);
+    for (int c = 0; c < 4; ++c) stats[1 + c] = (float)t[c];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Forward pass over a row that is not kept: C blocks stream it with running triples.
+struct ForwardArgs {
+  float* logp; float* lse; float* entropy;      // out, may be null
+  float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
+  float4* coef;                                 // policy: out (M, log2 S, g, g + h H ...), see below
+};
+constexpr int TF_THREADS = 256;
+// POLICY: the rows' loss terms and gradient coefficients too (rows that are too long to be kept in registers).
+template <int KIND, bool POLICY>
+__global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ ForwardArgs f,
+                                                                      const __grid_constant__ PolicyArgs q, int C) {
+  constexpr int NV = 4;
+  __shared__ float4 sh[TK_MAX_CLUSTER * (TF_THREADS / 32)];
+  if (C > 1) cluster_arrive_relaxed();
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t row = blockIdx.x / C;
+  const int rank = C > 1 ? (int)cluster_rank() : 0;
+  const long long y = p.y[row];
+  if (C > 1) cluster_wait();
+  if (y < 0) {
+    if (rank == 0 && threadIdx.x == 0) {
+      if (f.logp) f.logp[row] = 0.f;
+      if (f.lse) f.lse[row] = 0.f;
+      if (f.entropy) f.entropy[row] = 0.f;
+      if (f.stat) f.stat[row] = make_float2(0.f, 0.f);
+      if (POLICY) { f.coef[row] = make_float4(0.f, 0.f, 0.f, 0.f); q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    }
+    return;
+  }
+  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
+  const int G = r.granules(), per = (G + C - 1) / C, g0 = rank * per, g1 = min(G, g0 + per);
+  const float zy = target_logit<KIND>(p, row, y);
+  const uint32_t ni = neg_inf_word<KIND>();
+  Triple a; a.m = TK_LOWEST; a.s = a.t = 0.f;
+  for (int gb = g0 + (int)threadIdx.x; gb < g1; gb += NV * TF_THREADS) {
+    uint4 v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int g = gb + i * TF_THREADS;
+      v[i] = make_uint4(ni, ni, ni, ni);
+      if (g < g1) v[i] = r.load(g);
+    }
+    rebase(a, fmaxf(a.m, batch_max<KIND, NV>(v)), p.k);
+    accumulate<KIND, NV>(a, v, p.k);
+  }
+  row_combine<TF_THREADS>(a, p.k, C, sh);
+  if (rank != 0 || threadIdx.x != 0) return;
+  const RowStat st = row_stat(a, zy, p.inv_tau);
+  if (f.logp) f.logp[row] = st.logp;
+  if (f.lse) f.lse[row] = st.lse;
+  if (f.entropy) f.entropy[row] = st.H;
+  if (f.stat) f.stat[row] = make_float2(st.M, st.ls2);
+  if (POLICY) {
+    const PolicyToken o = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q);
+    q.terms[row] = o.terms;
+    f.stat[row] = make_float2(st.M, st.ls2);
+    f.coef[row] = make_float4(o.g, o.h, st.H, 0.f);
+  }
+}
+
+// Gradient pass: one block per piece of NV * THREADS granules of a row.
+struct BackwardArgs {
+  const float* lse;          // of the forward call, or
+  const float2* stat;        // (M, log2 S), more exact where lse is large
+  const float* g;            // d loss / d logp
+  const float* h;            // d loss / d entropy, or null
+  const float* entropy;      // with h
+  const float4* coef;        // (g, h, H, -) instead of the three
+  float scale;
+};
+constexpr int TB2_THREADS = 256;
+template <int KIND, bool ENT>
+__global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, uint32_t pieces) {
+  constexpr int NV = 4;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t row = blockIdx.x / pieces;
+  const int piece = (int)(blockIdx.x - (uint32_t)row * pieces);
+  const long long y = p.y[row];
+  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
+  char* drow = p.dz + row * p.lddz * Gran<KIND>::B;
+  const bool same = same_alignment(r, drow);
+  const int G = r.granules(), g0 = piece * NV * TB2_THREADS, g1 = min(G, g0 + NV * TB2_THREADS);
+  if (g0 >= g1) return;
+  if (y < 0) {
+    for (int g = g0 + threadIdx.x; g < g1; g += TB2_THREADS) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+    return;
+  }
+  uint4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
+    if (g < g1) v[i] = r.load(g);
+  }
+  float gg, hh = 0.f, H = 0.f;
+  if (b.coef) { const float4 c = b.coef[row]; gg = c.x; hh = c.y; H = c.z; }
+  else { gg = b.g[row]; if (ENT) { hh = b.h[row]; H = b.entropy[row]; } }
+  const float sc = b.scale * p.inv_tau;
+  GradCoef gc; gc.k = p.k;
+  if (b.stat) { const float2 s = b.stat[row]; gc.M = s.x; gc.ls2 = s.y; }
+  else { gc.M = 0.f; gc.ls2 = b.lse[row] * 1.4426950408889634f; }
+  gc.c0 = -(ENT ? fmaf(hh, H, gg) : gg) * sc; gc.c1 = -hh * TK_LN2 * sc;
+  const int gy = y < p.V ? (r.mis + (int)y) / Gran<KIND>::E : -1;
+  const bool mine = gy >= g0 && gy < g1 && (gy - g0) % TB2_THREADS == (int)threadIdx.x;
+  float zy = 0.f;
+  if (mine) zy = target_logit<KIND>(p, row, y);      // before this thread overwrites it, where the gradient replaces the logits
+  if (y >= p.V) gc.c0 = __int_as_float(0x7fc00000);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
+    if (g < g1) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+  }
+  if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, gg * sc));
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Pairs of answers.  R_s = beta * sum over the rows of answer s of (logp - ref), h = R_chosen - R_rejected,
+// loss = -(1 - eps) log sigma(h) - eps log sigma(-h), averaged over the pairs; d loss / d logp = +-beta/B (sigma(h) - (1 - eps)).
+struct PairArgs {
+  const int* starts;          // 2 * pairs + 1 rows; answer s has rows [starts[s], starts[s + 1])
+  const float* ref;
+  const float* logp;
+  const long long* y;
+  int64_t rows;
+  int pairs;
+  float beta, smoothing;
+  float* g;                   // out: d loss / d logp of each row of the answers
+  float* rewards;             // out: R_s
+  double* terms;              // out: loss of each pair
+};
+constexpr int TP_THREADS = 256;
+__global__ void __launch_bounds__(TP_THREADS) pair_kernel(const __grid_constant__ PairArgs a) {
+  __shared__ double sh[TP_THREADS / 32];
+  __shared__ float coef;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int b = blockIdx.x;
+  double R[2];
+  int64_t s0[2], s1[2];
+  for (int c = 0; c < 2; ++c) {
+    int64_t lo = a.starts[2 * b + c], hi = a.starts[2 * b + c + 1];      // bounds that make no sense never leave [0, rows]
+    lo = lo < 0 ? 0 : (lo > a.rows ? a.rows : lo);
+    hi = hi < lo ? lo : (hi > a.rows ? a.rows : hi);
+    s0[c] = lo; s1[c] = hi;
+    double s = 0.0;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += TP_THREADS)
+      if (a.y[i] >= 0) s += (double)a.logp[i] - (double)a.ref[i];
+    R[c] = (double)a.beta * block_sum(s, sh);
+  }
+  if (threadIdx.x == 0) {
+    const double h = R[0] - R[1], e = (double)a.smoothing;
+    const double tail = log1p(exp(-fabs(h)));                            // -log sigma(x) = max(-x, 0) + tail
+    a.terms[b] = (1.0 - e) * (fmax(-h, 0.0) + tail) + e * (fmax(h, 0.0) + tail);
+    if (h != h) a.terms[b] = h;
+    a.rewards[2 * b] = (float)R[0]; a.rewards[2 * b + 1] = (float)R[1];
+    coef = (float)((double)a.beta * (1.0 / (1.0 + exp(-h)) - (1.0 - e)) / (double)a.pairs);
+  }
+  __syncthreads();
+  if (!a.g) return;
+  for (int c = 0; c < 2; ++c)
+    for (int64_t i = s0[c] + threadIdx.x; i < s1[c]; i += TP_THREADS) a.g[i] = c == 0 ? coef : -coef;
+}
+__global__ void __launch_bounds__(TP_THREADS) pair_sum_kernel(const double* __restrict__ terms, int pairs, float* __restrict__ loss) {
+  __shared__ double sh[TP_THREADS / 32];
+  griddep_wait();
+  griddep_launch_dependents();
+  double s = 0.0;
+  for (int i = threadIdx.x; i < pairs; i += TP_THREADS) s += terms[i];
+  s = block_sum(s, sh);
+  if (threadIdx.x == 0) *loss = pairs > 0 ? (float)(s / (double)pairs) : 0.f;
+}
+// rows outside every answer take no part
+__global__ void __launch_bounds__(TP_THREADS) zero_floats_kernel(float* __restrict__ x, int64_t n) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t i = (int64_t)blockIdx.x * TP_THREADS + threadIdx.x;
+  if (i < n) x[i] = 0.f;
+}
+
+}  // namespace tg

@@ -1,0 +1,430 @@
+// Host side of the operators around the optimizer step: argument checks, launch shapes, workspace layout.
+#include <cmath>
+#include <cstring>
+
+#include "../../include/tgrad.h"
+#include "launch.cuh"
+#include "lists.cuh"
+#include "tokens.cuh"
+
+using namespace tg;
+
+namespace {
+
+#define TG_TRY(expr) do { tgrad_status s_ = (expr); if (s_ != TGRAD_OK) return s_; } while (0)
+
+int sm_count() {
+  int dev = 0, sm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sm < 1) return 148;
+  return sm;
+}
+inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// ---- lists ----
+constexpr int kListSmall = 128, kListLarge = 1024;       // tensors per launch: 2.6 KB and 20 KB of kernel parameters
+constexpr int kAdamwSmall = 64, kAdamwLarge = 512;       // 3.4 KB and 27 KB
+constexpr uint32_t kMaxListBlocks = 2048;
+
+// storage kind and reals per entry; false for a type that the lists do not take
+bool list_type(int32_t dtype, int& kind, int& reals) {
+  switch (dtype) {
+    case TGRAD_C64: kind = LS_F32; reals = 2; return true;
+    case TGRAD_C32H: kind = LS_F16; reals = 2; return true;
+    case TGRAD_C32B: kind = LS_BF16; reals = 2; return true;
+    case TGRAD_R32: kind = LS_F32; reals = 1; return true;
+    case TGRAD_R16H: kind = LS_F16; reals = 1; return true;
+    case TGRAD_R16B: kind = LS_BF16; reals = 1; return true;
+  }
+  return false;
+}
+
+tgrad_status check_list(const tgrad_tensor* list, int32_t n) {
+  if (n < 0 || (n > 0 && !list)) return TGRAD_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    int kind, reals;
+    if (!list_type(list[i].dtype, kind, reals)) return TGRAD_ERR_INVALID_ARG;
+    if (list[i].numel < 0 || list[i].numel >= ((int64_t)1 << 48)) return TGRAD_ERR_INVALID_ARG;
+    if (list[i].numel > 0 && (!list[i].d_data || misaligned(list[i].d_data, kind == LS_F32 ? 4 : 2))) return TGRAD_ERR_INVALID_ARG;
+  }
+  return TGRAD_OK;
+}
+
+size_t norm_bytes(int32_t n) {
+  const int per = n < kListLarge ? n : kListLarge;
+  return align_up((size_t)(kMaxListBlocks + per) * 8) + align_up((size_t)(n / kListLarge + 1) * 8);
+}
+
+// Fills the parameters for tensors [0, n) of `list`; returns the number of blocks (0: nothing in the list).
+template <int CAP>
+uint32_t fill_list(const tgrad_tensor* list, int n, int sm, ListParams<CAP>& p) {
+  p.n = n;
+  uint64_t granules = 0;
+  for (int i = 0; i < n; ++i) {
+    int kind = 0, reals = 1;
+    list_type(list[i].dtype, kind, reals);
+    p.e[i].ptr = static_cast<char*>(list[i].d_data);
+    p.e[i].count = (uint64_t)list[i].numel * reals | ((uint64_t)kind << 62);
+    granules += list_granules(p.e[i]);
+  }
+  // Chunks of 32 KB (eight 16-byte loads per thread in flight), down to 4 KB where there would be too few to give
+  // every SM several blocks.
+  uint32_t lg = 11;
+  while (lg > 8 && (granules >> lg) < (uint64_t)sm * 8) --lg;
+  while ((granules >> lg) > ((uint64_t)1 << 31)) ++lg;
+  p.gpc_log2 = lg;
+  uint64_t at = 0;
+  for (int i = 0; i < n; ++i) {
+    p.first[i] = (uint32_t)at;
+    at += (list_granules(p.e[i]) + (1ull << lg) - 1) >> lg;
+  }
+  p.first[n] = p.total = (uint32_t)at;
+  uint64_t grid = (uint64_t)sm * 4;
+  if (grid > at) grid = at;
+  return (uint32_t)(grid > kMaxListBlocks ? kMaxListBlocks : grid);
+}
+
+template <int CAP>
+tgrad_status norm_slices(const tgrad_tensor* list, int32_t n, float max_norm, float* out, void* ws, cudaStream_t st) {
+  const int sm = sm_count(), per = n < kListLarge ? n : kListLarge;
+  double* partial = static_cast<double*>(ws);
+  double* slice_sum = reinterpret_cast<double*>(static_cast<char*>(ws) + align_up((size_t)(kMaxListBlocks + per) * 8));
+  for (int base = 0, slice = 0; slice == 0 || base < n; base += CAP, ++slice) {
+    ListParams<CAP> p;
+    const int cnt = n - base < CAP ? n - base : CAP;
+    const uint32_t grid = fill_list<CAP>(list + base, cnt, sm, p);
+    if (grid > 0) {
+      launch_chained(list_sumsq_kernel<CAP>, dim3(grid), dim3(LS_THREADS), 0, st, p, partial);
+      TG_LAUNCH_CHECK();
+    }
+    launch_chained(list_norm_kernel<CAP>, dim3(1), dim3(LF_THREADS), 0, st, p, partial, grid, base, slice, base + CAP >= n ? 1 : 0, slice_sum, max_norm, out);
+    TG_LAUNCH_CHECK();
+  }
+  return TGRAD_OK;
+}
+template <int CAP>
+tgrad_status scale_slices(const tgrad_tensor* list, int32_t n, const float* coefficient, cudaStream_t st) {
+  const int sm = sm_count();
+  for (int base = (n - 1) / CAP * CAP; base >= 0; base -= CAP) {
+    ListParams<CAP> p;
+    const int cnt = n - base < CAP ? n - base : CAP;
+    const uint32_t grid = fill_list<CAP>(list + base, cnt, sm, p);
+    if (grid == 0) continue;
+    launch_chained(list_scale_kernel<CAP>, dim3(grid), dim3(LS_THREADS), 0, st, p, coefficient);
+    TG_LAUNCH_CHECK();
+  }
+  return TGRAD_OK;
+}
+
+tgrad_status norm_impl(const tgrad_tensor* grads, int32_t n, float max_norm, float* d_out, void* ws, size_t ws_bytes, bool clip, cudaStream_t st) {
+  TG_TRY(check_list(grads, n));
+  if (!(max_norm > 0.f) || !d_out || misaligned(d_out, 4) || !ws || misaligned(ws, 256)) return TGRAD_ERR_INVALID_ARG;
+  if (ws_bytes < norm_bytes(n)) return TGRAD_ERR_BUFFER_TOO_SMALL;
+  const bool small = n <= kListSmall;
+  TG_TRY(small ? norm_slices<kListSmall>(grads, n, max_norm, d_out, ws, st) : norm_slices<kListLarge>(grads, n, max_norm, d_out, ws, st));
+  if (!clip || n == 0) return TGRAD_OK;
+  return small ? scale_slices<kListSmall>(grads, n, d_out + 1, st) : scale_slices<kListLarge>(grads, n, d_out + 1, st);
+}
+
+template <int CAP>
+tgrad_status adamw_slices(const tgrad_adamw_tensor* list, int32_t n, const AdamwScalars& a, cudaStream_t st) {
+  const int sm = sm_count();
+  for (int base = 0; base < n; base += CAP) {
+    AdamwParams<CAP> p;
+    p.n = n - base < CAP ? n - base : CAP;
+    uint64_t entries = 0;
+    for (int i = 0; i < p.n; ++i) {
+      const tgrad_adamw_tensor& t = list[base + i];
+      const int kind = t.dtype == TGRAD_C64 ? LS_C64 : t.dtype == TGRAD_R32 ? LS_F32 : t.dtype == TGRAD_R16H ? LS_F16 : LS_BF16;
+      const int b = kind == LS_C64 ? 8 : kind == LS_F32 ? 4 : 2, vl = kind == LS_C64 ? 2 : 4, mb = kind == LS_C64 ? 8 : 4;
+      AdamwEntry& e = p.e[i];
+      e.w = static_cast<char*>(t.d_weight); e.g = static_cast<const char*>(t.d_grad);
+      e.m = static_cast<float*>(t.d_exp_avg); e.v = t.d_exp_avg_sq; e.master = t.d_master;
+      e.count = (uint64_t)t.numel | ((uint64_t)kind << 62);
+      p.head[i] = 255;
+      for (int h = vl - 1; h >= 0; --h)
+        if (!misaligned(e.w + h * b, vl * b) && !misaligned(e.g + h * b, vl * b) && !misaligned(reinterpret_cast<char*>(e.m) + h * mb, vl * mb) &&
+            !misaligned(e.v + h, vl * 4) && (!e.master || !misaligned(e.master + h, vl * 4)))
+          p.head[i] = (uint8_t)h;
+      entries += (uint64_t)t.numel;
+    }
+    // chunks of 4096 entries (two vectors of four per thread and turn), fewer where there would be too few of them
+    uint32_t lg = 12;
+    while (lg > 9 && (entries >> lg) < (uint64_t)sm * 8) --lg;
+    while ((entries >> lg) > ((uint64_t)1 << 31)) ++lg;
+    p.epc_log2 = lg;
+    uint64_t at = 0;
+    for (int i = 0; i < p.n; ++i) {
+      p.first[i] = (uint32_t)at;
+      at += ((uint64_t)list[base + i].numel + (1ull << lg) - 1) >> lg;
+    }
+    p.first[p.n] = p.total = (uint32_t)at;
+    if (at == 0) continue;
+    uint64_t grid = (uint64_t)sm * 8;
+    if (grid > at) grid = at;
+    launch_chained(list_adamw_kernel<CAP>, dim3((unsigned)grid), dim3(LS_THREADS), 0, st, p, a);
+    TG_LAUNCH_CHECK();
+  }
+  return TGRAD_OK;
+}
+
+// ---- rows of logits ----
+int token_kind(int32_t dtype) { return dtype == TGRAD_R32 ? LS_F32 : dtype == TGRAD_R16H ? LS_F16 : dtype == TGRAD_R16B ? LS_BF16 : -1; }
+
+tgrad_status check_logits(const tgrad_logits* in) {
+  if (!in) return TGRAD_ERR_INVALID_ARG;
+  const int kind = token_kind(in->dtype);
+  if (kind < 0 || in->rows < 0 || in->vocab < 1 || in->vocab > ((int64_t)1 << 30)) return TGRAD_ERR_INVALID_ARG;
+  if (in->rows > 1 && in->row_stride < in->vocab) return TGRAD_ERR_INVALID_ARG;
+  if (!(in->temperature > 0.f) || !std::isfinite(in->temperature) || !std::isfinite(1.5f / in->temperature)) return TGRAD_ERR_INVALID_ARG;
+  if (in->rows > 0 && (!in->d_logits || misaligned(in->d_logits, kind == LS_F32 ? 4 : 2) || !in->d_targets || misaligned(in->d_targets, 8))) return TGRAD_ERR_INVALID_ARG;
+  if (in->rows >= ((int64_t)1 << 31) / TK_MAX_CLUSTER) return TGRAD_ERR_UNSUPPORTED;
+  return TGRAD_OK;
+}
+tgrad_status check_dlogits(const tgrad_logits* in, const void* d, int64_t stride) {
+  if (in->rows > 0 && (!d || misaligned(d, token_kind(in->dtype) == LS_F32 ? 4 : 2))) return TGRAD_ERR_INVALID_ARG;
+  if (in->rows > 1 && stride < in->vocab) return TGRAD_ERR_INVALID_ARG;
+  // the gradient may take the logits' place, entry by entry, and must not overlap them in another way
+  if (d == in->d_logits && in->rows > 1 && stride != in->row_stride) return TGRAD_ERR_INVALID_ARG;
+  return TGRAD_OK;
+}
+inline bool bad_floats(const void* p, bool wanted) { return wanted ? (!p || misaligned(p, 4)) : misaligned(p, 4); }
+
+TokenArgs token_args(const tgrad_logits* in, void* d_dlogits, int64_t stride) {
+  TokenArgs a;
+  a.z = static_cast<const char*>(in->d_logits); a.dz = static_cast<char*>(d_dlogits);
+  a.ldz = in->row_stride; a.lddz = stride; a.y = reinterpret_cast<const long long*>(in->d_targets); a.V = (int)in->vocab;
+  a.inv_tau = (float)(1.0 / (double)in->temperature);
+  a.k = (float)(1.4426950408889634 / (double)in->temperature);
+  return a;
+}
+// most granules that a row can touch, whatever its alignment
+inline int64_t max_granules(int64_t vocab, int kind) { const int e = kind == LS_F32 ? 4 : 8; return (vocab + 2 * (e - 1)) / e; }
+
+template <bool POLICY>
+tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a, const ForwardArgs& f, const PolicyArgs& q, cudaStream_t st) {
+  // blocks per row: one while the rows alone fill the GPU, more (of at least one batch of loads each) where they do not
+  const int sm = sm_count();
+  const int64_t g = max_granules(in->vocab, kind);
+  int C = 1;
+  while (C < TK_MAX_CLUSTER && in->rows * C < (int64_t)4 * sm && g > (int64_t)C * TF_THREADS * 4) C *= 2;
+  const dim3 grid((unsigned)(in->rows * C));
+  if (kind == LS_F32) launch_cluster(token_forward_kernel<LS_F32, POLICY>, grid, dim3(TF_THREADS), 0, C, st, a, f, q, C);
+  else if (kind == LS_F16) launch_cluster(token_forward_kernel<LS_F16, POLICY>, grid, dim3(TF_THREADS), 0, C, st, a, f, q, C);
+  else launch_cluster(token_forward_kernel<LS_BF16, POLICY>, grid, dim3(TF_THREADS), 0, C, st, a, f, q, C);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
+
+template <bool ENT>
+tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
+  const int64_t pieces = (max_granules(in->vocab, kind) + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
+  if (in->rows * pieces >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(in->rows * pieces));
+  if (kind == LS_F32) launch_chained(token_backward_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
+  else if (kind == LS_F16) launch_chained(token_backward_kernel<LS_F16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
+  else launch_chained(token_backward_kernel<LS_BF16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
+
+// The one-pass policy kernel: C blocks of THREADS threads with eight granules each hold a row.
+struct HoldPlan { int threads, C; };
+HoldPlan hold_plan(int64_t granules) {
+  const int sizes[4] = {128, 256, 512, 1024};
+  for (int i = 0; i < 4; ++i)
+    for (int C = 1; C <= TK_MAX_CLUSTER; C *= 2) {
+      // blocks of 256 threads, four to an SM, are preferred; a row that eight of them cannot hold takes larger ones
+      if (sizes[i] < 256 && C > 1) break;
+      if (granules <= (int64_t)sizes[i] * 8 * C) return HoldPlan{sizes[i], C};
+    }
+  return HoldPlan{0, 0};
+}
+template <int KIND, bool ENT>
+tgrad_status launch_policy(const HoldPlan& h, int64_t rows, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
+  const dim3 grid((unsigned)(rows * h.C));
+  switch (h.threads) {
+    case 128: launch_cluster(policy_row_kernel<KIND, 128, ENT>, grid, dim3(128), 0, h.C, st, a, q, h.C); break;
+    case 256: launch_cluster(policy_row_kernel<KIND, 256, ENT>, grid, dim3(256), 0, h.C, st, a, q, h.C); break;
+    case 512: launch_cluster(policy_row_kernel<KIND, 512, ENT>, grid, dim3(512), 0, h.C, st, a, q, h.C); break;
+    default: launch_cluster(policy_row_kernel<KIND, 1024, ENT>, grid, dim3(1024), 0, h.C, st, a, q, h.C); break;
+  }
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
+template <bool ENT>
+tgrad_status launch_policy_kind(int kind, const HoldPlan& h, int64_t rows, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
+  return kind == LS_F32 ? launch_policy<LS_F32, ENT>(h, rows, a, q, st)
+         : kind == LS_F16 ? launch_policy<LS_F16, ENT>(h, rows, a, q, st) : launch_policy<LS_BF16, ENT>(h, rows, a, q, st);
+}
+
+size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16) * 2 + align_up((size_t)rows * 8); }
+size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + align_up((size_t)rows * 4) + align_up((size_t)pairs * 8); }
+
+}  // namespace
+
+extern "C" {
+
+tgrad_status tgrad_grad_norm_bytes(int32_t n, size_t* workspace_bytes) {
+  if (n < 0 || !workspace_bytes) return TGRAD_ERR_INVALID_ARG;
+  *workspace_bytes = norm_bytes(n);
+  return TGRAD_OK;
+}
+tgrad_status tgrad_grad_norm(const tgrad_tensor* grads, int32_t n, float max_norm, float* d_out, void* d_workspace,
+                             size_t workspace_bytes, void* cuda_stream) {
+  return norm_impl(grads, n, max_norm, d_out, d_workspace, workspace_bytes, false, static_cast<cudaStream_t>(cuda_stream));
+}
+tgrad_status tgrad_clip_grads(const tgrad_tensor* grads, int32_t n, float max_norm, float* d_out, void* d_workspace,
+                              size_t workspace_bytes, void* cuda_stream) {
+  return norm_impl(grads, n, max_norm, d_out, d_workspace, workspace_bytes, true, static_cast<cudaStream_t>(cuda_stream));
+}
+
+tgrad_status tgrad_adamw_step(const tgrad_adamw_tensor* list, int32_t n, const tgrad_adamw_config* c, void* cuda_stream) {
+  if (n < 0 || (n > 0 && !list) || !c) return TGRAD_ERR_INVALID_ARG;
+  if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0) || !(c->eps >= 0.0) || c->step < 1 ||
+      !std::isfinite(c->lr) || !std::isfinite(c->weight_decay) || misaligned(c->d_grad_scale, 4)) return TGRAD_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    const tgrad_adamw_tensor& t = list[i];
+    const bool c64 = t.dtype == TGRAD_C64, half = t.dtype == TGRAD_R16H || t.dtype == TGRAD_R16B;
+    if (t.dtype == TGRAD_C32H || t.dtype == TGRAD_C32B) return TGRAD_ERR_UNSUPPORTED;
+    if (!c64 && !half && t.dtype != TGRAD_R32) return TGRAD_ERR_INVALID_ARG;
+    if (t.d_master && !half) return TGRAD_ERR_INVALID_ARG;
+    if (t.numel < 0 || t.numel >= ((int64_t)1 << 48)) return TGRAD_ERR_INVALID_ARG;
+    if (t.numel == 0) continue;
+    const uintptr_t al = half ? 2 : 4;
+    if (!t.d_weight || !t.d_grad || !t.d_exp_avg || !t.d_exp_avg_sq) return TGRAD_ERR_INVALID_ARG;
+    if (misaligned(t.d_weight, al) || misaligned(t.d_grad, al) || misaligned(t.d_exp_avg, 4) || misaligned(t.d_exp_avg_sq, 4) || misaligned(t.d_master, 4))
+      return TGRAD_ERR_INVALID_ARG;
+  }
+  AdamwScalars a;
+  const double c1 = 1.0 - std::pow(c->beta1, (double)c->step), c2 = 1.0 - std::pow(c->beta2, (double)c->step);
+  a.beta1 = (float)c->beta1; a.beta2 = (float)c->beta2; a.omb1 = (float)(1.0 - c->beta1); a.omb2 = (float)(1.0 - c->beta2);
+  a.step_size = (float)(c->lr / c1); a.inv_sqrt_c2 = (float)(1.0 / std::sqrt(c2));
+  a.eps = (float)c->eps; a.keep = (float)(1.0 - c->lr * c->weight_decay);
+  a.gscale = c->d_grad_scale;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return n <= kAdamwSmall ? adamw_slices<kAdamwSmall>(list, n, a, st) : adamw_slices<kAdamwLarge>(list, n, a, st);
+}
+
+tgrad_status tgrad_token_logprob(const tgrad_logits* in, float* d_logp, float* d_lse, float* d_entropy, void* cuda_stream) {
+  TG_TRY(check_logits(in));
+  if (bad_floats(d_logp, false) || bad_floats(d_lse, false) || bad_floats(d_entropy, false)) return TGRAD_ERR_INVALID_ARG;
+  if (in->rows == 0) return TGRAD_OK;
+  ForwardArgs f; memset(&f, 0, sizeof(f));
+  f.logp = d_logp; f.lse = d_lse; f.entropy = d_entropy;
+  PolicyArgs q; memset(&q, 0, sizeof(q));
+  return launch_forward<false>(token_kind(in->dtype), in, token_args(in, nullptr, 0), f, q, static_cast<cudaStream_t>(cuda_stream));
+}
+
+tgrad_status tgrad_token_logprob_backward(const tgrad_logits* in, const float* d_lse, const float* d_entropy, const float* d_grad_logp,
+                                          const float* d_grad_entropy, void* d_dlogits, int64_t dlogits_stride, void* cuda_stream) {
+  TG_TRY(check_logits(in));
+  TG_TRY(check_dlogits(in, d_dlogits, dlogits_stride));
+  const bool any = in->rows > 0;
+  if (bad_floats(d_lse, any) || bad_floats(d_grad_logp, any) || bad_floats(d_grad_entropy, false) || bad_floats(d_entropy, any && d_grad_entropy)) return TGRAD_ERR_INVALID_ARG;
+  if (!any) return TGRAD_OK;
+  BackwardArgs b; memset(&b, 0, sizeof(b));
+  b.lse = d_lse; b.entropy = d_entropy; b.g = d_grad_logp; b.h = d_grad_entropy; b.scale = 1.f;
+  const TokenArgs a = token_args(in, d_dlogits, dlogits_stride);
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return d_grad_entropy ? launch_backward<true>(token_kind(in->dtype), in, a, b, st) : launch_backward<false>(token_kind(in->dtype), in, a, b, st);
+}
+
+tgrad_status tgrad_policy_loss_bytes(int64_t rows, size_t* workspace_bytes) {
+  if (rows < 0 || !workspace_bytes) return TGRAD_ERR_INVALID_ARG;
+  *workspace_bytes = policy_bytes(rows) + 256;
+  return TGRAD_OK;
+}
+tgrad_status tgrad_policy_loss(const tgrad_logits* in, const tgrad_policy_args* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream) {
+  TG_TRY(check_logits(in));
+  if (!c) return TGRAD_ERR_INVALID_ARG;
+  const bool any = in->rows > 0;
+  if (bad_floats(c->d_old_logp, any) || bad_floats(c->d_advantages, any) || bad_floats(c->d_weights, any) || bad_floats(c->d_ref_logp, false) ||
+      bad_floats(c->d_stats, true) || bad_floats(c->d_logp, false) || bad_floats(c->d_entropy, false)) return TGRAD_ERR_INVALID_ARG;
+  if (c->d_dlogits) TG_TRY(check_dlogits(in, c->d_dlogits, c->dlogits_stride));
+  if (!(c->clip_low >= 0.f && c->clip_low <= 1.f) || !(c->clip_high >= 0.f) || !std::isfinite(c->kl_coef) || !std::isfinite(c->entropy_coef) || !std::isfinite(c->grad_scale))
+    return TGRAD_ERR_INVALID_ARG;
+  if (!d_workspace || misaligned(d_workspace, 256)) return TGRAD_ERR_INVALID_ARG;
+  if (workspace_bytes < policy_bytes(in->rows)) return TGRAD_ERR_BUFFER_TOO_SMALL;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* ws = static_cast<char*>(d_workspace);
+  const size_t r16 = align_up((size_t)in->rows * 16);
+  PolicyArgs q; memset(&q, 0, sizeof(q));
+  q.old_logp = c->d_old_logp; q.ref_logp = c->d_ref_logp; q.adv = c->d_advantages; q.weight = c->d_weights;
+  q.low = 1.f - c->clip_low; q.high = 1.f + c->clip_high; q.kl_coef = c->kl_coef; q.ent_coef = c->entropy_coef; q.grad_scale = c->grad_scale;
+  q.logp = c->d_logp; q.entropy = c->d_entropy; q.terms = reinterpret_cast<float4*>(ws);
+  const int kind = token_kind(in->dtype);
+  if (any) {
+    const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
+    const HoldPlan h = hold_plan(max_granules(in->vocab, kind));
+    const bool ent = c->entropy_coef != 0.f;
+    if (c->d_dlogits && h.threads) {
+      TG_TRY(ent ? launch_policy_kind<true>(kind, h, in->rows, a, q, st) : launch_policy_kind<false>(kind, h, in->rows, a, q, st));
+    } else {
+      ForwardArgs f; memset(&f, 0, sizeof(f));
+      f.logp = c->d_logp; f.entropy = c->d_entropy;
+      f.coef = reinterpret_cast<float4*>(ws + r16); f.stat = reinterpret_cast<float2*>(ws + 2 * r16);
+      TG_TRY(launch_forward<true>(kind, in, a, f, q, st));
+      if (c->d_dlogits) {
+        BackwardArgs b; memset(&b, 0, sizeof(b));
+        b.coef = f.coef; b.stat = f.stat; b.scale = c->grad_scale;
+        TG_TRY(ent ? launch_backward<true>(kind, in, a, b, st) : launch_backward<false>(kind, in, a, b, st));
+      }
+    }
+  }
+  launch_chained(policy_sum_kernel, dim3(1), dim3(1024), 0, st, q.terms, in->rows, c->kl_coef, c->entropy_coef, c->d_stats);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
+
+tgrad_status tgrad_preference_loss_bytes(int64_t rows, int32_t pairs, size_t* workspace_bytes) {
+  if (rows < 0 || pairs < 0 || !workspace_bytes) return TGRAD_ERR_INVALID_ARG;
+  *workspace_bytes = preference_bytes(rows, pairs) + 256;
+  return TGRAD_OK;
+}
+tgrad_status tgrad_preference_loss(const tgrad_logits* in, const tgrad_preference_args* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream) {
+  TG_TRY(check_logits(in));
+  if (!c || c->pairs < 0) return TGRAD_ERR_INVALID_ARG;
+  const bool any = in->rows > 0;
+  if (bad_floats(c->d_ref_logp, any) || bad_floats(c->d_logp, any) || bad_floats(c->d_loss, true) || bad_floats(c->d_rewards, c->pairs > 0) ||
+      !c->d_starts || misaligned(c->d_starts, 4)) return TGRAD_ERR_INVALID_ARG;
+  if (c->d_dlogits) TG_TRY(check_dlogits(in, c->d_dlogits, c->dlogits_stride));
+  if (!std::isfinite(c->beta) || !(c->label_smoothing >= 0.f && c->label_smoothing <= 1.f) || !std::isfinite(c->grad_scale)) return TGRAD_ERR_INVALID_ARG;
+  if (!d_workspace || misaligned(d_workspace, 256)) return TGRAD_ERR_INVALID_ARG;
+  if (workspace_bytes < preference_bytes(in->rows, c->pairs)) return TGRAD_ERR_BUFFER_TOO_SMALL;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* ws = static_cast<char*>(d_workspace);
+  float2* stat = reinterpret_cast<float2*>(ws);
+  float* g = reinterpret_cast<float*>(ws + align_up((size_t)in->rows * 8));
+  double* terms = reinterpret_cast<double*>(ws + align_up((size_t)in->rows * 8) + align_up((size_t)in->rows * 4));
+  const int kind = token_kind(in->dtype);
+  const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
+  if (any) {
+    ForwardArgs f; memset(&f, 0, sizeof(f));
+    f.logp = c->d_logp; f.stat = stat;
+    PolicyArgs q; memset(&q, 0, sizeof(q));
+    if (c->d_dlogits) {
+      launch_chained(zero_floats_kernel, dim3((unsigned)((in->rows + TP_THREADS - 1) / TP_THREADS)), dim3(TP_THREADS), 0, st, g, in->rows);
+      TG_LAUNCH_CHECK();
+    }
+    TG_TRY(launch_forward<false>(kind, in, a, f, q, st));
+  }
+  if (c->pairs > 0) {
+    PairArgs p; memset(&p, 0, sizeof(p));
+    p.starts = c->d_starts; p.ref = c->d_ref_logp; p.logp = c->d_logp; p.y = reinterpret_cast<const long long*>(in->d_targets);
+    p.rows = in->rows; p.pairs = c->pairs; p.beta = c->beta; p.smoothing = c->label_smoothing;
+    p.g = c->d_dlogits ? g : nullptr; p.rewards = c->d_rewards; p.terms = terms;
+    launch_chained(pair_kernel, dim3((unsigned)c->pairs), dim3(TP_THREADS), 0, st, p);
+    TG_LAUNCH_CHECK();
+  }
+  launch_chained(pair_sum_kernel, dim3(1), dim3(TP_THREADS), 0, st, terms, c->pairs, c->d_loss);
+  TG_LAUNCH_CHECK();
+  if (any && c->d_dlogits) {
+    BackwardArgs b; memset(&b, 0, sizeof(b));
+    b.stat = stat; b.g = g; b.scale = c->grad_scale;
+    TG_TRY(launch_backward<false>(kind, in, a, b, st));
+  }
+  return TGRAD_OK;
+}
+
+}  // extern "C"
