@@ -92,6 +92,16 @@ __device__ __forceinline__ float sumsq_word(uint32_t w, float s) {
   return fmaf(x.y, x.y, fmaf(x.x, x.x, s));
 }
 template <int KIND>
+__device__ __forceinline__ float sumsq_batch(const uint4 (&v)[8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s = sumsq_word<KIND>(v[i].x, s); s = sumsq_word<KIND>(v[i].y, s);
+    s = sumsq_word<KIND>(v[i].z, s); s = sumsq_word<KIND>(v[i].w, s);
+  }
+  return s;
+}
+template <int KIND>
 __device__ __noinline__ double sumsq_words_double(const uint4* v, int n) {
   double acc = 0.0;
   for (int i = 0; i < n; ++i) {
@@ -103,36 +113,40 @@ __device__ __noinline__ double sumsq_words_double(const uint4* v, int n) {
   }
   return acc;
 }
+template <int KIND>
+__device__ __noinline__ double sumsq_entries(const char* p, uint32_t bytes) {
+  double acc = 0.0;
+  for (uint32_t b = 0; b < bytes; b += KIND == LS_F32 ? 4 : 2) { const double x = ld_real<KIND>(p + b); acc += x * x; }
+  return acc;
+}
+__device__ __forceinline__ double sumsq_edge(int kind, const char* p, uint32_t bytes) {
+  return kind == LS_F32 ? sumsq_entries<LS_F32>(p, bytes) : kind == LS_F16 ? sumsq_entries<LS_F16>(p, bytes) : sumsq_entries<LS_BF16>(p, bytes);
+}
 
 // Sum of squares of one chunk's share of a thread.  The up to 64 squares of one batch are added in fp32 and the batches
 // in fp64: 2^-24 per term, and no loss in the long sum.  A batch whose fp32 sum leaves the range in which no square can
 // have overflowed or been flushed (but is not all zeros) is added again in fp64, so gradients of 1e-30 or 1e30 count.
-template <int KIND>
 __device__ __forceinline__ double sumsq_chunk(const ListEntry& e, uint32_t chunk, uint32_t gpc_log2) {
-  const uint64_t n = list_count(e.count);
-  constexpr int LB = KIND == LS_F32 ? 2 : 1;
+  const int kind = list_kind(e.count);
   const uint32_t mis = (uint32_t)((uintptr_t)e.ptr & 15);
   const char* base = e.ptr - mis;
-  const uint64_t g0 = (uint64_t)chunk << gpc_log2, bytes = n << LB, end = mis + bytes;      // bytes from `base`
-  const uint64_t gfull = end >> 4;                                                          // granules [.., gfull) end inside
+  const uint64_t end = mis + (list_count(e.count) << list_log2_bytes(e.count)), gfull = end >> 4, gall = (end + 15) >> 4;
+  const uint64_t g0 = (uint64_t)chunk << gpc_log2;
   uint64_t g1 = g0 + (1ull << gpc_log2);
-  const uint64_t gall = (end + 15) >> 4;
-  if (g1 > gall) g1 = gall;
+  const bool last = g1 >= gall;
+  if (g1 > gfull) g1 = gfull;                                        // whole granules [first, g1) of the chunk
+  const uint64_t first = g0 == 0 && mis != 0 ? 1 : g0;
   double acc = 0.0;
-  for (uint64_t gb = g0; gb < g1; gb += 8 * LS_THREADS) {
+  for (uint64_t gb = first + threadIdx.x; gb < g1; gb += 8 * LS_THREADS) {
+    const uint4* at = reinterpret_cast<const uint4*>(base) + gb;
+    const uint32_t left = (uint32_t)(g1 - gb < 8 * LS_THREADS ? g1 - gb : 8 * LS_THREADS);
     uint4 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint64_t g = gb + threadIdx.x + (uint64_t)i * LS_THREADS;
       v[i] = make_uint4(0, 0, 0, 0);
-      if (g < g1 && g < gfull && (g > 0 || mis == 0)) v[i] = ld_stream(reinterpret_cast<const uint4*>(base) + g);
+      if (i * LS_THREADS < left) v[i] = ld_stream(at + i * LS_THREADS);
     }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s = sumsq_word<KIND>(v[i].x, s); s = sumsq_word<KIND>(v[i].y, s);
-      s = sumsq_word<KIND>(v[i].z, s); s = sumsq_word<KIND>(v[i].w, s);
-    }
+    const float s = kind == LS_F32 ? sumsq_batch<LS_F32>(v) : kind == LS_F16 ? sumsq_batch<LS_F16>(v) : sumsq_batch<LS_BF16>(v);
     if (s > 1e-20f && s < 1e38f) acc += (double)s;
     else {
       uint32_t any = 0;
@@ -142,18 +156,13 @@ __device__ __forceinline__ double sumsq_chunk(const ListEntry& e, uint32_t chunk
         uint4 w[8];      // a copy, so that the values of the usual case stay in registers
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = v[i];
-        acc += sumsq_words_double<KIND>(w, 8);
+        acc += kind == LS_F32 ? sumsq_words_double<LS_F32>(w, 8) : kind == LS_F16 ? sumsq_words_double<LS_F16>(w, 8) : sumsq_words_double<LS_BF16>(w, 8);
       }
     }
   }
   // the outer granules hold entries of other tensors too: entry by entry, by one thread each
-  if (threadIdx.x == 0 && g0 == 0 && mis != 0) {
-    const uint64_t stop = end < 16 ? end : 16;
-    for (uint64_t b = mis; b < stop; b += 1 << LB) { const double x = ld_real<KIND>(base + b); acc += x * x; }
-  }
-  if (threadIdx.x == 32 && g1 == gall && (end & 15) != 0 && !(gfull == 0 && mis != 0)) {
-    for (uint64_t b = gfull << 4; b < end; b += 1 << LB) { const double x = ld_real<KIND>(base + b); acc += x * x; }
-  }
+  if (threadIdx.x == 0 && g0 == 0 && mis != 0) acc += sumsq_edge(kind, e.ptr, (uint32_t)((end < 16 ? end : 16) - mis));
+  if (threadIdx.x == 32 && last && (end & 15) != 0 && !(gfull == 0 && mis != 0)) acc += sumsq_edge(kind, base + (gfull << 4), (uint32_t)(end & 15));
   return acc;
 }
 
@@ -185,12 +194,7 @@ __global__ void __launch_bounds__(LS_THREADS, 4) list_sumsq_kernel(const __grid_
     const ListEntry e = p.e[t];
     const uint32_t stop = p.first[t + 1] < c1 ? p.first[t + 1] : c1;
     double acc = 0.0;
-    const int kind = list_kind(e.count);
-    for (; c < stop; ++c) {
-      const uint32_t k = c - p.first[t];
-      acc += kind == LS_F32 ? sumsq_chunk<LS_F32>(e, k, p.gpc_log2)
-             : kind == LS_F16 ? sumsq_chunk<LS_F16>(e, k, p.gpc_log2) : sumsq_chunk<LS_BF16>(e, k, p.gpc_log2);
-    }
+    for (; c < stop; ++c) acc += sumsq_chunk(e, c - p.first[t], p.gpc_log2);
     const double sum = block_sum(acc, sh);
     if (threadIdx.x == 0) partial[blockIdx.x + t] = sum;
   }
@@ -241,36 +245,45 @@ __device__ __forceinline__ uint32_t scale_word(uint32_t w, float c) {
   return narrow2<KIND>(x.x * c, x.y * c);
 }
 template <int KIND>
+__device__ __forceinline__ uint4 scale_granule(uint4 v, float c) {
+  return make_uint4(scale_word<KIND>(v.x, c), scale_word<KIND>(v.y, c), scale_word<KIND>(v.z, c), scale_word<KIND>(v.w, c));
+}
+template <int KIND>
+__device__ __noinline__ void scale_entries(char* p, uint32_t bytes, float c) {
+  for (uint32_t b = 0; b < bytes; b += KIND == LS_F32 ? 4 : 2) st_real<KIND>(p + b, ld_real<KIND>(p + b) * c);
+}
+__device__ __forceinline__ void scale_edge(int kind, char* p, uint32_t bytes, float c) {
+  if (kind == LS_F32) scale_entries<LS_F32>(p, bytes, c);
+  else if (kind == LS_F16) scale_entries<LS_F16>(p, bytes, c);
+  else scale_entries<LS_BF16>(p, bytes, c);
+}
 __device__ __forceinline__ void scale_chunk(const ListEntry& e, uint32_t chunk, uint32_t gpc_log2, float c) {
-  const uint64_t n = list_count(e.count);
-  constexpr int LB = KIND == LS_F32 ? 2 : 1;
+  const int kind = list_kind(e.count);
   const uint32_t mis = (uint32_t)((uintptr_t)e.ptr & 15);
   char* base = e.ptr - mis;
-  const uint64_t g0 = (uint64_t)chunk << gpc_log2, end = mis + (n << LB), gfull = end >> 4, gall = (end + 15) >> 4;
+  const uint64_t end = mis + (list_count(e.count) << list_log2_bytes(e.count)), gfull = end >> 4, gall = (end + 15) >> 4;
+  const uint64_t g0 = (uint64_t)chunk << gpc_log2;
   uint64_t g1 = g0 + (1ull << gpc_log2);
-  if (g1 > gall) g1 = gall;
-  for (uint64_t gb = g0; gb < g1; gb += 8 * LS_THREADS) {
+  const bool last = g1 >= gall;
+  if (g1 > gfull) g1 = gfull;                                        // whole granules [first, g1) of the chunk
+  const uint64_t first = g0 == 0 && mis != 0 ? 1 : g0;
+  for (uint64_t gb = first + threadIdx.x; gb < g1; gb += 8 * LS_THREADS) {
+    uint4* at = reinterpret_cast<uint4*>(base) + gb;
+    const uint32_t left = (uint32_t)(g1 - gb < 8 * LS_THREADS ? g1 - gb : 8 * LS_THREADS);
     uint4 v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint64_t g = gb + threadIdx.x + (uint64_t)i * LS_THREADS;
-      if (g < g1 && g < gfull && (g > 0 || mis == 0)) v[i] = ld_stream(reinterpret_cast<const uint4*>(base) + g);
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i * LS_THREADS < left) v[i] = ld_stream(at + i * LS_THREADS);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint64_t g = gb + threadIdx.x + (uint64_t)i * LS_THREADS;
-      if (g < g1 && g < gfull && (g > 0 || mis == 0))
-        st_stream(reinterpret_cast<uint4*>(base) + g, make_uint4(scale_word<KIND>(v[i].x, c), scale_word<KIND>(v[i].y, c),
-                                                                 scale_word<KIND>(v[i].z, c), scale_word<KIND>(v[i].w, c)));
-    }
+    for (int i = 0; i < 8; ++i)
+      v[i] = kind == LS_F32 ? scale_granule<LS_F32>(v[i], c) : kind == LS_F16 ? scale_granule<LS_F16>(v[i], c) : scale_granule<LS_BF16>(v[i], c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i * LS_THREADS < left) st_stream(at + i * LS_THREADS, v[i]);
   }
-  if (threadIdx.x == 0 && g0 == 0 && mis != 0) {
-    const uint64_t stop = end < 16 ? end : 16;
-    for (uint64_t b = mis; b < stop; b += 1 << LB) st_real<KIND>(base + b, ld_real<KIND>(base + b) * c);
-  }
-  if (threadIdx.x == 32 && g1 == gall && (end & 15) != 0 && !(gfull == 0 && mis != 0)) {
-    for (uint64_t b = gfull << 4; b < end; b += 1 << LB) st_real<KIND>(base + b, ld_real<KIND>(base + b) * c);
-  }
+  // the outer granules hold entries of other tensors too: entry by entry, by one thread each
+  if (threadIdx.x == 0 && g0 == 0 && mis != 0) scale_edge(kind, e.ptr, (uint32_t)((end < 16 ? end : 16) - mis), c);
+  if (threadIdx.x == 32 && last && (end & 15) != 0 && !(gfull == 0 && mis != 0)) scale_edge(kind, base + (gfull << 4), (uint32_t)(end & 15), c);
 }
 
 // Scales every tensor by the coefficient that list_norm_kernel wrote.  A coefficient of 1 leaves every entry as it is,
@@ -291,11 +304,7 @@ __global__ void __launch_bounds__(LS_THREADS, 4) list_scale_kernel(const __grid_
     --c;
     while (p.first[t] > c) --t;
     const ListEntry e = p.e[t];
-    const uint32_t k = c - p.first[t];
-    const int kind = list_kind(e.count);
-    if (kind == LS_F32) scale_chunk<LS_F32>(e, k, p.gpc_log2, s);
-    else if (kind == LS_F16) scale_chunk<LS_F16>(e, k, p.gpc_log2, s);
-    else scale_chunk<LS_BF16>(e, k, p.gpc_log2, s);
+    scale_chunk(e, c - p.first[t], p.gpc_log2, s);
   }
 }
 
@@ -317,7 +326,7 @@ struct AdamwEntry {
   float* m;
   float* v;
   float* master;         // fp32 weights of 16-bit ones, or null
-  uint64_t count;        // entries (complex ones for kind 3), kind in the top two bits
+  uint64_t count;        // entries (complex ones for LS_C64)
 };
 constexpr int LS_C64 = 3;
 template <int CAP>
@@ -455,8 +464,9 @@ __device__ __forceinline__ void adamw_chunk(const AdamwEntry& e, uint64_t i0, ui
   for (uint64_t i = a1 + threadIdx.x; i < i1; i += LS_THREADS) adamw_one<KIND>(e, i, c, a);
 }
 
-template <int CAP>
-__global__ void __launch_bounds__(LS_THREADS) list_adamw_kernel(const __grid_constant__ AdamwParams<CAP> p, const __grid_constant__ AdamwScalars a) {
+// All tensors of one launch have the same storage, so that each has its own registers and no branch in the loop.
+template <int KIND, bool MASTER, int CAP>
+__global__ void __launch_bounds__(LS_THREADS, 4) list_adamw_kernel(const __grid_constant__ AdamwParams<CAP> p, const __grid_constant__ AdamwScalars a) {
   griddep_wait();
   griddep_launch_dependents();
   const float c = a.gscale ? *a.gscale : 1.f;
@@ -468,26 +478,15 @@ __global__ void __launch_bounds__(LS_THREADS) list_adamw_kernel(const __grid_con
   int t = lo;
   for (; k < k1; ++k) {
     while (p.first[t + 1] <= k) ++t;
-    const AdamwEntry e = p.e[t];
-    const uint64_t n = list_count(e.count);
+    const AdamwEntry& e = p.e[t];
+    const uint64_t n = e.count;
     // chunk boundaries lie `head` past multiples of the chunk length, so that every chunk but the first starts with a vector
     const int head = p.head[t], shift = head == 255 ? 0 : head;
     const uint32_t j = k - p.first[t], last = p.first[t + 1] - p.first[t] - 1;
     const uint64_t i0 = j == 0 ? 0 : ((uint64_t)j << p.epc_log2) + shift;
     uint64_t i1 = j == last ? n : ((uint64_t)(j + 1) << p.epc_log2) + shift;
-    const int h = head == 255 ? 255 : (j == 0 ? head : 0);
     if (i1 > n) i1 = n;
-    if (i0 >= i1) continue;
-    switch (list_kind(e.count)) {
-      case LS_F32: adamw_chunk<LS_F32, false>(e, i0, i1, h, c, a); break;
-      case LS_F16:
-        if (e.master) adamw_chunk<LS_F16, true>(e, i0, i1, h, c, a); else adamw_chunk<LS_F16, false>(e, i0, i1, h, c, a);
-        break;
-      case LS_BF16:
-        if (e.master) adamw_chunk<LS_BF16, true>(e, i0, i1, h, c, a); else adamw_chunk<LS_BF16, false>(e, i0, i1, h, c, a);
-        break;
-      default: adamw_chunk<LS_C64, false>(e, i0, i1, h, c, a); break;
-    }
+    if (i0 < i1) adamw_chunk<KIND, MASTER>(e, i0, i1, head == 255 ? 255 : (j == 0 ? head : 0), c, a);
   }
 }
 

@@ -61,6 +61,12 @@ __device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {     // la
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 template <int KIND>
+__device__ __forceinline__ uint32_t max_nan_word(uint32_t a, uint32_t b) {     // the same; a NaN stays (16-bit storage)
+  if (KIND == LS_F16) { const __half2 r = __hmax2_nan(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b)); return *reinterpret_cast<const uint32_t*>(&r); }
+  const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <int KIND>
 __device__ __forceinline__ float max_of_word(uint32_t a) {
   if (KIND == LS_F32) return __uint_as_float(a);
   const float2 x = widen2<KIND>(a);
@@ -292,65 +298,291 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Policy loss, forward and backward in one pass: the row stays in the registers of the C blocks that share it (16-byte
-// granules, NV per thread), so the logits are read once and the gradient written once.
-template <int KIND, int THREADS, bool ENT>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int C) {
-  constexpr int NV = 8;
-  __shared__ float4 sh[TK_MAX_CLUSTER * (THREADS / 32)];
-  if (C > 1) cluster_arrive_relaxed();
+// Policy loss, forward and backward in one pass over device memory: a block works on one row at a time, reads it once for
+// the sums and once more, from shared memory, for the gradient.
+//
+// The row's whole granules come in chunks of 64 granules per arithmetic warp, by bulk copies into a ring of N places that
+// one further warp keeps full.  Chunks that stay for the second reading are released after it; where a row has more chunks
+// than the ring has places, the ones too many go through it first, and again (from L2) at the end:
+//   asked for:  e_1 .. e_x  r_1 .. r_n  e_1 .. e_x      released in the same order, so that the ring is a queue:
+//   sums of     e_1 .. e_x  r_1 .. r_n
+//   gradient of             r_1 .. r_n  e_1 .. e_x
+// While the gradient frees places the next row's chunks arrive in them.  The up to E - 1 entries before the first and after
+// the last whole granule are taken one by one by the first warp.
+//
+// Why a block and not a cluster per row: with the row in the registers of eight blocks the exchange of the sums (3,000 to
+// 5,000 cycles between the last logit's arrival and the first gradient, most of it latency) was paid for every 32 KB
+// instead of for every row; 8192 x 131072 bf16 logits took 0.95 ms so, and 1.2 ms with the rows fetched ahead.
+constexpr int RW_MAX_WARPS = 24, RW_MAX_PLACES = 32;
+struct RowGeom {
+  int W, N;              // arithmetic warps, places of the ring
+  float reach, lowest;   // 200 / k; lowest value that the clamp may take in the storage type
+  float slack;           // 40 / k
+};
+
+__device__ __forceinline__ void bar_sync_n(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// Running sums of a warp relative to a reference that all its lanes share and that need not be the maximum: it is moved
+// when a logit exceeds it by more than 2^40 (so the sums neither overflow nor lose anything).
+struct WarpSums { float base, thr, nm, delta; uint32_t clamp; bool fast; uint64_t s2, t2; };
+template <int KIND>
+__device__ __forceinline__ void move_base(WarpSums& a, float top, const RowGeom& geo, float k) {
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float d = fmaxf(fmaf(a.base - top, k, -a.delta), -1e30f), f = ex2(d);
+  const float2 s = upk2(a.s2), t = upk2(a.t2);
+  a.s2 = pk2(s.x * f, s.y * f);
+  a.t2 = pk2(f * fmaf(s.x, d, t.x), f * fmaf(s.y, d, t.y));
+  a.base = top; a.thr = top + geo.slack;
+  // one fma per exponent, d = x k - fl(base k), and -inf clamped before it is widened, where both are possible; else the
+  // difference first, which never overflows
+  const float low = top - geo.reach;      // 2^-200 of the reference
+  a.fast = fabsf(top) < 1e30f && low > geo.lowest;
+  a.nm = a.fast ? -(top * k) : -top;
+  a.delta = a.fast ? fmaf(top, k, a.nm) : 0.f;      // 2^(x k - fl(base k)) is 2^delta too large
+  a.clamp = narrow2<KIND == LS_F32 ? LS_BF16 : KIND>(low, low);
+}
+template <int KIND, bool FAST>
+__device__ __forceinline__ void add_granule(WarpSums& a, const uint4& v, uint64_t nm, uint64_t kk) {
+#pragma unroll
+  for (int j = 0; j < Gran<KIND>::E / 2; ++j) {
+    float2 x;
+    if (KIND == LS_F32 || !FAST) x = gpair<KIND>(v, j);
+    else x = widen2<KIND>(max_nan_word<KIND>(j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w, a.clamp));
+    uint64_t d2 = FAST ? fma2(pk2(x.x, x.y), kk, nm) : mul2(add2(pk2(x.x, x.y), nm), kk);
+    const float2 d = upk2(d2);
+    const uint64_t e = pk2(ex2(d.x), ex2(d.y));
+    a.s2 = add2(a.s2, e);
+    if (KIND == LS_F32 || !FAST) d2 = pk2(max_nan(d.x, -200.f), max_nan(d.y, -200.f));      // 0 * -inf is not wanted
+    a.t2 = fma2(e, d2, a.t2);
+  }
+}
+template <int KIND>
+__device__ __forceinline__ float granule_max(const uint4& v) {
+  return max_of_word<KIND>(max_word<KIND>(max_word<KIND>(v.x, v.y), max_word<KIND>(v.z, v.w)));
+}
+template <int KIND>
+__device__ __forceinline__ void add_chunk(WarpSums& a, const uint4 (&v)[2], const RowGeom& geo, float k) {
+  const float top = fmaxf(granule_max<KIND>(v[0]), granule_max<KIND>(v[1]));
+  if (__any_sync(0xffffffffu, top > a.thr)) move_base<KIND>(a, top, geo, k);
+  const uint64_t nm = pk2(a.nm, a.nm), kk = pk2(k, k);
+  if (a.fast) { add_granule<KIND, true>(a, v[0], nm, kk); add_granule<KIND, true>(a, v[1], nm, kk); }
+  else { add_granule<KIND, false>(a, v[0], nm, kk); add_granule<KIND, false>(a, v[1], nm, kk); }
+}
+
+// What the row's sums give the gradient.
+struct RowGrad { float M, nb, ls2, c0, c1, target, zy; int owner; };
+template <int KIND, bool ENT, bool FAST>
+__device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, float k) {
+  const uint64_t kk = pk2(k, k), c0 = pk2(h.c0, h.c0), c1 = pk2(h.c1, h.c1);
+  uint32_t w[4];
+#pragma unroll
+  for (int q = 0; q < Gran<KIND>::E / 2; ++q) {
+    const float2 x = gpair<KIND>(v, q);
+    const uint64_t x2 = pk2(x.x, x.y);
+    const float2 l = upk2(FAST ? fma2(x2, kk, pk2(h.nb, h.nb)) : fma2(add2(x2, pk2(-h.M, -h.M)), kk, pk2(-h.ls2, -h.ls2)));
+    uint64_t c = c0;
+    if (ENT) c = fma2(pk2(max_nan(l.x, -200.f), max_nan(l.y, -200.f)), c1, c0);
+    const float2 d = upk2(mul2(pk2(ex2(l.x), ex2(l.y)), c));
+    if (KIND == LS_F32) { w[2 * q] = __float_as_uint(d.x); w[2 * q + 1] = __float_as_uint(d.y); }
+    else w[q] = narrow2<KIND>(d.x, d.y);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int KIND, bool ENT>
+__global__ void __maxnreg__(72) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int64_t rows, const __grid_constant__ RowGeom geo) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ float4 sums[RW_MAX_WARPS];
+  __shared__ __align__(16) RowGrad handed;
+  __shared__ volatile int bad;           // a wait ran out of its bound
+  __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES];
+  constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
+  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = 2 * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    bad = 0;
+    for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
+    fence_mbar_init();
+  }
+  __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t row = blockIdx.x / C;
-  const int rank = C > 1 ? (int)cluster_rank() : 0;
-  const long long y = p.y[row];
-  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
-  char* drow = p.dz + row * p.lddz * Gran<KIND>::B;
-  const bool same = same_alignment(r, drow);
-  const int G = r.granules(), per = (G + C - 1) / C, g0 = rank * per, g1 = min(G, g0 + per);
-  if (C > 1) cluster_wait();
-  if (y < 0) {
-    for (int g = g0 + threadIdx.x; g < g1; g += THREADS) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
-    if (rank == 0 && threadIdx.x == 0) {
-      if (q.logp) q.logp[row] = 0.f;
-      if (q.entropy) q.entropy[row] = 0.f;
-      q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int64_t first = blockIdx.x, step = gridDim.x;
+  int s = 0;
+  uint32_t ph = 0;
+  bool ok = true;
+
+  if (warp == W) {
+    // ---- the fetching warp ----
+    uint32_t used = 0;
+    for (int64_t r0 = first; r0 < rows && ok; r0 += 32 * step) {
+      const int64_t mine = r0 + lane * step;
+      uint32_t live = __ballot_sync(0xffffffffu, mine < rows && p.y[mine < rows ? mine : r0] >= 0);
+      if (lane == 0) {
+        for (; live && ok; live &= live - 1) {
+          const Row<KIND> r(p.z + (r0 + (__ffs(live) - 1) * step) * p.ldz * B, p.V);
+          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = K <= N ? K : N - 2;
+          for (int j = 0; j < 2 * K - n && ok; ++j) {
+            const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
+            ok = mbar_wait_bounded(&empty[s], ph ^ 1);
+            if (!ok) break;
+            mbar_expect_tx(&full[s], (uint32_t)len * 16);
+            bulk_g2s(ring + (size_t)s * chunk * 16, r.base + (size_t)(wa + at) * 16, (uint32_t)len * 16, &full[s]);
+            used |= 1u << s;
+            if (++s == N) { s = 0; ph ^= 1; }
+          }
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
     }
+    // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
+    if (lane == 0)
+      for (int i = 0; i < N; ++i)
+        if (used >> i & 1) (void)mbar_wait_bounded(&full[i], i < s ? ph : ph ^ 1);
     return;
   }
-  uint4 v[NV];
+
+  // ---- the arithmetic warps ----
   const uint32_t ni = neg_inf_word<KIND>();
+  const uint4* const places = reinterpret_cast<const uint4*>(ring);
+  long long y_next = first < rows ? p.y[first] : -1;
+  for (int64_t row = first; row < rows; row += step) {
+    const long long y = y_next;
+    if (row + step < rows) y_next = p.y[row + step];
+    const Row<KIND> r(p.z + row * p.ldz * B, p.V);
+    char* drow = p.dz + row * p.lddz * B;
+    const bool same = same_alignment(r, drow);
+    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = (nw + chunk - 1) / chunk, n = K <= N ? K : N - 2, x = K - n;
+    if (y < 0) {
+      for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      if (tid == 0) {
+        if (q.logp) q.logp[row] = 0.f;
+        if (q.entropy) q.entropy[row] = 0.f;
+        q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      continue;
+    }
+    // the entries outside the whole granules: one per lane of the first warp at most
+    int edge = -1;
+    float xe = 0.f;
+    if (warp == 0) {
+      const int h = min(p.V, wa * E - r.mis * wa), t0 = max(h, wb * E - r.mis);
+      if (lane < h) edge = lane;
+      else if (lane >= 16 && t0 + lane - 16 < p.V) edge = t0 + lane - 16;
+      if (edge >= 0) xe = ld_real<KIND>(r.base + (int64_t)(r.mis + edge) * B);
+    }
+    float zy = 0.f, old = 0.f, adv = 0.f, wt = 0.f, ref = 0.f;
+    if (warp == W - 1) {
+      zy = target_logit<KIND>(p, row, y);
+      old = q.old_logp[row]; adv = q.adv[row]; wt = q.weight[row];
+      if (q.ref_logp) ref = q.ref_logp[row];
+    }
+    // ---- sums ----
+    WarpSums a;
+    a.base = a.thr = TK_LOWEST; a.nm = -TK_LOWEST; a.delta = 0.f; a.clamp = ni; a.fast = false; a.s2 = a.t2 = pk2(0.f, 0.f);
+    int rs = s;
+    for (int j = 0; j < K; ++j) {
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph));
+      if (!ok) { bad = 1; break; }
+      if (j == x) rs = s;
+      const int id = j < x ? n + j : j - x, len = min(chunk, nw - id * chunk);
+      const uint4* place = places + s * chunk + tid;
+      uint4 v[2];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int g = g0 + (int)threadIdx.x + i * THREADS;
-    v[i] = make_uint4(ni, ni, ni, ni);
-    if (g < g1) v[i] = r.load(g);
-  }
-  const float zy = target_logit<KIND>(p, row, y);
-  const float old = q.old_logp[row], A = q.adv[row], w = q.weight[row], ref = q.ref_logp ? q.ref_logp[row] : 0.f;
-  Triple a;
-  a.m = batch_max<KIND, NV>(v); a.s = a.t = 0.f;
-  accumulate<KIND, NV>(a, v, p.k);
-  row_combine<THREADS>(a, p.k, C, sh);
-  const RowStat st = row_stat(a, zy, p.inv_tau);
-  const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, A, w, q);
-  if (rank == 0 && threadIdx.x == 0) {
-    if (q.logp) q.logp[row] = st.logp;
-    if (q.entropy) q.entropy[row] = st.H;
-    q.terms[row] = o.terms;
-  }
-  const float sc = q.grad_scale * p.inv_tau;
-  GradCoef gc; gc.M = st.M; gc.k = p.k; gc.ls2 = st.ls2;
-  gc.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; gc.c1 = -o.h * TK_LN2 * sc;
+      for (int u = 0; u < 2; ++u) {
+        v[u] = make_uint4(ni, ni, ni, ni);
+        if (tid + u * threads < len) v[u] = place[u * threads];
+      }
+      if (j < x) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[s]);
+      }
+      if (++s == N) { s = 0; ph ^= 1; }
+      add_chunk<KIND>(a, v, geo, p.k);
+    }
+    Triple c;
+    {
+      const float2 s2 = upk2(a.s2), t2 = upk2(a.t2);
+      c.m = a.base; c.s = s2.x + s2.y; c.t = t2.x + t2.y;
+      const float f = ex2(-a.delta);
+      c.t = f * fmaf(c.s, -a.delta, c.t); c.s *= f;
+      if (edge >= 0) {
+        Triple b; b.m = fmaxf(xe, TK_LOWEST); b.s = xe == -INFINITY ? 0.f : xe - xe + 1.f; b.t = 0.f;      // NaN and inf give NaN
+        const float m = fmaxf(c.m, b.m);
+        rebase(c, m, p.k); rebase(b, m, p.k);
+        c.s += b.s; c.t += b.t;
+      }
+      warp_combine(c, p.k);
+    }
+    if (lane == 0) sums[warp] = make_float4(c.m, c.s, c.t, 0.f);
+    bar_sync_n(1, threads);
+    const bool stop = bad != 0;      // nobody sets it between the two barriers, so that all warps stop together
+    if (warp == W - 1) {
+      c.m = TK_LOWEST; c.s = c.t = 0.f;
+      if (lane < W) { const float4 o = sums[lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
+      warp_combine(c, p.k);
+      const RowStat st = row_stat(c, zy, p.inv_tau);
+      const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, adv, wt, q);
+      if (lane == 0) {
+        const float sc = q.grad_scale * p.inv_tau;
+        RowGrad h;
+        h.M = st.M; h.ls2 = st.ls2; h.nb = fmaf(-st.M, p.k, -st.ls2);
+        h.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; h.c1 = -o.h * TK_LN2 * sc;
+        h.target = o.g * sc; h.zy = zy;
+        // the thread that writes the target's granule (an edge entry: the lane that has it)
+        const int l = y < p.V ? (r.mis + (int)y) / E - wa : -1;
+        h.owner = l >= 0 && l < nw ? (l % chunk) % threads : -1;
+        handed = h;
+        if (q.logp) q.logp[row] = st.logp;
+        if (q.entropy) q.entropy[row] = st.H;
+        q.terms[row] = o.terms;
+      }
+      __syncwarp();
+    }
+    bar_sync_n(1, threads);
+    ok = !stop;
+    if (stop) break;
+    // ---- gradient ----
+    const RowGrad h = handed;
+    const bool fast = KIND != LS_F32 && fabsf(h.M) < 1e30f;
+    if (edge >= 0) {
+      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.c0; gc.c1 = h.c1;
+      st_real<KIND>(drow + (int64_t)edge * B, grad_target<KIND, ENT>(xe, gc, edge == y ? h.target : 0.f));
+    }
+    for (int j = 0; j < K; ++j) {
+      int at = rs + j;
+      if (j < n) { if (at >= N) at -= N; }
+      else {
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph));
+        if (!ok) { bad = 1; break; }
+        at = s;
+        if (++s == N) { s = 0; ph ^= 1; }
+      }
+      const int len = min(chunk, nw - j * chunk), g0 = wa + j * chunk;
+      const uint4* place = places + at * chunk + tid;
+      uint4 v[2];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int g = g0 + (int)threadIdx.x + i * THREADS;
-    if (g < g1) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+      for (int u = 0; u < 2; ++u)
+        if (tid + u * threads < len) v[u] = place[u * threads];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[at]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int l = tid + u * threads;
+        if (l < len) {
+          const uint4 o = fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k);
+          if (same) st_stream(reinterpret_cast<uint4*>(drow - r.mis * B) + g0 + l, o);
+          else store_entries<KIND>(drow, r.mis, p.V, g0 + l, o);
+        }
+      }
+    }
+    // the target's entry once more, by the thread that wrote its granule
+    if (tid == h.owner) {
+      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.c0; gc.c1 = h.c1;
+      st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(h.zy, gc, h.target));
+    }
   }
-  // the target's entry once more, by the thread that wrote its granule
-  const int gy = y < p.V ? (r.mis + (int)y) / Gran<KIND>::E : -1;
-  if (gy >= g0 && gy < g1 && (gy - g0) % THREADS == (int)threadIdx.x)
-    st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
+  // a wait that ran out of its bound (nothing this kernel does leads there): the loss says so
+  if (!ok && tid == 0) { const float n = __int_as_float(0x7fc00000); q.terms[first] = make_float4(n, n, n, n); }
 }
 
 // Deterministic sum of the rows' terms by one block: stats = loss, policy, KL, entropy, clipped weight.

@@ -1,5 +1,7 @@
 // Host side of the operators around the optimizer step: argument checks, launch shapes, workspace layout.
 #include <cmath>
+#include <cstdio>
+#include <cstdlib>
 #include <cstring>
 
 #include "../../include/tgrad.h"
@@ -126,46 +128,54 @@ tgrad_status norm_impl(const tgrad_tensor* grads, int32_t n, float max_norm, flo
   return small ? scale_slices<kListSmall>(grads, n, d_out + 1, st) : scale_slices<kListLarge>(grads, n, d_out + 1, st);
 }
 
-template <int CAP>
+// One launch per storage and CAP tensors.
+template <int KIND, bool MASTER, int CAP>
 tgrad_status adamw_slices(const tgrad_adamw_tensor* list, int32_t n, const AdamwScalars& a, cudaStream_t st) {
+  constexpr int b = KIND == LS_C64 ? 8 : KIND == LS_F32 ? 4 : 2, vl = KIND == LS_C64 ? 2 : 4, mb = KIND == LS_C64 ? 8 : 4;
+  const int32_t dtype = KIND == LS_C64 ? TGRAD_C64 : KIND == LS_F32 ? TGRAD_R32 : KIND == LS_F16 ? TGRAD_R16H : TGRAD_R16B;
   const int sm = sm_count();
-  for (int base = 0; base < n; base += CAP) {
+  for (int i = 0; i < n;) {
     AdamwParams<CAP> p;
-    p.n = n - base < CAP ? n - base : CAP;
+    p.n = 0;
     uint64_t entries = 0;
-    for (int i = 0; i < p.n; ++i) {
-      const tgrad_adamw_tensor& t = list[base + i];
-      const int kind = t.dtype == TGRAD_C64 ? LS_C64 : t.dtype == TGRAD_R32 ? LS_F32 : t.dtype == TGRAD_R16H ? LS_F16 : LS_BF16;
-      const int b = kind == LS_C64 ? 8 : kind == LS_F32 ? 4 : 2, vl = kind == LS_C64 ? 2 : 4, mb = kind == LS_C64 ? 8 : 4;
-      AdamwEntry& e = p.e[i];
+    for (; i < n && p.n < CAP; ++i) {
+      const tgrad_adamw_tensor& t = list[i];
+      if (t.dtype != dtype || (t.d_master != nullptr) != MASTER || t.numel == 0) continue;
+      AdamwEntry& e = p.e[p.n];
       e.w = static_cast<char*>(t.d_weight); e.g = static_cast<const char*>(t.d_grad);
       e.m = static_cast<float*>(t.d_exp_avg); e.v = t.d_exp_avg_sq; e.master = t.d_master;
-      e.count = (uint64_t)t.numel | ((uint64_t)kind << 62);
-      p.head[i] = 255;
+      e.count = (uint64_t)t.numel;
+      p.head[p.n] = 255;
       for (int h = vl - 1; h >= 0; --h)
         if (!misaligned(e.w + h * b, vl * b) && !misaligned(e.g + h * b, vl * b) && !misaligned(reinterpret_cast<char*>(e.m) + h * mb, vl * mb) &&
-            !misaligned(e.v + h, vl * 4) && (!e.master || !misaligned(e.master + h, vl * 4)))
-          p.head[i] = (uint8_t)h;
-      entries += (uint64_t)t.numel;
+            !misaligned(e.v + h, vl * 4) && (!MASTER || !misaligned(e.master + h, vl * 4)))
+          p.head[p.n] = (uint8_t)h;
+      entries += e.count;
+      ++p.n;
     }
+    if (p.n == 0) continue;
     // chunks of 4096 entries (two vectors of four per thread and turn), fewer where there would be too few of them
     uint32_t lg = 12;
     while (lg > 9 && (entries >> lg) < (uint64_t)sm * 8) --lg;
     while ((entries >> lg) > ((uint64_t)1 << 31)) ++lg;
     p.epc_log2 = lg;
     uint64_t at = 0;
-    for (int i = 0; i < p.n; ++i) {
-      p.first[i] = (uint32_t)at;
-      at += ((uint64_t)list[base + i].numel + (1ull << lg) - 1) >> lg;
+    for (int t = 0; t < p.n; ++t) {
+      p.first[t] = (uint32_t)at;
+      at += (p.e[t].count + (1ull << lg) - 1) >> lg;
     }
     p.first[p.n] = p.total = (uint32_t)at;
-    if (at == 0) continue;
     uint64_t grid = (uint64_t)sm * 8;
     if (grid > at) grid = at;
-    launch_chained(list_adamw_kernel<CAP>, dim3((unsigned)grid), dim3(LS_THREADS), 0, st, p, a);
+    launch_chained(list_adamw_kernel<KIND, MASTER, CAP>, dim3((unsigned)grid), dim3(LS_THREADS), 0, st, p, a);
     TG_LAUNCH_CHECK();
   }
   return TGRAD_OK;
+}
+template <int KIND, bool MASTER>
+tgrad_status adamw_kind(int count, const tgrad_adamw_tensor* list, int32_t n, const AdamwScalars& a, cudaStream_t st) {
+  if (count == 0) return TGRAD_OK;
+  return count <= kAdamwSmall ? adamw_slices<KIND, MASTER, kAdamwSmall>(list, n, a, st) : adamw_slices<KIND, MASTER, kAdamwLarge>(list, n, a, st);
 }
 
 // ---- rows of logits ----
@@ -198,14 +208,19 @@ TokenArgs token_args(const tgrad_logits* in, void* d_dlogits, int64_t stride) {
   a.k = (float)(1.4426950408889634 / (double)in->temperature);
   return a;
 }
-// most granules that a row can touch, whatever its alignment
-inline int64_t max_granules(int64_t vocab, int kind) { const int e = kind == LS_F32 ? 4 : 8; return (vocab + 2 * (e - 1)) / e; }
+// most granules that a row of these logits touches: rows whose stride is a multiple of 16 bytes all lie alike
+inline int64_t max_granules(const tgrad_logits* in) {
+  const int kind = token_kind(in->dtype), b = kind == LS_F32 ? 4 : 2, e = 16 / b;
+  const int64_t mis = (int64_t)(reinterpret_cast<uintptr_t>(in->d_logits) & 15) / b;
+  if (in->rows <= 1 || in->row_stride * b % 16 == 0) return (mis + in->vocab + e - 1) / e;
+  return (in->vocab + 2 * (e - 1)) / e;
+}
 
 template <bool POLICY>
 tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a, const ForwardArgs& f, const PolicyArgs& q, cudaStream_t st) {
   // blocks per row: one while the rows alone fill the GPU, more (of at least one batch of loads each) where they do not
   const int sm = sm_count();
-  const int64_t g = max_granules(in->vocab, kind);
+  const int64_t g = max_granules(in);
   int C = 1;
   while (C < TK_MAX_CLUSTER && in->rows * C < (int64_t)4 * sm && g > (int64_t)C * TF_THREADS * 4) C *= 2;
   const dim3 grid((unsigned)(in->rows * C));
@@ -218,7 +233,7 @@ tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a
 
 template <bool ENT>
 tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
-  const int64_t pieces = (max_granules(in->vocab, kind) + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
+  const int64_t pieces = (max_granules(in) + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
   if (in->rows * pieces >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(in->rows * pieces));
   if (kind == LS_F32) launch_chained(token_backward_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
@@ -228,34 +243,38 @@ tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& 
   return TGRAD_OK;
 }
 
-// The one-pass policy kernel: C blocks of THREADS threads with eight granules each hold a row.
-struct HoldPlan { int threads, C; };
-HoldPlan hold_plan(int64_t granules) {
-  const int sizes[4] = {128, 256, 512, 1024};
-  for (int i = 0; i < 4; ++i)
-    for (int C = 1; C <= TK_MAX_CLUSTER; C *= 2) {
-      // blocks of 256 threads, four to an SM, are preferred; a row that eight of them cannot hold takes larger ones
-      if (sizes[i] < 256 && C > 1) break;
-      if (granules <= (int64_t)sizes[i] * 8 * C) return HoldPlan{sizes[i], C};
-    }
-  return HoldPlan{0, 0};
-}
+// The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 24 arithmetic warps for all of them.
+constexpr size_t kRingBytes = 208 * 1024;
 template <int KIND, bool ENT>
-tgrad_status launch_policy(const HoldPlan& h, int64_t rows, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
-  const dim3 grid((unsigned)(rows * h.C));
-  switch (h.threads) {
-    case 128: launch_cluster(policy_row_kernel<KIND, 128, ENT>, grid, dim3(128), 0, h.C, st, a, q, h.C); break;
-    case 256: launch_cluster(policy_row_kernel<KIND, 256, ENT>, grid, dim3(256), 0, h.C, st, a, q, h.C); break;
-    case 512: launch_cluster(policy_row_kernel<KIND, 512, ENT>, grid, dim3(512), 0, h.C, st, a, q, h.C); break;
-    default: launch_cluster(policy_row_kernel<KIND, 1024, ENT>, grid, dim3(1024), 0, h.C, st, a, q, h.C); break;
+tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
+  const int sm = sm_count();
+  const int64_t bytes = max_granules(in) * 16;
+  RowGeom g; memset(&g, 0, sizeof(g));
+  // the smallest blocks whose share of the ring holds a row and a quarter of the next
+  const int sizes[5] = {2, 4, 8, 12, 24};
+  int per_sm = 1;
+  for (int i = 0; i < 5; ++i) {
+    g.W = sizes[i]; per_sm = g.W == 2 ? 9 : RW_MAX_WARPS / g.W;
+    if (g.W == 4) per_sm = 5;
+    if (bytes * 5 / 4 <= (int64_t)(kRingBytes / per_sm)) break;
   }
+  const size_t chunk = (size_t)g.W * 1024;
+  const int64_t places = (int64_t)(kRingBytes / per_sm / chunk);
+  g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
+  g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
+  auto kern = policy_row_kernel<KIND, ENT>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess) return TGRAD_ERR_CUDA;
+  int64_t grid = (int64_t)sm * per_sm;
+  if (grid > in->rows) grid = in->rows;
+  if (getenv("TGRAD_DBG")) printf("row W %d N %d per_sm %d\n", g.W, g.N, per_sm);
+  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), chunk * g.N, st, a, q, in->rows, g);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
 template <bool ENT>
-tgrad_status launch_policy_kind(int kind, const HoldPlan& h, int64_t rows, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
-  return kind == LS_F32 ? launch_policy<LS_F32, ENT>(h, rows, a, q, st)
-         : kind == LS_F16 ? launch_policy<LS_F16, ENT>(h, rows, a, q, st) : launch_policy<LS_BF16, ENT>(h, rows, a, q, st);
+tgrad_status launch_policy_kind(int kind, const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
+  return kind == LS_F32 ? launch_policy_row<LS_F32, ENT>(in, a, q, st)
+         : kind == LS_F16 ? launch_policy_row<LS_F16, ENT>(in, a, q, st) : launch_policy_row<LS_BF16, ENT>(in, a, q, st);
 }
 
 size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16) * 2 + align_up((size_t)rows * 8); }
@@ -303,7 +322,15 @@ tgrad_status tgrad_adamw_step(const tgrad_adamw_tensor* list, int32_t n, const t
   a.eps = (float)c->eps; a.keep = (float)(1.0 - c->lr * c->weight_decay);
   a.gscale = c->d_grad_scale;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return n <= kAdamwSmall ? adamw_slices<kAdamwSmall>(list, n, a, st) : adamw_slices<kAdamwLarge>(list, n, a, st);
+  int count[6] = {0, 0, 0, 0, 0, 0};
+  for (int i = 0; i < n; ++i)
+    if (list[i].numel > 0) ++count[list[i].dtype == TGRAD_C64 ? 0 : list[i].dtype == TGRAD_R32 ? 1 : (list[i].dtype == TGRAD_R16H ? 2 : 4) + (list[i].d_master ? 1 : 0)];
+  TG_TRY((adamw_kind<LS_C64, false>(count[0], list, n, a, st)));
+  TG_TRY((adamw_kind<LS_F32, false>(count[1], list, n, a, st)));
+  TG_TRY((adamw_kind<LS_F16, false>(count[2], list, n, a, st)));
+  TG_TRY((adamw_kind<LS_F16, true>(count[3], list, n, a, st)));
+  TG_TRY((adamw_kind<LS_BF16, false>(count[4], list, n, a, st)));
+  return adamw_kind<LS_BF16, true>(count[5], list, n, a, st);
 }
 
 tgrad_status tgrad_token_logprob(const tgrad_logits* in, float* d_logp, float* d_lse, float* d_entropy, void* cuda_stream) {
@@ -356,20 +383,14 @@ tgrad_status tgrad_policy_loss(const tgrad_logits* in, const tgrad_policy_args* 
   const int kind = token_kind(in->dtype);
   if (any) {
     const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
-    const HoldPlan h = hold_plan(max_granules(in->vocab, kind));
     const bool ent = c->entropy_coef != 0.f;
-    if (c->d_dlogits && h.threads) {
-      TG_TRY(ent ? launch_policy_kind<true>(kind, h, in->rows, a, q, st) : launch_policy_kind<false>(kind, h, in->rows, a, q, st));
+    if (c->d_dlogits) {
+      TG_TRY(ent ? launch_policy_kind<true>(kind, in, a, q, st) : launch_policy_kind<false>(kind, in, a, q, st));
     } else {
       ForwardArgs f; memset(&f, 0, sizeof(f));
       f.logp = c->d_logp; f.entropy = c->d_entropy;
       f.coef = reinterpret_cast<float4*>(ws + r16); f.stat = reinterpret_cast<float2*>(ws + 2 * r16);
       TG_TRY(launch_forward<true>(kind, in, a, f, q, st));
-      if (c->d_dlogits) {
-        BackwardArgs b; memset(&b, 0, sizeof(b));
-        b.coef = f.coef; b.stat = f.stat; b.scale = c->grad_scale;
-        TG_TRY(ent ? launch_backward<true>(kind, in, a, b, st) : launch_backward<false>(kind, in, a, b, st));
-      }
     }
   }
   launch_chained(policy_sum_kernel, dim3(1), dim3(1024), 0, st, q.terms, in->rows, c->kl_coef, c->entropy_coef, c->d_stats);
