@@ -301,7 +301,7 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
 // Policy loss, forward and backward in one pass over device memory: a block works on one row at a time, reads it once for
 // the sums and once more, from shared memory, for the gradient.
 //
-// The row's whole granules come in chunks of 64 granules per arithmetic warp, by bulk copies into a ring of N places that
+// The row's whole granules come in chunks of 128 granules per arithmetic warp, by bulk copies into a ring of N places that
 // one further warp keeps full.  Chunks that stay for the second reading are released after it; where a row has more chunks
 // than the ring has places, the ones too many go through it first, and again (from L2) at the end:
 //   asked for:  e_1 .. e_x  r_1 .. r_n  e_1 .. e_x      released in the same order, so that the ring is a queue:
@@ -313,7 +313,7 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
 // Why a block and not a cluster per row: with the row in the registers of eight blocks the exchange of the sums (3,000 to
 // 5,000 cycles between the last logit's arrival and the first gradient, most of it latency) was paid for every 32 KB
 // instead of for every row; 8192 x 131072 bf16 logits took 0.95 ms so, and 1.2 ms with the rows fetched ahead.
-constexpr int RW_MAX_WARPS = 24, RW_MAX_PLACES = 32;
+constexpr int RW_MAX_WARPS = 16, RW_MAX_PLACES = 16, RW_NV = 4;      // RW_NV: granules of a chunk per thread
 struct RowGeom {
   int W, N;              // arithmetic warps, places of the ring
   float reach, lowest;   // 200 / k; lowest value that the clamp may take in the storage type
@@ -357,16 +357,17 @@ __device__ __forceinline__ void add_granule(WarpSums& a, const uint4& v, uint64_
   }
 }
 template <int KIND>
-__device__ __forceinline__ float granule_max(const uint4& v) {
-  return max_of_word<KIND>(max_word<KIND>(max_word<KIND>(v.x, v.y), max_word<KIND>(v.z, v.w)));
-}
-template <int KIND>
-__device__ __forceinline__ void add_chunk(WarpSums& a, const uint4 (&v)[2], const RowGeom& geo, float k) {
-  const float top = fmaxf(granule_max<KIND>(v[0]), granule_max<KIND>(v[1]));
+__device__ __forceinline__ void add_chunk(WarpSums& a, const uint4 (&v)[RW_NV], const RowGeom& geo, float k) {
+  const float top = batch_max<KIND, RW_NV>(v);
   if (__any_sync(0xffffffffu, top > a.thr)) move_base<KIND>(a, top, geo, k);
   const uint64_t nm = pk2(a.nm, a.nm), kk = pk2(k, k);
-  if (a.fast) { add_granule<KIND, true>(a, v[0], nm, kk); add_granule<KIND, true>(a, v[1], nm, kk); }
-  else { add_granule<KIND, false>(a, v[0], nm, kk); add_granule<KIND, false>(a, v[1], nm, kk); }
+  if (a.fast) {
+#pragma unroll
+    for (int u = 0; u < RW_NV; ++u) add_granule<KIND, true>(a, v[u], nm, kk);
+  } else {
+#pragma unroll
+    for (int u = 0; u < RW_NV; ++u) add_granule<KIND, false>(a, v[u], nm, kk);
+  }
 }
 
 // What the row's sums give the gradient.
@@ -390,14 +391,14 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
 }
 
 template <int KIND, bool ENT>
-__global__ void __maxnreg__(72) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int64_t rows, const __grid_constant__ RowGeom geo) {
+__global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int64_t rows, const __grid_constant__ RowGeom geo) {
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ float4 sums[RW_MAX_WARPS];
   __shared__ __align__(16) RowGrad handed;
   __shared__ volatile int bad;           // a wait ran out of its bound
   __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES];
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
-  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = 2 * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     bad = 0;
     for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
@@ -486,11 +487,16 @@ __global__ void __maxnreg__(72) policy_row_kernel(const __grid_constant__ TokenA
       if (j == x) rs = s;
       const int id = j < x ? n + j : j - x, len = min(chunk, nw - id * chunk);
       const uint4* place = places + s * chunk + tid;
-      uint4 v[2];
+      uint4 v[RW_NV];
+      if (len == chunk) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        v[u] = make_uint4(ni, ni, ni, ni);
-        if (tid + u * threads < len) v[u] = place[u * threads];
+        for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
+      } else {
+#pragma unroll
+        for (int u = 0; u < RW_NV; ++u) {
+          v[u] = make_uint4(ni, ni, ni, ni);
+          if (tid + u * threads < len) v[u] = place[u * threads];
+        }
       }
       if (j < x) {
         __syncwarp();
@@ -559,20 +565,25 @@ __global__ void __maxnreg__(72) policy_row_kernel(const __grid_constant__ TokenA
       }
       const int len = min(chunk, nw - j * chunk), g0 = wa + j * chunk;
       const uint4* place = places + at * chunk + tid;
-      uint4 v[2];
+      uint4 v[RW_NV];
+      if (len == chunk && same) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (tid + u * threads < len) v[u] = place[u * threads];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[at]);
+        for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[at]);
+        uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + g0 + tid;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int l = tid + u * threads;
-        if (l < len) {
-          const uint4 o = fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k);
-          if (same) st_stream(reinterpret_cast<uint4*>(drow - r.mis * B) + g0 + l, o);
-          else store_entries<KIND>(drow, r.mis, p.V, g0 + l, o);
-        }
+        for (int u = 0; u < RW_NV; ++u)
+          st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
+      } else {
+#pragma unroll
+        for (int u = 0; u < RW_NV; ++u)
+          if (tid + u * threads < len) v[u] = place[u * threads];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[at]);
+#pragma unroll
+        for (int u = 0; u < RW_NV; ++u)
+          if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
       }
     }
     // the target's entry once more, by the thread that wrote its granule

@@ -243,23 +243,22 @@ tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& 
   return TGRAD_OK;
 }
 
-// The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 24 arithmetic warps for all of them.
-constexpr size_t kRingBytes = 208 * 1024;
+// The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 16 arithmetic warps for all of them at most.
+constexpr size_t kRingBytes = 224 * 1024;
 template <int KIND, bool ENT>
 tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
   const int sm = sm_count();
   const int64_t bytes = max_granules(in) * 16;
   RowGeom g; memset(&g, 0, sizeof(g));
   // the smallest blocks whose share of the ring holds a row and a quarter of the next
-  const int sizes[5] = {2, 4, 8, 12, 24};
+  const int warps[4] = {2, 4, 8, 16}, blocks[4] = {6, 4, 2, 1};
   int per_sm = 1;
-  for (int i = 0; i < 5; ++i) {
-    g.W = sizes[i]; per_sm = g.W == 2 ? 9 : RW_MAX_WARPS / g.W;
-    if (g.W == 4) per_sm = 5;
-    if (bytes * 5 / 4 <= (int64_t)(kRingBytes / per_sm)) break;
+  for (int i = 0; i < 4; ++i) {
+    g.W = warps[i]; per_sm = blocks[i];
+    if (bytes * 5 / 4 <= (int64_t)((kRingBytes + 1024 - 2560 * per_sm) / per_sm)) break;
   }
-  const size_t chunk = (size_t)g.W * 1024;
-  const int64_t places = (int64_t)(kRingBytes / per_sm / chunk);
+  const size_t chunk = (size_t)g.W * 32 * RW_NV * 16;
+  const int64_t places = (int64_t)((kRingBytes + 2560 - 2560 * per_sm) / per_sm / chunk);      // a block's own shared memory: 2.5 KB
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
   g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
   auto kern = policy_row_kernel<KIND, ENT>;
