@@ -313,12 +313,34 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
 // Why a block and not a cluster per row: with the row in the registers of eight blocks the exchange of the sums (3,000 to
 // 5,000 cycles between the last logit's arrival and the first gradient, most of it latency) was paid for every 32 KB
 // instead of for every row; 8192 x 131072 bf16 logits took 0.95 ms so, and 1.2 ms with the rows fetched ahead.
-constexpr int RW_MAX_WARPS = 16, RW_MAX_PLACES = 16, RW_NV = 4;      // RW_NV: granules of a chunk per thread
+constexpr int RW_MAX_WARPS = 16, RW_MAX_PLACES = 16, RW_JOBS = 4, RW_NV = 4;      // RW_NV: granules of a chunk per thread
 struct RowGeom {
   int W, N;              // arithmetic warps, places of the ring
+  int unit;              // rows that a block takes at a time
   float reach, lowest;   // 200 / k; lowest value that the clamp may take in the storage type
   float slack;           // 40 / k
 };
+
+// Work distribution by the hardware's queue of blocks: a running block takes over one that has not been started.  The
+// answer is 16 bytes in shared memory, counted on an mbarrier; once it was "none left", no further block may be asked for.
+__device__ __forceinline__ void next_block_ask(uint4* answer, uint64_t* bar) {
+  fence_async_smem();
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ int next_block_get(const uint4* answer) {      // its index, or -1
+  const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(answer);
+  uint32_t some, x;
+  asm volatile(
+      "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t"
+      "mov.b128 r, {%2, %3};\n\t"
+      "mov.b32 %1, 0;\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(some), "=r"(x) : "l"(a.x), "l"(a.y) : "memory");
+  return some ? (int)x : -1;
+}
 
 __device__ __forceinline__ void bar_sync_n(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
@@ -396,31 +418,38 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
   __shared__ float4 sums[RW_MAX_WARPS];
   __shared__ __align__(16) RowGrad handed;
   __shared__ volatile int bad;           // a wait ran out of its bound
-  __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES];
+  __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES], jfull[RW_JOBS], jempty[RW_JOBS], nbar;
+  __shared__ __align__(16) uint4 answer;
+  __shared__ longlong2 job[RW_JOBS];     // unit of rows (-1: no more), target of its first row
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
   const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     bad = 0;
     for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
+    for (int i = 0; i < RW_JOBS; ++i) { mbar_init(&jfull[i], 1); mbar_init(&jempty[i], W); }
+    mbar_init(&nbar, 1);
     fence_mbar_init();
   }
   __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t first = blockIdx.x, step = gridDim.x;
-  int s = 0;
-  uint32_t ph = 0;
+  int s = 0, js = 0;
+  uint32_t ph = 0, jph = 0;
   bool ok = true;
 
   if (warp == W) {
     // ---- the fetching warp ----
-    uint32_t used = 0;
-    for (int64_t r0 = first; r0 < rows && ok; r0 += 32 * step) {
-      const int64_t mine = r0 + lane * step;
-      uint32_t live = __ballot_sync(0xffffffffu, mine < rows && p.y[mine < rows ? mine : r0] >= 0);
+    uint32_t used = 0, nph = 0;
+    for (int64_t unit = blockIdx.x; ok;) {
+      if (lane == 0) next_block_ask(&answer, &nbar);
+      const int64_t r0 = unit * geo.unit, mine = r0 + lane;
+      const long long ym = lane < geo.unit && mine < rows ? p.y[mine] : -1;
+      uint32_t live = __ballot_sync(0xffffffffu, ym >= 0);
       if (lane == 0) {
+        ok = mbar_wait_bounded(&jempty[js], jph ^ 1);
+        if (ok) { job[js] = make_longlong2(unit, ym); mbar_arrive(&jfull[js]); }
         for (; live && ok; live &= live - 1) {
-          const Row<KIND> r(p.z + (r0 + (__ffs(live) - 1) * step) * p.ldz * B, p.V);
+          const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
           const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = K <= N ? K : N - 2;
           for (int j = 0; j < 2 * K - n && ok; ++j) {
             const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
@@ -433,8 +462,16 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
           }
         }
       }
+      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
+      // (the answer is taken, after a failure too, before the block may end)
+      const bool got = __all_sync(0xffffffffu, mbar_wait_bounded(&nbar, nph));
+      nph ^= 1;
+      unit = got ? next_block_get(&answer) : -1;
+      __syncwarp();
       ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+      if (unit < 0) break;
     }
+    if (lane == 0 && ok && mbar_wait_bounded(&jempty[js], jph ^ 1)) { job[js] = make_longlong2(-1, 0); mbar_arrive(&jfull[js]); }
     // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
     if (lane == 0)
       for (int i = 0; i < N; ++i)
@@ -445,10 +482,22 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
   // ---- the arithmetic warps ----
   const uint32_t ni = neg_inf_word<KIND>();
   const uint4* const places = reinterpret_cast<const uint4*>(ring);
-  long long y_next = first < rows ? p.y[first] : -1;
-  for (int64_t row = first; row < rows; row += step) {
+  int64_t row = 0, row_end = 0;
+  long long y_next = -1;
+  for (;; ++row) {
+    if (row == row_end) {      // the next unit of rows
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&jfull[js], jph));
+      if (!ok) break;          // (the fetching warp has stopped: no warp gets another unit)
+      const longlong2 jb = job[js];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&jempty[js]);
+      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
+      if (jb.x < 0) break;
+      row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
+      y_next = jb.y;
+    }
     const long long y = y_next;
-    if (row + step < rows) y_next = p.y[row + step];
+    if (row + 1 < row_end) y_next = p.y[row + 1];
     const Row<KIND> r(p.z + row * p.ldz * B, p.V);
     char* drow = p.dz + row * p.lddz * B;
     const bool same = same_alignment(r, drow);
@@ -593,7 +642,7 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
     }
   }
   // a wait that ran out of its bound (nothing this kernel does leads there): the loss says so
-  if (!ok && tid == 0) { const float n = __int_as_float(0x7fc00000); q.terms[first] = make_float4(n, n, n, n); }
+  if (!ok && tid == 0) { const float n = __int_as_float(0x7fc00000); q.terms[(int64_t)blockIdx.x * geo.unit] = make_float4(n, n, n, n); }
 }
 
 // Deterministic sum of the rows' terms by one block: stats = loss, policy, KL, entropy, clipped weight.

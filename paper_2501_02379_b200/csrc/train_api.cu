@@ -263,9 +263,13 @@ tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const
   g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
   auto kern = policy_row_kernel<KIND, ENT>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess) return TGRAD_ERR_CUDA;
-  int64_t grid = (int64_t)sm * per_sm;
-  if (grid > in->rows) grid = in->rows;
-  if (getenv("TGRAD_DBG")) printf("row W %d N %d per_sm %d\n", g.W, g.N, per_sm);
+  // units of about 64 KB of logits, at most a warp's width of rows, and several for every block
+  int64_t unit = (64 << 10) / bytes;
+  if (unit > 32) unit = 32;
+  const int64_t fair = in->rows / ((int64_t)sm * per_sm * 4);
+  if (unit > fair) unit = fair;
+  g.unit = (int)(unit < 1 ? 1 : unit);
+  const int64_t grid = (in->rows + g.unit - 1) / g.unit;
   launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), chunk * g.N, st, a, q, in->rows, g);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
