@@ -277,7 +277,6 @@ struct PolicyArgs {
   const float* old_logp; const float* ref_logp; const float* adv; const float* weight;   // ref_logp may be null
   float low, high;           // bounds of the ratio
   float kl_coef, ent_coef, grad_scale;
-  float* logp; float* entropy;             // out, may be null
   float4* terms;                           // out: weighted policy, KL, entropy and clipping terms of each row
 };
 struct PolicyToken { float g, h; float4 terms; };
@@ -412,10 +411,25 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int KIND, bool ENT>
-__global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, int64_t rows, const __grid_constant__ RowGeom geo) {
+struct ForwardArgs {
+  float* logp; float* lse; float* entropy;      // out, may be null
+  float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
+};
+// MODE: RW_FORWARD log-probabilities only (every chunk goes through the ring once, and the last warp's work on a row
+// overlaps with the others' on the next), RW_POLICY the policy loss with its gradient, RW_ENTROPY with an entropy bonus.
+enum { RW_FORWARD = 0, RW_POLICY = 1, RW_ENTROPY = 2 };
+__device__ __forceinline__ void store_stat(const ForwardArgs& f, int64_t row, const RowStat& st) {
+  if (f.logp) f.logp[row] = st.logp;
+  if (f.lse) f.lse[row] = st.lse;
+  if (f.entropy) f.entropy[row] = st.H;
+  if (f.stat) f.stat[row] = make_float2(st.M, st.ls2);
+}
+template <int KIND, int MODE>
+__global__ void __maxnreg__(96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
+                                                  int64_t rows, const __grid_constant__ RowGeom geo) {
+  constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
   extern __shared__ __align__(128) unsigned char ring[];
-  __shared__ float4 sums[RW_MAX_WARPS];
+  __shared__ float4 sums[2][RW_MAX_WARPS];
   __shared__ __align__(16) RowGrad handed;
   __shared__ volatile int bad;           // a wait ran out of its bound
   __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES], jfull[RW_JOBS], jempty[RW_JOBS], nbar;
@@ -450,8 +464,8 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
         if (ok) { job[js] = make_longlong2(unit, ym); mbar_arrive(&jfull[js]); }
         for (; live && ok; live &= live - 1) {
           const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
-          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = K <= N ? K : N - 2;
-          for (int j = 0; j < 2 * K - n && ok; ++j) {
+          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = !BACK ? 0 : K <= N ? K : N - 2;
+          for (int j = 0; j < (BACK ? 2 * K - n : K) && ok; ++j) {
             const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
             ok = mbar_wait_bounded(&empty[s], ph ^ 1);
             if (!ok) break;
@@ -484,6 +498,7 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
   const uint4* const places = reinterpret_cast<const uint4*>(ring);
   int64_t row = 0, row_end = 0;
   long long y_next = -1;
+  int side = 0;      // of the double-buffered sums
   for (;; ++row) {
     if (row == row_end) {      // the next unit of rows
       ok = __all_sync(0xffffffffu, mbar_wait_bounded(&jfull[js], jph));
@@ -501,13 +516,14 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
     const Row<KIND> r(p.z + row * p.ldz * B, p.V);
     char* drow = p.dz + row * p.lddz * B;
     const bool same = same_alignment(r, drow);
-    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = (nw + chunk - 1) / chunk, n = K <= N ? K : N - 2, x = K - n;
+    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = (nw + chunk - 1) / chunk, n = !BACK ? 0 : K <= N ? K : N - 2, x = K - n;
     if (y < 0) {
-      for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      if (BACK)
+        for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
       if (tid == 0) {
-        if (q.logp) q.logp[row] = 0.f;
-        if (q.entropy) q.entropy[row] = 0.f;
-        q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+        RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+        store_stat(f, row, none);
+        if (BACK) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
       continue;
     }
@@ -523,8 +539,10 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
     float zy = 0.f, old = 0.f, adv = 0.f, wt = 0.f, ref = 0.f;
     if (warp == W - 1) {
       zy = target_logit<KIND>(p, row, y);
-      old = q.old_logp[row]; adv = q.adv[row]; wt = q.weight[row];
-      if (q.ref_logp) ref = q.ref_logp[row];
+      if (BACK) {
+        old = q.old_logp[row]; adv = q.adv[row]; wt = q.weight[row];
+        if (q.ref_logp) ref = q.ref_logp[row];
+      }
     }
     // ---- sums ----
     WarpSums a;
@@ -568,14 +586,17 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
       }
       warp_combine(c, p.k);
     }
-    if (lane == 0) sums[warp] = make_float4(c.m, c.s, c.t, 0.f);
+    side ^= 1;
+    if (lane == 0) sums[side][warp] = make_float4(c.m, c.s, c.t, 0.f);
     bar_sync_n(1, threads);
     const bool stop = bad != 0;      // nobody sets it between the two barriers, so that all warps stop together
     if (warp == W - 1) {
       c.m = TK_LOWEST; c.s = c.t = 0.f;
-      if (lane < W) { const float4 o = sums[lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
+      if (lane < W) { const float4 o = sums[side][lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
       warp_combine(c, p.k);
       const RowStat st = row_stat(c, zy, p.inv_tau);
+      if (lane == 0) store_stat(f, row, st);
+      if (BACK) {
       const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, adv, wt, q);
       if (lane == 0) {
         const float sc = q.grad_scale * p.inv_tau;
@@ -587,11 +608,15 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
         const int l = y < p.V ? (r.mis + (int)y) / E - wa : -1;
         h.owner = l >= 0 && l < nw ? (l % chunk) % threads : -1;
         handed = h;
-        if (q.logp) q.logp[row] = st.logp;
-        if (q.entropy) q.entropy[row] = st.H;
         q.terms[row] = o.terms;
       }
       __syncwarp();
+      }
+    }
+    if (!BACK) {
+      // (the next row's sums go to the other side, and nobody passes its barrier before the last warp has read this one's)
+      if (stop) { ok = false; break; }
+      continue;
     }
     bar_sync_n(1, threads);
     ok = !stop;
@@ -642,7 +667,12 @@ __global__ void __maxnreg__(96) policy_row_kernel(const __grid_constant__ TokenA
     }
   }
   // a wait that ran out of its bound (nothing this kernel does leads there): the loss says so
-  if (!ok && tid == 0) { const float n = __int_as_float(0x7fc00000); q.terms[(int64_t)blockIdx.x * geo.unit] = make_float4(n, n, n, n); }
+  if (!ok && tid == 0) {
+    const float n = __int_as_float(0x7fc00000);
+    if (BACK) q.terms[(int64_t)blockIdx.x * geo.unit] = make_float4(n, n, n, n);
+    RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = n;
+    store_stat(f, (int64_t)blockIdx.x * geo.unit, none);
+  }
 }
 
 // Deterministic sum of the rows' terms by one block: stats = loss, policy, KL, entropy, clipped weight.
@@ -672,14 +702,8 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(const float4* __restri
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Forward pass over a row that is not kept: C blocks stream it with running triples.
-struct ForwardArgs {
-  float* logp; float* lse; float* entropy;      // out, may be null
-  float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
-  float4* coef;                                 // policy: out (M, log2 S, g, g + h H ...), see below
-};
+// Forward pass over a few rows: C blocks stream a row with running triples.  POLICY: the rows' loss terms too.
 constexpr int TF_THREADS = 256;
-// POLICY: the rows' loss terms and gradient coefficients too (rows that are too long to be kept in registers).
 template <int KIND, bool POLICY>
 __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ ForwardArgs f,
                                                                       const __grid_constant__ PolicyArgs q, int C) {
@@ -694,11 +718,9 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   if (C > 1) cluster_wait();
   if (y < 0) {
     if (rank == 0 && threadIdx.x == 0) {
-      if (f.logp) f.logp[row] = 0.f;
-      if (f.lse) f.lse[row] = 0.f;
-      if (f.entropy) f.entropy[row] = 0.f;
-      if (f.stat) f.stat[row] = make_float2(0.f, 0.f);
-      if (POLICY) { f.coef[row] = make_float4(0.f, 0.f, 0.f, 0.f); q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f); }
+      RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+      store_stat(f, row, none);
+      if (POLICY) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     return;
   }
@@ -721,16 +743,8 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   row_combine<TF_THREADS>(a, p.k, C, sh);
   if (rank != 0 || threadIdx.x != 0) return;
   const RowStat st = row_stat(a, zy, p.inv_tau);
-  if (f.logp) f.logp[row] = st.logp;
-  if (f.lse) f.lse[row] = st.lse;
-  if (f.entropy) f.entropy[row] = st.H;
-  if (f.stat) f.stat[row] = make_float2(st.M, st.ls2);
-  if (POLICY) {
-    const PolicyToken o = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q);
-    q.terms[row] = o.terms;
-    f.stat[row] = make_float2(st.M, st.ls2);
-    f.coef[row] = make_float4(o.g, o.h, st.H, 0.f);
-  }
+  store_stat(f, row, st);
+  if (POLICY) q.terms[row] = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q).terms;
 }
 
 // Gradient pass: one block per piece of NV * THREADS granules of a row.
@@ -740,7 +754,6 @@ struct BackwardArgs {
   const float* g;            // d loss / d logp
   const float* h;            // d loss / d entropy, or null
   const float* entropy;      // with h
-  const float4* coef;        // (g, h, H, -) instead of the three
   float scale;
 };
 constexpr int TB2_THREADS = 256;
@@ -768,8 +781,8 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __
     if (g < g1) v[i] = r.load(g);
   }
   float gg, hh = 0.f, H = 0.f;
-  if (b.coef) { const float4 c = b.coef[row]; gg = c.x; hh = c.y; H = c.z; }
-  else { gg = b.g[row]; if (ENT) { hh = b.h[row]; H = b.entropy[row]; } }
+  gg = b.g[row];
+  if (ENT) { hh = b.h[row]; H = b.entropy[row]; }
   const float sc = b.scale * p.inv_tau;
   GradCoef gc; gc.k = p.k;
   if (b.stat) { const float2 s = b.stat[row]; gc.M = s.x; gc.ls2 = s.y; }

@@ -1,7 +1,5 @@
 // Host side of the operators around the optimizer step: argument checks, launch shapes, workspace layout.
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 #include <cstring>
 
 #include "../../include/tgrad.h"
@@ -245,8 +243,8 @@ tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& 
 
 // The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 16 arithmetic warps for all of them at most.
 constexpr size_t kRingBytes = 224 * 1024;
-template <int KIND, bool ENT>
-tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
+template <int KIND, int MODE>
+tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
   const int sm = sm_count();
   const int64_t bytes = max_granules(in) * 16;
   RowGeom g; memset(&g, 0, sizeof(g));
@@ -255,13 +253,14 @@ tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const
   int per_sm = 1;
   for (int i = 0; i < 4; ++i) {
     g.W = warps[i]; per_sm = blocks[i];
+    if (MODE == RW_FORWARD && g.W == 4) break;      // (nothing stays: blocks of four warps whatever the row's length)
     if (bytes * 5 / 4 <= (int64_t)((kRingBytes + 1024 - 2560 * per_sm) / per_sm)) break;
   }
   const size_t chunk = (size_t)g.W * 32 * RW_NV * 16;
   const int64_t places = (int64_t)((kRingBytes + 2560 - 2560 * per_sm) / per_sm / chunk);      // a block's own shared memory: 2.5 KB
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
   g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
-  auto kern = policy_row_kernel<KIND, ENT>;
+  auto kern = token_row_kernel<KIND, MODE>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess) return TGRAD_ERR_CUDA;
   // units of about 64 KB of logits, at most a warp's width of rows, and several for every block
   int64_t unit = (64 << 10) / bytes;
@@ -270,17 +269,24 @@ tgrad_status launch_policy_row(const tgrad_logits* in, const TokenArgs& a, const
   if (unit > fair) unit = fair;
   g.unit = (int)(unit < 1 ? 1 : unit);
   const int64_t grid = (in->rows + g.unit - 1) / g.unit;
-  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), chunk * g.N, st, a, q, in->rows, g);
+  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), chunk * g.N, st, a, q, f, in->rows, g);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
-template <bool ENT>
-tgrad_status launch_policy_kind(int kind, const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, cudaStream_t st) {
-  return kind == LS_F32 ? launch_policy_row<LS_F32, ENT>(in, a, q, st)
-         : kind == LS_F16 ? launch_policy_row<LS_F16, ENT>(in, a, q, st) : launch_policy_row<LS_BF16, ENT>(in, a, q, st);
+template <int MODE>
+tgrad_status launch_row_kind(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
+  const int kind = token_kind(in->dtype);
+  return kind == LS_F32 ? launch_row<LS_F32, MODE>(in, a, q, f, st)
+         : kind == LS_F16 ? launch_row<LS_F16, MODE>(in, a, q, f, st) : launch_row<LS_BF16, MODE>(in, a, q, f, st);
+}
+// Log-probabilities: several blocks on each of a few rows, the ring where the rows alone keep every block busy.
+tgrad_status launch_logprob(const tgrad_logits* in, const TokenArgs& a, const ForwardArgs& f, cudaStream_t st) {
+  PolicyArgs q; memset(&q, 0, sizeof(q));
+  if (in->rows >= (int64_t)sm_count() * 8) return launch_row_kind<RW_FORWARD>(in, a, q, f, st);
+  return launch_forward<false>(token_kind(in->dtype), in, a, f, q, st);
 }
 
-size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16) * 2 + align_up((size_t)rows * 8); }
+size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16); }
 size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + align_up((size_t)rows * 4) + align_up((size_t)pairs * 8); }
 
 }  // namespace
@@ -342,8 +348,7 @@ tgrad_status tgrad_token_logprob(const tgrad_logits* in, float* d_logp, float* d
   if (in->rows == 0) return TGRAD_OK;
   ForwardArgs f; memset(&f, 0, sizeof(f));
   f.logp = d_logp; f.lse = d_lse; f.entropy = d_entropy;
-  PolicyArgs q; memset(&q, 0, sizeof(q));
-  return launch_forward<false>(token_kind(in->dtype), in, token_args(in, nullptr, 0), f, q, static_cast<cudaStream_t>(cuda_stream));
+  return launch_logprob(in, token_args(in, nullptr, 0), f, static_cast<cudaStream_t>(cuda_stream));
 }
 
 tgrad_status tgrad_token_logprob_backward(const tgrad_logits* in, const float* d_lse, const float* d_entropy, const float* d_grad_logp,
@@ -378,23 +383,17 @@ tgrad_status tgrad_policy_loss(const tgrad_logits* in, const tgrad_policy_args* 
   if (workspace_bytes < policy_bytes(in->rows)) return TGRAD_ERR_BUFFER_TOO_SMALL;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* ws = static_cast<char*>(d_workspace);
-  const size_t r16 = align_up((size_t)in->rows * 16);
   PolicyArgs q; memset(&q, 0, sizeof(q));
   q.old_logp = c->d_old_logp; q.ref_logp = c->d_ref_logp; q.adv = c->d_advantages; q.weight = c->d_weights;
   q.low = 1.f - c->clip_low; q.high = 1.f + c->clip_high; q.kl_coef = c->kl_coef; q.ent_coef = c->entropy_coef; q.grad_scale = c->grad_scale;
-  q.logp = c->d_logp; q.entropy = c->d_entropy; q.terms = reinterpret_cast<float4*>(ws);
-  const int kind = token_kind(in->dtype);
+  q.terms = reinterpret_cast<float4*>(ws);
   if (any) {
     const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
-    const bool ent = c->entropy_coef != 0.f;
-    if (c->d_dlogits) {
-      TG_TRY(ent ? launch_policy_kind<true>(kind, in, a, q, st) : launch_policy_kind<false>(kind, in, a, q, st));
-    } else {
-      ForwardArgs f; memset(&f, 0, sizeof(f));
-      f.logp = c->d_logp; f.entropy = c->d_entropy;
-      f.coef = reinterpret_cast<float4*>(ws + r16); f.stat = reinterpret_cast<float2*>(ws + 2 * r16);
-      TG_TRY(launch_forward<true>(kind, in, a, f, q, st));
-    }
+    ForwardArgs f; memset(&f, 0, sizeof(f));
+    f.logp = c->d_logp; f.entropy = c->d_entropy;
+    if (!c->d_dlogits) TG_TRY(launch_forward<true>(token_kind(in->dtype), in, a, f, q, st));
+    else if (c->entropy_coef != 0.f) TG_TRY(launch_row_kind<RW_ENTROPY>(in, a, q, f, st));
+    else TG_TRY(launch_row_kind<RW_POLICY>(in, a, q, f, st));
   }
   launch_chained(policy_sum_kernel, dim3(1), dim3(1024), 0, st, q.terms, in->rows, c->kl_coef, c->entropy_coef, c->d_stats);
   TG_LAUNCH_CHECK();
@@ -426,12 +425,11 @@ tgrad_status tgrad_preference_loss(const tgrad_logits* in, const tgrad_preferenc
   if (any) {
     ForwardArgs f; memset(&f, 0, sizeof(f));
     f.logp = c->d_logp; f.stat = stat;
-    PolicyArgs q; memset(&q, 0, sizeof(q));
     if (c->d_dlogits) {
       launch_chained(zero_floats_kernel, dim3((unsigned)((in->rows + TP_THREADS - 1) / TP_THREADS)), dim3(TP_THREADS), 0, st, g, in->rows);
       TG_LAUNCH_CHECK();
     }
-    TG_TRY(launch_forward<false>(kind, in, a, f, q, st));
+    TG_TRY(launch_logprob(in, a, f, st));
   }
   if (c->pairs > 0) {
     PairArgs p; memset(&p, 0, sizeof(p));
