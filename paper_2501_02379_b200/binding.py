@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -210,8 +211,7 @@ def _stream_ptr(stream) -> Optional[int]:
 def _scalar_ptr(scale) -> Optional[int]:
     if scale is None:
         return None
-    import torch
-    if scale.dtype != torch.float32 or scale.numel() != 1 or not scale.is_cuda:
+    if scale.dtype is not _torch()[2] or scale.numel() != 1 or not scale.is_cuda:
         raise ValueError("a scale is an fp32 CUDA tensor of one entry")
     return scale.data_ptr()
 
@@ -360,9 +360,19 @@ def select_topk_noalloc(grad, numel: int, k: int, omega_out, values_out, half_st
 # Everything below runs on the current stream of the tensors' device, or on `stream` (a torch stream or its address).
 # Results and workspaces that a call allocates belong to that stream.
 
+_torch_types = None       # torch, {dtype: tgrad_dtype}, torch.float32
+
+
+def _torch():
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        _torch_types = (torch, {torch.float32: R32, torch.float16: R16H, torch.bfloat16: R16B, torch.complex64: C64}, torch.float32)
+    return _torch_types
+
+
 def _dtype_of(t) -> int:
-    import torch
-    d = {torch.float32: R32, torch.float16: R16H, torch.bfloat16: R16B, torch.complex64: C64}.get(t.dtype)
+    d = _torch()[1].get(t.dtype)
     if d is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
     return d
@@ -380,29 +390,44 @@ def _dense(t) -> bool:
     return True
 
 
-class _on_stream:
-    """Context: allocations and calls on `stream` of the tensors' device; enters as the stream's address."""
+def _elsewhere(index, stream) -> bool:
+    """Whether a call has to change the current device or stream first."""
+    return stream is not None or index != _torch()[0]._C._cuda_getDevice()
 
-    def __init__(self, device, stream):
-        import torch
-        self._ctx = []
-        if device.index != torch.cuda.current_device():
-            self._ctx.append(torch.cuda.device(device))
-        if stream is not None:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            self._ctx.append(torch.cuda.stream(stream))
-        self._device = device.index
 
-    def __enter__(self):
-        import torch
-        for c in self._ctx:
-            c.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self._device)
+def _there(index, stream, call, *args, **kw):
+    """call(...) with the device `index` and the stream current."""
+    torch = _torch()[0]
+    with torch.cuda.device(index):
+        if stream is None:
+            return call(*args, **kw)
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=index)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
 
-    def __exit__(self, *exc):
-        for c in reversed(self._ctx):
-            c.__exit__(*exc)
+
+def _raw_stream(index) -> int:
+    return _torch()[0]._C._cuda_getCurrentRawStream(index)
+
+
+# The argument structures as bytes (struct.pack costs a third of filling a ctypes structure).
+_pack_logits = struct.Struct("@PqqqPif").pack
+_pack_adamw = struct.Struct("@dddddqP").pack
+_pack_policy = struct.Struct("@PPPPffffffPPPPq").pack
+_pack_preference = struct.Struct("@PPifffPPPPq").pack
+_workspace_bytes = {}
+
+
+def _workspace(entry, *args) -> int:
+    b = _workspace_bytes.get((entry, args))
+    if b is None:
+        n = C.c_size_t(0)
+        _check(getattr(lib(), entry)(*args, C.byref(n)), entry)
+        if len(_workspace_bytes) > 4096:
+            _workspace_bytes.clear()
+        b = _workspace_bytes[(entry, args)] = int(n.value)
+    return b
 
 
 class TensorList:
@@ -422,17 +447,15 @@ class TensorList:
         self.array = (TgradTensor * max(n, 1))()
         for a, t in zip(self.array, self.tensors):
             a.data, a.numel, a.dtype = t.data_ptr(), t.numel(), _dtype_of(t)
-        b = C.c_size_t(0)
-        _check(lib().tgrad_grad_norm_bytes(n, C.byref(b)), "tgrad_grad_norm_bytes")
-        self.workspace_bytes = int(b.value)
+        self.address = C.addressof(self.array)
+        self.floats = 64 + (2 + n + 63) // 64 * 64 + _workspace("tgrad_grad_norm_bytes", n) // 4      # results, then the workspace
         self._adamw = None
 
     def __len__(self):
         return len(self.tensors)
 
-    def device(self):
-        import torch
-        return self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
+    def device_index(self) -> int:
+        return self.tensors[0].get_device() if self.tensors else _torch()[0].cuda.current_device()
 
 
 def _as_list(x) -> TensorList:
@@ -440,14 +463,16 @@ def _as_list(x) -> TensorList:
 
 
 def _norm_call(name, grads, max_norm, stream):
-    import torch
+    torch, _, f32 = _torch()
     grads = _as_list(grads)
-    device = grads.device()
-    with _on_stream(device, stream) as st:
-        out = torch.empty(2 + len(grads), dtype=torch.float32, device=device)
-        ws = torch.empty(grads.workspace_bytes, dtype=torch.uint8, device=device)
-        _check(getattr(lib(), name)(C.addressof(grads.array), len(grads), max_norm, out.data_ptr(), ws.data_ptr(), grads.workspace_bytes, st), name)
-    return out
+    index = grads.device_index()
+    if _elsewhere(index, stream):
+        return _there(index, stream, _norm_call, name, grads, max_norm, None)
+    n = len(grads.tensors)
+    buf = torch.empty(grads.floats, dtype=f32, device=index)
+    base, head = buf.data_ptr(), (2 + n + 63) // 64 * 64
+    _check(getattr(lib(), name)(grads.address, n, max_norm, base, base + 4 * head, 4 * (grads.floats - head), _raw_stream(index)), name)
+    return buf[:2 + n]
 
 
 def grad_norm(grads, max_norm: float = float("inf"), stream=None):
@@ -467,7 +492,7 @@ def _adamw_array(params, grads, exp_avgs, exp_avg_sqs, masters):
     lists = [params, grads, exp_avgs, exp_avg_sqs] + ([masters] if masters is not None else [])
     if len({len(x) for x in lists}) != 1:
         raise ValueError("the lists differ in length")
-    if any(x.device() != params.device() for x in lists):
+    if any(x.device_index() != params.device_index() for x in lists):
         raise ValueError("the lists live on one device")
     array = (TgradAdamwTensor * max(len(params), 1))()
     for i, a in enumerate(array[:len(params)]):
@@ -494,51 +519,54 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
     same dtype; fp32 moments).  `step` counts from 1.  `grad_scale`: device scalar that multiplies the gradients.
     `masters`: fp32 weights of 16-bit ones, which are then what is updated.  For complex weights the second moment is
     real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once."""
-    lists = [_as_list(params), _as_list(grads), _as_list(exp_avgs), _as_list(exp_avg_sqs), _as_list(masters) if masters is not None else None]
-    kept = lists[0]._adamw
-    if kept is None or any(a is not b for a, b in zip(kept[0], lists[1:])):
-        kept = lists[0]._adamw = (lists[1:], _adamw_array(*lists))
-    cfg = TgradAdamwConfig(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale))
-    with _on_stream(lists[0].device(), stream) as st:
-        _check(lib().tgrad_adamw_step(C.addressof(kept[1]), len(lists[0]), C.addressof(cfg), st), "tgrad_adamw_step")
+    lists = (_as_list(params), _as_list(grads), _as_list(exp_avgs), _as_list(exp_avg_sqs), _as_list(masters) if masters is not None else None)
+    params = lists[0]
+    kept = params._adamw
+    if kept is None or any(a is not b for a, b in zip(kept[0], lists)):
+        kept = params._adamw = (lists, _adamw_array(*lists))
+    index = params.device_index()
+    if _elsewhere(index, stream):
+        return _there(index, stream, adamw_step, *lists[:4], step, lr, beta1, beta2, eps, weight_decay, grad_scale, lists[4])
+    cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale) or 0)
+    _check(lib().tgrad_adamw_step(C.addressof(kept[1]), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
 
 
 def _logits(logits, targets, temperature):
-    """The logits' description for the library; checks what the library cannot see."""
-    import torch
+    """(the logits' description for the library, rows, vocabulary, device index); checks what the library cannot see."""
+    torch, types, _ = _torch()
     if logits.dim() != 2 or not logits.is_cuda:
         raise ValueError("logits are a CUDA tensor [rows, vocabulary]")
     rows, vocab = logits.shape
-    d = _dtype_of(logits)
-    if d == C64:
-        raise ValueError("logits are real")
-    if vocab > 1 and logits.stride(1) != 1:
+    d = types.get(logits.dtype)
+    if d is None or d == C64:
+        raise ValueError("logits are fp32, fp16 or bfloat16")
+    stride, inner = logits.stride()
+    if inner != 1 and vocab > 1:
         raise ValueError("the entries of a row of logits are adjacent")
-    if targets.dtype != torch.int64 or targets.shape != (rows,) or targets.device != logits.device or not targets.is_contiguous():
+    index = logits.get_device()
+    if targets.dtype is not torch.int64 or targets.shape != (rows,) or targets.get_device() != index or not targets.is_contiguous():
         raise ValueError("targets are a contiguous int64 tensor [rows] on the logits' device")
-    stride = logits.stride(0) if rows > 1 else vocab
-    return TgradLogits(logits.data_ptr(), rows, vocab, stride, targets.data_ptr(), d, temperature)
+    return _pack_logits(logits.data_ptr(), rows, vocab, stride if rows > 1 else vocab, targets.data_ptr(), d, temperature), rows, vocab, index
 
 
-def _rows_f32(logits, **tensors):
-    import torch
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.float32 or t.shape != logits.shape[:1] or t.device != logits.device or not t.is_contiguous()):
-            raise ValueError(f"{name} is a contiguous fp32 tensor [rows] on the logits' device")
+def _row_ptr(name, t, rows, index) -> int:
+    """Address of an fp32 tensor [rows]."""
+    if t.dtype is not _torch_types[2] or t.shape != (rows,) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous fp32 tensor [rows] on the logits' device")
+    return t.data_ptr()
 
 
-def _dlogits(logits, out):
-    """The gradient's tensor: `out` after a check, or a new one whose rows lie like those of the logits, so that both
-    are accessed 16 bytes at a time."""
-    import torch
-    rows, vocab = logits.shape
+def _dlogits(logits, rows, vocab, out):
+    """The gradient's tensor and row stride: `out` after a check, or a new one whose rows lie like those of the logits,
+    so that both are accessed 16 bytes at a time."""
     if out is None:
+        lead = (logits.data_ptr() & 15) // logits.element_size()
         stride = logits.stride(0) if rows > 1 else vocab
         if not vocab <= stride <= vocab + 128:
             stride = vocab
-        lead = (logits.data_ptr() & 15) // logits.element_size()
-        out = torch.empty(rows * stride + lead, dtype=logits.dtype, device=logits.device)
-        return out.as_strided((rows, vocab), (stride, 1), lead), stride
+        if stride == vocab and not lead:
+            return logits.new_empty((rows, vocab)), vocab
+        return logits.new_empty(rows * stride + lead).as_strided((rows, vocab), (stride, 1), lead), stride
     if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (vocab > 1 and out.stride(1) != 1):
         raise ValueError("dlogits has the logits' shape, dtype and device, and the entries of a row are adjacent")
     return out, out.stride(0) if rows > 1 else vocab
@@ -547,27 +575,31 @@ def _dlogits(logits, out):
 def token_logprob(logits, targets, temperature: float = 1.0, stream=None):
     """(logp, lse, entropy), each fp32 [rows], of softmax(logits / temperature): log-probability of the row's target,
     log-sum-exp and entropy.  Rows with a negative target are ignored (0, and their logits are not read)."""
-    import torch
-    desc = _logits(logits, targets, temperature)
-    with _on_stream(logits.device, stream) as st:
-        out = torch.empty(3, logits.shape[0], dtype=torch.float32, device=logits.device)
-        logp, lse, entropy = out.unbind(0)
-        _check(lib().tgrad_token_logprob(C.addressof(desc), logp.data_ptr(), lse.data_ptr(), entropy.data_ptr(), st), "tgrad_token_logprob")
-    return logp, lse, entropy
+    desc, rows, _, index = _logits(logits, targets, temperature)
+    if _elsewhere(index, stream):
+        return _there(index, stream, token_logprob, logits, targets, temperature)
+    torch, _, f32 = _torch_types
+    out = torch.empty((3, rows), dtype=f32, device=index)
+    base = out.data_ptr()
+    _check(lib().tgrad_token_logprob(desc, base, base + 4 * rows, base + 8 * rows, _raw_stream(index)), "tgrad_token_logprob")
+    return out.unbind(0)
 
 
 def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_entropy=None, temperature: float = 1.0, dlogits=None, stream=None):
     """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits.  `dlogits` may be the
     logits themselves."""
-    desc = _logits(logits, targets, temperature)
+    desc, rows, vocab, index = _logits(logits, targets, temperature)
+    if _elsewhere(index, stream):
+        return _there(index, stream, token_logprob_backward, logits, targets, lse, grad_logp, entropy, grad_entropy, temperature, dlogits)
     if grad_entropy is not None and entropy is None:
         raise ValueError("grad_entropy needs the entropy of the forward call")
-    _rows_f32(logits, lse=lse, grad_logp=grad_logp, entropy=entropy, grad_entropy=grad_entropy)
-    with _on_stream(logits.device, stream) as st:
-        out, stride = _dlogits(logits, dlogits)
-        _check(lib().tgrad_token_logprob_backward(C.addressof(desc), lse.data_ptr(), entropy.data_ptr() if grad_entropy is not None else None,
-                                                  grad_logp.data_ptr(), grad_entropy.data_ptr() if grad_entropy is not None else None,
-                                                  out.data_ptr(), stride, st), "tgrad_token_logprob_backward")
+    lse_p, g_p = _row_ptr("lse", lse, rows, index), _row_ptr("grad_logp", grad_logp, rows, index)
+    e_p = h_p = None
+    if grad_entropy is not None:
+        e_p, h_p = _row_ptr("entropy", entropy, rows, index), _row_ptr("grad_entropy", grad_entropy, rows, index)
+    out, stride = _dlogits(logits, rows, vocab, dlogits)
+    _check(lib().tgrad_token_logprob_backward(desc, lse_p, e_p, g_p, h_p, out.data_ptr(), stride, _raw_stream(index)),
+           "tgrad_token_logprob_backward")
     return out
 
 
@@ -593,22 +625,23 @@ def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, c
     - entropy_coef H), r = exp(logp - old_logp), u = ref_logp - logp.  The weights carry mask and normalisation; rows
     with a negative target are ignored.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
     `dlogits` may be the logits themselves."""
-    import torch
-    desc = _logits(logits, targets, temperature)
-    _rows_f32(logits, old_logp=old_logp, advantages=advantages, weights=weights, ref_logp=ref_logp)
-    rows = logits.shape[0]
-    b = C.c_size_t(0)
-    _check(lib().tgrad_policy_loss_bytes(rows, C.byref(b)), "tgrad_policy_loss_bytes")
-    with _on_stream(logits.device, stream) as st:
-        grad, stride = (None, 0) if forward_only else _dlogits(logits, dlogits)
-        out = torch.empty(8 + 2 * rows, dtype=torch.float32, device=logits.device)
-        ws = torch.empty(b.value, dtype=torch.uint8, device=logits.device)
-        base = out.data_ptr()
-        args = TgradPolicyArgs(old_logp.data_ptr(), ref_logp.data_ptr() if ref_logp is not None else None, advantages.data_ptr(),
-                               weights.data_ptr(), clip_low, clip_high, kl_coef, entropy_coef, grad_scale, 0.0, base, base + 32,
-                               base + 32 + 4 * rows, grad.data_ptr() if grad is not None else None, stride)
-        _check(lib().tgrad_policy_loss(C.addressof(desc), C.addressof(args), ws.data_ptr(), b.value, st), "tgrad_policy_loss")
-    return PolicyLoss(out[:5], out[8:8 + rows], out[8 + rows:], grad)
+    desc, rows, vocab, index = _logits(logits, targets, temperature)
+    if _elsewhere(index, stream):
+        return _there(index, stream, policy_loss, logits, targets, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl_coef,
+                      entropy_coef, temperature, grad_scale, dlogits, forward_only)
+    torch, _, f32 = _torch_types
+    grad, stride = (None, 0) if forward_only else _dlogits(logits, rows, vocab, dlogits)
+    ws = _workspace("tgrad_policy_loss_bytes", rows)
+    out = torch.empty(ws // 4 + 5 + 2 * rows, dtype=f32, device=index)
+    base = out.data_ptr()
+    stats = base + ws
+    args = _pack_policy(_row_ptr("old_logp", old_logp, rows, index), _row_ptr("ref_logp", ref_logp, rows, index) if ref_logp is not None else 0,
+                        _row_ptr("advantages", advantages, rows, index), _row_ptr("weights", weights, rows, index), clip_low, clip_high,
+                        kl_coef, entropy_coef, grad_scale, 0.0, stats, stats + 20, stats + 20 + 4 * rows,
+                        grad.data_ptr() if grad is not None else 0, stride)
+    _check(lib().tgrad_policy_loss(desc, args, base, ws, _raw_stream(index)), "tgrad_policy_loss")
+    _, stats, logp, entropy = out.split_with_sizes((ws // 4, 5, rows, rows))
+    return PolicyLoss(stats, logp, entropy, grad)
 
 
 def preference_loss(logits, targets, starts, ref_logp, beta: float = 0.1, label_smoothing: float = 0.0, temperature: float = 1.0,
@@ -617,20 +650,20 @@ def preference_loss(logits, targets, starts, ref_logp, beta: float = 0.1, label_
     2 * pairs + 1 row numbers, answers 2 b and 2 b + 1 are the chosen and the rejected one of pair b; rows of prompts
     have a negative target.  rewards_s = beta * sum (logp - ref_logp), h = rewards_chosen - rewards_rejected, loss = mean of
     -(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h)."""
-    import torch
-    desc = _logits(logits, targets, temperature)
-    _rows_f32(logits, ref_logp=ref_logp)
-    if starts.dtype != torch.int32 or starts.dim() != 1 or starts.numel() % 2 != 1 or starts.device != logits.device or not starts.is_contiguous():
+    desc, rows, vocab, index = _logits(logits, targets, temperature)
+    if _elsewhere(index, stream):
+        return _there(index, stream, preference_loss, logits, targets, starts, ref_logp, beta, label_smoothing, temperature, grad_scale, dlogits, forward_only)
+    torch, _, f32 = _torch_types
+    if starts.dtype is not torch.int32 or starts.dim() != 1 or starts.numel() % 2 != 1 or starts.get_device() != index or not starts.is_contiguous():
         raise ValueError("starts is a contiguous int32 tensor of 2 * pairs + 1 entries on the logits' device")
-    rows, pairs = logits.shape[0], starts.numel() // 2
-    b = C.c_size_t(0)
-    _check(lib().tgrad_preference_loss_bytes(rows, pairs, C.byref(b)), "tgrad_preference_loss_bytes")
-    with _on_stream(logits.device, stream) as st:
-        grad, stride = (None, 0) if forward_only else _dlogits(logits, dlogits)
-        out = torch.empty(4 + rows + 2 * pairs, dtype=torch.float32, device=logits.device)
-        ws = torch.empty(b.value, dtype=torch.uint8, device=logits.device)
-        base = out.data_ptr()
-        args = TgradPreferenceArgs(starts.data_ptr(), ref_logp.data_ptr(), pairs, beta, label_smoothing, grad_scale, base,
-                                   base + 16 + 4 * rows, base + 16, grad.data_ptr() if grad is not None else None, stride)
-        _check(lib().tgrad_preference_loss(C.addressof(desc), C.addressof(args), ws.data_ptr(), b.value, st), "tgrad_preference_loss")
-    return PreferenceLoss(out[0], out[4 + rows:], out[4:4 + rows], grad)
+    pairs = starts.numel() // 2
+    grad, stride = (None, 0) if forward_only else _dlogits(logits, rows, vocab, dlogits)
+    ws = _workspace("tgrad_preference_loss_bytes", rows, pairs)
+    out = torch.empty(ws // 4 + 1 + rows + 2 * pairs, dtype=f32, device=index)
+    base = out.data_ptr()
+    loss = base + ws
+    args = _pack_preference(starts.data_ptr(), _row_ptr("ref_logp", ref_logp, rows, index), pairs, beta, label_smoothing, grad_scale, loss,
+                            loss + 4 + 4 * rows, loss + 4, grad.data_ptr() if grad is not None else 0, stride)
+    _check(lib().tgrad_preference_loss(desc, args, base, ws, _raw_stream(index)), "tgrad_preference_loss")
+    _, loss, logp, rewards = out.split_with_sizes((ws // 4, 1, rows, 2 * pairs))
+    return PreferenceLoss(loss[0], rewards, logp, grad)

@@ -414,6 +414,8 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
 struct ForwardArgs {
   float* logp; float* lse; float* entropy;      // out, may be null
   float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
+  float* g;                                     // zeroed, may be null: gradient of rows that no later kernel gives one
+  unsigned* ticket;                             // zeroed with it
 };
 // MODE: RW_FORWARD log-probabilities only (every chunk goes through the ring once, and the last warp's work on a row
 // overlaps with the others' on the next), RW_POLICY the policy loss with its gradient, RW_ENTROPY with an entropy bonus.
@@ -423,9 +425,11 @@ __device__ __forceinline__ void store_stat(const ForwardArgs& f, int64_t row, co
   if (f.lse) f.lse[row] = st.lse;
   if (f.entropy) f.entropy[row] = st.H;
   if (f.stat) f.stat[row] = make_float2(st.M, st.ls2);
+  if (f.g) f.g[row] = 0.f;
+  if (f.ticket && row == 0) *f.ticket = 0;
 }
 template <int KIND, int MODE>
-__global__ void __maxnreg__(96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
+__global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
                                                   int64_t rows, const __grid_constant__ RowGeom geo) {
   constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
   extern __shared__ __align__(128) unsigned char ring[];
@@ -675,6 +679,75 @@ __global__ void __maxnreg__(96) token_row_kernel(const __grid_constant__ TokenAr
   }
 }
 
+// Short rows: a warp takes one at a time and keeps it in its registers, NV granules per lane.  Nothing is shared, so the
+// latency of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers
+// for every row took 66 us instead of SHORT us for 16384 rows of 1000 bf16 logits).
+constexpr int SR_WARPS = 4;
+template <int KIND, int MODE, int NV>
+__global__ void __launch_bounds__(32 * SR_WARPS, NV > 4 ? 4 : 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
+                                                                                 int64_t rows) {
+  constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
+  constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
+  const int lane = threadIdx.x & 31;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t step = (int64_t)gridDim.x * SR_WARPS;
+  int64_t row = (int64_t)blockIdx.x * SR_WARPS + (threadIdx.x >> 5);
+  long long y_next = row < rows ? p.y[row] : -1;
+  const uint32_t ni = neg_inf_word<KIND>();
+  for (; row < rows; row += step) {
+    const long long y = y_next;
+    if (row + step < rows) y_next = p.y[row + step];
+    const Row<KIND> r(p.z + row * p.ldz * B, p.V);
+    const int G = r.granules();
+    char* drow = p.dz + row * p.lddz * B;
+    const bool same = same_alignment(r, drow);
+    if (y < 0) {
+      if (BACK)
+        for (int g = lane; g < G; g += 32) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      if (lane == 0) {
+        RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+        store_stat(f, row, none);
+        if (BACK) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      continue;
+    }
+    uint4 v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int g = lane + 32 * i;
+      v[i] = make_uint4(ni, ni, ni, ni);
+      if (g < G) v[i] = r.load(g);
+    }
+    const float zy = target_logit<KIND>(p, row, y);
+    float old = 0.f, adv = 0.f, wt = 0.f, ref = 0.f;
+    if (BACK) {
+      old = q.old_logp[row]; adv = q.adv[row]; wt = q.weight[row];
+      if (q.ref_logp) ref = q.ref_logp[row];
+    }
+    Triple a;
+    a.m = batch_max<KIND, NV>(v); a.s = a.t = 0.f;
+    accumulate<KIND, NV>(a, v, p.k);
+    warp_combine(a, p.k);
+    const RowStat st = row_stat(a, zy, p.inv_tau);
+    if (lane == 0) store_stat(f, row, st);
+    if (!BACK) continue;
+    const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, adv, wt, q);
+    if (lane == 0) q.terms[row] = o.terms;
+    const float sc = q.grad_scale * p.inv_tau;
+    GradCoef gc; gc.M = st.M; gc.k = p.k; gc.ls2 = st.ls2;
+    gc.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; gc.c1 = -o.h * TK_LN2 * sc;
+    const int gy = y < p.V ? (r.mis + (int)y) / E : -1;
+    __syncwarp();      // every lane has read the target's logit before it is overwritten
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int g = lane + 32 * i;
+      if (g < G) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+    }
+    if (gy >= 0 && (gy & 31) == lane) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
+  }
+}
+
 // Deterministic sum of the rows' terms by one block: stats = loss, policy, KL, entropy, clipped weight.
 __global__ void __launch_bounds__(1024) policy_sum_kernel(const float4* __restrict__ terms, int64_t rows, float kl_coef, float ent_coef, float* __restrict__ stats) {
   __shared__ double sh[4][32];
@@ -747,7 +820,8 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   if (POLICY) q.terms[row] = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q).terms;
 }
 
-// Gradient pass: one block per piece of NV * THREADS granules of a row.
+// Gradient pass: one block per piece of NV * THREADS granules of a row, or (SHORT, rows of fewer granules) of the granules of
+// all rows one after the other.
 struct BackwardArgs {
   const float* lse;          // of the forward call, or
   const float2* stat;        // (M, log2 S), more exact where lse is large
@@ -757,6 +831,41 @@ struct BackwardArgs {
   float scale;
 };
 constexpr int TB2_THREADS = 256;
+template <int KIND, bool ENT>
+__device__ __forceinline__ void backward_coef(const TokenArgs& p, const BackwardArgs& b, int64_t row, long long y, GradCoef& gc, float& target) {
+  const float gg = b.g[row];
+  float hh = 0.f, H = 0.f;
+  if (ENT) { hh = b.h[row]; H = b.entropy[row]; }
+  const float sc = b.scale * p.inv_tau;
+  gc.k = p.k;
+  if (b.stat) { const float2 s = b.stat[row]; gc.M = s.x; gc.ls2 = s.y; }
+  else { gc.M = 0.f; gc.ls2 = b.lse[row] * 1.4426950408889634f; }
+  gc.c0 = -(ENT ? fmaf(hh, H, gg) : gg) * sc; gc.c1 = -hh * TK_LN2 * sc;
+  if (y >= p.V) gc.c0 = __int_as_float(0x7fc00000);
+  target = gg * sc;
+}
+template <int KIND, bool ENT>
+__global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, int64_t rows, uint32_t G) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t at = (int64_t)blockIdx.x * TB2_THREADS + threadIdx.x, row = at / G;
+  const int g = (int)(at - row * G);
+  if (row >= rows) return;
+  const long long y = p.y[row];
+  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
+  if (g >= r.granules()) return;
+  char* drow = p.dz + row * p.lddz * Gran<KIND>::B;
+  const bool same = same_alignment(r, drow);
+  if (y < 0) { store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0)); return; }
+  const uint4 v = r.load(g);
+  GradCoef gc; float target;
+  backward_coef<KIND, ENT>(p, b, row, y, gc, target);
+  const bool mine = y < p.V && (r.mis + (int)y) / Gran<KIND>::E == g;
+  float zy = 0.f;
+  if (mine) zy = target_logit<KIND>(p, row, y);
+  store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v, gc));
+  if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
+}
 template <int KIND, bool ENT>
 __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, uint32_t pieces) {
   constexpr int NV = 4;
@@ -780,25 +889,18 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __
     const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
     if (g < g1) v[i] = r.load(g);
   }
-  float gg, hh = 0.f, H = 0.f;
-  gg = b.g[row];
-  if (ENT) { hh = b.h[row]; H = b.entropy[row]; }
-  const float sc = b.scale * p.inv_tau;
-  GradCoef gc; gc.k = p.k;
-  if (b.stat) { const float2 s = b.stat[row]; gc.M = s.x; gc.ls2 = s.y; }
-  else { gc.M = 0.f; gc.ls2 = b.lse[row] * 1.4426950408889634f; }
-  gc.c0 = -(ENT ? fmaf(hh, H, gg) : gg) * sc; gc.c1 = -hh * TK_LN2 * sc;
+  GradCoef gc; float target;
+  backward_coef<KIND, ENT>(p, b, row, y, gc, target);
   const int gy = y < p.V ? (r.mis + (int)y) / Gran<KIND>::E : -1;
   const bool mine = gy >= g0 && gy < g1 && (gy - g0) % TB2_THREADS == (int)threadIdx.x;
   float zy = 0.f;
   if (mine) zy = target_logit<KIND>(p, row, y);      // before this thread overwrites it, where the gradient replaces the logits
-  if (y >= p.V) gc.c0 = __int_as_float(0x7fc00000);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
     if (g < g1) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
   }
-  if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, gg * sc));
+  if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -815,54 +917,70 @@ struct PairArgs {
   float* g;                   // out: d loss / d logp of each row of the answers
   float* rewards;             // out: R_s
   double* terms;              // out: loss of each pair
+  unsigned* ticket;           // 0; the last block to take one adds the terms up
+  float* loss;
 };
-constexpr int TP_THREADS = 256;
+constexpr int TP_THREADS = 512;
 __global__ void __launch_bounds__(TP_THREADS) pair_kernel(const __grid_constant__ PairArgs a) {
-  __shared__ double sh[TP_THREADS / 32];
+  __shared__ double sh[2][TP_THREADS / 32];
   __shared__ float coef;
+  __shared__ int last;
   griddep_wait();
   griddep_launch_dependents();
-  const int b = blockIdx.x;
+  const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int64_t at[4];
   double R[2];
-  int64_t s0[2], s1[2];
+#pragma unroll
   for (int c = 0; c < 2; ++c) {
     int64_t lo = a.starts[2 * b + c], hi = a.starts[2 * b + c + 1];      // bounds that make no sense never leave [0, rows]
     lo = lo < 0 ? 0 : (lo > a.rows ? a.rows : lo);
     hi = hi < lo ? lo : (hi > a.rows ? a.rows : hi);
-    s0[c] = lo; s1[c] = hi;
-    double s = 0.0;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += TP_THREADS)
-      if (a.y[i] >= 0) s += (double)a.logp[i] - (double)a.ref[i];
-    R[c] = (double)a.beta * block_sum(s, sh);
+    at[2 * c] = lo; at[2 * c + 1] = hi;
   }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    double s = 0.0;
+    for (int64_t i = at[2 * c] + threadIdx.x; i < at[2 * c + 1]; i += TP_THREADS) {
+      const float lp = a.logp[i], rf = a.ref[i];
+      if (a.y[i] >= 0) s += (double)lp - (double)rf;
+    }
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    R[c] = s;
+  }
+  if (lane == 0) { sh[0][warp] = R[0]; sh[1][warp] = R[1]; }
+  __syncthreads();
   if (threadIdx.x == 0) {
+    R[0] = R[1] = 0.0;
+    for (int w = 0; w < TP_THREADS / 32; ++w) { R[0] += sh[0][w]; R[1] += sh[1][w]; }
+    R[0] *= (double)a.beta; R[1] *= (double)a.beta;
     const double h = R[0] - R[1], e = (double)a.smoothing;
-    const double tail = log1p(exp(-fabs(h)));                            // -log sigma(x) = max(-x, 0) + tail
-    a.terms[b] = (1.0 - e) * (fmax(-h, 0.0) + tail) + e * (fmax(h, 0.0) + tail);
-    if (h != h) a.terms[b] = h;
+    const double x = exp(-fabs(h)), tail = log1p(x);                     // -log sigma(z) = max(-z, 0) + tail
+    a.terms[b] = h != h ? h : (1.0 - e) * (fmax(-h, 0.0) + tail) + e * (fmax(h, 0.0) + tail);
     a.rewards[2 * b] = (float)R[0]; a.rewards[2 * b + 1] = (float)R[1];
-    coef = (float)((double)a.beta * (1.0 / (1.0 + exp(-h)) - (1.0 - e)) / (double)a.pairs);
+    const double right = h >= 0.0 ? 1.0 / (1.0 + x) : x / (1.0 + x);
+    coef = (float)((double)a.beta * (right - (1.0 - e)) / (double)a.pairs);
+    __threadfence();
+    last = atomicAdd(a.ticket, 1u) == (unsigned)a.pairs - 1;
   }
   __syncthreads();
-  if (!a.g) return;
-  for (int c = 0; c < 2; ++c)
-    for (int64_t i = s0[c] + threadIdx.x; i < s1[c]; i += TP_THREADS) a.g[i] = c == 0 ? coef : -coef;
-}
-__global__ void __launch_bounds__(TP_THREADS) pair_sum_kernel(const double* __restrict__ terms, int pairs, float* __restrict__ loss) {
-  __shared__ double sh[TP_THREADS / 32];
-  griddep_wait();
-  griddep_launch_dependents();
+  if (a.g) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      for (int64_t i = at[2 * c] + threadIdx.x; i < at[2 * c + 1]; i += TP_THREADS) a.g[i] = c == 0 ? coef : -coef;
+  }
+  if (!last) return;
+  // every block's term is there; they are added in the order of the pairs whichever block is the last
+  __threadfence();
   double s = 0.0;
-  for (int i = threadIdx.x; i < pairs; i += TP_THREADS) s += terms[i];
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) *loss = pairs > 0 ? (float)(s / (double)pairs) : 0.f;
-}
-// rows outside every answer take no part
-__global__ void __launch_bounds__(TP_THREADS) zero_floats_kernel(float* __restrict__ x, int64_t n) {
-  griddep_wait();
-  griddep_launch_dependents();
-  const int64_t i = (int64_t)blockIdx.x * TP_THREADS + threadIdx.x;
-  if (i < n) x[i] = 0.f;
+  for (int i = threadIdx.x; i < a.pairs; i += TP_THREADS) s += __ldcg(a.terms + i);
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) sh[0][warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < TP_THREADS / 32; ++w) s += sh[0][w];
+    *a.loss = (float)(s / (double)a.pairs);
+  }
 }
 
 }  // namespace tg

@@ -231,7 +231,17 @@ tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a
 
 template <bool ENT>
 tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
-  const int64_t pieces = (max_granules(in) + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
+  const int64_t G = max_granules(in), pieces = (G + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
+  if (G <= 2 * TB2_THREADS) {      // a block for each row would be half empty or worse
+    const int64_t blocks = (in->rows * G + TB2_THREADS - 1) / TB2_THREADS;
+    if (blocks >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks);
+    if (kind == LS_F32) launch_chained(token_backward_short_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
+    else if (kind == LS_F16) launch_chained(token_backward_short_kernel<LS_F16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
+    else launch_chained(token_backward_short_kernel<LS_BF16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
+    TG_LAUNCH_CHECK();
+    return TGRAD_OK;
+  }
   if (in->rows * pieces >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(in->rows * pieces));
   if (kind == LS_F32) launch_chained(token_backward_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
@@ -243,13 +253,36 @@ tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& 
 
 // The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 16 arithmetic warps for all of them at most.
 constexpr size_t kRingBytes = 224 * 1024;
+// Dynamic shared memory beyond the default, once per kernel and device.
+template <typename F>
+tgrad_status allow_shared(F kern, size_t bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return TGRAD_ERR_CUDA;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return TGRAD_OK;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return TGRAD_ERR_CUDA;
+  if (dev < 64) done.fetch_or(bit, std::memory_order_release);
+  return TGRAD_OK;
+}
+// Rows that a warp can keep.
+template <int KIND, int MODE, int NV>
+tgrad_status launch_short(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
+  int64_t grid = (in->rows + SR_WARPS - 1) / SR_WARPS;
+  const int64_t most = (int64_t)sm_count() * (NV > 4 ? 4 : 8);
+  if (grid > most) grid = most;
+  launch_chained(token_short_kernel<KIND, MODE, NV>, dim3((unsigned)grid), dim3(32 * SR_WARPS), 0, st, a, q, f, in->rows);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
 template <int KIND, int MODE>
 tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
-  const int sm = sm_count();
   const int64_t bytes = max_granules(in) * 16;
+  if (bytes <= 128 * 16) return launch_short<KIND, MODE, 4>(in, a, q, f, st);
+  if (bytes <= 512 * 16) return launch_short<KIND, MODE, 16>(in, a, q, f, st);
+  const int sm = sm_count();
   RowGeom g; memset(&g, 0, sizeof(g));
   // the smallest blocks whose share of the ring holds a row and a quarter of the next
-  const int warps[4] = {2, 4, 8, 16}, blocks[4] = {6, 4, 2, 1};
+  const int warps[4] = {2, 4, 8, 16}, blocks[4] = {6, MODE == RW_FORWARD ? 6 : 4, 2, 1};
   int per_sm = 1;
   for (int i = 0; i < 4; ++i) {
     g.W = warps[i]; per_sm = blocks[i];
@@ -261,7 +294,8 @@ tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const Policy
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
   g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
   auto kern = token_row_kernel<KIND, MODE>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes) != cudaSuccess) return TGRAD_ERR_CUDA;
+  static std::atomic<uint64_t> done{0};
+  TG_TRY(allow_shared(kern, kRingBytes, done));
   // units of about 64 KB of logits, at most a warp's width of rows, and several for every block
   int64_t unit = (64 << 10) / bytes;
   if (unit > 32) unit = 32;
@@ -282,12 +316,12 @@ tgrad_status launch_row_kind(const tgrad_logits* in, const TokenArgs& a, const P
 // Log-probabilities: several blocks on each of a few rows, the ring where the rows alone keep every block busy.
 tgrad_status launch_logprob(const tgrad_logits* in, const TokenArgs& a, const ForwardArgs& f, cudaStream_t st) {
   PolicyArgs q; memset(&q, 0, sizeof(q));
-  if (in->rows >= (int64_t)sm_count() * 8) return launch_row_kind<RW_FORWARD>(in, a, q, f, st);
+  if (in->rows >= (int64_t)sm_count() * 8 || max_granules(in) <= 512) return launch_row_kind<RW_FORWARD>(in, a, q, f, st);
   return launch_forward<false>(token_kind(in->dtype), in, a, f, q, st);
 }
 
 size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16); }
-size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + align_up((size_t)rows * 4) + align_up((size_t)pairs * 8); }
+size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + align_up((size_t)rows * 4) + align_up((size_t)pairs * 8) + 256; }
 
 }  // namespace
 
@@ -420,27 +454,24 @@ tgrad_status tgrad_preference_loss(const tgrad_logits* in, const tgrad_preferenc
   float2* stat = reinterpret_cast<float2*>(ws);
   float* g = reinterpret_cast<float*>(ws + align_up((size_t)in->rows * 8));
   double* terms = reinterpret_cast<double*>(ws + align_up((size_t)in->rows * 8) + align_up((size_t)in->rows * 4));
+  unsigned* ticket = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(terms) + align_up((size_t)c->pairs * 8));
   const int kind = token_kind(in->dtype);
   const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
   if (any) {
     ForwardArgs f; memset(&f, 0, sizeof(f));
     f.logp = c->d_logp; f.stat = stat;
-    if (c->d_dlogits) {
-      launch_chained(zero_floats_kernel, dim3((unsigned)((in->rows + TP_THREADS - 1) / TP_THREADS)), dim3(TP_THREADS), 0, st, g, in->rows);
-      TG_LAUNCH_CHECK();
-    }
+    f.g = c->d_dlogits ? g : nullptr; f.ticket = ticket;
     TG_TRY(launch_logprob(in, a, f, st));
   }
+  else if (cudaMemsetAsync(ticket, 0, sizeof(*ticket), st) != cudaSuccess) return TGRAD_ERR_CUDA;
   if (c->pairs > 0) {
     PairArgs p; memset(&p, 0, sizeof(p));
     p.starts = c->d_starts; p.ref = c->d_ref_logp; p.logp = c->d_logp; p.y = reinterpret_cast<const long long*>(in->d_targets);
     p.rows = in->rows; p.pairs = c->pairs; p.beta = c->beta; p.smoothing = c->label_smoothing;
-    p.g = c->d_dlogits ? g : nullptr; p.rewards = c->d_rewards; p.terms = terms;
+    p.g = c->d_dlogits ? g : nullptr; p.rewards = c->d_rewards; p.terms = terms; p.ticket = ticket; p.loss = c->d_loss;
     launch_chained(pair_kernel, dim3((unsigned)c->pairs), dim3(TP_THREADS), 0, st, p);
     TG_LAUNCH_CHECK();
-  }
-  launch_chained(pair_sum_kernel, dim3(1), dim3(TP_THREADS), 0, st, terms, c->pairs, c->d_loss);
-  TG_LAUNCH_CHECK();
+  } else if (cudaMemsetAsync(c->d_loss, 0, sizeof(float), st) != cudaSuccess) return TGRAD_ERR_CUDA;
   if (any && c->d_dlogits) {
     BackwardArgs b; memset(&b, 0, sizeof(b));
     b.stat = stat; b.g = g; b.scale = c->grad_scale;
