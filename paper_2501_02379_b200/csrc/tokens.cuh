@@ -106,6 +106,10 @@ struct Row {
     if (whole(g)) return ld_stream(reinterpret_cast<const uint4*>(base) + g);
     return partial(g);
   }
+  __device__ __forceinline__ uint4 load_cached(int g) const {      // the same, kept in the L1 cache
+    if (whole(g)) return *(reinterpret_cast<const uint4*>(base) + g);
+    return partial(g);
+  }
 };
 
 // ---- (M, S, T) ----
@@ -679,13 +683,14 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   }
 }
 
-// Short rows: a warp takes one at a time and keeps it in its registers, NV granules per lane.  Nothing is shared, so the
-// latency of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers
-// for every row took 66 us instead of SHORT us for 16384 rows of 1000 bf16 logits).
-constexpr int SR_WARPS = 4;
-template <int KIND, int MODE, int NV>
-__global__ void __launch_bounds__(32 * SR_WARPS, NV > 4 ? 4 : 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
-                                                                                 int64_t rows) {
+// Short rows (up to 8 KB): a warp takes one at a time, four granules per lane in a batch.  Nothing is shared, so the latency
+// of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers for every
+// row took 66 us instead of 23 us for 16384 rows of 1000 bf16 logits).  A row of more than one batch is read again for the
+// gradient, from the L1 cache, which the 32 rows in work on an SM fit (keeping it in 64 registers per lane leaves room for
+// half as many warps: 64 us instead of SHORT us for 12384 rows of 3001 bf16 logits).
+constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 512;
+template <int KIND, int MODE>
+__global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f, int64_t rows) {
   constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
   const int lane = threadIdx.x & 31;
@@ -712,22 +717,24 @@ __global__ void __launch_bounds__(32 * SR_WARPS, NV > 4 ? 4 : 8) token_short_ker
       }
       continue;
     }
-    uint4 v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int g = lane + 32 * i;
-      v[i] = make_uint4(ni, ni, ni, ni);
-      if (g < G) v[i] = r.load(g);
-    }
     const float zy = target_logit<KIND>(p, row, y);
     float old = 0.f, adv = 0.f, wt = 0.f, ref = 0.f;
     if (BACK) {
       old = q.old_logp[row]; adv = q.adv[row]; wt = q.weight[row];
       if (q.ref_logp) ref = q.ref_logp[row];
     }
+    uint4 v[SR_NV];
     Triple a;
-    a.m = batch_max<KIND, NV>(v); a.s = a.t = 0.f;
-    accumulate<KIND, NV>(a, v, p.k);
+    a.m = TK_LOWEST; a.s = a.t = 0.f;
+    for (int g0 = lane; g0 < G; g0 += 32 * SR_NV) {
+#pragma unroll
+      for (int i = 0; i < SR_NV; ++i) {
+        v[i] = make_uint4(ni, ni, ni, ni);
+        if (g0 + 32 * i < G) v[i] = r.load_cached(g0 + 32 * i);
+      }
+      rebase(a, fmaxf(a.m, batch_max<KIND, SR_NV>(v)), p.k);
+      accumulate<KIND, SR_NV>(a, v, p.k);
+    }
     warp_combine(a, p.k);
     const RowStat st = row_stat(a, zy, p.inv_tau);
     if (lane == 0) store_stat(f, row, st);
@@ -739,10 +746,15 @@ __global__ void __launch_bounds__(32 * SR_WARPS, NV > 4 ? 4 : 8) token_short_ker
     gc.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; gc.c1 = -o.h * TK_LN2 * sc;
     const int gy = y < p.V ? (r.mis + (int)y) / E : -1;
     __syncwarp();      // every lane has read the target's logit before it is overwritten
+    for (int g0 = lane; g0 < G; g0 += 32 * SR_NV) {
+      if (G > 32 * SR_NV) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int g = lane + 32 * i;
-      if (g < G) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+        for (int i = 0; i < SR_NV; ++i)
+          if (g0 + 32 * i < G) v[i] = r.load_cached(g0 + 32 * i);
+      }
+#pragma unroll
+      for (int i = 0; i < SR_NV; ++i)
+        if (g0 + 32 * i < G) store_granule<KIND>(r, drow, same, g0 + 32 * i, grad_granule<KIND, ENT>(v[i], gc));
     }
     if (gy >= 0 && (gy & 31) == lane) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
   }

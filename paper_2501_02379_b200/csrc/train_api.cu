@@ -264,21 +264,20 @@ tgrad_status allow_shared(F kern, size_t bytes, std::atomic<uint64_t>& done) {
   if (dev < 64) done.fetch_or(bit, std::memory_order_release);
   return TGRAD_OK;
 }
-// Rows that a warp can keep.
-template <int KIND, int MODE, int NV>
+// Rows that a warp takes alone.
+template <int KIND, int MODE>
 tgrad_status launch_short(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
   int64_t grid = (in->rows + SR_WARPS - 1) / SR_WARPS;
-  const int64_t most = (int64_t)sm_count() * (NV > 4 ? 4 : 8);
+  const int64_t most = (int64_t)sm_count() * 8;
   if (grid > most) grid = most;
-  launch_chained(token_short_kernel<KIND, MODE, NV>, dim3((unsigned)grid), dim3(32 * SR_WARPS), 0, st, a, q, f, in->rows);
+  launch_chained(token_short_kernel<KIND, MODE>, dim3((unsigned)grid), dim3(32 * SR_WARPS), 0, st, a, q, f, in->rows);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
 template <int KIND, int MODE>
 tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
   const int64_t bytes = max_granules(in) * 16;
-  if (bytes <= 128 * 16) return launch_short<KIND, MODE, 4>(in, a, q, f, st);
-  if (bytes <= 512 * 16) return launch_short<KIND, MODE, 16>(in, a, q, f, st);
+  if (bytes <= SR_MAX_GRANULES * 16) return launch_short<KIND, MODE>(in, a, q, f, st);
   const int sm = sm_count();
   RowGeom g; memset(&g, 0, sizeof(g));
   // the smallest blocks whose share of the ring holds a row and a quarter of the next
@@ -316,7 +315,7 @@ tgrad_status launch_row_kind(const tgrad_logits* in, const TokenArgs& a, const P
 // Log-probabilities: several blocks on each of a few rows, the ring where the rows alone keep every block busy.
 tgrad_status launch_logprob(const tgrad_logits* in, const TokenArgs& a, const ForwardArgs& f, cudaStream_t st) {
   PolicyArgs q; memset(&q, 0, sizeof(q));
-  if (in->rows >= (int64_t)sm_count() * 8 || max_granules(in) <= 512) return launch_row_kind<RW_FORWARD>(in, a, q, f, st);
+  if (in->rows >= (int64_t)sm_count() * 8 || max_granules(in) <= SR_MAX_GRANULES) return launch_row_kind<RW_FORWARD>(in, a, q, f, st);
   return launch_forward<false>(token_kind(in->dtype), in, a, f, q, st);
 }
 
