@@ -151,11 +151,16 @@ __device__ __forceinline__ float batch_max(const uint4 (&v)[NV]) {
   }
   return fmaxf(max_of_word<KIND>(m), TK_LOWEST);      // also for a batch of NaN
 }
-__device__ __forceinline__ void warp_combine(Triple& a, float k) {
-  float m = a.m;
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  rebase(a, m, k);
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Combines the triples of the lanes; lanes from `width` on have none (m lowest, s and t 0).
+__device__ __forceinline__ void warp_combine(Triple& a, float k, int width = 32) {
+  rebase(a, warp_max(a.m), k);
   for (int o = 16; o; o >>= 1) {
+    if (o >= width) continue;
     a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
     a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
   }
@@ -324,6 +329,21 @@ struct RowGeom {
   float slack;           // 40 / k
 };
 
+// A bounded wait that asks the hardware to keep the warp asleep for up to 20 us at a time: the other warps need the issue
+// slots that frequent polling takes (more than half of all instructions on rows of 8000 logits).
+__device__ __forceinline__ bool mbar_wait_asleep(uint64_t* bar, uint32_t parity) {
+  for (uint32_t i = 0; i < (1u << 17); ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000u) : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+
 // Work distribution by the hardware's queue of blocks: a running block takes over one that has not been started.  The
 // answer is 16 bytes in shared memory, counted on an mbarrier; once it was "none left", no further block may be asked for.
 __device__ __forceinline__ void next_block_ask(uint4* answer, uint64_t* bar) {
@@ -352,7 +372,7 @@ __device__ __forceinline__ void bar_sync_n(int id, int threads) { asm volatile("
 struct WarpSums { float base, thr, nm, delta; uint32_t clamp; bool fast; uint64_t s2, t2; };
 template <int KIND>
 __device__ __forceinline__ void move_base(WarpSums& a, float top, const RowGeom& geo, float k) {
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  top = warp_max(top);
   const float d = fmaxf(fmaf(a.base - top, k, -a.delta), -1e30f), f = ex2(d);
   const float2 s = upk2(a.s2), t = upk2(a.t2);
   a.s2 = pk2(s.x * f, s.y * f);
@@ -468,14 +488,14 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       const long long ym = lane < geo.unit && mine < rows ? p.y[mine] : -1;
       uint32_t live = __ballot_sync(0xffffffffu, ym >= 0);
       if (lane == 0) {
-        ok = mbar_wait_bounded(&jempty[js], jph ^ 1);
+        ok = mbar_wait_asleep(&jempty[js], jph ^ 1);
         if (ok) { job[js] = make_longlong2(unit, ym); mbar_arrive(&jfull[js]); }
         for (; live && ok; live &= live - 1) {
           const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
           const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = !BACK ? 0 : K <= N ? K : N - 2;
           for (int j = 0; j < (BACK ? 2 * K - n : K) && ok; ++j) {
             const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
-            ok = mbar_wait_bounded(&empty[s], ph ^ 1);
+            ok = mbar_wait_asleep(&empty[s], ph ^ 1);
             if (!ok) break;
             mbar_expect_tx(&full[s], (uint32_t)len * 16);
             bulk_g2s(ring + (size_t)s * chunk * 16, r.base + (size_t)(wa + at) * 16, (uint32_t)len * 16, &full[s]);
@@ -486,18 +506,18 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       }
       if (++js == RW_JOBS) { js = 0; jph ^= 1; }
       // (the answer is taken, after a failure too, before the block may end)
-      const bool got = __all_sync(0xffffffffu, mbar_wait_bounded(&nbar, nph));
+      const bool got = __all_sync(0xffffffffu, mbar_wait_asleep(&nbar, nph));
       nph ^= 1;
       unit = got ? next_block_get(&answer) : -1;
       __syncwarp();
       ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
       if (unit < 0) break;
     }
-    if (lane == 0 && ok && mbar_wait_bounded(&jempty[js], jph ^ 1)) { job[js] = make_longlong2(-1, 0); mbar_arrive(&jfull[js]); }
+    if (lane == 0 && ok && mbar_wait_asleep(&jempty[js], jph ^ 1)) { job[js] = make_longlong2(-1, 0); mbar_arrive(&jfull[js]); }
     // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
     if (lane == 0)
       for (int i = 0; i < N; ++i)
-        if (used >> i & 1) (void)mbar_wait_bounded(&full[i], i < s ? ph : ph ^ 1);
+        if (used >> i & 1) (void)mbar_wait_asleep(&full[i], i < s ? ph : ph ^ 1);
     return;
   }
 
@@ -509,7 +529,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   int side = 0;      // of the double-buffered sums
   for (;; ++row) {
     if (row == row_end) {      // the next unit of rows
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&jfull[js], jph));
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&jfull[js], jph));
       if (!ok) break;          // (the fetching warp has stopped: no warp gets another unit)
       const longlong2 jb = job[js];
       __syncwarp();
@@ -557,7 +577,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     a.base = a.thr = TK_LOWEST; a.nm = -TK_LOWEST; a.delta = 0.f; a.clamp = ni; a.fast = false; a.s2 = a.t2 = pk2(0.f, 0.f);
     int rs = s;
     for (int j = 0; j < K; ++j) {
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph));
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
       if (!ok) { bad = 1; break; }
       if (j == x) rs = s;
       const int id = j < x ? n + j : j - x, len = min(chunk, nw - id * chunk);
@@ -601,7 +621,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     if (warp == W - 1) {
       c.m = TK_LOWEST; c.s = c.t = 0.f;
       if (lane < W) { const float4 o = sums[side][lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
-      warp_combine(c, p.k);
+      warp_combine(c, p.k, W);      // (lane 0 uses the result)
       const RowStat st = row_stat(c, zy, p.inv_tau);
       if (lane == 0) store_stat(f, row, st);
       if (BACK) {
@@ -640,7 +660,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       int at = rs + j;
       if (j < n) { if (at >= N) at -= N; }
       else {
-        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph));
+        ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
         if (!ok) { bad = 1; break; }
         at = s;
         if (++s == N) { s = 0; ph ^= 1; }
