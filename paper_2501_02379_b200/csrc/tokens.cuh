@@ -325,6 +325,7 @@ constexpr int RW_MAX_WARPS = 16, RW_MAX_PLACES = 16, RW_JOBS = 4, RW_NV = 4;    
 struct RowGeom {
   int W, N;              // arithmetic warps, places of the ring
   int unit;              // rows that a block takes at a time
+  int K, last;           // chunks of the longest row, granules before the last of them; others have at most one chunk less
   float reach, lowest;   // 200 / k; lowest value that the clamp may take in the storage type
   float slack;           // 40 / k
 };
@@ -492,7 +493,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
         if (ok) { job[js] = make_longlong2(unit, ym); mbar_arrive(&jfull[js]); }
         for (; live && ok; live &= live - 1) {
           const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
-          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = (nw + chunk - 1) / chunk, n = !BACK ? 0 : K <= N ? K : N - 2;
+          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = geo.K - (nw <= geo.last), n = !BACK ? 0 : K <= N ? K : N - 2;
           for (int j = 0; j < (BACK ? 2 * K - n : K) && ok; ++j) {
             const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
             ok = mbar_wait_asleep(&empty[s], ph ^ 1);
@@ -524,10 +525,13 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   // ---- the arithmetic warps ----
   const uint32_t ni = neg_inf_word<KIND>();
   const uint4* const places = reinterpret_cast<const uint4*>(ring);
+  const int64_t zstep = p.ldz * B, dstep = p.lddz * B;
+  const char* zrow = p.z;
+  char* drow = p.dz;
   int64_t row = 0, row_end = 0;
   long long y_next = -1;
   int side = 0;      // of the double-buffered sums
-  for (;; ++row) {
+  for (;; ++row, zrow += zstep, drow += dstep) {
     if (row == row_end) {      // the next unit of rows
       ok = __all_sync(0xffffffffu, mbar_wait_asleep(&jfull[js], jph));
       if (!ok) break;          // (the fetching warp has stopped: no warp gets another unit)
@@ -538,13 +542,14 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       if (jb.x < 0) break;
       row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
       y_next = jb.y;
+      zrow = p.z + row * zstep; drow = p.dz + row * dstep;
     }
     const long long y = y_next;
     if (row + 1 < row_end) y_next = p.y[row + 1];
-    const Row<KIND> r(p.z + row * p.ldz * B, p.V);
-    char* drow = p.dz + row * p.lddz * B;
+    const Row<KIND> r(zrow, p.V);
     const bool same = same_alignment(r, drow);
-    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = (nw + chunk - 1) / chunk, n = !BACK ? 0 : K <= N ? K : N - 2, x = K - n;
+    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = geo.K - (nw <= geo.last), n = !BACK ? 0 : K <= N ? K : N - 2, x = K - n;
+    const int tail = nw - (K - 1) * chunk;      // granules of the last chunk
     if (y < 0) {
       if (BACK)
         for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
@@ -580,17 +585,17 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
       if (!ok) { bad = 1; break; }
       if (j == x) rs = s;
-      const int id = j < x ? n + j : j - x, len = min(chunk, nw - id * chunk);
+      const bool end = j == (x > 0 ? x : K) - 1;      // the row's last chunk
       const uint4* place = places + s * chunk + tid;
       uint4 v[RW_NV];
-      if (len == chunk) {
+      if (!end || tail == chunk) {
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
       } else {
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) {
           v[u] = make_uint4(ni, ni, ni, ni);
-          if (tid + u * threads < len) v[u] = place[u * threads];
+          if (tid + u * threads < tail) v[u] = place[u * threads];
         }
       }
       if (j < x) {
@@ -634,7 +639,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
         h.target = o.g * sc; h.zy = zy;
         // the thread that writes the target's granule (an edge entry: the lane that has it)
         const int l = y < p.V ? (r.mis + (int)y) / E - wa : -1;
-        h.owner = l >= 0 && l < nw ? (l % chunk) % threads : -1;
+        h.owner = l >= 0 && l < nw ? l % threads : -1;
         handed = h;
         q.terms[row] = o.terms;
       }
@@ -656,28 +661,27 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.c0; gc.c1 = h.c1;
       st_real<KIND>(drow + (int64_t)edge * B, grad_target<KIND, ENT>(xe, gc, edge == y ? h.target : 0.f));
     }
-    for (int j = 0; j < K; ++j) {
-      int at = rs + j;
-      if (j < n) { if (at >= N) at -= N; }
-      else {
+    uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + wa + tid;
+    int at = rs;
+    for (int j = 0; j < K; ++j, dst += chunk) {
+      if (j >= n) {
         ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
         if (!ok) { bad = 1; break; }
         at = s;
         if (++s == N) { s = 0; ph ^= 1; }
       }
-      const int len = min(chunk, nw - j * chunk), g0 = wa + j * chunk;
       const uint4* place = places + at * chunk + tid;
       uint4 v[RW_NV];
-      if (len == chunk && same) {
+      if (same && (j < K - 1 || tail == chunk)) {
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[at]);
-        uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + g0 + tid;
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
       } else {
+        const int len = j < K - 1 ? chunk : tail, g0 = wa + j * chunk;
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) v[u] = place[u * threads];
@@ -687,6 +691,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
       }
+      if (++at == N) at = 0;
     }
     // the target's entry once more, by the thread that wrote its granule
     if (tid == h.owner) {
@@ -703,12 +708,12 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   }
 }
 
-// Short rows (up to 8 KB): a warp takes one at a time, four granules per lane in a batch.  Nothing is shared, so the latency
+// Short rows (up to 16 KB): a warp takes one at a time, four granules per lane in a batch.  Nothing is shared, so the latency
 // of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers for every
 // row took 66 us instead of 23 us for 16384 rows of 1000 bf16 logits).  A row of more than one batch is read again for the
 // gradient, from the L1 cache, which the 32 rows in work on an SM fit (keeping it in 64 registers per lane leaves room for
 // half as many warps: 64 us instead of SHORT us for 12384 rows of 3001 bf16 logits).
-constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 512;
+constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 1024;
 template <int KIND, int MODE>
 __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f, int64_t rows) {
   constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
@@ -880,7 +885,7 @@ template <int KIND, bool ENT>
 __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, int64_t rows, uint32_t G) {
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t at = (int64_t)blockIdx.x * TB2_THREADS + threadIdx.x, row = at / G;
+  const int64_t at = (int64_t)(gridDim.x - 1 - blockIdx.x) * TB2_THREADS + threadIdx.x, row = at / G;
   const int g = (int)(at - row * G);
   if (row >= rows) return;
   const long long y = p.y[row];
@@ -903,8 +908,10 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __
   constexpr int NV = 4;
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t row = blockIdx.x / pieces;
-  const int piece = (int)(blockIdx.x - (uint32_t)row * pieces);
+  // last rows first: what the forward pass read last is still in the L2 cache
+  const uint32_t block = gridDim.x - 1 - blockIdx.x;
+  const int64_t row = block / pieces;
+  const int piece = (int)(block - (uint32_t)row * pieces);
   const long long y = p.y[row];
   const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
   char* drow = p.dz + row * p.lddz * Gran<KIND>::B;

@@ -280,16 +280,17 @@ tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const Policy
   if (bytes <= SR_MAX_GRANULES * 16) return launch_short<KIND, MODE>(in, a, q, f, st);
   const int sm = sm_count();
   RowGeom g; memset(&g, 0, sizeof(g));
-  // the smallest blocks whose share of the ring holds a row and a quarter of the next
-  const int warps[4] = {2, 4, 8, 16}, blocks[4] = {6, MODE == RW_FORWARD ? 6 : 4, 2, 1};
-  int per_sm = 1;
-  for (int i = 0; i < 4; ++i) {
-    g.W = warps[i]; per_sm = blocks[i];
-    if (MODE == RW_FORWARD && g.W == 4) break;      // (nothing stays: blocks of four warps whatever the row's length)
-    if (bytes * 5 / 4 <= (int64_t)((kRingBytes + 1024 - 2560 * per_sm) / per_sm)) break;
-  }
+  // The smallest blocks in whose rings at least half of a row stays: more of them share an SM, and one computes while
+  // another waits at its barriers.  Measured with 4 / 8 / 16 warps (4 / 2 / 1 blocks per SM): rows of 16 KB 114 / 147 / - us,
+  // 64 KB 203 / 221 / - us, 100 KB 320 / 347 / 426 us, 128 KB 228 / 201 / 219 us, 200 KB 366 / 304 / 322 us, 256 KB 877 / 795 / 678 us.
+  // Log-probabilities alone keep nothing of a row: always four warps, six blocks.
+  int per_sm = MODE == RW_FORWARD ? 6 : 4;
+  g.W = 4;
+  while (MODE != RW_FORWARD && g.W < RW_MAX_WARPS && bytes > 2 * (int64_t)(kRingBytes / per_sm)) { g.W *= 2; per_sm /= 2; }
   const size_t chunk = (size_t)g.W * 32 * RW_NV * 16;
   const int64_t places = (int64_t)((kRingBytes + 2560 - 2560 * per_sm) / per_sm / chunk);      // a block's own shared memory: 2.5 KB
+  const int64_t G = max_granules(in), per = (int64_t)g.W * 32 * RW_NV;
+  g.K = (int)((G + per - 1) / per); g.last = (int)((g.K - 1) * per);
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
   g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
   auto kern = token_row_kernel<KIND, MODE>;
