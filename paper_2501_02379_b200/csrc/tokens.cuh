@@ -436,6 +436,66 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+struct RowBarriers {
+  uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES], jfull[RW_JOBS], jempty[RW_JOBS], nbar;
+  alignas(16) uint4 answer;
+  longlong2 job[RW_JOBS];     // unit of rows (-1: no more), target of its first row
+  __device__ __forceinline__ void init(int N, int W) {
+    for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
+    for (int i = 0; i < RW_JOBS; ++i) { mbar_init(&jfull[i], 1); mbar_init(&jempty[i], W); }
+    mbar_init(&nbar, 1);
+    fence_mbar_init();
+  }
+};
+
+// The fetching warp: takes units of rows, passes them on, and asks for the chunks of their live rows.  STAY: chunks stay
+// for a second reading (n of them, see above); else each goes through the ring once.  LAST_FIRST: the units from the end.
+template <int KIND, bool STAY, bool LAST_FIRST>
+__device__ __forceinline__ void fetch_rows(const TokenArgs& p, int64_t rows, const RowGeom& geo, unsigned char* ring, RowBarriers& rb, int lane, int chunk) {
+  constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
+  const int N = geo.N;
+  int s = 0, js = 0;
+  uint32_t ph = 0, jph = 0, used = 0, nph = 0;
+  bool ok = true;
+  for (int64_t block = blockIdx.x; ok;) {
+    if (lane == 0) next_block_ask(&rb.answer, &rb.nbar);
+    const int64_t unit = LAST_FIRST ? (int64_t)gridDim.x - 1 - block : block, r0 = unit * geo.unit, mine = r0 + lane;
+    const long long ym = lane < geo.unit && mine < rows ? p.y[mine] : -1;
+    uint32_t live = __ballot_sync(0xffffffffu, ym >= 0);
+    if (lane == 0) {
+      ok = mbar_wait_asleep(&rb.jempty[js], jph ^ 1);
+      if (ok) { rb.job[js] = make_longlong2(unit, ym); mbar_arrive(&rb.jfull[js]); }
+      for (; live && ok; live &= live - 1) {
+        const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
+        const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = geo.K - (nw <= geo.last), n = !STAY ? 0 : K <= N ? K : N - 2;
+        for (int j = 0; j < (STAY ? 2 * K - n : K) && ok; ++j) {
+          const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
+          ok = mbar_wait_asleep(&rb.empty[s], ph ^ 1);
+          if (!ok) break;
+          mbar_expect_tx(&rb.full[s], (uint32_t)len * 16);
+          bulk_g2s(ring + (size_t)s * chunk * 16, r.base + (size_t)(wa + at) * 16, (uint32_t)len * 16, &rb.full[s]);
+          used |= 1u << s;
+          if (++s == N) { s = 0; ph ^= 1; }
+        }
+      }
+    }
+    if (++js == RW_JOBS) { js = 0; jph ^= 1; }
+    // (the answer is taken, after a failure too, before the block may end)
+    const bool got = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.nbar, nph));
+    nph ^= 1;
+    const int next = got ? next_block_get(&rb.answer) : -1;
+    __syncwarp();
+    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    if (next < 0) break;
+    block = next;
+  }
+  if (lane == 0 && ok && mbar_wait_asleep(&rb.jempty[js], jph ^ 1)) { rb.job[js] = make_longlong2(-1, 0); mbar_arrive(&rb.jfull[js]); }
+  // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
+  if (lane == 0)
+    for (int i = 0; i < N; ++i)
+      if (used >> i & 1) (void)mbar_wait_asleep(&rb.full[i], i < s ? ph : ph ^ 1);
+}
+
 struct ForwardArgs {
   float* logp; float* lse; float* entropy;      // out, may be null
   float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
@@ -461,17 +521,12 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   __shared__ float4 sums[2][RW_MAX_WARPS];
   __shared__ __align__(16) RowGrad handed;
   __shared__ volatile int bad;           // a wait ran out of its bound
-  __shared__ __align__(8) uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES], jfull[RW_JOBS], jempty[RW_JOBS], nbar;
-  __shared__ __align__(16) uint4 answer;
-  __shared__ longlong2 job[RW_JOBS];     // unit of rows (-1: no more), target of its first row
+  __shared__ RowBarriers rb;
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
   const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     bad = 0;
-    for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
-    for (int i = 0; i < RW_JOBS; ++i) { mbar_init(&jfull[i], 1); mbar_init(&jempty[i], W); }
-    mbar_init(&nbar, 1);
-    fence_mbar_init();
+    rb.init(N, W);
   }
   __syncthreads();
   griddep_wait();
@@ -481,44 +536,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   bool ok = true;
 
   if (warp == W) {
-    // ---- the fetching warp ----
-    uint32_t used = 0, nph = 0;
-    for (int64_t unit = blockIdx.x; ok;) {
-      if (lane == 0) next_block_ask(&answer, &nbar);
-      const int64_t r0 = unit * geo.unit, mine = r0 + lane;
-      const long long ym = lane < geo.unit && mine < rows ? p.y[mine] : -1;
-      uint32_t live = __ballot_sync(0xffffffffu, ym >= 0);
-      if (lane == 0) {
-        ok = mbar_wait_asleep(&jempty[js], jph ^ 1);
-        if (ok) { job[js] = make_longlong2(unit, ym); mbar_arrive(&jfull[js]); }
-        for (; live && ok; live &= live - 1) {
-          const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
-          const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = geo.K - (nw <= geo.last), n = !BACK ? 0 : K <= N ? K : N - 2;
-          for (int j = 0; j < (BACK ? 2 * K - n : K) && ok; ++j) {
-            const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
-            ok = mbar_wait_asleep(&empty[s], ph ^ 1);
-            if (!ok) break;
-            mbar_expect_tx(&full[s], (uint32_t)len * 16);
-            bulk_g2s(ring + (size_t)s * chunk * 16, r.base + (size_t)(wa + at) * 16, (uint32_t)len * 16, &full[s]);
-            used |= 1u << s;
-            if (++s == N) { s = 0; ph ^= 1; }
-          }
-        }
-      }
-      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
-      // (the answer is taken, after a failure too, before the block may end)
-      const bool got = __all_sync(0xffffffffu, mbar_wait_asleep(&nbar, nph));
-      nph ^= 1;
-      unit = got ? next_block_get(&answer) : -1;
-      __syncwarp();
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-      if (unit < 0) break;
-    }
-    if (lane == 0 && ok && mbar_wait_asleep(&jempty[js], jph ^ 1)) { job[js] = make_longlong2(-1, 0); mbar_arrive(&jfull[js]); }
-    // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
-    if (lane == 0)
-      for (int i = 0; i < N; ++i)
-        if (used >> i & 1) (void)mbar_wait_asleep(&full[i], i < s ? ph : ph ^ 1);
+    fetch_rows<KIND, BACK, false>(p, rows, geo, ring, rb, lane, chunk);
     return;
   }
 
@@ -533,11 +551,11 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   int side = 0;      // of the double-buffered sums
   for (;; ++row, zrow += zstep, drow += dstep) {
     if (row == row_end) {      // the next unit of rows
-      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&jfull[js], jph));
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], jph));
       if (!ok) break;          // (the fetching warp has stopped: no warp gets another unit)
-      const longlong2 jb = job[js];
+      const longlong2 jb = rb.job[js];
       __syncwarp();
-      if (lane == 0) mbar_arrive(&jempty[js]);
+      if (lane == 0) mbar_arrive(&rb.jempty[js]);
       if (++js == RW_JOBS) { js = 0; jph ^= 1; }
       if (jb.x < 0) break;
       row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
@@ -582,7 +600,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     a.base = a.thr = TK_LOWEST; a.nm = -TK_LOWEST; a.delta = 0.f; a.clamp = ni; a.fast = false; a.s2 = a.t2 = pk2(0.f, 0.f);
     int rs = s;
     for (int j = 0; j < K; ++j) {
-      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
       if (!ok) { bad = 1; break; }
       if (j == x) rs = s;
       const bool end = j == (x > 0 ? x : K) - 1;      // the row's last chunk
@@ -600,7 +618,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       }
       if (j < x) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[s]);
+        if (lane == 0) mbar_arrive(&rb.empty[s]);
       }
       if (++s == N) { s = 0; ph ^= 1; }
       add_chunk<KIND>(a, v, geo, p.k);
@@ -665,7 +683,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     int at = rs;
     for (int j = 0; j < K; ++j, dst += chunk) {
       if (j >= n) {
-        ok = __all_sync(0xffffffffu, mbar_wait_asleep(&full[s], ph));
+        ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
         if (!ok) { bad = 1; break; }
         at = s;
         if (++s == N) { s = 0; ph ^= 1; }
@@ -676,7 +694,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
         __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[at]);
+        if (lane == 0) mbar_arrive(&rb.empty[at]);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
@@ -686,7 +704,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) v[u] = place[u * threads];
         __syncwarp();
-        if (lane == 0) mbar_arrive(&empty[at]);
+        if (lane == 0) mbar_arrive(&rb.empty[at]);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
@@ -857,8 +875,8 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   if (POLICY) q.terms[row] = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q).terms;
 }
 
-// Gradient pass: one block per piece of NV * THREADS granules of a row, or (SHORT, rows of fewer granules) of the granules of
-// all rows one after the other.
+// Gradient pass: short rows, one granule per thread and all rows one after the other; longer ones through the ring.  The
+// rows are taken from the end: what the forward pass read last is still in the L2 cache.
 struct BackwardArgs {
   const float* lse;          // of the forward call, or
   const float2* stat;        // (M, log2 S), more exact where lse is large
@@ -903,43 +921,105 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_short_kernel(co
   store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v, gc));
   if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
 }
+
 template <int KIND, bool ENT>
-__global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, uint32_t pieces) {
-  constexpr int NV = 4;
+__global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, int64_t rows, const __grid_constant__ RowGeom geo) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ RowBarriers rb;
+  constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
+  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) rb.init(N, W);
+  __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
-  // last rows first: what the forward pass read last is still in the L2 cache
-  const uint32_t block = gridDim.x - 1 - blockIdx.x;
-  const int64_t row = block / pieces;
-  const int piece = (int)(block - (uint32_t)row * pieces);
-  const long long y = p.y[row];
-  const Row<KIND> r(p.z + row * p.ldz * Gran<KIND>::B, p.V);
-  char* drow = p.dz + row * p.lddz * Gran<KIND>::B;
-  const bool same = same_alignment(r, drow);
-  const int G = r.granules(), g0 = piece * NV * TB2_THREADS, g1 = min(G, g0 + NV * TB2_THREADS);
-  if (g0 >= g1) return;
-  if (y < 0) {
-    for (int g = g0 + threadIdx.x; g < g1; g += TB2_THREADS) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+  if (warp == W) {
+    fetch_rows<KIND, false, true>(p, rows, geo, ring, rb, lane, chunk);
     return;
   }
-  uint4 v[NV];
+  const uint4* const places = reinterpret_cast<const uint4*>(ring);
+  const int64_t zstep = p.ldz * B, dstep = p.lddz * B;
+  const char* zrow = p.z;
+  char* drow = p.dz;
+  int s = 0, js = 0;
+  uint32_t ph = 0, jph = 0;
+  int64_t row = 0, row_end = 0;
+  long long y_next = -1;
+  GradCoef c_next; float t_next = 0.f;      // of the next row, asked for while this one is worked on
+  c_next.M = c_next.k = c_next.ls2 = c_next.c0 = c_next.c1 = 0.f;
+  bool ok = true;
+  for (;; ++row, zrow += zstep, drow += dstep) {
+    if (row == row_end) {      // the next unit of rows
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], jph));
+      if (!ok) break;
+      const longlong2 jb = rb.job[js];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&rb.jempty[js]);
+      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
+      if (jb.x < 0) break;
+      row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
+      y_next = jb.y;
+      zrow = p.z + row * zstep; drow = p.dz + row * dstep;
+      if (y_next >= 0) backward_coef<KIND, ENT>(p, b, row, y_next, c_next, t_next);
+    }
+    const long long y = y_next;
+    const GradCoef gc = c_next;
+    const float target = t_next;
+    if (row + 1 < row_end) {
+      y_next = p.y[row + 1];
+      backward_coef<KIND, ENT>(p, b, row + 1, y_next, c_next, t_next);      // (of an ignored row: read, not used)
+    }
+    const Row<KIND> r(zrow, p.V);
+    const bool same = same_alignment(r, drow);
+    if (y < 0) {
+      for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      continue;
+    }
+    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = geo.K - (nw <= geo.last), tail = nw - (K - 1) * chunk;
+    // the entries outside the whole granules, and the target's logit, by the threads that overwrite them
+    if (warp == 0) {
+      const int h = min(p.V, wa * E - r.mis * wa), t0 = max(h, wb * E - r.mis);
+      const int edge = lane < h ? lane : (lane >= 16 && t0 + lane - 16 < p.V ? t0 + lane - 16 : -1);
+      if (edge >= 0) st_real<KIND>(drow + (int64_t)edge * B, grad_target<KIND, ENT>(ld_real<KIND>(r.base + (int64_t)(r.mis + edge) * B), gc, edge == y ? target : 0.f));
+    }
+    const int ly = y < p.V ? (r.mis + (int)y) / E - wa : -1;
+    const bool mine = ly >= 0 && ly < nw && (ly - tid) % threads == 0;
+    float zy = 0.f;
+    if (mine) zy = target_logit<KIND>(p, row, y);
+    RowGrad h;
+    h.M = gc.M; h.ls2 = gc.ls2; h.c0 = gc.c0; h.c1 = gc.c1; h.nb = fmaf(-gc.M, p.k, -gc.ls2);
+    const bool fast = KIND != LS_F32 && fabsf(h.M) < 1e30f;
+    uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + wa + tid;
+    for (int j = 0; j < K; ++j, dst += chunk) {
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
+      if (!ok) break;
+      const uint4* place = places + s * chunk + tid;
+      uint4 v[RW_NV];
+      if (same && (j < K - 1 || tail == chunk)) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
-    if (g < g1) v[i] = r.load(g);
-  }
-  GradCoef gc; float target;
-  backward_coef<KIND, ENT>(p, b, row, y, gc, target);
-  const int gy = y < p.V ? (r.mis + (int)y) / Gran<KIND>::E : -1;
-  const bool mine = gy >= g0 && gy < g1 && (gy - g0) % TB2_THREADS == (int)threadIdx.x;
-  float zy = 0.f;
-  if (mine) zy = target_logit<KIND>(p, row, y);      // before this thread overwrites it, where the gradient replaces the logits
+        for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&rb.empty[s]);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int g = g0 + (int)threadIdx.x + i * TB2_THREADS;
-    if (g < g1) store_granule<KIND>(r, drow, same, g, grad_granule<KIND, ENT>(v[i], gc));
+        for (int u = 0; u < RW_NV; ++u)
+          st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
+      } else {
+        const int len = j < K - 1 ? chunk : tail, g0 = wa + j * chunk;
+#pragma unroll
+        for (int u = 0; u < RW_NV; ++u)
+          if (tid + u * threads < len) v[u] = place[u * threads];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&rb.empty[s]);
+#pragma unroll
+        for (int u = 0; u < RW_NV; ++u)
+          if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
+      }
+      if (++s == N) { s = 0; ph ^= 1; }
+    }
+    if (!ok) break;
+    if (mine) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, target));
   }
-  if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
+  // a wait that ran out of its bound (nothing this kernel does leads there) leaves a NaN in the gradient
+  if (!ok && tid == 0) st_real<KIND>(p.dz, __int_as_float(0x7fc00000));
 }
 
 // ---------------------------------------------------------------------------------------------------------------

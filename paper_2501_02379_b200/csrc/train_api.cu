@@ -229,28 +229,6 @@ tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a
   return TGRAD_OK;
 }
 
-template <bool ENT>
-tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
-  const int64_t G = max_granules(in), pieces = (G + 4 * TB2_THREADS - 1) / (4 * TB2_THREADS);
-  if (G <= 2 * TB2_THREADS) {      // a block for each row would be half empty or worse
-    const int64_t blocks = (in->rows * G + TB2_THREADS - 1) / TB2_THREADS;
-    if (blocks >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks);
-    if (kind == LS_F32) launch_chained(token_backward_short_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
-    else if (kind == LS_F16) launch_chained(token_backward_short_kernel<LS_F16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
-    else launch_chained(token_backward_short_kernel<LS_BF16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
-    TG_LAUNCH_CHECK();
-    return TGRAD_OK;
-  }
-  if (in->rows * pieces >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)(in->rows * pieces));
-  if (kind == LS_F32) launch_chained(token_backward_kernel<LS_F32, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
-  else if (kind == LS_F16) launch_chained(token_backward_kernel<LS_F16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
-  else launch_chained(token_backward_kernel<LS_BF16, ENT>, grid, dim3(TB2_THREADS), 0, st, a, b, (uint32_t)pieces);
-  TG_LAUNCH_CHECK();
-  return TGRAD_OK;
-}
-
 // The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 16 arithmetic warps for all of them at most.
 constexpr size_t kRingBytes = 224 * 1024;
 // Dynamic shared memory beyond the default, once per kernel and device.
@@ -274,38 +252,68 @@ tgrad_status launch_short(const tgrad_logits* in, const TokenArgs& a, const Poli
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
-template <int KIND, int MODE>
-tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
-  const int64_t bytes = max_granules(in) * 16;
-  if (bytes <= SR_MAX_GRANULES * 16) return launch_short<KIND, MODE>(in, a, q, f, st);
+// Ring of a kernel on rows: `stay`, a row is read twice; else blocks of four warps, `blocks` of them to an SM.
+RowGeom row_geom(const tgrad_logits* in, float k, bool stay, int blocks, int64_t* grid) {
   const int sm = sm_count();
+  const int64_t G = max_granules(in), bytes = G * 16;
   RowGeom g; memset(&g, 0, sizeof(g));
   // The smallest blocks in whose rings at least half of a row stays: more of them share an SM, and one computes while
   // another waits at its barriers.  Measured with 4 / 8 / 16 warps (4 / 2 / 1 blocks per SM): rows of 16 KB 114 / 147 / - us,
   // 64 KB 203 / 221 / - us, 100 KB 320 / 347 / 426 us, 128 KB 228 / 201 / 219 us, 200 KB 366 / 304 / 322 us, 256 KB 877 / 795 / 678 us.
-  // Log-probabilities alone keep nothing of a row: always four warps, six blocks.
-  int per_sm = MODE == RW_FORWARD ? 6 : 4;
+  int per_sm = blocks;
   g.W = 4;
-  while (MODE != RW_FORWARD && g.W < RW_MAX_WARPS && bytes > 2 * (int64_t)(kRingBytes / per_sm)) { g.W *= 2; per_sm /= 2; }
+  while (stay && g.W < RW_MAX_WARPS && bytes > 2 * (int64_t)(kRingBytes / per_sm)) { g.W *= 2; per_sm /= 2; }
   const size_t chunk = (size_t)g.W * 32 * RW_NV * 16;
   const int64_t places = (int64_t)((kRingBytes + 2560 - 2560 * per_sm) / per_sm / chunk);      // a block's own shared memory: 2.5 KB
-  const int64_t G = max_granules(in), per = (int64_t)g.W * 32 * RW_NV;
+  const int64_t per = (int64_t)g.W * 32 * RW_NV;
   g.K = (int)((G + per - 1) / per); g.last = (int)((g.K - 1) * per);
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
-  g.reach = 200.f / a.k; g.slack = 40.f / a.k; g.lowest = KIND == LS_F16 ? -65000.f : -1e38f;
-  auto kern = token_row_kernel<KIND, MODE>;
-  static std::atomic<uint64_t> done{0};
-  TG_TRY(allow_shared(kern, kRingBytes, done));
+  g.reach = 200.f / k; g.slack = 40.f / k; g.lowest = token_kind(in->dtype) == LS_F16 ? -65000.f : -1e38f;
   // units of about 64 KB of logits, at most a warp's width of rows, and several for every block
   int64_t unit = (64 << 10) / bytes;
   if (unit > 32) unit = 32;
   const int64_t fair = in->rows / ((int64_t)sm * per_sm * 4);
   if (unit > fair) unit = fair;
   g.unit = (int)(unit < 1 ? 1 : unit);
-  const int64_t grid = (in->rows + g.unit - 1) / g.unit;
-  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), chunk * g.N, st, a, q, f, in->rows, g);
+  *grid = (in->rows + g.unit - 1) / g.unit;
+  return g;
+}
+inline size_t ring_bytes(const RowGeom& g) { return (size_t)g.W * 32 * RW_NV * 16 * g.N; }
+
+template <int KIND, int MODE>
+tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
+  if (max_granules(in) <= SR_MAX_GRANULES) return launch_short<KIND, MODE>(in, a, q, f, st);
+  int64_t grid;
+  const RowGeom g = row_geom(in, a.k, MODE != RW_FORWARD, MODE == RW_FORWARD ? 6 : 4, &grid);
+  auto kern = token_row_kernel<KIND, MODE>;
+  static std::atomic<uint64_t> done{0};
+  TG_TRY(allow_shared(kern, kRingBytes, done));
+  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), ring_bytes(g), st, a, q, f, in->rows, g);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
+}
+template <int KIND, bool ENT>
+tgrad_status launch_gradient(const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
+  const int64_t G = max_granules(in);
+  if (G <= SR_MAX_GRANULES) {
+    const int64_t blocks = (in->rows * G + TB2_THREADS - 1) / TB2_THREADS;
+    if (blocks >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
+    launch_chained(token_backward_short_kernel<KIND, ENT>, dim3((unsigned)blocks), dim3(TB2_THREADS), 0, st, a, b, in->rows, (uint32_t)G);
+  } else {
+    int64_t grid;
+    const RowGeom g = row_geom(in, a.k, false, 4, &grid);
+    auto kern = token_gradient_kernel<KIND, ENT>;
+    static std::atomic<uint64_t> done{0};
+    TG_TRY(allow_shared(kern, kRingBytes, done));
+    launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), ring_bytes(g), st, a, b, in->rows, g);
+  }
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
+template <bool ENT>
+tgrad_status launch_backward(int kind, const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
+  return kind == LS_F32 ? launch_gradient<LS_F32, ENT>(in, a, b, st)
+         : kind == LS_F16 ? launch_gradient<LS_F16, ENT>(in, a, b, st) : launch_gradient<LS_BF16, ENT>(in, a, b, st);
 }
 template <int MODE>
 tgrad_status launch_row_kind(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
