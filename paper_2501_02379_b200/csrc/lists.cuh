@@ -179,7 +179,8 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
 }
 
 // Partial sums of squares.  Block b writes one per tensor t it has chunks of, at slot b + t: along the list each next
-// (block, tensor) pair has a larger b + t, so the slots are distinct and a tensor's slots are b0 + t .. b1 + t.
+// (block, tensor) pair has a larger b + t, so the slots are distinct and a tensor's slots are b0 + t .. b1 + t.  Slots that
+// no pair has are set to zero by the block before them, so that all grid + n of them may be added up.
 template <int CAP>
 __global__ void __launch_bounds__(LS_THREADS, 4) list_sumsq_kernel(const __grid_constant__ ListParams<CAP> p, double* __restrict__ partial) {
   __shared__ double sh[LS_THREADS / 32];
@@ -189,6 +190,8 @@ __global__ void __launch_bounds__(LS_THREADS, 4) list_sumsq_kernel(const __grid_
   const uint32_t c1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * p.total / gridDim.x);
   if (c >= c1) return;
   int t = list_find(p, c);
+  if (blockIdx.x == 0)
+    for (int i = (int)threadIdx.x; i < t; i += LS_THREADS) partial[i] = 0.0;
   while (c < c1) {
     while (p.first[t + 1] <= c) ++t;
     const ListEntry e = p.e[t];
@@ -197,44 +200,71 @@ __global__ void __launch_bounds__(LS_THREADS, 4) list_sumsq_kernel(const __grid_
     for (; c < stop; ++c) acc += sumsq_chunk(e, c - p.first[t], p.gpc_log2);
     const double sum = block_sum(acc, sh);
     if (threadIdx.x == 0) partial[blockIdx.x + t] = sum;
+    // up to the next pair's slot
+    int next = t + 1;
+    uint32_t slot = blockIdx.x;
+    if (c >= c1) ++slot;                                     // the next block's first tensor, or the end of the slots
+    if (c < p.total) { next = t; while (p.first[next + 1] <= c) ++next; } else { next = p.n; }
+    for (uint32_t i = blockIdx.x + t + 1 + threadIdx.x; i < slot + next; i += LS_THREADS) partial[i] = 0.0;
   }
 }
 
-// One block: the tensors' norms, and after the last slice of a long list the global norm and the coefficient.
+// The coefficient that brings a global norm down to max_norm.
+__device__ __forceinline__ float clip_coefficient(float norm, float max_norm) {
+  const float c = max_norm < __int_as_float(0x7f800000) ? max_norm / (norm + 1e-6f) : 1.f;
+  return c < 1.f || c != c ? c : 1.f;
+}
+// The tensors' norms, and after the last slice of a long list the global norm and the coefficient, by one block.
 // out[0] norm, out[1] coefficient, out[2 + i] norm of tensor i.  slice_sum[s] keeps the sums of the slices so far.
-constexpr int LF_THREADS = 1024;
+struct NormArgs {
+  const double* partial;
+  uint32_t grid;         // of the kernel that wrote them
+  int base, slice, last;
+  double* slice_sum;
+  float max_norm;
+  float* out;
+};
+// All partial sums of one slice, in a fixed order; valid in every thread.  sh: 8 doubles.
+__device__ __forceinline__ double norm_sum(const double* __restrict__ partial, uint32_t slots, double* sh) {
+  double s = 0.0;
+  for (uint32_t i = threadIdx.x; i < slots; i += LS_THREADS) s += partial[i];
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < LS_THREADS / 32; ++w) s += sh[w];
+  return s;
+}
+// One tensor's norm per warp, all at once (they are latency and nothing else), and by the first block the global results.
 template <int CAP>
-__global__ void __launch_bounds__(LF_THREADS) list_norm_kernel(const __grid_constant__ ListParams<CAP> p, const double* __restrict__ partial,
-                                                               uint32_t grid, int base, int slice, int last, double* slice_sum,
-                                                               float max_norm, float* __restrict__ out) {
-  __shared__ double sh[LF_THREADS / 32];
-  griddep_wait();
-  griddep_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  double mine = 0.0;
-  for (int t = warp; t < p.n; t += LF_THREADS / 32) {
+__device__ __forceinline__ void write_norms(const ListParams<CAP>& p, const NormArgs& a, uint32_t block, double* sh) {
+  const int t = (int)block * (LS_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (t < p.n) {
     const uint32_t f0 = p.first[t], f1 = p.first[t + 1];
     double s = 0.0;
     if (f1 > f0) {      // the blocks of chunks f0 and f1 - 1
-      const uint32_t b0 = (uint32_t)((((uint64_t)f0 + 1) * grid - 1) / p.total), b1 = (uint32_t)(((uint64_t)f1 * grid - 1) / p.total);
-      for (uint32_t b = b0 + lane; b <= b1; b += 32) s += partial[b + t];
+      const uint32_t b0 = (uint32_t)((((uint64_t)f0 + 1) * a.grid - 1) / p.total), b1 = (uint32_t)(((uint64_t)f1 * a.grid - 1) / p.total);
+      for (uint32_t b = b0 + lane; b <= b1; b += 32) s += a.partial[b + t];
       for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     }
-    if (lane == 0) out[2 + base + t] = (float)sqrt(s);
-    mine += s;
+    if (lane == 0) a.out[2 + a.base + t] = (float)sqrt(s);
   }
-  if (lane == 0) sh[warp] = mine;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int w = 0; w < LF_THREADS / 32; ++w) s += sh[w];
-    if (!last) { slice_sum[slice] = s; return; }
-    for (int i = 0; i < slice; ++i) s += slice_sum[i];
-    const float norm = (float)sqrt(s);
-    const float c = max_norm < __int_as_float(0x7f800000) ? max_norm / (norm + 1e-6f) : 1.f;
-    out[0] = norm;
-    out[1] = c < 1.f || c != c ? c : 1.f;
-  }
+  if (block != 0) return;
+  double s = a.grid > 0 ? norm_sum(a.partial, a.grid + p.n - 1, sh) : 0.0;
+  if (threadIdx.x != 0) return;
+  if (!a.last) { a.slice_sum[a.slice] = s; return; }
+  for (int i = 0; i < a.slice; ++i) s += a.slice_sum[i];
+  const float norm = (float)sqrt(s);
+  a.out[0] = norm;
+  a.out[1] = clip_coefficient(norm, a.max_norm);
+}
+template <int CAP>
+__global__ void __launch_bounds__(LS_THREADS) list_norm_kernel(const __grid_constant__ ListParams<CAP> p, const __grid_constant__ NormArgs a) {
+  __shared__ double sh[LS_THREADS / 32];
+  griddep_wait();
+  griddep_launch_dependents();
+  write_norms<CAP>(p, a, blockIdx.x, sh);
 }
 
 // x <- c x for one chunk: every entry is multiplied in fp32 and rounded once to its storage type.
@@ -286,18 +316,27 @@ __device__ __forceinline__ void scale_chunk(const ListEntry& e, uint32_t chunk, 
   if (threadIdx.x == 32 && last && (end & 15) != 0 && !(gfull == 0 && mis != 0)) scale_edge(kind, base + (gfull << 4), (uint32_t)(end & 15), c);
 }
 
-// Scales every tensor by the coefficient that list_norm_kernel wrote.  A coefficient of 1 leaves every entry as it is,
-// so nothing is read or written then.
-template <int CAP>
-__global__ void __launch_bounds__(LS_THREADS, 4) list_scale_kernel(const __grid_constant__ ListParams<CAP> p, const float* __restrict__ coefficient) {
+// Scales every tensor by the coefficient.  A coefficient of 1 leaves every entry as it is, so nothing is read or written
+// then.  WRITE: the list is one slice, and this kernel forms the norm itself, each block for itself, from the partial sums,
+// while some further blocks write the results: a launch less on the way.
+template <int CAP, bool WRITE>
+__global__ void __launch_bounds__(LS_THREADS, 4) list_scale_kernel(const __grid_constant__ ListParams<CAP> p, const __grid_constant__ NormArgs a) {
+  __shared__ double sh[LS_THREADS / 32];
   griddep_wait();
   griddep_launch_dependents();
-  const float s = *coefficient;
+  const uint32_t writers = WRITE ? (p.n + LS_THREADS / 32 - 1) / (LS_THREADS / 32) : 0, blocks = gridDim.x - writers;
+  float s;
+  if (WRITE) {
+    if (blockIdx.x < writers) { write_norms<CAP>(p, a, blockIdx.x, sh); return; }
+    s = clip_coefficient((float)sqrt(norm_sum(a.partial, a.grid + p.n - 1, sh)), a.max_norm);
+  } else {
+    s = a.out[1];
+  }
   if (s == 1.f) return;
   // back to front: what the norm's pass read last is still in the caches
   const uint32_t b = gridDim.x - 1 - blockIdx.x;
-  const uint32_t lo = (uint32_t)((uint64_t)b * p.total / gridDim.x);
-  uint32_t c = (uint32_t)((uint64_t)(b + 1) * p.total / gridDim.x);
+  const uint32_t lo = (uint32_t)((uint64_t)b * p.total / blocks);
+  uint32_t c = (uint32_t)((uint64_t)(b + 1) * p.total / blocks);
   if (lo >= c) return;
   int t = list_find(p, c - 1);
   while (c > lo) {

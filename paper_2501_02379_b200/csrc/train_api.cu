@@ -22,7 +22,7 @@ inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<ui
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // ---- lists ----
-constexpr int kListSmall = 128, kListLarge = 1024;       // tensors per launch: 2.6 KB and 20 KB of kernel parameters
+constexpr int kListSmall = 192, kListLarge = 1024;       // tensors per launch: 3.9 KB and 20 KB of kernel parameters
 constexpr int kAdamwSmall = 64, kAdamwLarge = 512;       // 3.4 KB and 27 KB
 constexpr uint32_t kMaxListBlocks = 2048;
 
@@ -84,33 +84,45 @@ uint32_t fill_list(const tgrad_tensor* list, int n, int sm, ListParams<CAP>& p) 
   return (uint32_t)(grid > kMaxListBlocks ? kMaxListBlocks : grid);
 }
 
-template <int CAP>
-tgrad_status norm_slices(const tgrad_tensor* list, int32_t n, float max_norm, float* out, void* ws, cudaStream_t st) {
-  const int sm = sm_count(), per = n < kListLarge ? n : kListLarge;
-  double* partial = static_cast<double*>(ws);
-  double* slice_sum = reinterpret_cast<double*>(static_cast<char*>(ws) + align_up((size_t)(kMaxListBlocks + per) * 8));
-  for (int base = 0, slice = 0; slice == 0 || base < n; base += CAP, ++slice) {
-    ListParams<CAP> p;
-    const int cnt = n - base < CAP ? n - base : CAP;
-    const uint32_t grid = fill_list<CAP>(list + base, cnt, sm, p);
-    if (grid > 0) {
-      launch_chained(list_sumsq_kernel<CAP>, dim3(grid), dim3(LS_THREADS), 0, st, p, partial);
-      TG_LAUNCH_CHECK();
-    }
-    launch_chained(list_norm_kernel<CAP>, dim3(1), dim3(LF_THREADS), 0, st, p, partial, grid, base, slice, base + CAP >= n ? 1 : 0, slice_sum, max_norm, out);
-    TG_LAUNCH_CHECK();
-  }
-  return TGRAD_OK;
+inline uint32_t norm_blocks(int n) { return (uint32_t)(n + LS_THREADS / 32 - 1) / (LS_THREADS / 32); }
+// Blocks of the scaling pass: about six chunks for each, so that the hardware hands them out as SMs become free (973 MB:
+// 464 us, 492 us with four blocks per SM), but no more than fill the GPU once where that is less, since each adds up the
+// partial sums for itself (80 MB in 145 tensors: 25 us, 36 us with one chunk for each block).
+inline uint32_t scale_blocks(uint32_t chunks, int sm) {
+  const uint32_t few = (uint32_t)sm * 4, most = (uint32_t)sm * 32, want = chunks / 6;
+  const uint32_t blocks = want < few ? few : (want > most ? most : want);
+  return blocks < chunks ? blocks : chunks;
 }
 template <int CAP>
-tgrad_status scale_slices(const tgrad_tensor* list, int32_t n, const float* coefficient, cudaStream_t st) {
-  const int sm = sm_count();
-  for (int base = (n - 1) / CAP * CAP; base >= 0; base -= CAP) {
-    ListParams<CAP> p;
+tgrad_status norm_slices(const tgrad_tensor* list, int32_t n, float max_norm, float* out, void* ws, bool clip, cudaStream_t st) {
+  const int sm = sm_count(), per = n < kListLarge ? n : kListLarge;
+  ListParams<CAP> p;
+  NormArgs a;
+  a.partial = static_cast<double*>(ws);
+  a.slice_sum = reinterpret_cast<double*>(static_cast<char*>(ws) + align_up((size_t)(kMaxListBlocks + per) * 8));
+  a.max_norm = max_norm; a.out = out;
+  const bool one = n <= CAP;
+  for (int base = 0, slice = 0; slice == 0 || base < n; base += CAP, ++slice) {
     const int cnt = n - base < CAP ? n - base : CAP;
-    const uint32_t grid = fill_list<CAP>(list + base, cnt, sm, p);
-    if (grid == 0) continue;
-    launch_chained(list_scale_kernel<CAP>, dim3(grid), dim3(LS_THREADS), 0, st, p, coefficient);
+    a.grid = fill_list<CAP>(list + base, cnt, sm, p);
+    a.base = base; a.slice = slice; a.last = base + CAP >= n ? 1 : 0;
+    if (a.grid > 0) {
+      launch_chained(list_sumsq_kernel<CAP>, dim3(a.grid), dim3(LS_THREADS), 0, st, p, static_cast<double*>(ws));
+      TG_LAUNCH_CHECK();
+    }
+    if (one && clip && a.grid > 0) {
+      launch_chained(list_scale_kernel<CAP, true>, dim3(scale_blocks(p.total, sm) + norm_blocks(cnt)), dim3(LS_THREADS), 0, st, p, a);
+      TG_LAUNCH_CHECK();
+      return TGRAD_OK;
+    }
+    launch_chained(list_norm_kernel<CAP>, dim3(cnt ? norm_blocks(cnt) : 1), dim3(LS_THREADS), 0, st, p, a);
+    TG_LAUNCH_CHECK();
+  }
+  if (!clip || one) return TGRAD_OK;
+  for (int base = (n - 1) / CAP * CAP; base >= 0; base -= CAP) {
+    const int cnt = n - base < CAP ? n - base : CAP;
+    if (fill_list<CAP>(list + base, cnt, sm, p) == 0) continue;
+    launch_chained(list_scale_kernel<CAP, false>, dim3(scale_blocks(p.total, sm)), dim3(LS_THREADS), 0, st, p, a);
     TG_LAUNCH_CHECK();
   }
   return TGRAD_OK;
@@ -120,10 +132,7 @@ tgrad_status norm_impl(const tgrad_tensor* grads, int32_t n, float max_norm, flo
   TG_TRY(check_list(grads, n));
   if (!(max_norm > 0.f) || !d_out || misaligned(d_out, 4) || !ws || misaligned(ws, 256)) return TGRAD_ERR_INVALID_ARG;
   if (ws_bytes < norm_bytes(n)) return TGRAD_ERR_BUFFER_TOO_SMALL;
-  const bool small = n <= kListSmall;
-  TG_TRY(small ? norm_slices<kListSmall>(grads, n, max_norm, d_out, ws, st) : norm_slices<kListLarge>(grads, n, max_norm, d_out, ws, st));
-  if (!clip || n == 0) return TGRAD_OK;
-  return small ? scale_slices<kListSmall>(grads, n, d_out + 1, st) : scale_slices<kListLarge>(grads, n, d_out + 1, st);
+  return n <= kListSmall ? norm_slices<kListSmall>(grads, n, max_norm, d_out, ws, clip, st) : norm_slices<kListLarge>(grads, n, max_norm, d_out, ws, clip, st);
 }
 
 // One launch per storage and CAP tensors.
@@ -163,7 +172,8 @@ tgrad_status adamw_slices(const tgrad_adamw_tensor* list, int32_t n, const Adamw
       at += (p.e[t].count + (1ull << lg) - 1) >> lg;
     }
     p.first[p.n] = p.total = (uint32_t)at;
-    uint64_t grid = (uint64_t)sm * 8;
+    // many short blocks, handed out as SMs become free (135 M bf16 weights with masters: 594 us, 660 us with 8 per SM)
+    uint64_t grid = (uint64_t)sm * 64;
     if (grid > at) grid = at;
     launch_chained(list_adamw_kernel<KIND, MASTER, CAP>, dim3((unsigned)grid), dim3(LS_THREADS), 0, st, p, a);
     TG_LAUNCH_CHECK();
