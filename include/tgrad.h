@@ -375,7 +375,7 @@ typedef struct {
   int64_t row_stride;        /* entries from one row to the next, >= vocab */
   const int64_t* d_targets;  /* rows */
   int32_t dtype;             /* TGRAD_R32, TGRAD_R16H or TGRAD_R16B */
-  float temperature;         /* > 0 */
+  double temperature;        /* > 0 (1e-30 to 1e30) */
 } tgrad_logits;
 
 /* Each output (rows fp32) may be NULL. */

@@ -68,7 +68,7 @@ class TgradAdamwConfig(C.Structure):
 
 class TgradLogits(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64),
-                ("targets", C.c_void_p), ("dtype", C.c_int32), ("temperature", C.c_float)]
+                ("targets", C.c_void_p), ("dtype", C.c_int32), ("temperature", C.c_double)]
 
 
 class TgradPolicyArgs(C.Structure):
@@ -412,7 +412,7 @@ def _raw_stream(index) -> int:
 
 
 # The argument structures as bytes (struct.pack costs a third of filling a ctypes structure).
-_pack_logits = struct.Struct("@PqqqPif").pack
+_pack_logits = struct.Struct("@PqqqPid").pack
 _pack_adamw = struct.Struct("@dddddqP").pack
 _pack_policy = struct.Struct("@PPPPffffffPPPPq").pack
 _pack_preference = struct.Struct("@PPifffPPPPq").pack

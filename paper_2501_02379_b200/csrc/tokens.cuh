@@ -6,8 +6,14 @@
 //   H = -sum p ln p = ln2 (log2 S - T / S),
 //   d(g log p_y + h H) / d logit_j = (g 1[j = y] - p_j (g + h H + h ln p_j)) / tau.
 // All three sums are held as (M, S, T) triples that combine associatively, so a row is read once, in any split.
-// d_j is formed from the difference, not as logit k - M k: the difference of 16-bit values is exact or nearly so, and
-// nothing overflows on rows whose entries are all the type's lowest value.
+// M may be any reference in their place; where an exponent is formed by one fma, x k - fl(M k), the rounding of M k is
+// corrected in the sums, and rows with entries so large that M k could overflow take the difference first.
+//
+// What bounds these kernels: a 16-bit logit is 2 bytes read (and 2 written), for which the memory takes 87 (174) cycles per
+// SM and 1000 logits at the measured copy rate; an exponential for the sums and one for the gradient take 62 cycles each
+// of the special-function unit (16 per clock and SM), and the arithmetic around them 5 and 3 instructions per logit in packed
+// fp32 (two per instruction), 60 cycles in all at four instructions per clock.  So loads, exponentials and stores have to
+// overlap throughout: bulk copies fetch ahead, several blocks share an SM, and one's barriers are another's arithmetic.
 //
 // Rows whose target is negative are ignored: their logits are not read (they may hold anything) and their gradient is
 // zero.  A target beyond the vocabulary gives NaN.
@@ -23,6 +29,7 @@ struct TokenArgs {
   const long long* y;    // targets
   int V;
   float k, inv_tau;      // log2(e) / tau, 1 / tau
+  float k_lo, inv_lo;    // what their rounding to fp32 has left out: of k relative to it, of 1 / tau absolute
 };
 
 constexpr float TK_LN2 = 0.6931471805599453f;
@@ -211,16 +218,17 @@ __device__ __forceinline__ void row_combine(Triple& a, float k, int C, float4* s
   warp_combine(a, k);
 }
 
-// What the sums say about one row.
+// What the sums say about one row.  The exponents were formed with k rounded to fp32, d (1 + k_lo) being the true ones: S is
+// off by k_lo ln2 T to first order, the same way in every row, which the sums over an answer's tokens would show.
 struct RowStat { float M, ls2, lse, logp, H; };
-__device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, float inv_tau) {
+__device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, const TokenArgs& p) {
   RowStat r;
   r.M = a.m;
-  const float ls = logf(a.s);
+  const float mean = TK_LN2 * (a.t / a.s), ls = fmaf(p.k_lo, mean, logf(a.s));
   r.ls2 = ls * 1.4426950408889634f;
-  r.lse = fmaf(a.m, inv_tau, ls);
-  r.logp = fmaf(zy - a.m, inv_tau, -ls);
-  r.H = fmaf(-TK_LN2, a.t / a.s, ls);
+  r.lse = fmaf(a.m, p.inv_tau, fmaf(a.m, p.inv_lo, ls));
+  r.logp = fmaf(zy - a.m, p.inv_tau, fmaf(zy - a.m, p.inv_lo, -ls));
+  r.H = ls - mean;
   return r;
 }
 template <int KIND>
@@ -645,7 +653,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       c.m = TK_LOWEST; c.s = c.t = 0.f;
       if (lane < W) { const float4 o = sums[side][lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
       warp_combine(c, p.k, W);      // (lane 0 uses the result)
-      const RowStat st = row_stat(c, zy, p.inv_tau);
+      const RowStat st = row_stat(c, zy, p);
       if (lane == 0) store_stat(f, row, st);
       if (BACK) {
       const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, adv, wt, q);
@@ -730,7 +738,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
 // of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers for every
 // row took 66 us instead of 23 us for 16384 rows of 1000 bf16 logits).  A row of more than one batch is read again for the
 // gradient, from the L1 cache, which the 32 rows in work on an SM fit (keeping it in 64 registers per lane leaves room for
-// half as many warps: 64 us instead of SHORT us for 12384 rows of 3001 bf16 logits).
+// half as many warps: 64 us instead of 51 us for 12384 rows of 3001 bf16 logits).
 constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 1024;
 template <int KIND, int MODE>
 __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f, int64_t rows) {
@@ -779,7 +787,7 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
       accumulate<KIND, SR_NV>(a, v, p.k);
     }
     warp_combine(a, p.k);
-    const RowStat st = row_stat(a, zy, p.inv_tau);
+    const RowStat st = row_stat(a, zy, p);
     if (lane == 0) store_stat(f, row, st);
     if (!BACK) continue;
     const PolicyToken o = policy_token(st.logp, st.H, old, ref, q.ref_logp != nullptr, adv, wt, q);
@@ -870,7 +878,7 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   }
   row_combine<TF_THREADS>(a, p.k, C, sh);
   if (rank != 0 || threadIdx.x != 0) return;
-  const RowStat st = row_stat(a, zy, p.inv_tau);
+  const RowStat st = row_stat(a, zy, p);
   store_stat(f, row, st);
   if (POLICY) q.terms[row] = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q).terms;
 }
