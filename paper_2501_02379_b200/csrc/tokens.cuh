@@ -284,6 +284,17 @@ __device__ __forceinline__ void store_granule(const Row<KIND>& r, char* drow, bo
   if (same && r.whole(g)) st_stream(reinterpret_cast<uint4*>(drow - r.mis * Gran<KIND>::B) + g, v);
   else store_entries<KIND>(drow, r.mis, r.V, g, v);
 }
+// A gradient row of zeros, by `threads` threads.
+template <int KIND>
+__device__ __forceinline__ void zero_row(char* drow, int V, int tid, int threads) {
+  constexpr int E = Gran<KIND>::E;
+  const Row<KIND> d(drow, V);
+  const int lo = d.mis ? 1 : 0, hi = (d.mis + V) / E;      // the whole granules
+  uint4* at = reinterpret_cast<uint4*>(drow - d.mis * Gran<KIND>::B) + lo + tid;
+  for (int g = lo + tid; g < hi; g += threads, at += threads) st_stream(at, make_uint4(0, 0, 0, 0));
+  if (tid == 0 && lo) store_entries<KIND>(drow, d.mis, V, 0, make_uint4(0, 0, 0, 0));
+  if (tid == 1 && hi >= lo && (d.mis + V) % E) store_entries<KIND>(drow, d.mis, V, hi, make_uint4(0, 0, 0, 0));
+}
 template <int KIND>
 __device__ __forceinline__ bool same_alignment(const Row<KIND>& r, const char* drow) {
   return (int)((uintptr_t)drow & 15) == r.mis * Gran<KIND>::B;
@@ -521,7 +532,7 @@ __device__ __forceinline__ void store_stat(const ForwardArgs& f, int64_t row, co
   if (f.g) f.g[row] = 0.f;
   if (f.ticket && row == 0) *f.ticket = 0;
 }
-template <int KIND, int MODE>
+template <int KIND, int MODE, int W>
 __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
                                                   int64_t rows, const __grid_constant__ RowGeom geo) {
   constexpr bool BACK = MODE != RW_FORWARD, ENT = MODE == RW_ENTROPY;
@@ -531,7 +542,8 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   __shared__ volatile int bad;           // a wait ran out of its bound
   __shared__ RowBarriers rb;
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
-  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int threads = 32 * W, chunk = RW_NV * threads;
+  const int N = geo.N, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     bad = 0;
     rb.init(N, W);
@@ -577,8 +589,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = geo.K - (nw <= geo.last), n = !BACK ? 0 : K <= N ? K : N - 2, x = K - n;
     const int tail = nw - (K - 1) * chunk;      // granules of the last chunk
     if (y < 0) {
-      if (BACK)
-        for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      if (BACK) zero_row<KIND>(drow, p.V, tid, threads);
       if (tid == 0) {
         RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
         store_stat(f, row, none);
@@ -759,8 +770,7 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
     char* drow = p.dz + row * p.lddz * B;
     const bool same = same_alignment(r, drow);
     if (y < 0) {
-      if (BACK)
-        for (int g = lane; g < G; g += 32) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      if (BACK) zero_row<KIND>(drow, p.V, lane, 32);
       if (lane == 0) {
         RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
         store_stat(f, row, none);
@@ -930,12 +940,13 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_short_kernel(co
   if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
 }
 
-template <int KIND, bool ENT>
+template <int KIND, bool ENT, int W>
 __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, int64_t rows, const __grid_constant__ RowGeom geo) {
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ RowBarriers rb;
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
-  const int W = geo.W, N = geo.N, threads = 32 * W, chunk = RW_NV * threads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int threads = 32 * W, chunk = RW_NV * threads;
+  const int N = geo.N, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) rb.init(N, W);
   __syncthreads();
   griddep_wait();
@@ -979,7 +990,7 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
     const Row<KIND> r(zrow, p.V);
     const bool same = same_alignment(r, drow);
     if (y < 0) {
-      for (int g = tid; g < r.granules(); g += threads) store_granule<KIND>(r, drow, same, g, make_uint4(0, 0, 0, 0));
+      zero_row<KIND>(drow, p.V, tid, threads);
       continue;
     }
     const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E, nw = max(0, wb - wa), K = geo.K - (nw <= geo.last), tail = nw - (K - 1) * chunk;

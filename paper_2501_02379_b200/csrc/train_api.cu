@@ -298,17 +298,26 @@ RowGeom row_geom(const tgrad_logits* in, float k, bool stay, int blocks, int64_t
 }
 inline size_t ring_bytes(const RowGeom& g) { return (size_t)g.W * 32 * RW_NV * 16 * g.N; }
 
+template <int KIND, int MODE, int W>
+tgrad_status launch_row_warps(const RowGeom& g, int64_t grid, const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
+  auto kern = token_row_kernel<KIND, MODE, W>;
+  static std::atomic<uint64_t> done{0};
+  TG_TRY(allow_shared(kern, kRingBytes, done));
+  launch_chained(kern, dim3((unsigned)grid), dim3(32 * (W + 1)), ring_bytes(g), st, a, q, f, in->rows, g);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
 template <int KIND, int MODE>
 tgrad_status launch_row(const tgrad_logits* in, const TokenArgs& a, const PolicyArgs& q, const ForwardArgs& f, cudaStream_t st) {
   if (one_warp_each(in)) return launch_short<KIND, MODE>(in, a, q, f, st);
   int64_t grid;
   const RowGeom g = row_geom(in, a.k, MODE != RW_FORWARD, MODE == RW_FORWARD ? 6 : 4, &grid);
-  auto kern = token_row_kernel<KIND, MODE>;
-  static std::atomic<uint64_t> done{0};
-  TG_TRY(allow_shared(kern, kRingBytes, done));
-  launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), ring_bytes(g), st, a, q, f, in->rows, g);
-  TG_LAUNCH_CHECK();
-  return TGRAD_OK;
+  if constexpr (MODE == RW_FORWARD) {
+    return launch_row_warps<KIND, MODE, 4>(g, grid, in, a, q, f, st);
+  } else {
+    return g.W == 4 ? launch_row_warps<KIND, MODE, 4>(g, grid, in, a, q, f, st)
+           : g.W == 8 ? launch_row_warps<KIND, MODE, 8>(g, grid, in, a, q, f, st) : launch_row_warps<KIND, MODE, 16>(g, grid, in, a, q, f, st);
+  }
 }
 template <int KIND, bool ENT>
 tgrad_status launch_gradient(const tgrad_logits* in, const TokenArgs& a, const BackwardArgs& b, cudaStream_t st) {
@@ -320,10 +329,10 @@ tgrad_status launch_gradient(const tgrad_logits* in, const TokenArgs& a, const B
   } else {
     int64_t grid;
     const RowGeom g = row_geom(in, a.k, false, 4, &grid);
-    auto kern = token_gradient_kernel<KIND, ENT>;
+    auto kern = token_gradient_kernel<KIND, ENT, 4>;
     static std::atomic<uint64_t> done{0};
     TG_TRY(allow_shared(kern, kRingBytes, done));
-    launch_chained(kern, dim3((unsigned)grid), dim3((unsigned)(32 * (g.W + 1))), ring_bytes(g), st, a, b, in->rows, g);
+    launch_chained(kern, dim3((unsigned)grid), dim3(32 * 5), ring_bytes(g), st, a, b, in->rows, g);
   }
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
