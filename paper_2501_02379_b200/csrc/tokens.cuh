@@ -113,10 +113,6 @@ struct Row {
     if (whole(g)) return ld_stream(reinterpret_cast<const uint4*>(base) + g);
     return partial(g);
   }
-  __device__ __forceinline__ uint4 load_cached(int g) const {      // the same, kept in the L1 cache
-    if (whole(g)) return *(reinterpret_cast<const uint4*>(base) + g);
-    return partial(g);
-  }
 };
 
 // ---- (M, S, T) ----
@@ -128,6 +124,13 @@ __device__ __forceinline__ void rebase(Triple& a, float m, float k) {
   a.t = f * fmaf(a.s, d, a.t);
   a.s *= f;
   a.m = m;
+}
+// adds one logit
+__device__ __forceinline__ void add_entry(Triple& a, float x, float k) {
+  Triple b; b.m = fmaxf(x, TK_LOWEST); b.s = x == -INFINITY ? 0.f : x - x + 1.f; b.t = 0.f;      // NaN and inf give NaN
+  const float m = fmaxf(a.m, b.m);
+  rebase(a, m, k); rebase(b, m, k);
+  a.s += b.s; a.t += b.t;
 }
 // adds a batch of granules whose maximum is not above a.m
 template <int KIND, int NV>
@@ -648,12 +651,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       c.m = a.base; c.s = s2.x + s2.y; c.t = t2.x + t2.y;
       const float f = ex2(-a.delta);
       c.t = f * fmaf(c.s, -a.delta, c.t); c.s *= f;
-      if (edge >= 0) {
-        Triple b; b.m = fmaxf(xe, TK_LOWEST); b.s = xe == -INFINITY ? 0.f : xe - xe + 1.f; b.t = 0.f;      // NaN and inf give NaN
-        const float m = fmaxf(c.m, b.m);
-        rebase(c, m, p.k); rebase(b, m, p.k);
-        c.s += b.s; c.t += b.t;
-      }
+      if (edge >= 0) add_entry(c, xe, p.k);
       warp_combine(c, p.k);
     }
     side ^= 1;
@@ -766,7 +764,7 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
     const long long y = y_next;
     if (row + step < rows) y_next = p.y[row + step];
     const Row<KIND> r(p.z + row * p.ldz * B, p.V);
-    const int G = r.granules();
+    const int wa = r.mis ? 1 : 0, wb = (r.mis + p.V) / E;      // the whole granules
     char* drow = p.dz + row * p.lddz * B;
     const bool same = same_alignment(r, drow);
     if (y < 0) {
@@ -778,6 +776,11 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
       }
       continue;
     }
+    // the entries outside the whole granules: one per lane at most
+    const int h = min(p.V, wa * E - r.mis * wa), t0 = max(h, wb * E - r.mis);
+    const int edge = lane < h ? lane : (lane >= 16 && t0 + lane - 16 < p.V ? t0 + lane - 16 : -1);
+    float xe = 0.f;
+    if (edge >= 0) xe = ld_real<KIND>(r.base + (int64_t)(r.mis + edge) * B);
     const float zy = target_logit<KIND>(p, row, y);
     float old = 0.f, adv = 0.f, wt = 0.f, ref = 0.f;
     if (BACK) {
@@ -787,15 +790,17 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
     uint4 v[SR_NV];
     Triple a;
     a.m = TK_LOWEST; a.s = a.t = 0.f;
-    for (int g0 = lane; g0 < G; g0 += 32 * SR_NV) {
+    const uint4* src = reinterpret_cast<const uint4*>(r.base);
+    for (int g0 = wa + lane; g0 < wb; g0 += 32 * SR_NV) {
 #pragma unroll
       for (int i = 0; i < SR_NV; ++i) {
         v[i] = make_uint4(ni, ni, ni, ni);
-        if (g0 + 32 * i < G) v[i] = r.load_cached(g0 + 32 * i);
+        if (g0 + 32 * i < wb) v[i] = src[g0 + 32 * i];      // (kept in the L1 cache)
       }
       rebase(a, fmaxf(a.m, batch_max<KIND, SR_NV>(v)), p.k);
       accumulate<KIND, SR_NV>(a, v, p.k);
     }
+    if (edge >= 0) add_entry(a, xe, p.k);
     warp_combine(a, p.k);
     const RowStat st = row_stat(a, zy, p);
     if (lane == 0) store_stat(f, row, st);
@@ -807,17 +812,22 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
     gc.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; gc.c1 = -o.h * TK_LN2 * sc;
     const int gy = y < p.V ? (r.mis + (int)y) / E : -1;
     __syncwarp();      // every lane has read the target's logit before it is overwritten
-    for (int g0 = lane; g0 < G; g0 += 32 * SR_NV) {
-      if (G > 32 * SR_NV) {
+    uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B);
+    for (int g0 = wa + lane; g0 < wb; g0 += 32 * SR_NV) {
+      if (wb - wa > 32 * SR_NV) {
 #pragma unroll
         for (int i = 0; i < SR_NV; ++i)
-          if (g0 + 32 * i < G) v[i] = r.load_cached(g0 + 32 * i);
+          if (g0 + 32 * i < wb) v[i] = src[g0 + 32 * i];
       }
 #pragma unroll
       for (int i = 0; i < SR_NV; ++i)
-        if (g0 + 32 * i < G) store_granule<KIND>(r, drow, same, g0 + 32 * i, grad_granule<KIND, ENT>(v[i], gc));
+        if (g0 + 32 * i < wb) {
+          const uint4 d = grad_granule<KIND, ENT>(v[i], gc);
+          if (same) st_stream(dst + g0 + 32 * i, d); else store_entries<KIND>(drow, r.mis, p.V, g0 + 32 * i, d);
+        }
     }
-    if (gy >= 0 && (gy & 31) == lane) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
+    if (edge >= 0) st_real<KIND>(drow + (int64_t)edge * B, grad_target<KIND, ENT>(xe, gc, edge == y ? o.g * sc : 0.f));
+    if (gy >= wa && gy < wb && ((gy - wa) & 31) == lane) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, o.g * sc));
   }
 }
 
