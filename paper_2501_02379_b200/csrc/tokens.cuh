@@ -470,6 +470,15 @@ struct RowBarriers {
   }
 };
 
+// This warp has read a place of the ring.  The fence comes first because nothing else keeps the warp's shared loads, which
+// may still be under way, before the asynchronous copy that the arrival lets into the place (without it, a few granules at
+// the start of a chunk came out as those of the chunk N later, once in some thousand rows).
+__device__ __forceinline__ void release_place(uint64_t* empty, int lane) {
+  fence_async_smem();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(empty);
+}
+
 // The fetching warp: takes units of rows, passes them on, and asks for the chunks of their live rows.  STAY: chunks stay
 // for a second reading (n of them, see above); else each goes through the ring once.  LAST_FIRST: the units from the end.
 template <int KIND, bool STAY, bool LAST_FIRST>
@@ -639,8 +648,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
         }
       }
       if (j < x) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&rb.empty[s]);
+        release_place(&rb.empty[s], lane);
       }
       if (++s == N) { s = 0; ph ^= 1; }
       add_chunk<KIND>(a, v, geo, p.k);
@@ -710,8 +718,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       if (same && (j < K - 1 || tail == chunk)) {
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&rb.empty[at]);
+        release_place(&rb.empty[at], lane);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
@@ -720,8 +727,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) v[u] = place[u * threads];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&rb.empty[at]);
+        release_place(&rb.empty[at], lane);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
@@ -1026,8 +1032,7 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
       if (same && (j < K - 1 || tail == chunk)) {
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u) v[u] = place[u * threads];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&rb.empty[s]);
+        release_place(&rb.empty[s], lane);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           st_stream(dst + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));
@@ -1036,8 +1041,7 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) v[u] = place[u * threads];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&rb.empty[s]);
+        release_place(&rb.empty[s], lane);
 #pragma unroll
         for (int u = 0; u < RW_NV; ++u)
           if (tid + u * threads < len) store_granule<KIND>(r, drow, same, g0 + tid + u * threads, fast ? row_gradient<KIND, ENT, true>(v[u], h, p.k) : row_gradient<KIND, ENT, false>(v[u], h, p.k));

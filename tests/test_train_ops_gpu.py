@@ -390,6 +390,73 @@ def test_policy_loss(rows, V, pad, lead, dtype, ent):
         assert got.dlogits[rows - 1, 5] == 0
 
 
+@pytest.mark.parametrize("dtype,rows,V,pad,lead", [("bf16", 151, 9001, 0, 3), ("f16", 160, 33000, 1, 0), ("f32", 150, 16390, 0, 1), ("bf16", 150, 70001, 3, 0)])
+def test_policy_loss_more_rows_than_sms(dtype, rows, V, pad, lead):
+    z, y = make_rows(dtype, rows, V, pad, 8, lead)
+    y[3::5] = -7
+    check_policy(z, y, 1.1, dtype, V, ent=0.02, grad_scale=64.0)
+
+
+@pytest.mark.parametrize("dtype,rows,V,pad", [("bf16", 6001, 9001, 0), ("bf16", 2600, 40001, 3), ("f16", 9473, 2051, 0), ("f32", 5003, 4099, 1), ("bf16", 1300, 131073, 0)])
+def test_many_rows(dtype, rows, V, pad):
+    """Thousands of rows, handed out in units, through the ring or a warp each, against 64-bit arithmetic on the GPU; the
+    bounds are those of token_tols, grad_tol and check_policy."""
+    z, y = make_rows(dtype, rows, V, pad, 3)
+    y[::7] = -1
+    z[7] = float("nan")
+    g = gen(2)
+    n = lambda: torch.randn(rows, generator=g, device="cuda")  # noqa: E731
+    lp, lse, H = B.token_logprob(z, y)
+    shift, adv, w, gap = n() * 0.05, n(), n(), n() * 0.1
+    old, ref = lp - shift, lp + gap                                            # ratios far from the bounds 0.5 and 1.5
+    kl, ent = (float(np.float32(v)) for v in (0.1, 0.01))
+    got = B.policy_loss(z, y, old, adv, w, ref_logp=ref, clip_low=0.5, clip_high=0.5, kl_coef=kl, entropy_coef=ent)
+    grad = B.token_logprob_backward(z, y, lse, adv, entropy=H, grad_entropy=w)
+    sums, slack = torch.zeros(5, dtype=torch.float64, device="cuda"), 0.0
+    for a in range(0, rows, 100):
+        c = slice(a, min(rows, a + 100))
+        live = (y[c] >= 0)[:, None]
+        x = torch.where(live, z[c].double(), 0.0)
+        at = y[c].clamp(min=0)[:, None]
+        top = x.amax(1, keepdim=True)
+        d, q = top - x, torch.log_softmax(x, 1)
+        p = q.exp()
+        want_lse, want_lp, want_H = torch.logsumexp(x, 1), q.gather(1, at)[:, 0], -(p * q).sum(1)
+        es = sum_err(V) + 2 * 3 * U * (p * d).sum(1, keepdim=True) + 4 * U
+        rel = 2 * 4 * U * (d + top.abs() + math.log(V)) + es
+        tl = es[:, 0] + 2 * 3 * U * (d.gather(1, at)[:, 0] + math.log(V) + 1)
+        tH = 2 * (es[:, 0] + 2 * 3 * U) * (1 + (p * d).sum(1) + math.log(V))
+        m = live[:, 0]
+
+        def near(got_, want_, tol_, what):
+            off = ((got_.double() - torch.where(m, want_, 0.0)).abs() > tol_) & m | ~m & (got_ != 0)
+            assert not bool(off.any()) and not bool(got_.isnan().any()), what
+
+        near(lp[c], want_lp, tl, "logp"); near(got.logp[c], want_lp, tl, "policy logp"); near(got.entropy[c], want_H, tH, "policy entropy")
+        near(lse[c], want_lse, es[:, 0] + 2 * 3 * U * (top.abs()[:, 0] + math.log(V) + 1), "lse"); near(H[c], want_H, tH, "entropy")
+
+        def near_grad(got_, gg, hh, dg, what):
+            one = torch.zeros_like(p).scatter_(1, at, 1.0)
+            want_ = torch.where(live, gg[:, None] * (one - p) - hh[:, None] * p * (q + want_H[:, None]), 0.0)
+            per = gg.abs()[:, None] + hh.abs()[:, None] * (q.abs() + want_H[:, None])
+            tol = p * per * (rel + 8 * U) + p * hh.abs()[:, None] * rel * (1 + q.abs()) + p * dg[:, None] + one * (gg.abs() * 4 * U + dg)[:, None]
+            off = (got_.double() - want_).abs() > 2 * tol + 1.01 * HALF_ULP[dtype] * want_.abs() + TINY[dtype]
+            assert not bool(off.any()) and not bool(got_.isnan().any()), what
+
+        A, W = adv[c].double(), w[c].double()
+        near_grad(grad[c], A, W, W.abs() * tH, "gradient")
+        r, u = (want_lp - old[c].double()).exp(), ref[c].double() - want_lp
+        dl = tl + 4 * U * (old[c].abs() + ref[c].abs() + 2).double()
+        gg = W * (-r * A - kl * torch.expm1(u))
+        dg = 2 * W.abs() * (A.abs() * r * (dl + 8 * U) + kl * (u.exp() * dl + (u.exp() + 2) * 8 * U)) + ent * W.abs() * tH
+        near_grad(got.dlogits[c], gg, -ent * W, dg, "policy gradient")
+        terms = torch.stack([-r * A, torch.expm1(u) - u, want_H, torch.zeros_like(r)])
+        part = (W * terms * m).sum(1)
+        sums += torch.cat([(part[0] + kl * part[1] - ent * part[2]).reshape(1), part])
+        slack += float((W.abs() * m * (A.abs() * r * (dl + 8 * U) + (u.exp() + 3) * (dl + 8 * U) + tH)).sum())
+    assert float((got.stats.double() - sums).abs().max()) <= 2 * slack + 4 * U * float(sums.abs().max())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [1003, 20000, 131072, 270001])
 def test_policy_loss_in_place_elsewhere_and_forward_only(V, dtype):
