@@ -319,7 +319,8 @@ tgrad_status tgrad_get_stage_times(tgrad_state* st, void* cuda_stream, float* ms
  * Everything is enqueued on the stream, nothing synchronises, every sum has a
  * fixed order (the same inputs give the same bits), and all arithmetic is in
  * fp32 or wider with one rounding to the storage type at the end.
- * Pointers need the alignment of their element type only. */
+ * Pointers need the alignment of their element type only.  Every wait inside a kernel is bounded; one that ran out, which
+ * nothing in normal operation leads to, leaves NaN in the results (loss, log-probabilities or gradient). */
 
 typedef struct {
   void* d_data;        /* numel entries, contiguous in memory (in any order of the dimensions) */

@@ -181,6 +181,9 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
 // Partial sums of squares.  Block b writes one per tensor t it has chunks of, at slot b + t: along the list each next
 // (block, tensor) pair has a larger b + t, so the slots are distinct and a tensor's slots are b0 + t .. b1 + t.  Slots that
 // no pair has are set to zero by the block before them, so that all grid + n of them may be added up.
+// Bound: one read of the gradients.  Eight 16-byte loads per thread are under way at a time (128 KB per SM, three times what
+// the memory's latency needs); two fused multiply-adds per 16-bit pair are nowhere near the limit.  1.64 GB of complex64 and
+// bf16 gradients: 242 us, 6.8 TB/s.
 template <int CAP>
 __global__ void __launch_bounds__(LS_THREADS, 4) list_sumsq_kernel(const __grid_constant__ ListParams<CAP> p, double* __restrict__ partial) {
   __shared__ double sh[LS_THREADS / 32];
@@ -351,7 +354,9 @@ __global__ void __launch_bounds__(LS_THREADS, 4) list_scale_kernel(const __grid_
 // AdamW over a list.  m <- b1 m + (1 - b1) c g, v <- b2 v + (1 - b2) |c g|^2,
 // w <- (1 - lr wd) w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps), everything in fp32.  For complex tensors
 // |.| is the modulus and v has one real per complex entry, as in the optimizer's compressed space.
-// Each entry is read and written once (28 bytes per entry for fp32 weights); memory bandwidth is the bound.
+// Each entry is read and written once (28 bytes per entry for fp32 weights and for 16-bit ones with masters); memory bandwidth
+// is the bound: 135 M bf16 weights with masters 591 us, 6.4 TB/s.  Two vectors of four entries per thread are loaded before
+// the first is worked on (one: 670 us; four: 694 us, half the blocks).
 struct AdamwScalars {
   float beta1, beta2, omb1, omb2;   // decay rates and 1 - beta
   float step_size;                  // lr / (1 - beta1^t)

@@ -33,6 +33,7 @@ struct TokenArgs {
 };
 
 constexpr float TK_LN2 = 0.6931471805599453f;
+constexpr float TK_EX2_LOW = 4.8e-8f;
 constexpr float TK_LOWEST = -3.402823466e38f;
 
 // ---- packed pairs of fp32 (one instruction per two lanes on this architecture) ----
@@ -223,15 +224,38 @@ __device__ __forceinline__ void row_combine(Triple& a, float k, int C, float4* s
 
 // What the sums say about one row.  The exponents were formed with k rounded to fp32, d (1 + k_lo) being the true ones: S is
 // off by k_lo ln2 T to first order, the same way in every row, which the sums over an answer's tokens would show.
-struct RowStat { float M, ls2, lse, logp, H; };
+// The same holds for the special-function unit's exponentials, which come out 4.8e-8 low on average (measured over exponents
+// from -13 to -0.7, the same in each part of that range); the largest entry's, 2^0, is exact.
+// ln S is formed as hi + lo, hi a multiple of a short ln 2, and log p with the part that its rounding to fp32 leaves out: the
+// roundings of two numbers near 10 are more than half of the error of log p, and sums over an answer's tokens use both parts.
+struct RowStat { float M, ls2, lse, logp, logp_lo, H; };
 __device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, const TokenArgs& p) {
   RowStat r;
   r.M = a.m;
-  const float mean = TK_LN2 * (a.t / a.s), ls = fmaf(p.k_lo, mean, logf(a.s));
+  const float inv_s = 1.f / a.s, mean = TK_LN2 * (a.t * inv_s), drift = fmaf(p.k_lo, mean, TK_EX2_LOW * (1.f - inv_s));
+  float hi = 0.f, lo;
+  if (a.s > 1e-30f && a.s < 1e30f) {
+    uint32_t bits = __float_as_uint(a.s);
+    float e = (float)((int)(bits >> 23) - 127), m = __uint_as_float((bits & 0x007fffffu) | 0x3f800000u);
+    if (m > 1.5f) { m *= 0.5f; e += 1.f; }
+    hi = e * 0.693115234375f;                                      // 2839 / 4096: exact
+    lo = fmaf(e, 3.194618495e-05f, drift + logf(m));                // ln 2 - 2839 / 4096
+  } else lo = logf(a.s);
+  const float ls = hi + lo;
   r.ls2 = ls * 1.4426950408889634f;
   r.lse = fmaf(a.m, p.inv_tau, fmaf(a.m, p.inv_lo, ls));
-  r.logp = fmaf(zy - a.m, p.inv_tau, fmaf(zy - a.m, p.inv_lo, -ls));
   r.H = ls - mean;
+  const float d = zy - a.m, q = d * p.inv_tau;
+  r.logp_lo = 0.f;
+  if (fabsf(q) < 1e30f) {
+    const float db = d - zy, d_lo = (zy - (d - db)) + (-a.m - db);                            // zy - M = d + d_lo
+    const float q_lo = fmaf(d, p.inv_tau, -q) + fmaf(d, p.inv_lo, d_lo * p.inv_tau);          // times 1 / tau = q + q_lo
+    const float t = q - hi, tb = t - q, t_lo = (q - (t - tb)) + (-hi - tb);
+    const float rest = (q_lo - lo) + t_lo;
+    r.logp = t + rest;
+    r.logp_lo = rest - (r.logp - t);
+    if (r.logp_lo != r.logp_lo) r.logp_lo = 0.f;
+  } else r.logp = q - ls;
   return r;
 }
 template <int KIND>
@@ -529,6 +553,7 @@ __device__ __forceinline__ void fetch_rows(const TokenArgs& p, int64_t rows, con
 
 struct ForwardArgs {
   float* logp; float* lse; float* entropy;      // out, may be null
+  float* logp_lo;                               // out, may be null: what the rounding of logp has left out
   float2* stat;                                 // out, may be null: (M, log2 S) for a later gradient pass
   float* g;                                     // zeroed, may be null: gradient of rows that no later kernel gives one
   unsigned* ticket;                             // zeroed with it
@@ -539,11 +564,15 @@ enum { RW_FORWARD = 0, RW_POLICY = 1, RW_ENTROPY = 2 };
 __device__ __forceinline__ void store_stat(const ForwardArgs& f, int64_t row, const RowStat& st) {
   if (f.logp) f.logp[row] = st.logp;
   if (f.lse) f.lse[row] = st.lse;
+  if (f.logp_lo) f.logp_lo[row] = st.logp_lo;
   if (f.entropy) f.entropy[row] = st.H;
   if (f.stat) f.stat[row] = make_float2(st.M, st.ls2);
   if (f.g) f.g[row] = 0.f;
   if (f.ticket && row == 0) *f.ticket = 0;
 }
+// 96 registers: 80 leave the scheduler too little to interleave (0.73 instead of 0.68 ms at 8192 x 131072 bf16), 128 too few
+// warps (0.71 ms).  8192 x 131072 bf16 logits with gradient: 0.66 ms, 6.1 TB/s, after a cold start; 0.74 ms at the clocks that a
+// second of it settles at, where the arithmetic weighs more.  Log-probabilities of 16384 x 32000: 0.175 ms, 6.0 TB/s.
 template <int KIND, int MODE, int W>
 __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
                                                   int64_t rows, const __grid_constant__ RowGeom geo) {
@@ -603,7 +632,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     if (y < 0) {
       if (BACK) zero_row<KIND>(drow, p.V, tid, threads);
       if (tid == 0) {
-        RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+        RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = 0.f;
         store_stat(f, row, none);
         if (BACK) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
@@ -744,7 +773,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   if (!ok && tid == 0) {
     const float n = __int_as_float(0x7fc00000);
     if (BACK) q.terms[(int64_t)blockIdx.x * geo.unit] = make_float4(n, n, n, n);
-    RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = n;
+    RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = n;
     store_stat(f, (int64_t)blockIdx.x * geo.unit, none);
   }
 }
@@ -753,7 +782,8 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
 // of a row's loads and of its scalar arithmetic is hidden by the SM's other warps alone (a block and its barriers for every
 // row took 66 us instead of 23 us for 16384 rows of 1000 bf16 logits).  A row of more than one batch is read again for the
 // gradient, from the L1 cache, which the 32 rows in work on an SM fit (keeping it in 64 registers per lane leaves room for
-// half as many warps: 64 us instead of 51 us for 12384 rows of 3001 bf16 logits).
+// half as many warps: 64 us instead of 51 us for 12384 rows of 3001 bf16 logits, 41 us since the outer entries are taken one
+// by each lane).
 constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 1024;
 template <int KIND, int MODE>
 __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f, int64_t rows) {
@@ -776,7 +806,7 @@ __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __g
     if (y < 0) {
       if (BACK) zero_row<KIND>(drow, p.V, lane, 32);
       if (lane == 0) {
-        RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+        RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = 0.f;
         store_stat(f, row, none);
         if (BACK) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
@@ -864,7 +894,8 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(const float4* __restri
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Forward pass over a few rows: C blocks stream a row with running triples.  POLICY: the rows' loss terms too.
+// Forward pass over a few rows: C blocks stream a row with running triples, so that four rows of 131072 bf16 logits keep 32 SMs
+// busy (4.8 us, the launch included; what is read takes 0.2).  POLICY: the rows' loss terms too.
 constexpr int TF_THREADS = 256;
 template <int KIND, bool POLICY>
 __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ ForwardArgs f,
@@ -880,7 +911,7 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
   if (C > 1) cluster_wait();
   if (y < 0) {
     if (rank == 0 && threadIdx.x == 0) {
-      RowStat none; none.logp = none.lse = none.H = none.M = none.ls2 = 0.f;
+      RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = 0.f;
       store_stat(f, row, none);
       if (POLICY) q.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
@@ -956,6 +987,8 @@ __global__ void __launch_bounds__(TB2_THREADS, 4) token_backward_short_kernel(co
   if (mine) st_real<KIND>(drow + y * Gran<KIND>::B, grad_target<KIND, ENT>(zy, gc, target));
 }
 
+// Longer rows: 8192 x 32768 bf16 173 us, 6.2 TB/s of reading and writing (a block per piece of a row, loads and arithmetic one
+// after the other: 195 us).
 template <int KIND, bool ENT, int W>
 __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ BackwardArgs b, int64_t rows, const __grid_constant__ RowGeom geo) {
   extern __shared__ __align__(128) unsigned char ring[];
@@ -1061,7 +1094,7 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
 struct PairArgs {
   const int* starts;          // 2 * pairs + 1 rows; answer s has rows [starts[s], starts[s + 1])
   const float* ref;
-  const float* logp;
+  const float* logp; const float* logp_lo;
   const long long* y;
   int64_t rows;
   int pairs;
@@ -1093,8 +1126,8 @@ __global__ void __launch_bounds__(TP_THREADS) pair_kernel(const __grid_constant_
   for (int c = 0; c < 2; ++c) {
     double s = 0.0;
     for (int64_t i = at[2 * c] + threadIdx.x; i < at[2 * c + 1]; i += TP_THREADS) {
-      const float lp = a.logp[i], rf = a.ref[i];
-      if (a.y[i] >= 0) s += (double)lp - (double)rf;
+      const float lp = a.logp[i], lo = a.logp_lo[i], rf = a.ref[i];
+      if (a.y[i] >= 0) s += ((double)lp - (double)rf) + (double)lo;
     }
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     R[c] = s;

@@ -356,7 +356,7 @@ tgrad_status launch_logprob(const tgrad_logits* in, const TokenArgs& a, const Fo
 }
 
 size_t policy_bytes(int64_t rows) { return align_up((size_t)rows * 16); }
-size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + align_up((size_t)rows * 4) + align_up((size_t)pairs * 8) + 256; }
+size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)rows * 8) + 2 * align_up((size_t)rows * 4) + align_up((size_t)pairs * 8) + 256; }
 
 }  // namespace
 
@@ -488,20 +488,21 @@ tgrad_status tgrad_preference_loss(const tgrad_logits* in, const tgrad_preferenc
   char* ws = static_cast<char*>(d_workspace);
   float2* stat = reinterpret_cast<float2*>(ws);
   float* g = reinterpret_cast<float*>(ws + align_up((size_t)in->rows * 8));
-  double* terms = reinterpret_cast<double*>(ws + align_up((size_t)in->rows * 8) + align_up((size_t)in->rows * 4));
+  float* logp_lo = reinterpret_cast<float*>(ws + align_up((size_t)in->rows * 8) + align_up((size_t)in->rows * 4));
+  double* terms = reinterpret_cast<double*>(ws + align_up((size_t)in->rows * 8) + 2 * align_up((size_t)in->rows * 4));
   unsigned* ticket = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(terms) + align_up((size_t)c->pairs * 8));
   const int kind = token_kind(in->dtype);
   const TokenArgs a = token_args(in, c->d_dlogits, c->dlogits_stride);
   if (any) {
     ForwardArgs f; memset(&f, 0, sizeof(f));
-    f.logp = c->d_logp; f.stat = stat;
+    f.logp = c->d_logp; f.stat = stat; f.logp_lo = logp_lo;
     f.g = c->d_dlogits ? g : nullptr; f.ticket = ticket;
     TG_TRY(launch_logprob(in, a, f, st));
   }
   else if (cudaMemsetAsync(ticket, 0, sizeof(*ticket), st) != cudaSuccess) return TGRAD_ERR_CUDA;
   if (c->pairs > 0) {
     PairArgs p; memset(&p, 0, sizeof(p));
-    p.starts = c->d_starts; p.ref = c->d_ref_logp; p.logp = c->d_logp; p.y = reinterpret_cast<const long long*>(in->d_targets);
+    p.starts = c->d_starts; p.ref = c->d_ref_logp; p.logp = c->d_logp; p.logp_lo = logp_lo; p.y = reinterpret_cast<const long long*>(in->d_targets);
     p.rows = in->rows; p.pairs = c->pairs; p.beta = c->beta; p.smoothing = c->label_smoothing;
     p.g = c->d_dlogits ? g : nullptr; p.rewards = c->d_rewards; p.terms = terms; p.ticket = ticket; p.loss = c->d_loss;
     launch_chained(pair_kernel, dim3((unsigned)c->pairs), dim3(TP_THREADS), 0, st, p);
