@@ -7,7 +7,7 @@
 //   d(g log p_y + h H) / d logit_j = (g 1[j = y] - p_j (g + h H + h ln p_j)) / tau.
 // All three sums are held as (M, S, T) triples that combine associatively, so a row is read once, in any split.
 // M may be any reference in their place; where an exponent is formed by one fma, x k - fl(M k), the rounding of M k is
-// corrected in the sums, and rows with entries so large that M k could overflow take the difference first.
+// corrected in the sums, and rows whose M k is large take the difference first.
 //
 // What bounds these kernels: a 16-bit logit is 2 bytes read (and 2 written), for which the memory takes 87 (174) cycles per
 // SM and 1000 logits at the measured copy rate; an exponential for the sums and one for the gradient take 62 cycles each
@@ -425,10 +425,12 @@ __device__ __forceinline__ void move_base(WarpSums& a, float top, const RowGeom&
   a.s2 = pk2(s.x * f, s.y * f);
   a.t2 = pk2(f * fmaf(s.x, d, t.x), f * fmaf(s.y, d, t.y));
   a.base = top; a.thr = top + geo.slack;
-  // one fma per exponent, d = x k - fl(base k), and -inf clamped before it is widened, where both are possible; else the
-  // difference first, which never overflows
+  // One fma per exponent, d = x k - fl(base k), and -inf clamped before it is widened, where the reference lies within 2^12 of
+  // zero in units of an exponent (2,839 at a temperature of one); else the difference first, for any temperature and any
+  // logits.  Within the bound 2^delta is 1 +- 2^-13, and the clamp, which is rounded to the storage type, stays below
+  // 2^-180 of the reference: a step of bfloat16 at |low| <= |top| + 200 / k is at most 34 / k.
   const float low = top - geo.reach;      // 2^-200 of the reference
-  a.fast = fabsf(top) < 1e30f && low > geo.lowest;
+  a.fast = fabsf(top * k) < 4096.f && low > geo.lowest;
   a.nm = a.fast ? -(top * k) : -top;
   a.delta = a.fast ? fmaf(top, k, a.nm) : 0.f;      // 2^(x k - fl(base k)) is 2^delta too large
   a.clamp = narrow2<KIND == LS_F32 ? LS_BF16 : KIND>(low, low);

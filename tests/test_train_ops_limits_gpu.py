@@ -1,0 +1,106 @@
+"""The operators around the optimizer step at the ends of their ranges (run with -m gpu): temperatures far from one, logits far
+from zero, masked and infinite entries, thousands of rows, tensors that move or live on other streams.
+
+Bounds are those of test_train_ops_gpu (`sum_err` and the formulas of `token_tols`), here evaluated in 64 bits on the GPU.  A
+probability's bound does not grow with the logits' distance from zero: what the rounding of M / temperature leaves out of an
+exponent has to be taken back, so the exponent's error is that of its difference from the maximum d and of ln S alone."""
+import gc
+import math
+import weakref
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import train_oracle as orc
+from paper_2501_02379_b200 import binding as B
+from tests.test_train_ops_gpu import DT, HALF_ULP, TINY, U, f64, gen, make_rows, sum_err, within
+
+pytestmark = pytest.mark.gpu
+
+
+class Exact:
+    """64-bit values of rows of logits and the bounds on what fp32 arithmetic makes of them."""
+
+    def __init__(self, z, y, tau):
+        V = z.shape[1]
+        self.live = y >= 0
+        x = torch.where(self.live[:, None], z.double(), 0.0) / tau
+        self.at = y.clamp(min=0)[:, None]
+        self.top = x.amax(1, keepdim=True)
+        self.q = x - self.top
+        self.q -= self.q.exp().sum(1, keepdim=True).log()
+        self.p = self.q.exp()
+        d = torch.where(x > -math.inf, self.top - x, 0.0)
+        self.logp = self.q.gather(1, self.at)[:, 0]
+        self.lse = self.top[:, 0] - self.q.amax(1)
+        self.qf = torch.where(self.p > 0, self.q, 0.0)                       # 0 log 0 = 0
+        self.H = -(self.p * self.qf).sum(1)
+        self.es = sum_err(V) + 2 * 3 * U * (self.p * d).sum(1) + 4 * U
+        self.tl = self.es + 2 * 3 * U * (d.gather(1, self.at)[:, 0] + math.log(V) + 1)
+        self.ts = self.es + 2 * 3 * U * (self.top[:, 0].abs() + math.log(V) + 1)
+        self.tH = 2 * (self.es + 2 * 3 * U) * (1 + (self.p * d).sum(1) + math.log(V))
+        self.rel = 2 * 4 * U * (d + math.log(V) + 1) + self.es[:, None]
+
+    def near(self, got, want, tol, what):
+        want = torch.where(self.live, want, 0.0)
+        off = torch.where(self.live, (got.double() - want).abs() > tol, got != 0) | got.isnan()
+        assert not bool(off.any()), f"{what}: {int(off.sum())} of {off.numel()} rows off, e.g. {got[off][:4].tolist()} for {want[off][:4].tolist()}"
+
+    def near_grad(self, got, g, dg, dtype, scale_over_tau, what, rel=None):
+        """got against scale / tau * g (1[target] - p), g off by dg."""
+        s, rel = scale_over_tau, self.rel if rel is None else rel
+        one = torch.zeros_like(self.p).scatter_(1, self.at, 1.0)
+        want = torch.where(self.live[:, None], g[:, None] * (one - self.p), 0.0) * s
+        tol = (self.p * g.abs()[:, None] * (rel + 8 * U) + self.p * dg[:, None] + one * (g.abs() * 4 * U + dg)[:, None]) * s
+        tiny = TINY[dtype] + 2.0 ** -126 * g.abs()[:, None] * s                # a flushed result, a flushed probability times g
+        off = ((got.double() - want).abs() > 2 * tol + 1.01 * HALF_ULP[dtype] * want.abs() + tiny) | got.isnan()
+        assert not bool(off.any()), f"{what}: {int(off.sum())} entries off, e.g. {got[off][:4].tolist()} for {want[off][:4].tolist()}"
+
+
+# ------------------------------------------------------------------------------------------------ far from one
+FAR = [  # temperature, where the logits lie
+    (1e-2, 0.0), (1e-3, 0.0), (1e-4, 0.0), (1e-6, 0.0), (1e-9, 0.0), (1e-20, 0.0), (1e-2, 600.0), (0.1, 1e4), (0.1, -1e4), (1.0, 3e3), (1.0, 6e4),
+    (1.0, 1e5), (1.0, -1e5), (1.0, 1e8), (1.0, 1e12), (1e4, 0.0), (1e20, 1e5),
+]
+
+
+def far_rows(dtype, rows, V, tau, offset, seed=3):
+    """Logits around `offset` (a few units or a few of the type's steps apart), their maximum in five places of each row of
+    which the target is one, some entries masked, every seventh row ignored."""
+    g = gen(seed)
+    step = abs(offset) * 2 * HALF_ULP[dtype]
+    z = torch.randn(rows, V, generator=g, device="cuda").mul_(max(2.0, 3 * step)).add_(offset).to(DT[dtype])
+    z[:, 5] = -math.inf
+    z[:, V - 70:V - 61] = -math.inf
+    at = torch.randint(0, V, (rows, 4), generator=g, device="cuda")
+    z.scatter_(1, at, z.amax(1, keepdim=True).expand(rows, 4))
+    y = at[:, 0].clone()
+    y[3::7] = -1
+    z[3] = math.nan
+    return z, y
+
+
+def far_cases(dtype):
+    return [c for c in FAR if dtype != "f16" or abs(c[1]) <= 6e4]
+
+
+FAR_PARAMS = [pytest.param(d, t, o, id=f"{d}-{t:g}-{o:g}") for d in ("bf16", "f16", "f32") for t, o in far_cases(d)]
+
+
+@pytest.mark.parametrize("dtype,tau,offset", FAR_PARAMS)
+@pytest.mark.parametrize("rows,V", [(5, 40003), (1200, 20011), (5, 3001), (1200, 3001), (8, 140001)])
+def test_sums_far_from_one(rows, V, dtype, tau, offset):
+    """Log-probabilities, log-sum-exp and entropy of every kernel that forms them."""
+    z, y = far_rows(dtype, rows, V, tau, offset)
+    e = Exact(z, y, tau)
+    logp, lse, H = B.token_logprob(z, y, temperature=tau)
+    e.near(logp, e.logp, e.tl, "logp"); e.near(lse, e.lse, e.ts, "lse"); e.near(H, e.H, e.tH, "entropy")
+    one = torch.ones(rows, device="cuda")
+    for forward_only in (False, True):
+        r = B.policy_loss(z, y, torch.where(y >= 0, e.logp, 0.0).float(), one, one / rows, temperature=tau, forward_only=forward_only)
+        e.near(r.logp, e.logp, e.tl, "policy logp"); e.near(r.entropy, e.H, e.tH, "policy entropy")
+        want = -float(e.live.sum()) / rows                                  # the ratio is one
+        assert abs(float(r.stats[1]) - want) < 2 * float((e.tl + 8 * U + U * e.logp.abs()).max()) + 4 * U
+
+
