@@ -465,7 +465,20 @@ __device__ __forceinline__ void add_chunk(WarpSums& a, const uint4 (&v)[RW_NV], 
 }
 
 // What the row's sums give the gradient.
-struct RowGrad { float M, nb, ls2, c0, c1, target, zy; int owner; };
+struct RowGrad { float M, nb, ls2, c0, c1, e0, e1, target, zy; int owner, fast; };
+// c0, c1 are those of the loop over the granules, e0, e1 those of single entries (which take the difference first).  16-bit logits, |M k| below 2^20: an exponent is one fma, L = x k + nb, nb being
+// -(M k + log2 S) rounded.  The rounding, up to 2^-5 at that bound, is taken back here: p = 2^(L + off) = 2^off 2^L, in both
+// coefficients.  fp32 logits, whose results are not rounded to fewer bits, and rows further out take the difference first.
+template <int KIND, bool ENT>
+__device__ __forceinline__ void gradient_coef(RowGrad& h, float M, float ls2, float c0, float c1, float k) {
+  h.M = M; h.ls2 = ls2; h.c0 = c0; h.c1 = c1; h.nb = 0.f;
+  h.fast = KIND != LS_F32 && fabsf(M * k) < 1048576.f;
+  if (!h.fast) return;
+  h.nb = fmaf(-M, k, -ls2);
+  const float off = fmaf(-M, k, -h.nb) - ls2, f = ex2(off);
+  if (ENT) h.c0 = fmaf(c1, off, c0);
+  h.c0 *= f; h.c1 *= f;
+}
 template <int KIND, bool ENT, bool FAST>
 __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, float k) {
   const uint64_t kk = pk2(k, k), c0 = pk2(h.c0, h.c0), c1 = pk2(h.c1, h.c1);
@@ -708,8 +721,9 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       if (lane == 0) {
         const float sc = q.grad_scale * p.inv_tau;
         RowGrad h;
-        h.M = st.M; h.ls2 = st.ls2; h.nb = fmaf(-st.M, p.k, -st.ls2);
-        h.c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc; h.c1 = -o.h * TK_LN2 * sc;
+        const float c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc, c1 = -o.h * TK_LN2 * sc;
+        gradient_coef<KIND, ENT>(h, st.M, st.ls2, c0, c1, p.k);
+        h.e0 = c0; h.e1 = c1;
         h.target = o.g * sc; h.zy = zy;
         // the thread that writes the target's granule (an edge entry: the lane that has it)
         const int l = y < p.V ? (r.mis + (int)y) / E - wa : -1;
@@ -730,9 +744,9 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     if (stop) break;
     // ---- gradient ----
     const RowGrad h = handed;
-    const bool fast = KIND != LS_F32 && fabsf(h.M) < 1e30f;
+    const bool fast = KIND != LS_F32 && h.fast;
     if (edge >= 0) {
-      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.c0; gc.c1 = h.c1;
+      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.e0; gc.c1 = h.e1;
       st_real<KIND>(drow + (int64_t)edge * B, grad_target<KIND, ENT>(xe, gc, edge == y ? h.target : 0.f));
     }
     uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + wa + tid;
@@ -767,7 +781,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     }
     // the target's entry once more, by the thread that wrote its granule
     if (tid == h.owner) {
-      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.c0; gc.c1 = h.c1;
+      GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.e0; gc.c1 = h.e1;
       st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(h.zy, gc, h.target));
     }
   }
@@ -1056,8 +1070,8 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
     float zy = 0.f;
     if (mine) zy = target_logit<KIND>(p, row, y);
     RowGrad h;
-    h.M = gc.M; h.ls2 = gc.ls2; h.c0 = gc.c0; h.c1 = gc.c1; h.nb = fmaf(-gc.M, p.k, -gc.ls2);
-    const bool fast = KIND != LS_F32 && fabsf(h.M) < 1e30f;
+    gradient_coef<KIND, ENT>(h, gc.M, gc.ls2, gc.c0, gc.c1, p.k);
+    const bool fast = KIND != LS_F32 && h.fast;
     uint4* dst = reinterpret_cast<uint4*>(drow - r.mis * B) + wa + tid;
     for (int j = 0; j < K; ++j, dst += chunk) {
       ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));

@@ -104,3 +104,26 @@ def test_sums_far_from_one(rows, V, dtype, tau, offset):
         assert abs(float(r.stats[1]) - want) < 2 * float((e.tl + 8 * U + U * e.logp.abs()).max()) + 4 * U
 
 
+@pytest.mark.parametrize("dtype,tau,offset", FAR_PARAMS)
+@pytest.mark.parametrize("rows,V", [(5, 40003), (1200, 20011), (5, 3001), (1200, 3001)])
+def test_gradients_far_from_one(rows, V, dtype, tau, offset):
+    """The losses' gradients: the likeliest tokens' probabilities are as exact at a temperature of 1e-6 or around logits of 1e5
+    as they are elsewhere, and a row's gradient sums to zero."""
+    z, y = far_rows(dtype, rows, V, tau, offset)
+    e = Exact(z, y, tau)
+    r = torch.rand(rows, generator=gen(8), device="cuda")
+    old, adv = torch.where(y >= 0, e.logp, 0.0).float() - 0.05, r + 0.5
+    scale = tau                                                             # gradients of the size of the probabilities
+    got = B.policy_loss(z, y, old, adv, torch.ones_like(adv), temperature=tau, grad_scale=scale)
+    ratio = torch.where(e.live, (e.logp - old.double()).exp(), 0.0)
+    g = -ratio * adv.double()
+    dg = 2 * g.abs() * (e.tl + 8 * U + 4 * U * (old.abs() + 2).double()) + g.abs() * 4 * U
+    e.near_grad(got.dlogits, g, dg, dtype, scale / tau, "policy")
+    starts = torch.tensor([0, rows // 2, rows], dtype=torch.int32, device="cuda")
+    ref = torch.where(y >= 0, e.logp, 0.0).float()
+    s = B.preference_loss(z, y, starts, ref, 0.5, 0.0, temperature=tau, grad_scale=scale)
+    c = torch.where(torch.arange(rows, device="cuda") < rows // 2, -0.25, 0.25).double()     # at a margin of zero
+    margin = 0.5 * (e.tl + U * (e.logp.abs() + 1))[e.live].sum()            # what the margin may be off by
+    e.near_grad(s.dlogits, c, (0.5 * 0.25 * margin + 4 * U) * torch.ones_like(c), dtype, scale / tau, "pairs")
+
+
