@@ -118,9 +118,11 @@ struct Row {
 
 // ---- (M, S, T) ----
 struct Triple { float m, s, t; };
+// A factor of 2^d, d below this, is zero; times sums of up to 2^40 per entry it is still far from the end of the range.
+constexpr float TK_FAR_BELOW = -1e4f;
 // Moves a triple to a larger maximum.  A part that has seen nothing but -inf has m = lowest, s = t = 0 and stays so.
 __device__ __forceinline__ void rebase(Triple& a, float m, float k) {
-  const float d = fmaxf((a.m - m) * k, -1e30f);
+  const float d = fmaxf((a.m - m) * k, TK_FAR_BELOW);
   const float f = ex2(d);
   a.t = f * fmaf(a.s, d, a.t);
   a.s *= f;
@@ -420,7 +422,7 @@ struct WarpSums { float base, thr, nm, delta; uint32_t clamp; bool fast; uint64_
 template <int KIND>
 __device__ __forceinline__ void move_base(WarpSums& a, float top, const RowGeom& geo, float k) {
   top = warp_max(top);
-  const float d = fmaxf(fmaf(a.base - top, k, -a.delta), -1e30f), f = ex2(d);
+  const float d = fmaxf(fmaf(a.base - top, k, -a.delta), TK_FAR_BELOW), f = ex2(d);
   const float2 s = upk2(a.s2), t = upk2(a.t2);
   a.s2 = pk2(s.x * f, s.y * f);
   a.t2 = pk2(f * fmaf(s.x, d, t.x), f * fmaf(s.y, d, t.y));

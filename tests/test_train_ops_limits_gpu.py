@@ -127,3 +127,21 @@ def test_gradients_far_from_one(rows, V, dtype, tau, offset):
     e.near_grad(s.dlogits, c, (0.5 * 0.25 * margin + 4 * U) * torch.ones_like(c), dtype, scale / tau, "pairs")
 
 
+@pytest.mark.parametrize("V", [40003, 140001])
+def test_one_logit_far_above_the_others(V):
+    """One token has a logit of 1e32, and before it came the sums had grown relative to their reference: nothing but that token
+    is left, and no infinity times zero."""
+    z = torch.zeros(3, V, dtype=torch.bfloat16, device="cuda")
+    z[:, V // 2:] = 27.0                   # 2^39 above the zeros that come first
+    z[1, V - 100] = 1e32
+    z[2, V - 1] = 1e32
+    y = torch.tensor([V // 2, V - 100, 7], device="cuda")
+    e = Exact(z, y, 1.0)
+    one = torch.ones(3, device="cuda")
+    for r in (B.policy_loss(z, y, one * 0, one, one), B.policy_loss(z, y, one * 0, one, one, forward_only=True)):
+        e.near(r.logp, e.logp, e.tl, "logp"); e.near(r.entropy, e.H, e.tH, "entropy")
+    many = [x.view(400, 3) for x in B.token_logprob(z.repeat(400, 1), y.repeat(400))]
+    for i in range(400):                   # (the rows lie differently relative to 16 bytes)
+        e.near(many[0][i], e.logp, e.tl, "logp"); e.near(many[1][i], e.lse, e.ts, "lse"); e.near(many[2][i], e.H, e.tH, "entropy")
+
+
