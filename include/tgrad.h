@@ -392,8 +392,9 @@ tgrad_status tgrad_token_logprob_backward(const tgrad_logits* logits, const floa
  *   policy  = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
  *   kl      = exp(ref_logp - logp) - (ref_logp - logp) - 1      (0 without ref_logp)
  *   loss    = sum over the rows of weight (policy + kl_coef kl - entropy_coef entropy).
- * The weights carry the mask and the normalisation (1 / tokens for a mean).  Where the clipped term is the smaller one
- * no gradient flows through the ratio; at a tie it does.
+ * The weights carry the mask and the normalisation (1 / tokens for a mean): a row of weight 0 adds nothing to the sums and
+ * has a gradient of 0 whatever its old_logp, ref_logp and advantage are (its logits are read and have to be finite or
+ * -infinity).  Where the clipped term is the smaller one no gradient flows through the ratio; at a tie it does.
  * d_stats[5] = loss and the weighted sums of policy, kl, entropy and of the rows that were clipped.
  * d_dlogits = grad_scale * d loss / d logits; NULL: forward only.  d_logp and d_entropy (rows) may be NULL. */
 typedef struct {

@@ -622,8 +622,8 @@ def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, c
                 dlogits=None, forward_only: bool = False, stream=None) -> PolicyLoss:
     """Clipped policy loss with a KL term and an entropy bonus, and its gradient with respect to the logits in the same
     pass: loss = sum_i weights_i (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(u) - u - 1)
-    - entropy_coef H), r = exp(logp - old_logp), u = ref_logp - logp.  The weights carry mask and normalisation; rows
-    with a negative target are ignored.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
+    - entropy_coef H), r = exp(logp - old_logp), u = ref_logp - logp.  The weights carry mask and normalisation (what
+    stands beside a row of weight 0 does not count); rows with a negative target are ignored, their logits too.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
     `dlogits` may be the logits themselves."""
     desc, rows, vocab, index = _logits(logits, targets, temperature)
     if _elsewhere(index, stream):

@@ -339,8 +339,13 @@ struct PolicyArgs {
 struct PolicyToken { float g, h; float4 terms; };
 // r = exp(logp - old); the loss -min(r A, clip(r) A) has gradient -r A where the unclipped term is the smaller one or
 // they are equal, and none elsewhere; kl = exp(u) - u - 1 with u = ref - logp has gradient 1 - exp(u).
+// A weight of zero is a mask: whatever stands beside such a row (infinities, NaN, a ratio that overflows) does not count.
 __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float old, float ref, bool has_ref, float A, float w, const PolicyArgs& q) {
   PolicyToken o;
+  if (w == 0.f) {
+    o.g = o.h = 0.f; o.terms = make_float4(0.f, 0.f, 0.f, 0.f);
+    return o;
+  }
   const float r = expf(logp - old);
   const float free = r * A, bound = fminf(fmaxf(r, q.low), q.high) * A;
   const bool cut = free > bound;

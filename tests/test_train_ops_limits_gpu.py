@@ -145,3 +145,26 @@ def test_one_logit_far_above_the_others(V):
         e.near(many[0][i], e.logp, e.tl, "logp"); e.near(many[1][i], e.lse, e.ts, "lse"); e.near(many[2][i], e.H, e.tH, "entropy")
 
 
+# ------------------------------------------------------------------------------------------------ masked and infinite entries
+@pytest.mark.parametrize("forward_only", [False, True])
+@pytest.mark.parametrize("ent", [0.0, 0.02])
+@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f16", 9001), ("f32", 40003)])
+def test_rows_of_weight_zero_add_nothing(V, dtype, ent, forward_only):
+    """A mask in the weights: what stands beside a masked row (infinities, NaN, values whose ratio overflows) does not count."""
+    z, y = make_rows(dtype, 12, V, 0, 5)
+    w = torch.rand(12, generator=gen(1), device="cuda")
+    w[2:9] = 0
+    logp = B.token_logprob(z, y)[0]
+    old, ref, adv = logp - 0.1, logp + 0.2, torch.linspace(-1, 1, 12, device="cuda")
+    kw = dict(kl_coef=0.1, entropy_coef=ent, forward_only=forward_only)
+    want = B.policy_loss(z, y, old, adv, w, ref_logp=ref, **kw)
+    old, ref, adv = old.clone(), ref.clone(), adv.clone()
+    old[2], old[3], old[4], ref[5], ref[6], adv[7], adv[8] = -math.inf, -500.0, math.nan, math.inf, math.nan, math.nan, -math.inf
+    adv[2] = 0.0
+    got = B.policy_loss(z, y, old, adv, w, ref_logp=ref, **kw)
+    assert torch.equal(got.stats, want.stats) and torch.equal(got.logp, want.logp) and torch.equal(got.entropy, want.entropy)
+    if not forward_only:
+        assert torch.equal(got.dlogits, want.dlogits) and bool((got.dlogits[2:9] == 0).all())
+    assert bool(torch.isfinite(got.stats).all())
+
+
