@@ -351,8 +351,12 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
   const bool cut = free > bound;
   const float pg = cut ? -bound : -free;
   float kl = 0.f, dkl = 0.f;
-  if (has_ref) { const float u = ref - logp, em = expm1f(u); kl = em - u; dkl = -em; }
-  o.g = w * ((cut ? 0.f : -free) + q.kl_coef * dkl);
+  if (has_ref) {
+    const float u = ref - logp, em = expm1f(u);
+    kl = em < __int_as_float(0x7f800000) ? em - u : em;      // infinite, not NaN, where the policy forbids what the reference allows
+    dkl = q.kl_coef != 0.f ? q.kl_coef * -em : 0.f;          // (an infinite KL that is only looked at)
+  }
+  o.g = w * ((cut ? 0.f : -free) + dkl);
   o.h = -q.ent_coef * w;
   o.terms = make_float4(w * pg, w * kl, w * H, cut ? w : 0.f);
   return o;
@@ -911,7 +915,8 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(const float4* __restri
   if (threadIdx.x == 0) {
     double t[4];
     for (int c = 0; c < 4; ++c) { t[c] = 0.0; for (int w = 0; w < 32; ++w) t[c] += sh[c][w]; }
-    stats[0] = (float)(t[0] + (double)kl_coef * t[1] - (double)ent_coef * t[2]);
+    // (a term that is only looked at stays out of the loss, also an infinite one)
+    stats[0] = (float)(t[0] + (kl_coef != 0.f ? (double)kl_coef * t[1] : 0.0) - (ent_coef != 0.f ? (double)ent_coef * t[2] : 0.0));
     for (int c = 0; c < 4; ++c) stats[1 + c] = (float)t[c];
   }
 }

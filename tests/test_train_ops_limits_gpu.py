@@ -168,3 +168,30 @@ def test_rows_of_weight_zero_add_nothing(V, dtype, ent, forward_only):
     assert bool(torch.isfinite(got.stats).all())
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
+def test_policy_loss_with_an_infinite_kl(V, dtype):
+    """The reference forbids a token (-inf), or gives a token much that the policy forbids or almost does: the KL term is
+    infinite, not NaN, and with a coefficient of zero, where it is only looked at, loss and gradient do not know of it."""
+    z, y = make_rows(dtype, 6, V, 0, 9)
+    y[:] = 3
+    z[4, 3] = -math.inf                    # the policy forbids its own token
+    one = torch.ones(6, device="cuda")
+    logp = B.token_logprob(z, y)[0]
+    old = torch.where(logp.isfinite(), logp, -5.0) - 0.1
+    ref = torch.where(logp.isfinite(), logp, -5.0) + 0.1
+    ref[1], ref[2] = -math.inf, logp[2] + 200.0
+    plain = B.policy_loss(z, y, old, one, one / 6)
+    assert bool(torch.isfinite(plain.stats).all()) and bool(torch.isfinite(plain.dlogits).all())
+    for fwd in (False, True):
+        got = B.policy_loss(z, y, old, one, one / 6, ref_logp=ref, forward_only=fwd)
+        assert got.stats[2] == math.inf
+        within(f64(got.stats[[0, 1, 3, 4]]), f64(plain.stats[[0, 1, 3, 4]]), 1e-4 if fwd else 0.0)      # forward only: another order of sums
+        if not fwd:
+            assert torch.equal(got.dlogits, plain.dlogits)
+        got = B.policy_loss(z, y, old, one, one / 6, ref_logp=ref, kl_coef=0.1, forward_only=fwd)
+        assert got.stats[0] == math.inf and got.stats[2] == math.inf
+    ref[4], ref[2] = -5.0, logp[2]
+    ref[1] = logp[1]
+    assert B.policy_loss(z, y, old, one, one / 6, ref_logp=ref).stats[2] == math.inf
+
+
