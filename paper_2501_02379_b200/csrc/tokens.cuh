@@ -347,7 +347,8 @@ __device__ __forceinline__ PolicyToken policy_token(float logp, float H, float o
     return o;
   }
   const float r = expf(logp - old);
-  const float free = r * A, bound = fminf(fmaxf(r, q.low), q.high) * A;
+  const float free = A != 0.f ? r * A : 0.f;      // (0 also where the ratio overflows)
+  const float bound = fminf(fmaxf(r, q.low), q.high) * A;
   const bool cut = free > bound;
   const float pg = cut ? -bound : -free;
   float kl = 0.f, dkl = 0.f;

@@ -169,6 +169,19 @@ def test_rows_of_weight_zero_add_nothing(V, dtype, ent, forward_only):
 
 
 @pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
+def test_an_advantage_of_zero_leaves_no_policy_term(dtype, V):
+    """However far the policy has moved: a ratio that overflows times an advantage of zero is zero."""
+    z, y = make_rows(dtype, 4, V, 0, 6)
+    adv, w, old = torch.tensor([0.0, 0.0, 1.0, -1.0], device="cuda"), torch.ones(4, device="cuda") / 4, B.token_logprob(z, y)[0]
+    want = B.policy_loss(z, y, old, adv, w)
+    moved = old.clone()
+    moved[0], moved[1] = -200.0, -math.inf
+    got = B.policy_loss(z, y, moved, adv, w)
+    assert torch.equal(got.stats, want.stats) and torch.equal(got.dlogits, want.dlogits) and bool((got.dlogits[:2] == 0).all())
+    assert torch.equal(B.policy_loss(z, y, moved, adv, w, forward_only=True).stats, B.policy_loss(z, y, old, adv, w, forward_only=True).stats)
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
 def test_policy_loss_with_an_infinite_kl(V, dtype):
     """The reference forbids a token (-inf), or gives a token much that the policy forbids or almost does: the KL term is
     infinite, not NaN, and with a coefficient of zero, where it is only looked at, loss and gradient do not know of it."""
