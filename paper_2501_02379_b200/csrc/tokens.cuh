@@ -1169,7 +1169,8 @@ __global__ void __launch_bounds__(TP_THREADS) pair_kernel(const __grid_constant_
     R[0] *= (double)a.beta; R[1] *= (double)a.beta;
     const double h = R[0] - R[1], e = (double)a.smoothing;
     const double x = exp(-fabs(h)), tail = log1p(x);                     // -log sigma(z) = max(-z, 0) + tail
-    a.terms[b] = h != h ? h : (1.0 - e) * (fmax(-h, 0.0) + tail) + e * (fmax(h, 0.0) + tail);
+    // (h is infinite where a token of one answer has probability zero: a part that the smoothing leaves out stays out)
+    a.terms[b] = h != h ? h : (e < 1.0 ? (1.0 - e) * (fmax(-h, 0.0) + tail) : 0.0) + (e > 0.0 ? e * (fmax(h, 0.0) + tail) : 0.0);
     a.rewards[2 * b] = (float)R[0]; a.rewards[2 * b + 1] = (float)R[1];
     const double right = h >= 0.0 ? 1.0 / (1.0 + x) : x / (1.0 + x);
     coef = (float)((double)a.beta * (right - (1.0 - e)) / (double)a.pairs);

@@ -208,3 +208,27 @@ def test_policy_loss_with_an_infinite_kl(V, dtype):
     assert B.policy_loss(z, y, old, one, one / 6, ref_logp=ref).stats[2] == math.inf
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
+def test_pairs_with_a_forbidden_token(V, dtype):
+    """An answer with a token of probability zero has a reward of -inf.  As the rejected one it leaves a loss of zero without
+    smoothing and an infinite one with it, as the chosen one it is the other way round for a smoothing of one; both: NaN."""
+    z, y = make_rows(dtype, 8, V, 0, 4)
+    y[:] = 2
+    z[3, 2] = -math.inf                    # the second answer's
+    ref = torch.full((8,), -4.0, device="cuda")
+    st = lambda *s: torch.tensor(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    r = B.preference_loss(z, y, st(0, 2, 4), ref)
+    assert r.loss == 0 and r.rewards[1] == -math.inf and bool(torch.isfinite(r.rewards[0])) and bool((r.dlogits == 0).all())
+    assert B.preference_loss(z, y, st(0, 2, 4), ref, label_smoothing=0.1).loss == math.inf
+    r = B.preference_loss(z, y, st(2, 4, 6), ref, beta=0.1)
+    assert r.loss == math.inf and r.rewards[0] == -math.inf
+    one = torch.zeros(V, device="cuda").double()
+    p = torch.softmax(z[2].double(), 0)
+    one[2] = 1
+    within(f64(r.dlogits[2]), f64(-0.1 * (one - p)), 2 * (0.1 * f64(p) * 2e-5 + 1.01 * HALF_ULP[dtype] * 0.1 * f64((one - p).abs())) + TINY[dtype])
+    r = B.preference_loss(z, y, st(2, 4, 6), ref, label_smoothing=1.0)
+    assert r.loss == 0 and bool((r.dlogits == 0).all())
+    z[5, 2] = -math.inf                    # now the third answer's too
+    assert math.isnan(B.preference_loss(z, y, st(2, 4, 6), ref).loss)
+
+
