@@ -319,8 +319,9 @@ tgrad_status tgrad_get_stage_times(tgrad_state* st, void* cuda_stream, float* ms
  * Everything is enqueued on the stream, nothing synchronises, every sum has a
  * fixed order (the same inputs give the same bits), and all arithmetic is in
  * fp32 or wider with one rounding to the storage type at the end.
- * Pointers need the alignment of their element type only.  Every wait inside a kernel is bounded; one that ran out, which
- * nothing in normal operation leads to, leaves NaN in the results (loss, log-probabilities or gradient). */
+ * Pointers need the alignment of their element type only.  Every wait of a kernel on its copies or on another warp's
+ * progress is bounded; one that ran out, which nothing in normal operation leads to, leaves NaN in all results (loss,
+ * log-probabilities, entropy, gradient) of the rows that were not finished. */
 
 typedef struct {
   void* d_data;        /* numel entries, contiguous in memory (in any order of the dimensions) */
@@ -436,6 +437,11 @@ typedef struct {
 tgrad_status tgrad_preference_loss_bytes(int64_t rows, int32_t pairs, size_t* workspace_bytes);
 tgrad_status tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference_args* args, void* d_workspace,
                                    size_t workspace_bytes, void* cuda_stream);
+
+/* For tests of that reporting: the kernels that stream rows of logits through shared memory stop within the first row that takes
+ * more than so many copies (0: before any row), and the waits for further ones run out, after half a second.  Negative: never,
+ * the default.  For the whole process; the calls after this one take it. */
+tgrad_status tgrad_set_copy_limit(int32_t copies);
 
 #ifdef __cplusplus
 }

@@ -99,7 +99,7 @@ EXPORTS = [
     "tgrad_set_stage_timing", "tgrad_get_stage_times", "tgrad_select_topk_noalloc", "tgrad_diagnostics",
     "tgrad_step_scaled", "tgrad_step_batched_scaled", "tgrad_grad_norm_bytes", "tgrad_grad_norm", "tgrad_clip_grads",
     "tgrad_adamw_step", "tgrad_token_logprob", "tgrad_token_logprob_backward", "tgrad_policy_loss_bytes",
-    "tgrad_policy_loss", "tgrad_preference_loss_bytes", "tgrad_preference_loss",
+    "tgrad_policy_loss", "tgrad_preference_loss_bytes", "tgrad_preference_loss", "tgrad_set_copy_limit",
 ]
 
 
@@ -144,6 +144,7 @@ def lib() -> C.CDLL:
         l.tgrad_policy_loss.argtypes = [vp, vp, vp, sz, vp]
         l.tgrad_preference_loss_bytes.argtypes = [C.c_int64, C.c_int32, C.POINTER(sz)]
         l.tgrad_preference_loss.argtypes = [vp, vp, vp, sz, vp]
+        l.tgrad_set_copy_limit.argtypes = [C.c_int32]
         for name in EXPORTS:
             if name not in ("tgrad_status_string", "tgrad_launch_count"):
                 getattr(l, name).restype = C.c_int
@@ -601,6 +602,13 @@ def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_e
     _check(lib().tgrad_token_logprob_backward(desc, lse_p, e_p, g_p, h_p, out.data_ptr(), stride, _raw_stream(index)),
            "tgrad_token_logprob_backward")
     return out
+
+
+def set_copy_limit(copies: int = -1) -> None:
+    """For tests: the kernels that stream rows of logits through shared memory stop within the first row that takes more than so
+    many copies (0: before any row, -1: never).  The waits for further ones run out, which leaves NaN in the rows that were not
+    finished.  For the whole process."""
+    _check(lib().tgrad_set_copy_limit(int(copies)), "tgrad_set_copy_limit")
 
 
 class PolicyLoss(NamedTuple):

@@ -386,10 +386,13 @@ struct RowGeom {
   int K, last;           // chunks of the longest row, granules before the last of them; others have at most one chunk less
   float reach, lowest;   // 200 / k; lowest value that the clamp may take in the storage type
   float slack;           // 40 / k
+  int copies;            // of one row after which the fetching warp stops (for tests of what happens then), or 2^31 - 1
 };
 
 // A bounded wait that asks the hardware to keep the warp asleep for up to 20 us at a time: the other warps need the issue
 // slots that frequent polling takes (more than half of all instructions on rows of 8000 logits).
+// The bound, about half a second (a poll takes 4 us), is a constant: as a parameter it costs the policy loss 1 to 4 % (8192 x 131072
+// bf16: 689 to 710 us instead of 683).
 __device__ __forceinline__ bool mbar_wait_asleep(uint64_t* bar, uint32_t parity) {
   for (uint32_t i = 0; i < (1u << 17); ++i) {
     uint32_t ok;
@@ -509,17 +512,32 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Every wait on an mbarrier is bounded.  What happens when one runs out (nothing in normal operation leads there):
+// * An arithmetic warp whose wait has run out stops work and goes to the barrier that the others reach next, their next row's or
+//   the one at their end, having set `bad` for it.  All read `bad` behind that barrier and leave together, so nobody is left
+//   waiting for a warp that is gone.  `bad` alternates between two places, since a warp may still read it behind one barrier when
+//   another sets it for the next.
+// * The fetching warp stops asking.  All warps meet when they have left their loops; the rows of every unit that the block has
+//   taken and not finished then get NaN in all results.  At most seven units can be open: one in work, RW_JOBS handed on, one being
+//   fetched, one just taken.
+constexpr int RW_OPEN = 8;
 struct RowBarriers {
   uint64_t full[RW_MAX_PLACES], empty[RW_MAX_PLACES], jfull[RW_JOBS], jempty[RW_JOBS], nbar;
   alignas(16) uint4 answer;
   longlong2 job[RW_JOBS];     // unit of rows (-1: no more), target of its first row
+  int unit[RW_OPEN];          // the units that the block took last, the i-th at i modulo RW_OPEN
+  int taken;                  // how many it has taken
+  int done;                   // after a failure: how many all warps have finished
+  volatile int bad[2], failed;
   __device__ __forceinline__ void init(int N, int W) {
     for (int i = 0; i < N; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
     for (int i = 0; i < RW_JOBS; ++i) { mbar_init(&jfull[i], 1); mbar_init(&jempty[i], W); }
     mbar_init(&nbar, 1);
+    taken = 0; done = 0x7fffffff; bad[0] = bad[1] = failed = 0;
     fence_mbar_init();
   }
 };
+static_assert((RW_JOBS & (RW_JOBS - 1)) == 0 && RW_OPEN >= RW_JOBS + 3, "job slots and open units");
 
 // This warp has read a place of the ring.  The fence comes first because nothing else keeps the warp's shared loads, which
 // may still be under way, before the asynchronous copy that the arrival lets into the place (without it, a few granules at
@@ -536,21 +554,27 @@ template <int KIND, bool STAY, bool LAST_FIRST>
 __device__ __forceinline__ void fetch_rows(const TokenArgs& p, int64_t rows, const RowGeom& geo, unsigned char* ring, RowBarriers& rb, int lane, int chunk) {
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
   const int N = geo.N;
-  int s = 0, js = 0;
+  int s = 0, js = 0, taken = 0;
   uint32_t ph = 0, jph = 0, used = 0, nph = 0;
-  bool ok = true;
-  for (int64_t block = blockIdx.x; ok;) {
+  bool ok = true, lost = false;
+  int64_t block = blockIdx.x;
+  for (;;) {
+    const int64_t unit = LAST_FIRST ? (int64_t)gridDim.x - 1 - block : block;
+    if (lane == 0) rb.unit[taken % RW_OPEN] = (int)unit;
+    ++taken;
+    if (!ok) break;
     if (lane == 0) next_block_ask(&rb.answer, &rb.nbar);
-    const int64_t unit = LAST_FIRST ? (int64_t)gridDim.x - 1 - block : block, r0 = unit * geo.unit, mine = r0 + lane;
+    const int64_t r0 = unit * geo.unit, mine = r0 + lane;
     const long long ym = lane < geo.unit && mine < rows ? p.y[mine] : -1;
     uint32_t live = __ballot_sync(0xffffffffu, ym >= 0);
     if (lane == 0) {
-      ok = mbar_wait_asleep(&rb.jempty[js], jph ^ 1);
+      ok = geo.copies > 0 && mbar_wait_asleep(&rb.jempty[js], jph ^ 1);
       if (ok) { rb.job[js] = make_longlong2(unit, ym); mbar_arrive(&rb.jfull[js]); }
       for (; live && ok; live &= live - 1) {
         const Row<KIND> r(p.z + (r0 + __ffs(live) - 1) * p.ldz * B, p.V);
         const int wa = r.mis ? 1 : 0, nw = max(0, (r.mis + p.V) / E - wa), K = geo.K - (nw <= geo.last), n = !STAY ? 0 : K <= N ? K : N - 2;
-        for (int j = 0; j < (STAY ? 2 * K - n : K) && ok; ++j) {
+        const int all = STAY ? 2 * K - n : K, most = min(all, geo.copies);
+        for (int j = 0; j < most && ok; ++j) {
           const int x = K - n, id = j < x ? n + j : (j < K ? j - x : n + j - K), at = id * chunk, len = min(chunk, nw - at);
           ok = mbar_wait_asleep(&rb.empty[s], ph ^ 1);
           if (!ok) break;
@@ -559,6 +583,7 @@ __device__ __forceinline__ void fetch_rows(const TokenArgs& p, int64_t rows, con
           used |= 1u << s;
           if (++s == N) { s = 0; ph ^= 1; }
         }
+        ok = ok && most == all;
       }
     }
     if (++js == RW_JOBS) { js = 0; jph ^= 1; }
@@ -567,15 +592,24 @@ __device__ __forceinline__ void fetch_rows(const TokenArgs& p, int64_t rows, con
     nph ^= 1;
     const int next = got ? next_block_get(&rb.answer) : -1;
     __syncwarp();
-    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    ok = __shfl_sync(0xffffffffu, (int)(ok && got), 0) != 0;
+    lost = !got;
     if (next < 0) break;
     block = next;
   }
-  if (lane == 0 && ok && mbar_wait_asleep(&rb.jempty[js], jph ^ 1)) { rb.job[js] = make_longlong2(-1, 0); mbar_arrive(&rb.jfull[js]); }
-  // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
-  if (lane == 0)
+  if (lane == 0) {
+    if (ok) {
+      ok = mbar_wait_asleep(&rb.jempty[js], jph ^ 1);
+      if (ok) { rb.job[js] = make_longlong2(-1, 0); mbar_arrive(&rb.jfull[js]); }
+    }
+    // no copy is left in flight when the block ends: place i was last filled in phase ph (i < s) or the one before
     for (int i = 0; i < N; ++i)
       if (used >> i & 1) (void)mbar_wait_asleep(&rb.full[i], i < s ? ph : ph ^ 1);
+    rb.taken = taken;
+    if (lost) atomicMin(&rb.done, 0);      // a unit that this block may have been given and does not know of: NaN where it can
+    if (!ok) rb.failed = 1;
+  }
+  __syncwarp();
 }
 
 struct ForwardArgs {
@@ -597,6 +631,26 @@ __device__ __forceinline__ void store_stat(const ForwardArgs& f, int64_t row, co
   if (f.g) f.g[row] = 0.f;
   if (f.ticket && row == 0) *f.ticket = 0;
 }
+// The end of a block: all its warps, the fetching one too, once they have left their loops.  After a failure the rows of the units
+// that were not finished get NaN; `write(row, NaN)` sets what a row has besides its gradient.
+template <int KIND, int W, typename F>
+__device__ __noinline__ void row_block_failed(const RowBarriers& rb, const RowGeom& geo, const TokenArgs& p, int64_t rows, bool back, F write) {
+  const float nan = __int_as_float(0x7fc00000);
+  for (int i = max(rb.done, max(0, rb.taken - RW_OPEN)); i < rb.taken; ++i) {
+    const int64_t r0 = (int64_t)rb.unit[i % RW_OPEN] * geo.unit, r1 = min((long long)(r0 + geo.unit), (long long)rows);
+    for (int64_t row = r0; row < r1; ++row) {
+      if (threadIdx.x == 0) write(row, nan);
+      if (back)
+        for (int j = (int)threadIdx.x; j < p.V; j += 32 * (W + 1)) st_real<KIND>(p.dz + (row * p.lddz + j) * Gran<KIND>::B, nan);
+    }
+  }
+}
+template <int KIND, int W, typename F>
+__device__ __forceinline__ void row_block_end(const RowBarriers& rb, const RowGeom& geo, const TokenArgs& p, int64_t rows, bool back, F write) {
+  __syncwarp();
+  bar_sync_n(2, 32 * (W + 1));
+  if (rb.failed) row_block_failed<KIND, W>(rb, geo, p, rows, back, write);
+}
 // 96 registers: 80 leave the scheduler too little to interleave (0.73 instead of 0.68 ms at 8192 x 131072 bf16), 128 too few
 // warps (0.71 ms).  8192 x 131072 bf16 logits with gradient: 0.66 ms, 6.1 TB/s, after a cold start; 0.74 ms at the clocks that a
 // second of it settles at, where the arithmetic weighs more.  Log-probabilities of 16384 x 32000: 0.175 ms, 6.0 TB/s.
@@ -607,26 +661,27 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ float4 sums[2][RW_MAX_WARPS];
   __shared__ __align__(16) RowGrad handed;
-  __shared__ volatile int bad;           // a wait ran out of its bound
   __shared__ RowBarriers rb;
   constexpr int E = Gran<KIND>::E, B = Gran<KIND>::B;
   constexpr int threads = 32 * W, chunk = RW_NV * threads;
   const int N = geo.N, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid == 0) {
-    bad = 0;
-    rb.init(N, W);
-  }
+  if (tid == 0) rb.init(N, W);
   __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
-  int s = 0, js = 0;
-  uint32_t ph = 0, jph = 0;
-  bool ok = true;
-
+  const auto fail_row = [&](int64_t at, float nan) {
+    RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = nan;
+    store_stat(f, at, none);
+    if (BACK) q.terms[at] = make_float4(nan, nan, nan, nan);
+  };
   if (warp == W) {
     fetch_rows<KIND, BACK, false>(p, rows, geo, ring, rb, lane, chunk);
+    row_block_end<KIND, W>(rb, geo, p, rows, BACK, fail_row);
     return;
   }
+  int s = 0, jobs = 0;                // jobs: asked for so far, all but the last of them finished
+  uint32_t ph = 0;
+  bool ok = true, left = false;       // left: behind the barrier that all leave from
 
   // ---- the arithmetic warps ----
   const uint32_t ni = neg_inf_word<KIND>();
@@ -639,12 +694,13 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
   int side = 0;      // of the double-buffered sums
   for (;; ++row, zrow += zstep, drow += dstep) {
     if (row == row_end) {      // the next unit of rows
-      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], jph));
-      if (!ok) break;          // (the fetching warp has stopped: no warp gets another unit)
+      const int js = jobs % RW_JOBS;
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], (uint32_t)(jobs / RW_JOBS) & 1));
+      ++jobs;
+      if (!ok) break;
       const longlong2 jb = rb.job[js];
       __syncwarp();
       if (lane == 0) mbar_arrive(&rb.jempty[js]);
-      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
       if (jb.x < 0) break;
       row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
       y_next = jb.y;
@@ -688,7 +744,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     int rs = s;
     for (int j = 0; j < K; ++j) {
       ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
-      if (!ok) { bad = 1; break; }
+      if (!ok) break;
       if (j == x) rs = s;
       const bool end = j == (x > 0 ? x : K) - 1;      // the row's last chunk
       const uint4* place = places + s * chunk + tid;
@@ -719,9 +775,12 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       warp_combine(c, p.k);
     }
     side ^= 1;
-    if (lane == 0) sums[side][warp] = make_float4(c.m, c.s, c.t, 0.f);
+    if (lane == 0) {
+      sums[side][warp] = make_float4(c.m, c.s, c.t, 0.f);
+      if (!ok) rb.bad[side] = 1;
+    }
     bar_sync_n(1, threads);
-    const bool stop = bad != 0;      // nobody sets it between the two barriers, so that all warps stop together
+    const bool stop = rb.bad[side] != 0;
     if (warp == W - 1) {
       c.m = TK_LOWEST; c.s = c.t = 0.f;
       if (lane < W) { const float4 o = sums[side][lane]; c.m = o.x; c.s = o.y; c.t = o.z; }
@@ -748,12 +807,11 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     }
     if (!BACK) {
       // (the next row's sums go to the other side, and nobody passes its barrier before the last warp has read this one's)
-      if (stop) { ok = false; break; }
+      if (stop) { ok = false; left = true; break; }
       continue;
     }
     bar_sync_n(1, threads);
-    ok = !stop;
-    if (stop) break;
+    if (stop) { ok = false; left = true; break; }
     // ---- gradient ----
     const RowGrad h = handed;
     const bool fast = KIND != LS_F32 && h.fast;
@@ -766,7 +824,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     for (int j = 0; j < K; ++j, dst += chunk) {
       if (j >= n) {
         ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
-        if (!ok) { bad = 1; break; }
+        if (!ok) break;
         at = s;
         if (++s == N) { s = 0; ph ^= 1; }
       }
@@ -791,19 +849,21 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       }
       if (++at == N) at = 0;
     }
+    if (!ok) break;
     // the target's entry once more, by the thread that wrote its granule
     if (tid == h.owner) {
       GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.e0; gc.c1 = h.e1;
       st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(h.zy, gc, h.target));
     }
   }
-  // a wait that ran out of its bound (nothing this kernel does leads there): the loss says so
-  if (!ok && tid == 0) {
-    const float n = __int_as_float(0x7fc00000);
-    if (BACK) q.terms[(int64_t)blockIdx.x * geo.unit] = make_float4(n, n, n, n);
-    RowStat none; none.logp = none.logp_lo = none.lse = none.H = none.M = none.ls2 = n;
-    store_stat(f, (int64_t)blockIdx.x * geo.unit, none);
+  if (!left) {
+    side ^= 1;
+    if (!ok && lane == 0) rb.bad[side] = 1;
+    bar_sync_n(1, threads);
+    if (rb.bad[side]) ok = false;
   }
+  if (!ok && lane == 0) { atomicMin(&rb.done, jobs - 1); rb.failed = 1; }
+  row_block_end<KIND, W>(rb, geo, p, rows, BACK, fail_row);
 }
 
 // Short rows (up to 16 KB): a warp takes one at a time, four granules per lane in a batch.  Nothing is shared, so the latency
@@ -1029,16 +1089,18 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
   __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
+  const auto fail_row = [](int64_t, float) {};
   if (warp == W) {
     fetch_rows<KIND, false, true>(p, rows, geo, ring, rb, lane, chunk);
+    row_block_end<KIND, W>(rb, geo, p, rows, true, fail_row);
     return;
   }
   const uint4* const places = reinterpret_cast<const uint4*>(ring);
   const int64_t zstep = p.ldz * B, dstep = p.lddz * B;
   const char* zrow = p.z;
   char* drow = p.dz;
-  int s = 0, js = 0;
-  uint32_t ph = 0, jph = 0;
+  int s = 0, jobs = 0;                // as in the row kernel
+  uint32_t ph = 0;
   int64_t row = 0, row_end = 0;
   long long y_next = -1;
   GradCoef c_next; float t_next = 0.f;      // of the next row, asked for while this one is worked on
@@ -1046,12 +1108,13 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
   bool ok = true;
   for (;; ++row, zrow += zstep, drow += dstep) {
     if (row == row_end) {      // the next unit of rows
-      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], jph));
+      const int js = jobs % RW_JOBS;
+      ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.jfull[js], (uint32_t)(jobs / RW_JOBS) & 1));
+      ++jobs;
       if (!ok) break;
       const longlong2 jb = rb.job[js];
       __syncwarp();
       if (lane == 0) mbar_arrive(&rb.jempty[js]);
-      if (++js == RW_JOBS) { js = 0; jph ^= 1; }
       if (jb.x < 0) break;
       row = jb.x * geo.unit; row_end = min((long long)(row + geo.unit), (long long)rows);
       y_next = jb.y;
@@ -1113,8 +1176,8 @@ __global__ void __maxnreg__(80) token_gradient_kernel(const __grid_constant__ To
     if (!ok) break;
     if (mine) st_real<KIND>(drow + y * B, grad_target<KIND, ENT>(zy, gc, target));
   }
-  // a wait that ran out of its bound (nothing this kernel does leads there) leaves a NaN in the gradient
-  if (!ok && tid == 0) st_real<KIND>(p.dz, __int_as_float(0x7fc00000));
+  if (!ok && lane == 0) { atomicMin(&rb.done, jobs - 1); rb.failed = 1; }
+  row_block_end<KIND, W>(rb, geo, p, rows, true, fail_row);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -1156,7 +1219,7 @@ __global__ void __launch_bounds__(TP_THREADS) pair_kernel(const __grid_constant_
     double s = 0.0;
     for (int64_t i = at[2 * c] + threadIdx.x; i < at[2 * c + 1]; i += TP_THREADS) {
       const float lp = a.logp[i], lo = a.logp_lo[i], rf = a.ref[i];
-      if (a.y[i] >= 0) s += ((double)lp - (double)rf) + (double)lo;
+      s += a.y[i] >= 0 ? ((double)lp - (double)rf) + (double)lo : (double)lp;      // (an ignored row's is 0, or NaN after a failure)
     }
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     R[c] = s;

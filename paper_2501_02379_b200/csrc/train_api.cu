@@ -242,6 +242,8 @@ tgrad_status launch_forward(int kind, const tgrad_logits* in, const TokenArgs& a
 
 // The one-pass policy kernel: shared memory of an SM for the rings of its blocks, 16 arithmetic warps for all of them at most.
 constexpr size_t kRingBytes = 224 * 1024;
+constexpr int kNoCopyLimit = 0x7fffffff;
+std::atomic<int> g_copy_limit{kNoCopyLimit};
 // Dynamic shared memory beyond the default, once per kernel and device.
 template <typename F>
 tgrad_status allow_shared(F kern, size_t bytes, std::atomic<uint64_t>& done) {
@@ -286,6 +288,7 @@ RowGeom row_geom(const tgrad_logits* in, float k, bool stay, int blocks, int64_t
   const int64_t per = (int64_t)g.W * 32 * RW_NV;
   g.K = (int)((G + per - 1) / per); g.last = (int)((g.K - 1) * per);
   g.N = (int)(places > RW_MAX_PLACES ? RW_MAX_PLACES : places);
+  g.copies = g_copy_limit.load(std::memory_order_relaxed);
   g.reach = 200.f / k; g.slack = 40.f / k; g.lowest = token_kind(in->dtype) == LS_F16 ? -65000.f : -1e38f;
   // units of about 64 KB of logits, at most a warp's width of rows, and several for every block
   int64_t unit = (64 << 10) / bytes;
@@ -361,6 +364,11 @@ size_t preference_bytes(int64_t rows, int64_t pairs) { return align_up((size_t)r
 }  // namespace
 
 extern "C" {
+
+tgrad_status tgrad_set_copy_limit(int32_t copies) {
+  g_copy_limit.store(copies < 0 ? kNoCopyLimit : copies, std::memory_order_relaxed);
+  return TGRAD_OK;
+}
 
 tgrad_status tgrad_grad_norm_bytes(int32_t n, size_t* workspace_bytes) {
   if (n < 0 || !workspace_bytes) return TGRAD_ERR_INVALID_ARG;

@@ -169,19 +169,6 @@ def test_rows_of_weight_zero_add_nothing(V, dtype, ent, forward_only):
 
 
 @pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
-def test_an_advantage_of_zero_leaves_no_policy_term(dtype, V):
-    """However far the policy has moved: a ratio that overflows times an advantage of zero is zero."""
-    z, y = make_rows(dtype, 4, V, 0, 6)
-    adv, w, old = torch.tensor([0.0, 0.0, 1.0, -1.0], device="cuda"), torch.ones(4, device="cuda") / 4, B.token_logprob(z, y)[0]
-    want = B.policy_loss(z, y, old, adv, w)
-    moved = old.clone()
-    moved[0], moved[1] = -200.0, -math.inf
-    got = B.policy_loss(z, y, moved, adv, w)
-    assert torch.equal(got.stats, want.stats) and torch.equal(got.dlogits, want.dlogits) and bool((got.dlogits[:2] == 0).all())
-    assert torch.equal(B.policy_loss(z, y, moved, adv, w, forward_only=True).stats, B.policy_loss(z, y, old, adv, w, forward_only=True).stats)
-
-
-@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
 def test_policy_loss_with_an_infinite_kl(V, dtype):
     """The reference forbids a token (-inf), or gives a token much that the policy forbids or almost does: the KL term is
     infinite, not NaN, and with a coefficient of zero, where it is only looked at, loss and gradient do not know of it."""
@@ -209,6 +196,19 @@ def test_policy_loss_with_an_infinite_kl(V, dtype):
 
 
 @pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
+def test_an_advantage_of_zero_leaves_no_policy_term(dtype, V):
+    """However far the policy has moved: a ratio that overflows times an advantage of zero is zero."""
+    z, y = make_rows(dtype, 4, V, 0, 6)
+    adv, w, old = torch.tensor([0.0, 0.0, 1.0, -1.0], device="cuda"), torch.ones(4, device="cuda") / 4, B.token_logprob(z, y)[0]
+    want = B.policy_loss(z, y, old, adv, w)
+    moved = old.clone()
+    moved[0], moved[1] = -200.0, -math.inf
+    got = B.policy_loss(z, y, moved, adv, w)
+    assert torch.equal(got.stats, want.stats) and torch.equal(got.dlogits, want.dlogits) and bool((got.dlogits[:2] == 0).all())
+    assert torch.equal(B.policy_loss(z, y, moved, adv, w, forward_only=True).stats, B.policy_loss(z, y, old, adv, w, forward_only=True).stats)
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
 def test_pairs_with_a_forbidden_token(V, dtype):
     """An answer with a token of probability zero has a reward of -inf.  As the rejected one it leaves a loss of zero without
     smoothing and an infinite one with it, as the chosen one it is the other way round for a smoothing of one; both: NaN."""
@@ -230,5 +230,53 @@ def test_pairs_with_a_forbidden_token(V, dtype):
     assert r.loss == 0 and bool((r.dlogits == 0).all())
     z[5, 2] = -math.inf                    # now the third answer's too
     assert math.isnan(B.preference_loss(z, y, st(2, 4, 6), ref).loss)
+
+
+# ------------------------------------------------------------------------------------------------ waits that run out
+@pytest.fixture
+def copy_limit():
+    yield B.set_copy_limit
+    B.set_copy_limit()
+
+
+def every_result(z, y):
+    """{name: tensor with one row per row of logits} of all calls whose kernels wait, and the two losses."""
+    rows = len(y)
+    one, starts = torch.ones(rows, device="cuda"), torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    logp, lse, H = B.token_logprob(z, y)
+    p = B.policy_loss(z, y, one * -9, one, one / rows, entropy_coef=0.01)
+    s = B.preference_loss(z, y, starts, one * -9, 0.01)
+    d = B.token_logprob_backward(z, y, one * 9, one)
+    out = {"logp": logp, "lse": lse, "H": H, "policy logp": p.logp, "policy H": p.entropy, "policy gradient": p.dlogits, "pairs logp": s.logp,
+           "gradient": d}
+    return {k: v if v.dim() == 2 else v[:, None] for k, v in out.items()}, torch.stack((p.stats[0], s.loss)), s.dlogits
+
+
+@pytest.mark.parametrize("dtype,rows,V,copies", [
+    ("bf16", 5, 40003, 0), ("bf16", 5, 40003, 1), ("f32", 500, 9001, 0), ("f32", 500, 9001, 1), ("bf16", 1250, 20011, 0), ("bf16", 1250, 20011, 2),
+    ("f16", 200, 140001, 0), ("f16", 200, 140001, 2), ("f16", 200, 140001, 6), ("f16", 200, 140001, 10),      # sums, first and second reading
+])
+def test_waits_that_run_out_are_reported(copy_limit, dtype, rows, V, copies):
+    """The copies stop before the first row or inside one.  The calls end, each row of a result is what it should be or NaN
+    throughout, a loss is NaN where one of its rows is, and the next calls are as before."""
+    z, y = make_rows(dtype, rows, V, 0, 4)
+    y[::3] = -1
+    want, losses, grad = every_result(z, y)
+    assert all(bool(torch.isfinite(x).all()) for x in want.values())
+    copy_limit(copies)
+    got, lost, _ = every_result(z, y)
+    copy_limit(-1)
+    ring_forward = rows >= 8 * torch.cuda.get_device_properties(0).multi_processor_count      # fewer: clusters, without such waits
+    for k, v in got.items():
+        gone = v.isnan().all(1)
+        assert torch.equal(torch.where(gone[:, None], want[k], v), want[k]), k
+        if ring_forward or "policy" in k or "gradient" in k:
+            assert bool(gone.any()) and (copies > 0 or bool(gone.all())), k
+        else:
+            assert not bool(gone.any()), k
+    bad = torch.stack([got[k].isnan().any() for k in ("policy logp", "pairs logp")])      # also of an ignored row of an unfinished unit
+    assert torch.equal(lost.isnan(), bad) and torch.equal(torch.where(bad, losses, lost), losses)
+    again, l2, g2 = every_result(z, y)
+    assert all(torch.equal(again[k], want[k]) for k in want) and torch.equal(l2, losses) and torch.equal(g2, grad)
 
 
