@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import weakref
 from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -519,17 +520,23 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
     """One AdamW step in place on a list of dense tensors (fp32, fp16, bfloat16 or complex64 weights; gradients of the
     same dtype; fp32 moments).  `step` counts from 1.  `grad_scale`: device scalar that multiplies the gradients.
     `masters`: fp32 weights of 16-bit ones, which are then what is updated.  For complex weights the second moment is
-    real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once."""
-    lists = (_as_list(params), _as_list(grads), _as_list(exp_avgs), _as_list(exp_avg_sqs), _as_list(masters) if masters is not None else None)
+    real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once; the
+    first of them keeps that layout and none of the others, and nothing is kept of a call on plain sequences."""
+    given = (params, grads, exp_avgs, exp_avg_sqs, masters)
+    lists = tuple(_as_list(x) if x is not None else None for x in given)
     params = lists[0]
     kept = params._adamw
-    if kept is None or any(a is not b for a, b in zip(kept[0], lists)):
-        kept = params._adamw = (lists, _adamw_array(*lists))
+    if kept is not None and all(r is None if b is None else r is not None and r() is b for r, b in zip(kept[0], lists[1:])):
+        array = kept[1]
+    else:
+        array = _adamw_array(*lists)
+        if all(a is b for a, b in zip(given, lists)):
+            params._adamw = (tuple(None if x is None else weakref.ref(x) for x in lists[1:]), array)
     index = params.device_index()
     if _elsewhere(index, stream):
         return _there(index, stream, adamw_step, *lists[:4], step, lr, beta1, beta2, eps, weight_decay, grad_scale, lists[4])
     cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale) or 0)
-    _check(lib().tgrad_adamw_step(C.addressof(kept[1]), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
+    _check(lib().tgrad_adamw_step(C.addressof(array), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
 
 
 def _logits(logits, targets, temperature):

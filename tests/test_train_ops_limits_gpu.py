@@ -280,3 +280,32 @@ def test_waits_that_run_out_are_reported(copy_limit, dtype, rows, V, copies):
     assert all(torch.equal(again[k], want[k]) for k in want) and torch.equal(l2, losses) and torch.equal(g2, grad)
 
 
+# ------------------------------------------------------------------------------------------------ lists and tensors of the caller
+def test_adamw_lets_go_of_plain_sequences():
+    """Nothing of a call on plain sequences is kept, without the cycle collector's help; TensorLists keep their own tensors only."""
+    gc.collect()
+    gc.disable()
+    try:
+        w, m, v = ([torch.zeros(5, device="cuda")] for _ in range(3))
+        dead = []
+        for kept in (False, True):
+            lists = [B.TensorList(x) for x in (w, m, v)] if kept else [w, m, v]
+            for step in (1, 2, 3):
+                g = torch.ones(5, device="cuda")
+                dead.append(weakref.ref(g))
+                B.adamw_step(lists[0], [g], lists[1], lists[2], step=step, lr=0.1)
+                del g
+        full = lists[:1] + [B.TensorList([torch.ones(5, device="cuda")])] + lists[1:]
+        B.adamw_step(*full, step=4, lr=0.1)
+        halves = [B.TensorList([torch.ones(5, device="cuda", dtype=torch.bfloat16)]) for _ in range(2)]
+        master = B.TensorList([torch.ones(5, device="cuda")])
+        B.adamw_step(*halves, *lists[1:], step=1, lr=0.1, masters=master)
+        del master                                                          # the same lists without masters are another call
+        before = halves[0].tensors[0].clone()
+        B.adamw_step(*halves, *lists[1:], step=2, lr=0.1)
+        assert not torch.equal(halves[0].tensors[0], before)
+        dead += [weakref.ref(x) for x in full]
+        del lists, full, halves
+        assert [d() is None for d in dead] == [True] * 10
+    finally:
+        gc.enable()
