@@ -392,6 +392,13 @@ def _dense(t) -> bool:
     return True
 
 
+def _same_places(a, b) -> bool:
+    """Entries of the same index lie at the same place: equal shapes, and equal strides where a dimension has more than one
+    entry."""
+    return a.shape == b.shape and (a.stride() == b.stride() or a.numel() == 0 or
+                                   all(s == t for s, t, n in zip(a.stride(), b.stride(), a.shape) if n > 1))
+
+
 def _elsewhere(index, stream) -> bool:
     """Whether a call has to change the current device or stream first."""
     return stream is not None or index != _torch()[0]._C._cuda_getDevice()
@@ -505,7 +512,7 @@ def _adamw_array(params, grads, exp_avgs, exp_avg_sqs, masters):
         if w is not None and (w.dtype != torch.float32 or p.dtype not in (torch.float16, torch.bfloat16)):
             raise ValueError("master weights are the fp32 weights of 16-bit ones")
         for x in (g, m, v) + ((w,) if w is not None else ()):
-            if x.shape != p.shape or x.stride() != p.stride():
+            if not _same_places(x, p):
                 raise ValueError("weight, gradient and moments have the same shape and strides")
     for i in range(len(params)):
         a, p = array[i], params.tensors[i]

@@ -309,3 +309,14 @@ def test_adamw_lets_go_of_plain_sequences():
         assert [d() is None for d in dead] == [True] * 10
     finally:
         gc.enable()
+
+
+def test_adamw_takes_any_strides_of_dimensions_of_one():
+    p = torch.randn(7, 1, 5, device="cuda")
+    g = torch.randn(7, 5, device="cuda")
+    other = g.as_strided((7, 1, 5), (5, 35, 1))                             # the same places in memory
+    m, v = torch.zeros(7, 1, 5, device="cuda").as_strided((7, 1, 5), (5, 3, 1)), torch.zeros_like(p)
+    q, mq, vq = p.clone(), torch.zeros_like(p), torch.zeros_like(p)
+    B.adamw_step([p], [other], [m], [v], step=1, lr=0.1)
+    B.adamw_step([q], [g.view(7, 1, 5)], [mq], [vq], step=1, lr=0.1)
+    assert torch.equal(p, q) and torch.equal(m, mq) and torch.equal(v, vq)
