@@ -440,11 +440,14 @@ def _workspace(entry, *args) -> int:
 
 
 class TensorList:
-    """A list of CUDA tensors as the list calls take it, laid out once for tensors that stay where they are (it keeps
-    them alive).  Every call that takes one also takes a plain sequence of tensors."""
+    """A list of CUDA tensors as the list calls take it, laid out once for tensors that stay where they are.  It keeps the
+    tensors and the memory that they have when it is made, and the calls work on that memory: after anything that gives a
+    tensor other memory, another shape or another type (module.to(), .half(), p.data = .., resize_(), a gradient that is a
+    new tensor after zero_grad(set_to_none=True)) make a new list.  Every call that takes one also takes a plain sequence
+    of tensors, which is laid out anew each time."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
+        self.tensors = tuple(tensors)
         for t in self.tensors:
             if not t.is_cuda or t.device != self.tensors[0].device:
                 raise ValueError("the tensors of a list live on one CUDA device")
@@ -457,6 +460,7 @@ class TensorList:
         for a, t in zip(self.array, self.tensors):
             a.data, a.numel, a.dtype = t.data_ptr(), t.numel(), _dtype_of(t)
         self.address = C.addressof(self.array)
+        self._memory = [t.untyped_storage() for t in self.tensors]      # also after p.data = ..: nobody else is given it meanwhile
         self.floats = 64 + (2 + n + 63) // 64 * 64 + _workspace("tgrad_grad_norm_bytes", n) // 4      # results, then the workspace
         self._adamw = None
 
@@ -497,28 +501,27 @@ def clip_grads(grads, max_norm: float, stream=None):
 
 
 def _adamw_array(params, grads, exp_avgs, exp_avg_sqs, masters):
-    import torch
     lists = [params, grads, exp_avgs, exp_avg_sqs] + ([masters] if masters is not None else [])
     if len({len(x) for x in lists}) != 1:
         raise ValueError("the lists differ in length")
     if any(x.device_index() != params.device_index() for x in lists):
         raise ValueError("the lists live on one device")
+    # types, lengths and addresses are those that the lists keep (a tensor may have got other memory since), the order of the
+    # entries is that of the tensors
     array = (TgradAdamwTensor * max(len(params), 1))()
-    for i, a in enumerate(array[:len(params)]):
-        p, g, m, v = (x.tensors[i] for x in (params, grads, exp_avgs, exp_avg_sqs))
-        w = masters.tensors[i] if masters is not None else None
-        if g.dtype != p.dtype or v.dtype != torch.float32 or m.dtype != (torch.complex64 if p.is_complex() else torch.float32):
-            raise ValueError("gradients have the weights' dtype, moments are fp32 (the first one complex64 for complex weights)")
-        if w is not None and (w.dtype != torch.float32 or p.dtype not in (torch.float16, torch.bfloat16)):
-            raise ValueError("master weights are the fp32 weights of 16-bit ones")
-        for x in (g, m, v) + ((w,) if w is not None else ()):
-            if not _same_places(x, p):
-                raise ValueError("weight, gradient and moments have the same shape and strides")
     for i in range(len(params)):
-        a, p = array[i], params.tensors[i]
-        a.weight, a.grad, a.exp_avg, a.exp_avg_sq = (x.tensors[i].data_ptr() for x in (params, grads, exp_avgs, exp_avg_sqs))
-        a.master = masters.tensors[i].data_ptr() if masters is not None else None
-        a.numel, a.dtype = p.numel(), _dtype_of(p)
+        a, entries = array[i], [x.array[i] for x in lists]
+        p, g, m, v = entries[:4]
+        if g.dtype != p.dtype or v.dtype != R32 or m.dtype != (C64 if p.dtype == C64 else R32):
+            raise ValueError("gradients have the weights' dtype, moments are fp32 (the first one complex64 for complex weights)")
+        if masters is not None and (entries[4].dtype != R32 or p.dtype not in (R16H, R16B)):
+            raise ValueError("master weights are the fp32 weights of 16-bit ones")
+        for x, e in zip(lists[1:], entries[1:]):
+            if e.numel != p.numel or not _same_places(x.tensors[i], params.tensors[i]):
+                raise ValueError("weight, gradient and moments have the same shape and strides")
+        a.weight, a.grad, a.exp_avg, a.exp_avg_sq = p.data, g.data, m.data, v.data
+        a.master = entries[4].data if masters is not None else None
+        a.numel, a.dtype = p.numel, p.dtype
     return array
 
 

@@ -320,3 +320,28 @@ def test_adamw_takes_any_strides_of_dimensions_of_one():
     B.adamw_step([p], [other], [m], [v], step=1, lr=0.1)
     B.adamw_step([q], [g.view(7, 1, 5)], [mq], [vq], step=1, lr=0.1)
     assert torch.equal(p, q) and torch.equal(m, mq) and torch.equal(v, vq)
+
+
+def test_a_list_keeps_its_memory():
+    """What a list has laid out is its tensors' memory: a parameter that is given other memory (module.to(), p.data = ..) leaves
+    the old one with the list, so that no call writes to memory that has become somebody else's."""
+    n = 5 << 20
+    p = torch.nn.Parameter(torch.ones(n, device="cuda"))
+    g, m, v = (torch.full((n,), x, device="cuda") for x in (1.0, 0.0, 0.0))
+    lists = [B.TensorList([x]) for x in (p, g, m, v)]
+    B.adamw_step(*lists, step=1, lr=0.5)
+    where, before = p.data_ptr(), torch.cuda.memory_allocated()
+    p.data = torch.empty(0, device="cuda")
+    assert torch.cuda.memory_allocated() == before
+    others = [torch.full((n,), 7.0, device="cuda") for _ in range(4)]
+    assert where not in [x.data_ptr() for x in others]
+    B.adamw_step(*lists, step=2, lr=0.5)
+    B.clip_grads(lists[0], 1e-3)
+    assert all(bool((x == 7).all()) for x in others)
+    late = [B.TensorList([x]) for x in (g, g, m, v)]
+    g.data = torch.empty(0, device="cuda")
+    with pytest.raises(ValueError):                                         # laid out for the step after it has moved
+        B.adamw_step(*late, step=1, lr=0.5)
+    del lists, late
+    gc.collect()
+    assert torch.cuda.memory_allocated() == before + (2 * n << 2)           # the old weights and gradients are free, the others are four
