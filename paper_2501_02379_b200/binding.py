@@ -257,6 +257,8 @@ class TgradState:
         clipping coefficient grad_norm(...)[1:2]); costs no pass over the gradient."""
         _check(lib().tgrad_step_scaled(self.handle, weight.data_ptr(), grad.data_ptr(), _scalar_ptr(scale), _stream_ptr(stream)),
                "tgrad_step_scaled")
+        if stream is not None and scale is not None:
+            scale.record_stream(_as_stream(scale.get_device(), stream))
 
     def refresh_subspace(self, grad, stream=None):
         _check(lib().tgrad_refresh_subspace(self.handle, grad.data_ptr(), _stream_ptr(stream)),
@@ -335,6 +337,8 @@ def step_batched(states: Sequence[TgradState], weights, grads, stream=None, scal
     gs = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
     if scale is not None:
         _check(lib().tgrad_step_batched_scaled(hs, ws, gs, n, _scalar_ptr(scale), _stream_ptr(stream)), "tgrad_step_batched_scaled")
+        if stream is not None:
+            scale.record_stream(_as_stream(scale.get_device(), stream))
         return
     _check(lib().tgrad_step_batched(hs, ws, gs, n, _stream_ptr(stream)), "tgrad_step_batched")
 
@@ -360,7 +364,8 @@ def select_topk_noalloc(grad, numel: int, k: int, omega_out, values_out, half_st
 # --- around the step: gradient norm and clipping, AdamW, losses on logits ------------------------------------------
 #
 # Everything below runs on the current stream of the tensors' device, or on `stream` (a torch stream or its address).
-# Results and workspaces that a call allocates belong to that stream.
+# Results and workspaces that a call allocates belong to that stream.  As with torch's own operations the caller sees to
+# the order of the streams: inputs have to be ready on the call's stream, and results are used on it or after it.
 
 _torch_types = None       # torch, {dtype: tgrad_dtype}, torch.float32
 
@@ -404,16 +409,29 @@ def _elsewhere(index, stream) -> bool:
     return stream is not None or index != _torch()[0]._C._cuda_getDevice()
 
 
+def _as_stream(index, stream):
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return _torch()[0].cuda.ExternalStream(int(stream), device=index)
+
+
 def _there(index, stream, call, *args, **kw):
-    """call(...) with the device `index` and the stream current."""
+    """call(...) with the device `index` and the stream current.  The tensors among the arguments are marked as used on the
+    stream, so that what the caller lets go of is not given to somebody else before the call has run."""
     torch = _torch()[0]
     with torch.cuda.device(index):
         if stream is None:
             return call(*args, **kw)
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=index)
+        stream = _as_stream(index, stream)
+        if stream.device_index != index:
+            raise ValueError("the stream belongs to another device than the tensors")
         with torch.cuda.stream(stream):
-            return call(*args, **kw)
+            result = call(*args, **kw)
+        for x in args:
+            for t in x.tensors if isinstance(x, TensorList) else (x,):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+        return result
 
 
 def _raw_stream(index) -> int:
@@ -532,19 +550,20 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
     `masters`: fp32 weights of 16-bit ones, which are then what is updated.  For complex weights the second moment is
     real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once; the
     first of them keeps that layout and none of the others, and nothing is kept of a call on plain sequences."""
-    given = (params, grads, exp_avgs, exp_avg_sqs, masters)
-    lists = tuple(_as_list(x) if x is not None else None for x in given)
-    params = lists[0]
-    kept = params._adamw
-    if kept is not None and all(r is None if b is None else r is not None and r() is b for r, b in zip(kept[0], lists[1:])):
-        array = kept[1]
-    else:
-        array = _adamw_array(*lists)
+    kept = getattr(params, "_adamw", None)      # (references to the other lists, None: no masters, and the layout)
+    if kept is None or kept[0]() is not grads or kept[1]() is not exp_avgs or kept[2]() is not exp_avg_sqs or \
+            (masters is not None if kept[3] is None else masters is None or kept[3]() is not masters):
+        given = (params, grads, exp_avgs, exp_avg_sqs, masters)
+        lists = [_as_list(x) if x is not None else None for x in given]
+        array, params = _adamw_array(*lists), lists[0]
         if all(a is b for a, b in zip(given, lists)):
-            params._adamw = (tuple(None if x is None else weakref.ref(x) for x in lists[1:]), array)
+            params._adamw = tuple(None if x is None else weakref.ref(x) for x in lists[1:]) + (array,)
+        grads, exp_avgs, exp_avg_sqs, masters = lists[1:]
+    else:
+        array = kept[4]
     index = params.device_index()
     if _elsewhere(index, stream):
-        return _there(index, stream, adamw_step, *lists[:4], step, lr, beta1, beta2, eps, weight_decay, grad_scale, lists[4])
+        return _there(index, stream, adamw_step, params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1, beta2, eps, weight_decay, grad_scale, masters)
     cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale) or 0)
     _check(lib().tgrad_adamw_step(C.addressof(array), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
 

@@ -14,6 +14,8 @@ import torch
 
 from oracle import train_oracle as orc
 from paper_2501_02379_b200 import binding as B
+from paper_2501_02379_b200 import synth
+from tests.parity import to_device
 from tests.test_train_ops_gpu import DT, HALF_ULP, TINY, U, f64, gen, make_rows, sum_err, within
 
 pytestmark = pytest.mark.gpu
@@ -345,3 +347,72 @@ def test_a_list_keeps_its_memory():
     del lists, late
     gc.collect()
     assert torch.cuda.memory_allocated() == before + (2 * n << 2)           # the old weights and gradients are free, the others are four
+
+
+def test_inputs_outlive_a_call_on_another_stream():
+    """Tensors that the caller lets go of after a call on another stream are not given to somebody else before it has run."""
+    z, y = make_rows("bf16", 64, 10007, 0, 2)
+    one = torch.ones(64, device="cuda")
+    starts = torch.tensor([0, 20, 64], dtype=torch.int32, device="cuda")
+    weights, moments = torch.ones(64, device="cuda"), [torch.zeros(64, device="cuda") for _ in range(2)]
+    side = torch.cuda.Stream()
+    made = []
+
+    def fresh(value, n=64):                                                 # a tensor that nobody keeps
+        t = torch.full((n,), float(value), device="cuda")
+        made.append(t.data_ptr())
+        return t
+
+    calls = {
+        "policy": lambda s: B.policy_loss(z, y, fresh(-8), fresh(1), fresh(0.5), ref_logp=fresh(-9), kl_coef=0.1, stream=s).stats,
+        "pairs": lambda s: B.preference_loss(z, y, starts.clone(), fresh(-8), stream=s).rewards,
+        "logprob": lambda s: B.token_logprob(z.clone(), y.clone(), stream=s)[0],
+        "gradient": lambda s: B.token_logprob_backward(z, y, fresh(10), fresh(2), stream=s),
+        "norm": lambda s: B.grad_norm([fresh(3)], 1.0, stream=s),
+        "list": lambda s: B.grad_norm(B.TensorList([fresh(3)]), 1.0, stream=s),
+        "adamw": lambda s: B.adamw_step([weights], [fresh(2)], *([m] for m in moments), step=1, lr=0.1, grad_scale=fresh(0.5, 1), stream=s) or weights,
+    }
+    for name, call in calls.items():
+        want = call(None).clone()
+        if name == "adamw":
+            for t, x in zip([weights] + moments, (1, 0, 0)):
+                t.fill_(x)
+        torch.cuda.synchronize()
+        made.clear()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(int(4e8))
+        # (the inputs are filled on the default stream, long before the other one is through with its sleep)
+        got = call(side)
+        others = [torch.full((n,), 99.0, device="cuda") for n in (64, 1) for _ in range(12)]
+        others += [torch.full_like(z, 99.0), torch.full_like(y, 99), torch.full_like(starts, 99)]
+        assert not side.query(), "the test has to come before the call has run"
+        assert not set(made) & {x.data_ptr() for x in others}, name
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), name
+
+
+def test_a_scale_outlives_a_step_on_another_stream():
+    wl = synth.WORKLOADS["small4"]
+    src = synth.GradientSource(wl)
+    side, results = torch.cuda.Stream(), []
+    for batched in (False, True):
+        for stream in (None, side):
+            st = B.TgradState(B.make_config(wl.shape, wl.ranks, wl.k, wl.T))
+            w, g = to_device(src.weight(), False), to_device(src.gradient(0), False)
+            scale = torch.full((1,), 0.5, device="cuda")
+            where = scale.data_ptr()
+            torch.cuda.synchronize()
+            if stream is not None:
+                with torch.cuda.stream(side):
+                    torch.cuda._sleep(int(4e8))
+            if batched:
+                B.step_batched([st], [w], [g], stream=stream, scale=scale)
+            else:
+                st.step_scaled(w, g, scale, stream=stream)
+            del scale
+            if stream is not None:
+                others = [torch.full((1,), 99.0, device="cuda") for _ in range(12)]
+                assert not side.query() and where not in [x.data_ptr() for x in others]
+            torch.cuda.synchronize()
+            results.append((w.clone(), st.export(B.WHAT_M_L)))
+    assert all(torch.equal(a, results[0][0]) and np.array_equal(b, results[0][1]) for a, b in results)
