@@ -210,11 +210,11 @@ def _stream_ptr(stream) -> Optional[int]:
     return int(stream)
 
 
-def _scalar_ptr(scale) -> Optional[int]:
+def _scalar_ptr(scale, index) -> Optional[int]:
     if scale is None:
         return None
-    if scale.dtype is not _torch()[2] or scale.numel() != 1 or not scale.is_cuda:
-        raise ValueError("a scale is an fp32 CUDA tensor of one entry")
+    if scale.dtype is not _torch()[2] or scale.numel() != 1 or not scale.is_cuda or scale.get_device() != index:
+        raise ValueError("a scale is an fp32 CUDA tensor of one entry on the gradients' device")
     return scale.data_ptr()
 
 
@@ -255,7 +255,7 @@ class TgradState:
     def step_scaled(self, weight, grad, scale, stream=None):
         """step() with the gradient multiplied by the device scalar `scale` (an fp32 tensor of one entry, such as the
         clipping coefficient grad_norm(...)[1:2]); costs no pass over the gradient."""
-        _check(lib().tgrad_step_scaled(self.handle, weight.data_ptr(), grad.data_ptr(), _scalar_ptr(scale), _stream_ptr(stream)),
+        _check(lib().tgrad_step_scaled(self.handle, weight.data_ptr(), grad.data_ptr(), _scalar_ptr(scale, grad.get_device()), _stream_ptr(stream)),
                "tgrad_step_scaled")
         if stream is not None and scale is not None:
             scale.record_stream(_as_stream(scale.get_device(), stream))
@@ -336,7 +336,8 @@ def step_batched(states: Sequence[TgradState], weights, grads, stream=None, scal
     ws = (C.c_void_p * n)(*[w.data_ptr() for w in weights])
     gs = (C.c_void_p * n)(*[g.data_ptr() for g in grads])
     if scale is not None:
-        _check(lib().tgrad_step_batched_scaled(hs, ws, gs, n, _scalar_ptr(scale), _stream_ptr(stream)), "tgrad_step_batched_scaled")
+        scale_p = _scalar_ptr(scale, grads[0].get_device() if n else scale.get_device())
+        _check(lib().tgrad_step_batched_scaled(hs, ws, gs, n, scale_p, _stream_ptr(stream)), "tgrad_step_batched_scaled")
         if stream is not None:
             scale.record_stream(_as_stream(scale.get_device(), stream))
         return
@@ -564,7 +565,7 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
     index = params.device_index()
     if _elsewhere(index, stream):
         return _there(index, stream, adamw_step, params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1, beta2, eps, weight_decay, grad_scale, masters)
-    cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale) or 0)
+    cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale, index) or 0)
     _check(lib().tgrad_adamw_step(C.addressof(array), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
 
 
