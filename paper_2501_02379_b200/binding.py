@@ -369,12 +369,14 @@ def select_topk_noalloc(grad, numel: int, k: int, omega_out, values_out, half_st
 # the order of the streams: inputs have to be ready on the call's stream, and results are used on it or after it.
 
 _torch_types = None       # torch, {dtype: tgrad_dtype}, torch.float32
+_count_write = None       # tells autograd that tensors were written to
 
 
 def _torch():
-    global _torch_types
+    global _torch_types, _count_write
     if _torch_types is None:
         import torch
+        _count_write = torch.autograd.graph.increment_version
         _torch_types = (torch, {torch.float32: R32, torch.float16: R16H, torch.bfloat16: R16B, torch.complex64: C64}, torch.float32)
     return _torch_types
 
@@ -403,6 +405,12 @@ def _same_places(a, b) -> bool:
     entry."""
     return a.shape == b.shape and (a.stride() == b.stride() or a.numel() == 0 or
                                    all(s == t for s, t, n in zip(a.stride(), b.stride(), a.shape) if n > 1))
+
+
+def _written(t) -> None:
+    """autograd's check for operands that were overwritten is to see what a call has written to one of the caller's tensors."""
+    if not t.is_inference():
+        _count_write(t)
 
 
 def _elsewhere(index, stream) -> bool:
@@ -481,7 +489,14 @@ class TensorList:
         self.address = C.addressof(self.array)
         self._memory = [t.untyped_storage() for t in self.tensors]      # also after p.data = ..: nobody else is given it meanwhile
         self.floats = 64 + (2 + n + 63) // 64 * 64 + _workspace("tgrad_grad_norm_bytes", n) // 4      # results, then the workspace
-        self._adamw = None
+        self._adamw = self._counters = None
+
+    def written(self) -> None:
+        """As _written, for all of the list: views count on what they are views of."""
+        if self._counters is None:
+            owners = [t if t._base is None else t._base for t in self.tensors]
+            self._counters = tuple({id(t): t for t in owners if not t.is_inference()}.values())
+        _count_write(self._counters)
 
     def __len__(self):
         return len(self.tensors)
@@ -504,6 +519,8 @@ def _norm_call(name, grads, max_norm, stream):
     buf = torch.empty(grads.floats, dtype=f32, device=index)
     base, head = buf.data_ptr(), (2 + n + 63) // 64 * 64
     _check(getattr(lib(), name)(grads.address, n, max_norm, base, base + 4 * head, 4 * (grads.floats - head), _raw_stream(index)), name)
+    if name == "tgrad_clip_grads":
+        grads.written()
     return buf[:2 + n]
 
 
@@ -515,7 +532,7 @@ def grad_norm(grads, max_norm: float = float("inf"), stream=None):
 
 
 def clip_grads(grads, max_norm: float, stream=None):
-    """grad_norm, and every gradient multiplied by the coefficient in place."""
+    """grad_norm, and every gradient multiplied by the coefficient in place (autograd is told)."""
     return _norm_call("tgrad_clip_grads", grads, max_norm, stream)
 
 
@@ -549,8 +566,9 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
     """One AdamW step in place on a list of dense tensors (fp32, fp16, bfloat16 or complex64 weights; gradients of the
     same dtype; fp32 moments).  `step` counts from 1.  `grad_scale`: device scalar that multiplies the gradients.
     `masters`: fp32 weights of 16-bit ones, which are then what is updated.  For complex weights the second moment is
-    real and takes the squared modulus.  TensorLists that are passed again in the same roles are laid out once; the
-    first of them keeps that layout and none of the others, and nothing is kept of a call on plain sequences."""
+    real and takes the squared modulus.  autograd is told that the weights were written to.  TensorLists that are passed
+    again in the same roles are laid out once; the first of them keeps that layout and none of the others, and nothing is
+    kept of a call on plain sequences."""
     kept = getattr(params, "_adamw", None)      # (references to the other lists, None: no masters, and the layout)
     if kept is None or kept[0]() is not grads or kept[1]() is not exp_avgs or kept[2]() is not exp_avg_sqs or \
             (masters is not None if kept[3] is None else masters is None or kept[3]() is not masters):
@@ -567,6 +585,9 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float, beta1
         return _there(index, stream, adamw_step, params, grads, exp_avgs, exp_avg_sqs, step, lr, beta1, beta2, eps, weight_decay, grad_scale, masters)
     cfg = _pack_adamw(lr, beta1, beta2, eps, weight_decay, step, _scalar_ptr(grad_scale, index) or 0)
     _check(lib().tgrad_adamw_step(C.addressof(array), len(params.tensors), cfg, _raw_stream(index)), "tgrad_adamw_step")
+    params.written()      # (no graph holds moments: they are not counted, 5 us a step for 40 tensors)
+    if masters is not None:
+        masters.written()
 
 
 def _logits(logits, targets, temperature):
@@ -638,6 +659,8 @@ def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_e
     out, stride = _dlogits(logits, rows, vocab, dlogits)
     _check(lib().tgrad_token_logprob_backward(desc, lse_p, e_p, g_p, h_p, out.data_ptr(), stride, _raw_stream(index)),
            "tgrad_token_logprob_backward")
+    if dlogits is not None:
+        _written(dlogits)
     return out
 
 
@@ -685,6 +708,8 @@ def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, c
                         kl_coef, entropy_coef, grad_scale, 0.0, stats, stats + 20, stats + 20 + 4 * rows,
                         grad.data_ptr() if grad is not None else 0, stride)
     _check(lib().tgrad_policy_loss(desc, args, base, ws, _raw_stream(index)), "tgrad_policy_loss")
+    if dlogits is not None and grad is not None:
+        _written(dlogits)
     _, stats, logp, entropy = out.split_with_sizes((ws // 4, 5, rows, rows))
     return PolicyLoss(stats, logp, entropy, grad)
 
@@ -710,5 +735,7 @@ def preference_loss(logits, targets, starts, ref_logp, beta: float = 0.1, label_
     args = _pack_preference(starts.data_ptr(), _row_ptr("ref_logp", ref_logp, rows, index), pairs, beta, label_smoothing, grad_scale, loss,
                             loss + 4 + 4 * rows, loss + 4, grad.data_ptr() if grad is not None else 0, stride)
     _check(lib().tgrad_preference_loss(desc, args, base, ws, _raw_stream(index)), "tgrad_preference_loss")
+    if dlogits is not None and grad is not None:
+        _written(dlogits)
     _, loss, logp, rewards = out.split_with_sizes((ws // 4, 1, rows, 2 * pairs))
     return PreferenceLoss(loss[0], rewards, logp, grad)

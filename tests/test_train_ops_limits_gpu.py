@@ -324,6 +324,39 @@ def test_adamw_takes_any_strides_of_dimensions_of_one():
     assert torch.equal(p, q) and torch.equal(m, mq) and torch.equal(v, vq)
 
 
+def test_results_in_place_count_as_changes():
+    """autograd's own check of operands that were overwritten sees what the calls write."""
+    def bumped(t, call):
+        before = t._version
+        call()
+        return t._version > before
+
+    w, g, m, v = (torch.ones(4, device="cuda") for _ in range(4))
+    half, master = torch.ones(4, device="cuda", dtype=torch.bfloat16), torch.ones(4, device="cuda")
+    step = lambda: B.adamw_step([w], [g], [m], [v], step=1, lr=0.1)  # noqa: E731
+    assert bumped(w, step) and not bumped(g, step)
+    lists = [B.TensorList([x]) for x in (w, g, m, v)]
+    assert bumped(w, lambda: B.adamw_step(*lists, step=1, lr=0.1))
+    with_master = lambda: B.adamw_step([half], [half.clone()], [m], [v], step=1, lr=0.1, masters=[master])  # noqa: E731
+    assert bumped(half, with_master) and bumped(master, with_master)
+    assert bumped(g, lambda: B.clip_grads([g], 0.5)) and not bumped(g, lambda: B.grad_norm([g], 0.5))
+    z, y = make_rows("f32", 4, 10, 0, 0)
+    one, starts = torch.ones(4, device="cuda"), torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    assert bumped(z, lambda: B.policy_loss(z, y, one, one, one, dlogits=z))
+    assert bumped(z, lambda: B.preference_loss(z, y, starts, one, dlogits=z))
+    assert bumped(z, lambda: B.token_logprob_backward(z, y, one, one, dlogits=z))
+    assert not bumped(z, lambda: B.policy_loss(z, y, one, one, one))
+    x = torch.ones(3, device="cuda", requires_grad=True)
+    out = (x * 2).exp()                                                     # its backward needs its result
+    B.clip_grads([out.detach()], 1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+    with torch.inference_mode():
+        t = torch.ones(4, device="cuda")
+    B.clip_grads([t], 0.5)                                                  # has no version: as before
+    within(f64(t), np.full(4, 0.25), 1e-6)
+
+
 def test_a_list_keeps_its_memory():
     """What a list has laid out is its tensors' memory: a parameter that is given other memory (module.to(), p.data = ..) leaves
     the old one with the list, so that no call writes to memory that has become somebody else's."""
