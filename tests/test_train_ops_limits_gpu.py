@@ -449,3 +449,56 @@ def test_a_scale_outlives_a_step_on_another_stream():
             torch.cuda.synchronize()
             results.append((w.clone(), st.export(B.WHAT_M_L)))
     assert all(torch.equal(a, results[0][0]) and np.array_equal(b, results[0][1]) for a, b in results)
+
+
+@pytest.mark.parametrize("dtype,V,pad", [("bf16", 20011, 0), ("f16", 40000, 0), ("f32", 9001, 3), ("bf16", 3001, 1)])
+def test_pairs_of_thousands_of_rows(dtype, V, pad):
+    """Enough rows for the kernels that hand them out: rewards, loss and gradient against 64 bits.  What a sum over an answer's
+    tokens is off by is the sum of the tokens' bounds."""
+    lengths = [400, 1, 0, 777, 250, 250, 33, 500]
+    rows = 7 + sum(lengths) + 5                                             # some belong to no answer
+    z, y = make_rows(dtype, rows, V, pad, 12, std=3.0)
+    y[::5] = -3
+    z[5] = math.nan
+    starts = torch.tensor(np.cumsum([7] + lengths), dtype=torch.int32, device="cuda")
+    beta, eps, scale = 0.125, 0.25, 256.0                                   # exact in fp32
+    ref = B.token_logprob(z, y)[0] + torch.randn(rows, generator=gen(2), device="cuda") * 0.1
+    got = B.preference_loss(z, y, starts, ref, beta, eps, temperature=0.9, grad_scale=scale)
+    gap, tol, part = torch.zeros(rows, dtype=torch.float64, device="cuda"), torch.zeros(rows, dtype=torch.float64, device="cuda"), 200
+    for a in range(0, rows, part):
+        c = slice(a, min(rows, a + part))
+        e = Exact(z[c], y[c], 0.9)
+        e.near(got.logp[c], e.logp, e.tl, "logp")
+        gap[c] = torch.where(e.live, e.logp - ref[c].double(), 0.0)
+        tol[c] = torch.where(e.live, e.tl, 0.0)
+    at = starts.tolist()
+    R, tR = (torch.stack([x[i:j].sum() for i, j in zip(at, at[1:])]) * beta for x in (gap, tol))
+    tR = 2 * tR + 2 * U * R.abs() + 1e-30
+    assert bool(((got.rewards.double() - R).abs() <= tR).all())
+    h, th = R[0::2] - R[1::2], tR[0::2] + tR[1::2]
+    loss = ((1 - eps) * torch.nn.functional.softplus(-h) + eps * torch.nn.functional.softplus(h)).mean()
+    assert abs(float(got.loss) - float(loss)) <= float(th.mean()) + 4 * U * float(loss)
+    d = beta * (torch.sigmoid(h) - (1 - eps)) / len(h)
+    g, dg = torch.zeros(rows, dtype=torch.float64, device="cuda"), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    for s in range(len(lengths)):
+        g[at[s]:at[s + 1]] = d[s // 2] * (1 if s % 2 == 0 else -1)
+        dg[at[s]:at[s + 1]] = beta * th[s // 2] / len(h) + 8 * U * d[s // 2].abs()
+    for a in range(0, rows, part):
+        c = slice(a, min(rows, a + part))
+        Exact(z[c], y[c], 0.9).near_grad(got.dlogits[c], g[c], dg[c], dtype, scale / 0.9, "gradient")
+    assert bool((got.dlogits[:7] == 0).all()) and bool((got.dlogits[-5:] == 0).all())
+    fwd = B.preference_loss(z, y, starts, ref, beta, eps, temperature=0.9, forward_only=True)
+    assert torch.equal(fwd.loss, got.loss) and torch.equal(fwd.rewards, got.rewards)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tau,offset", [(1e-2, 0.0), (1e-3, 0.0), (1.0, 3e3), (1.0, -3e3), (1e4, 0.0)])
+@pytest.mark.parametrize("rows,V", [(5, 40003), (1200, 3001), (300, 20011)])
+def test_gradient_from_lse_is_as_exact_as_lse(rows, V, tau, offset, dtype):
+    """token_logprob_backward has nothing but lse, rounded to fp32: what that leaves out is in every probability."""
+    z, y = far_rows(dtype, rows, V, tau, offset)
+    e = Exact(z, y, tau)
+    g = torch.randn(rows, generator=gen(3), device="cuda")
+    d = B.token_logprob_backward(z, y, B.token_logprob(z, y, temperature=tau)[1], g * tau, temperature=tau)
+    rel = e.rel + 2 * 4 * U * e.top.abs()
+    e.near_grad(d, g.double(), torch.zeros_like(e.logp), dtype, 1.0, "gradient", rel)
