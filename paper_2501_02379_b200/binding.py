@@ -646,7 +646,8 @@ def token_logprob(logits, targets, temperature: float = 1.0, stream=None):
 
 def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_entropy=None, temperature: float = 1.0, dlogits=None, stream=None):
     """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits.  `dlogits` may be the
-    logits themselves."""
+    logits themselves.  The probabilities are as exact as lse is in fp32: at low temperatures or for logits far from zero
+    the losses' own gradients are more exact."""
     desc, rows, vocab, index = _logits(logits, targets, temperature)
     if _elsewhere(index, stream):
         return _there(index, stream, token_logprob_backward, logits, targets, lse, grad_logp, entropy, grad_entropy, temperature, dlogits)
@@ -691,7 +692,7 @@ def policy_loss(logits, targets, old_logp, advantages, weights, ref_logp=None, c
     """Clipped policy loss with a KL term and an entropy bonus, and its gradient with respect to the logits in the same
     pass: loss = sum_i weights_i (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(u) - u - 1)
     - entropy_coef H), r = exp(logp - old_logp), u = ref_logp - logp.  The weights carry mask and normalisation (what
-    stands beside a row of weight 0 does not count); rows with a negative target are ignored, their logits too.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
+    stands in or beside a row of weight 0 does not count); rows with a negative target are ignored, their logits too.  dlogits = grad_scale * d loss / d logits, ready for logits.backward(dlogits);
     `dlogits` may be the logits themselves."""
     desc, rows, vocab, index = _logits(logits, targets, temperature)
     if _elsewhere(index, stream):

@@ -170,6 +170,40 @@ def test_rows_of_weight_zero_add_nothing(V, dtype, ent, forward_only):
     assert bool(torch.isfinite(got.stats).all())
 
 
+@pytest.mark.parametrize("ent", [0.0, 0.02])
+@pytest.mark.parametrize("dtype,rows,V", [("bf16", 12, 1003), ("f16", 12, 9001), ("f32", 12, 40003), ("bf16", 1300, 3001), ("bf16", 1300, 20011), ("f16", 12, 270001)])
+def test_rows_without_a_part_in_the_loss_have_a_gradient_of_zero(rows, V, dtype, ent):
+    """Whatever their logits are: rows of weight zero, rows outside every answer, coefficients of zero."""
+    z, y = make_rows(dtype, rows, V, 0, 5)
+    y[1::4] = -1
+    out = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    out[2::5] = True
+    out[:2] = out[-3:] = True
+    zb = z.clone()
+    zb[out] = math.nan
+    zb[2], zb[-2] = math.inf, -math.inf
+    w = torch.where(out, 0.0, torch.rand(rows, generator=gen(1), device="cuda"))
+    logp, lse, H = B.token_logprob(z, y)
+    for logits in (z, zb):
+        for place in (None, logits.clone()):
+            src = logits if place is None else place
+            p = B.policy_loss(src, y, logp - 0.1, torch.ones_like(w), w, ref_logp=logp + 0.1, kl_coef=0.1, entropy_coef=ent, dlogits=place)
+            if logits is z and place is None:
+                want = p
+            assert bool((p.dlogits[out] == 0).all()) and torch.equal(p.dlogits, want.dlogits) and torch.equal(p.stats, want.stats)
+    lb, le, he = B.token_logprob(zb, y)
+    h = w * 2 if ent else None
+    a = B.token_logprob_backward(z, y, lse, w, entropy=H, grad_entropy=h)
+    b = B.token_logprob_backward(zb, y, le, w, entropy=he, grad_entropy=h)
+    assert torch.equal(a, b) and bool((b[out] == 0).all()) and bool((b[~out & (y >= 0)] != 0).any())
+    zb = z.clone()
+    zb[:2] = math.nan
+    zb[-3:] = math.inf
+    starts = torch.tensor([2, rows // 2, rows - 3], dtype=torch.int32, device="cuda")
+    a, b = (B.preference_loss(x, y, starts, logp - 0.1) for x in (z, zb))
+    assert torch.equal(a.dlogits, b.dlogits) and torch.equal(a.loss, b.loss) and bool((b.dlogits[:2] == 0).all()) and bool((b.dlogits[-3:] == 0).all())
+
+
 @pytest.mark.parametrize("dtype,V", [("bf16", 1003), ("f32", 40003)])
 def test_policy_loss_with_an_infinite_kl(V, dtype):
     """The reference forbids a token (-inf), or gives a token much that the policy forbids or almost does: the KL term is
