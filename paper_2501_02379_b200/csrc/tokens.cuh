@@ -33,7 +33,10 @@ struct TokenArgs {
 };
 
 constexpr float TK_LN2 = 0.6931471805599453f;
-constexpr float TK_EX2_LOW = 4.8e-8f;
+// The special-function unit's 2^x comes out low on average: by 5e-8 below x = -2, 4.3e-8 from there to -0.7, 2.2e-8 above
+// (measured on one B200, 2^24 exponents in each range; integers are exact).  EX2_LOW: what that makes of the sums of a warp or a
+// block; EX2_LOW_SPLIT: where every thread has its own reference, so that most of a sum is near it or exact.
+constexpr float TK_EX2_LOW = 4.8e-8f, TK_EX2_LOW_SPLIT = 2e-8f;
 constexpr float TK_LOWEST = -3.402823466e38f;
 
 // ---- packed pairs of fp32 (one instruction per two lanes on this architecture) ----
@@ -120,10 +123,22 @@ struct Row {
 struct Triple { float m, s, t; };
 // A factor of 2^d, d below this, is zero; times sums of up to 2^40 per entry it is still far from the end of the range.
 constexpr float TK_FAR_BELOW = -1e4f;
+// 2^d for d <= 0 without a mean error: the power of two nearest to it, times the first eight terms of exp(t ln 2), |t| <= 1/2
+// (what is left out is below 6e-9).
+__device__ __forceinline__ float exp2_even(float d) {
+  const float i = rintf(d), t = (d - i) * TK_LN2;
+  float p = 1.f / 5040.f;
+  p = fmaf(p, t, 1.f / 720.f); p = fmaf(p, t, 1.f / 120.f); p = fmaf(p, t, 1.f / 24.f);
+  p = fmaf(p, t, 1.f / 6.f); p = fmaf(p, t, 0.5f); p = fmaf(p, t, 1.f);
+  return fmaf(p, t, 1.f) * ex2(i);
+}
 // Moves a triple to a larger maximum.  A part that has seen nothing but -inf has m = lowest, s = t = 0 and stays so.
+// EVEN: where a sum is moved many times, the special-function unit's mean error in each factor would add up (to 5e-8 to 1.1e-7 in
+// the log-probabilities of token_forward_kernel; 2e-8 where it is moved a few times).
+template <bool EVEN = false>
 __device__ __forceinline__ void rebase(Triple& a, float m, float k) {
   const float d = fmaxf((a.m - m) * k, TK_FAR_BELOW);
-  const float f = ex2(d);
+  const float f = EVEN ? exp2_even(d) : ex2(d);
   a.t = f * fmaf(a.s, d, a.t);
   a.s *= f;
   a.m = m;
@@ -170,8 +185,9 @@ __device__ __forceinline__ float warp_max(float x) {
   return r;
 }
 // Combines the triples of the lanes; lanes from `width` on have none (m lowest, s and t 0).
+template <bool EVEN = false>
 __device__ __forceinline__ void warp_combine(Triple& a, float k, int width = 32) {
-  rebase(a, warp_max(a.m), k);
+  rebase<EVEN>(a, warp_max(a.m), k);
   for (int o = 16; o; o >>= 1) {
     if (o >= width) continue;
     a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
@@ -201,7 +217,7 @@ template <int THREADS>
 __device__ __forceinline__ void row_combine(Triple& a, float k, int C, float4* sh) {
   constexpr int W = THREADS / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  warp_combine(a, k);
+  warp_combine<true>(a, k);
   if (C == 1) {
     if (W == 1) return;
     if (lane == 0) sh[warp] = make_float4(a.m, a.s, a.t, 0.f);
@@ -218,23 +234,23 @@ __device__ __forceinline__ void row_combine(Triple& a, float k, int C, float4* s
     const float4 o = sh[i];
     Triple b; b.m = o.x; b.s = o.y; b.t = o.z;
     const float m = fmaxf(a.m, b.m);
-    rebase(a, m, k); rebase(b, m, k);
+    rebase<true>(a, m, k); rebase<true>(b, m, k);
     a.s += b.s; a.t += b.t;
   }
-  warp_combine(a, k);
+  warp_combine<true>(a, k);
 }
 
 // What the sums say about one row.  The exponents were formed with k rounded to fp32, d (1 + k_lo) being the true ones: S is
 // off by k_lo ln2 T to first order, the same way in every row, which the sums over an answer's tokens would show.
-// The same holds for the special-function unit's exponentials, which come out 4.8e-8 low on average (measured over exponents
-// from -13 to -0.7, the same in each part of that range); the largest entry's, 2^0, is exact.
+// The same holds for the special-function unit's mean error, `low`, of all but the largest entry, whose 2^0 is exact.  (Where M is
+// a reference below the maximum, that entry's is not; the correction is then off by less than its own size, 5e-8.)
 // ln S is formed as hi + lo, hi a multiple of a short ln 2, and log p with the part that its rounding to fp32 leaves out: the
 // roundings of two numbers near 10 are more than half of the error of log p, and sums over an answer's tokens use both parts.
 struct RowStat { float M, ls2, lse, logp, logp_lo, H; };
-__device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, const TokenArgs& p) {
+__device__ __forceinline__ RowStat row_stat(const Triple& a, float zy, const TokenArgs& p, float low = TK_EX2_LOW) {
   RowStat r;
   r.M = a.m;
-  const float inv_s = 1.f / a.s, mean = TK_LN2 * (a.t * inv_s), drift = fmaf(p.k_lo, mean, TK_EX2_LOW * (1.f - inv_s));
+  const float inv_s = 1.f / a.s, mean = TK_LN2 * (a.t * inv_s), drift = fmaf(p.k_lo, mean, low * (1.f - inv_s));
   float hi = 0.f, lo;
   if (a.s > 1e-30f && a.s < 1e30f) {
     uint32_t bits = __float_as_uint(a.s);
@@ -1047,12 +1063,12 @@ __global__ void __launch_bounds__(TF_THREADS, 4) token_forward_kernel(const __gr
       v[i] = make_uint4(ni, ni, ni, ni);
       if (g < g1) v[i] = r.load(g);
     }
-    rebase(a, fmaxf(a.m, batch_max<KIND, NV>(v)), p.k);
+    rebase<true>(a, fmaxf(a.m, batch_max<KIND, NV>(v)), p.k);
     accumulate<KIND, NV>(a, v, p.k);
   }
   row_combine<TF_THREADS>(a, p.k, C, sh);
   if (rank != 0 || threadIdx.x != 0) return;
-  const RowStat st = row_stat(a, zy, p);
+  const RowStat st = row_stat(a, zy, p, TK_EX2_LOW_SPLIT);
   store_stat(f, row, st);
   if (POLICY) q.terms[row] = policy_token(st.logp, st.H, q.old_logp[row], q.ref_logp ? q.ref_logp[row] : 0.f, q.ref_logp != nullptr, q.adv[row], q.weight[row], q).terms;
 }

@@ -536,3 +536,21 @@ def test_gradient_from_lse_is_as_exact_as_lse(rows, V, tau, offset, dtype):
     d = B.token_logprob_backward(z, y, B.token_logprob(z, y, temperature=tau)[1], g * tau, temperature=tau)
     rel = e.rel + 2 * 4 * U * e.top.abs()
     e.near_grad(d, g.double(), torch.zeros_like(e.logp), dtype, 1.0, "gradient", rel)
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.8])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,V", [(1100, 2377), (1100, 10579), (600, 34057), (100, 131073), (6000, 2377), (4000, 10579), (2000, 34057)])
+def test_log_probabilities_have_no_bias(rows, V, dtype, tau):
+    """The sum over an answer's tokens shows what every token is off by in the same way.  Roundings to nearest have none, the
+    exponential unit's mean error is corrected where it comes in; what is left on average is to be below half of an fp32
+    rounding of one, plus four standard errors of the mean."""
+    z, y = make_rows(dtype, rows, V, 0, 21)
+    z.scatter_add_(1, y[:, None], (torch.randn(rows, 1, generator=gen(5), device="cuda") * 2 + 7).to(z.dtype))      # a likely token
+    one = torch.ones(rows, device="cuda")
+    got = {"logprob": B.token_logprob(z, y, temperature=tau)[0], "policy": B.policy_loss(z, y, -one, one, one, temperature=tau).logp}
+    want = torch.cat([torch.log_softmax(a.double() / tau, 1).gather(1, b[:, None])[:, 0] for a, b in zip(z.split(200), y.split(200))])
+    for name, x in got.items():
+        err = x.double() - want
+        bias, se = float(err.mean()), float(err.std()) / rows ** 0.5
+        assert abs(bias) < U / 2 + 4 * se, f"{name}: {bias:.2e}, standard error {se:.1e}"
