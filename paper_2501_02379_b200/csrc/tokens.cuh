@@ -306,7 +306,7 @@ template <int KIND, bool ENT>
 __device__ __forceinline__ float grad_target(float zy, const GradCoef& gc, float g) {
   const float l = fmaf(zy - gc.M, gc.k, -gc.ls2);
   const float c = ENT ? fmaf(max_nan(l, -200.f), gc.c1, gc.c0) : gc.c0;
-  return fmaf(ex2(l), c, g);
+  return gc.c0 == 0.f && (!ENT || gc.c1 == 0.f) ? g : fmaf(ex2(l), c, g);      // (NaN times zero is not wanted)
 }
 // entry i of a granule
 template <int KIND>
@@ -501,27 +501,27 @@ __device__ __forceinline__ void add_chunk(WarpSums& a, const uint4 (&v)[RW_NV], 
   a.t2 = APART ? add2(a.t2, t2) : t2;
 }
 
-// What the row's sums give the gradient.  owner: the thread that writes the target's granule, -1 where the target is one of the
-// outer entries, RW_NO_GRADIENT where all coefficients are zero (a weight of zero, a clipped token): the gradient is then zero
-// whatever the logits are.
-constexpr int RW_NO_GRADIENT = -2;
+// What the row's sums give the gradient.  owner: the thread that writes the target's granule, or -1.
 struct RowGrad { float M, nb, ls2, c0, c1, e0, e1, target, zy; int owner, fast; };
-// c0, c1 are those of the loop over the granules, e0, e1 those of single entries (which take the difference first).  16-bit logits, |M k| below 2^20: an exponent is one fma, L = x k + nb, nb being
-// -(M k + log2 S) rounded.  The rounding, up to 2^-5 at that bound, is taken back here: p = 2^(L + off) = 2^off 2^L, in both
-// coefficients.  fp32 logits, whose results are not rounded to fewer bits, and rows further out take the difference first.
+// c0, c1 are those of the loop over the granules, e0, e1 those of single entries (which take the difference first).
+// 16-bit logits, |M k + log2 S| below 2^20: an exponent is one fma, L = x k + nb, nb being -(M k + log2 S) rounded.  The rounding,
+// up to 2^-5 at that bound, is taken back here: p = 2^(L + off) = 2^off 2^L, in both coefficients.  fp32 logits, whose results
+// are not rounded to fewer bits, rows further out and rows without a distribution take the difference first.
 template <int KIND, bool ENT>
 __device__ __forceinline__ void gradient_coef(RowGrad& h, float M, float ls2, float c0, float c1, float k) {
-  h.M = M; h.ls2 = ls2; h.c0 = c0; h.c1 = c1; h.nb = 0.f;
-  h.fast = KIND != LS_F32 && fabsf(M * k) < 1048576.f;
-  if (!h.fast) return;
+  h.M = M; h.ls2 = ls2; h.c0 = c0; h.c1 = c1;
   h.nb = fmaf(-M, k, -ls2);
+  h.fast = KIND != LS_F32 && fabsf(h.nb) < 1048576.f;
+  if (!h.fast) return;
   const float off = fmaf(-M, k, -h.nb) - ls2, f = ex2(off);
   if (ENT) h.c0 = fmaf(c1, off, c0);
   h.c0 *= f; h.c1 *= f;
 }
+// Coefficients of zero (a weight of zero, say) are to give zero whatever the logits are, so NaN too: such rows never are fast.
 template <int KIND, bool ENT, bool FAST>
 __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, float k) {
   const uint64_t kk = pk2(k, k), c0 = pk2(h.c0, h.c0), c1 = pk2(h.c1, h.c1);
+  const bool none = !FAST && h.c0 == 0.f && (!ENT || h.c1 == 0.f);
   uint32_t w[4];
 #pragma unroll
   for (int q = 0; q < Gran<KIND>::E / 2; ++q) {
@@ -534,6 +534,7 @@ __device__ __forceinline__ uint4 row_gradient(const uint4& v, const RowGrad& h, 
     if (KIND == LS_F32) { w[2 * q] = __float_as_uint(d.x); w[2 * q + 1] = __float_as_uint(d.y); }
     else w[q] = narrow2<KIND>(d.x, d.y);
   }
+  if (none) { w[0] = w[1] = w[2] = w[3] = 0; }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -820,14 +821,13 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
       if (lane == 0) {
         const float sc = q.grad_scale * p.inv_tau;
         RowGrad h;
-        const float c0 = -(ENT ? fmaf(o.h, st.H, o.g) : o.g) * sc, c1 = -o.h * TK_LN2 * sc;
+        const float c0 = ENT && o.h != 0.f ? -fmaf(o.h, st.H, o.g) * sc : -o.g * sc, c1 = -o.h * TK_LN2 * sc;
         gradient_coef<KIND, ENT>(h, st.M, st.ls2, c0, c1, p.k);
         h.e0 = c0; h.e1 = c1;
         h.target = o.g * sc; h.zy = zy;
         // the thread that writes the target's granule (an edge entry: the lane that has it)
         const int l = y < p.V ? (r.mis + (int)y) / E - wa : -1;
         h.owner = l >= 0 && l < nw ? l % threads : -1;
-        if (o.g == 0.f && (!ENT || o.h == 0.f)) h.owner = RW_NO_GRADIENT;
         handed = h;
         q.terms[row] = o.terms;
       }
@@ -843,22 +843,6 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
     if (stop) { ok = false; left = true; break; }
     // ---- gradient ----
     const RowGrad h = handed;
-    if (h.owner == RW_NO_GRADIENT) {
-      int at = rs;
-      for (int j = 0; j < K; ++j) {
-        if (j >= n) {
-          ok = __all_sync(0xffffffffu, mbar_wait_asleep(&rb.full[s], ph));
-          if (!ok) break;
-          at = s;
-          if (++s == N) { s = 0; ph ^= 1; }
-        }
-        release_place(&rb.empty[at], lane);
-        if (++at == N) at = 0;
-      }
-      if (!ok) break;
-      zero_row<KIND>(drow, p.V, tid, threads);
-      continue;
-    }
     const bool fast = KIND != LS_F32 && h.fast;
     if (edge >= 0) {
       GradCoef gc; gc.M = h.M; gc.k = p.k; gc.ls2 = h.ls2; gc.c0 = h.e0; gc.c1 = h.e1;
