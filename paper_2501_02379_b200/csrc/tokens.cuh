@@ -681,8 +681,8 @@ __device__ __forceinline__ void row_block_end(const RowBarriers& rb, const RowGe
   if (rb.failed) row_block_failed<KIND, W>(rb, geo, p, rows, back, write);
 }
 // 96 registers: 80 leave the scheduler too little to interleave (0.73 instead of 0.68 ms at 8192 x 131072 bf16), 128 too few
-// warps (0.71 ms).  8192 x 131072 bf16 logits with gradient: 0.69 ms, 5.9 TB/s, after a cold start; 0.74 ms at the clocks that a
-// second of it settles at, where the arithmetic weighs more.  Log-probabilities of 16384 x 32000: 0.178 ms, 5.9 TB/s.
+// warps (0.71 ms).  8192 x 131072 bf16 logits with gradient: 0.68 ms, 5.9 TB/s, after a cold start; 0.74 ms at the clocks that a
+// second of it settles at, where the arithmetic weighs more.  Log-probabilities of 16384 x 32000: 0.174 ms, 6.0 TB/s.
 template <int KIND, int MODE, int W>
 __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f,
                                                   int64_t rows, const __grid_constant__ RowGeom geo) {
@@ -900,7 +900,7 @@ __global__ void __maxnreg__(MODE == RW_FORWARD ? 64 : 96) token_row_kernel(const
 // row took 66 us instead of 23 us for 16384 rows of 1000 bf16 logits).  A row of more than one batch is read again for the
 // gradient: up to about 7 KB from the L1 cache, which the 32 rows in work on an SM fit then (keeping it in 64 registers per lane
 // leaves room for half as many warps: 64 us instead of 51 us for 12384 rows of 3001 bf16 logits, 41 us since the outer entries are
-// taken one by each lane), longer ones mostly from memory (12384 rows of 8000: 306 MB read for 198 MB of logits, 92 us).
+// taken one by each lane), longer ones mostly from memory (12384 rows of 8000: 306 MB read for 198 MB of logits, 94 us).
 constexpr int SR_WARPS = 4, SR_NV = 4, SR_MAX_GRANULES = 1024;
 template <int KIND, int MODE>
 __global__ void __launch_bounds__(32 * SR_WARPS, 8) token_short_kernel(const __grid_constant__ TokenArgs p, const __grid_constant__ PolicyArgs q, const __grid_constant__ ForwardArgs f, int64_t rows) {
