@@ -444,6 +444,119 @@ tgrad_status tgrad_preference_loss(const tgrad_logits* logits, const tgrad_prefe
  * the default.  For the whole process; the calls after this one take it. */
 tgrad_status tgrad_set_copy_limit(int32_t copies);
 
+/* ---------------------------------------------------------------------------
+ * What a block of a trained model keeps for its backward pass, and what computes from that.
+ *
+ * Kept activations take 8.25 bits an entry: a block of 32 entries of a row shares a power of two.  With E = floor(log2 of the largest
+ * magnitude) and e = max(E - 6, -126), an entry's code is x 2^-e rounded to nearest even and clamped to -127 .. 127, it reads back as
+ * code 2^e, and the block's byte is e + 127.  A block with an entry that is not finite reads back as NaN.  What reads back is exact in
+ * bfloat16 and fp32, and in fp16 where the entries were fp16.
+ * A packed matrix is one block of device memory, 16-byte aligned, of tgrad_packed_bytes(): rows of 32 B codes (B = ceil(width / 32), the last
+ * block filled with zeros), then rows of B bytes, each padded to a multiple of 4.
+ *
+ * As above: nothing is kept between calls, everything is enqueued on the stream, sums have a fixed order and are fp32, results are rounded
+ * to the storage type once.  Pointers need the alignment of their element type (packed ones 16 bytes).  A call's outputs must not overlap each other or
+ * its inputs. */
+
+typedef struct {
+  void* d_data;        /* row r, entry c: d_data[r * row_stride + c] */
+  int64_t row_stride;  /* entries, >= width where there is more than one row */
+} tgrad_rows;
+
+/* rows < 2^40 and rows * ceil(width / 32) < 2^48, width <= 2^30 */
+tgrad_status tgrad_packed_bytes(int64_t rows, int64_t width, size_t* bytes);
+/* dtype: TGRAD_R32, TGRAD_R16H or TGRAD_R16B, here and below. */
+tgrad_status tgrad_act_pack(const tgrad_rows* x, int64_t rows, int64_t width, int32_t dtype, void* d_packed, void* cuda_stream);
+tgrad_status tgrad_act_unpack(const void* d_packed, int64_t rows, int64_t width, int32_t dtype, const tgrad_rows* x, void* cuda_stream);
+
+/* Gated activation y = act(a) u, or act(a) where u is NULL; a and u are kept packed in d_packed_a and d_packed_u (both NULL: not).
+ * The backward call takes the kept ones:  da = dy u act'(a),  du = dy act(a);  d_packed_y, which may be NULL, receives y as
+ * computed from the kept inputs, rounded to dtype and packed: the input of the layer behind, for tgrad_weight_grad. */
+typedef enum {
+  TGRAD_ACT_SILU = 0,       /* a / (1 + exp(-a))                                              */
+  TGRAD_ACT_GELU = 1,       /* a times the normal distribution at a                            */
+  TGRAD_ACT_GELU_TANH = 2   /* a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2               */
+} tgrad_activation;
+typedef struct {
+  int64_t rows, width;
+  int32_t dtype, act;
+  tgrad_rows a, u;          /* forward: inputs; backward: their gradients */
+  tgrad_rows y;             /* forward: output; backward: its gradient    */
+  void* d_packed_a;
+  void* d_packed_u;         /* backward: NULL where there is no u         */
+  void* d_packed_y;         /* backward only                              */
+} tgrad_gated_args;
+tgrad_status tgrad_gated_act(const tgrad_gated_args* args, void* cuda_stream);
+tgrad_status tgrad_gated_act_backward(const tgrad_gated_args* args, void* cuda_stream);
+
+/* Norms around a block.  With n(v) = (v - mean) / sqrt(var + eps) * weight + bias of a row (layer norm) or
+ * v / sqrt(mean square + eps) * weight (RMS norm),
+ *   x' = scale x + gate * n_post(f),   h = n_pre(x').
+ * Without a block (f.d_data NULL) x' = scale x; with post = 0 the block's output is taken as it is.
+ * The gate (groups >= 1) has a row for each group of rows: groups of equal size, or with d_starts the rows [starts[g], starts[g + 1]) of group g,
+ * groups + 1 device numbers that do not decrease.  A row of no group has gate 0, whatever stands in f.  groups = rows: a gate for each row.
+ * Parameters are fp32 or of the activations' type, NULL: ones and zeros.  Sums of squares are fp32: entries above 1e18 overflow them.
+ * 1 <= width <= 16384 and rows < 2^31 (TGRAD_ERR_UNSUPPORTED otherwise). */
+typedef struct {
+  int64_t rows, width;
+  int32_t dtype, param_dtype;
+  int32_t layer;             /* 1: layer norm, 0: RMS norm               */
+  int32_t post;              /* 1: the block's output is normalised      */
+  float scale, eps;
+  int32_t groups;            /* rows of the gate; 0: none                */
+  int32_t reserved;
+  const int32_t* d_starts;   /* or NULL */
+  const void* d_weight;
+  const void* d_bias;        /* layer norm only, as d_post_bias */
+  const void* d_post_weight;
+  const void* d_post_bias;
+  tgrad_rows gate;
+} tgrad_norm_config;
+/* d_stats: [2][rows] fp32, 1 / deviation of f (1 where it is not normalised) and of x'; for layer norm [4][rows], their means
+ * behind.  x' and h are normalised before they are rounded.  out_x may be NULL; d_packed_*: kept copies of x' and h (as rounded) and of f, or NULL. */
+typedef struct {
+  tgrad_rows x, f, out_x, out_h;
+  void* d_packed_x;
+  void* d_packed_f;
+  void* d_packed_h;
+  float* d_stats;
+} tgrad_norm_forward;
+tgrad_status tgrad_residual_norm(const tgrad_norm_config* config, const tgrad_norm_forward* io, void* cuda_stream);
+/* Gradients, from those of h and x' (grad_x NULL: none), x' (x or d_packed_x), f (f or d_packed_f; neither: no block) and the forward call's
+ * statistics.  Each of the parameters' gradients may be NULL; they have the parameters' type and shape.  The workspace's size is that for the
+ * current device. */
+typedef struct {
+  tgrad_rows grad_h, grad_x, x, f;
+  const void* d_packed_x;
+  const void* d_packed_f;
+  const float* d_stats;
+  tgrad_rows dx, df, dgate;
+  void* d_dweight;
+  void* d_dbias;
+  void* d_dpost_weight;
+  void* d_dpost_bias;
+} tgrad_norm_backward;
+tgrad_status tgrad_residual_norm_backward_bytes(const tgrad_norm_config* config, size_t* workspace_bytes);
+tgrad_status tgrad_residual_norm_backward(const tgrad_norm_config* config, const tgrad_norm_backward* io, void* d_workspace,
+                                          size_t workspace_bytes, void* cuda_stream);
+
+/* Weight gradient of a linear layer whose input was kept packed:  d_out[n][k] = sum over rows of dy[row][n] x[row][k]  (+ d_out with accumulate).
+ * dy and what was packed have the same type; the result has that type or fp32.  Products are exact, sums fp32 (fp32 dy is multiplied in three
+ * bfloat16 parts that add up to it).  out, width <= 2^24, rows < 2^31.  The workspace's size is that for the current device and for these
+ * pointers and strides; 0 needs no workspace. */
+typedef struct {
+  int64_t rows, out, width;
+  int32_t dtype;             /* of dy and of the packed input */
+  int32_t out_dtype;
+  tgrad_rows dy;
+  const void* d_packed;
+  tgrad_rows d_weight;       /* out rows of width entries */
+  int32_t accumulate;
+  int32_t reserved;
+} tgrad_weight_grad_args;
+tgrad_status tgrad_weight_grad_bytes(const tgrad_weight_grad_args* args, size_t* workspace_bytes);
+tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* args, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

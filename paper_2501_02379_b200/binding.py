@@ -101,6 +101,9 @@ EXPORTS = [
     "tgrad_step_scaled", "tgrad_step_batched_scaled", "tgrad_grad_norm_bytes", "tgrad_grad_norm", "tgrad_clip_grads",
     "tgrad_adamw_step", "tgrad_token_logprob", "tgrad_token_logprob_backward", "tgrad_policy_loss_bytes",
     "tgrad_policy_loss", "tgrad_preference_loss_bytes", "tgrad_preference_loss", "tgrad_set_copy_limit",
+    "tgrad_packed_bytes", "tgrad_act_pack", "tgrad_act_unpack", "tgrad_gated_act", "tgrad_gated_act_backward",
+    "tgrad_residual_norm", "tgrad_residual_norm_backward_bytes", "tgrad_residual_norm_backward", "tgrad_weight_grad_bytes",
+    "tgrad_weight_grad",
 ]
 
 
@@ -146,6 +149,16 @@ def lib() -> C.CDLL:
         l.tgrad_preference_loss_bytes.argtypes = [C.c_int64, C.c_int32, C.POINTER(sz)]
         l.tgrad_preference_loss.argtypes = [vp, vp, vp, sz, vp]
         l.tgrad_set_copy_limit.argtypes = [C.c_int32]
+        l.tgrad_packed_bytes.argtypes = [C.c_int64, C.c_int64, C.POINTER(sz)]
+        l.tgrad_act_pack.argtypes = [vp, C.c_int64, C.c_int64, C.c_int32, vp, vp]
+        l.tgrad_act_unpack.argtypes = [vp, C.c_int64, C.c_int64, C.c_int32, vp, vp]
+        l.tgrad_gated_act.argtypes = [vp, vp]
+        l.tgrad_gated_act_backward.argtypes = [vp, vp]
+        l.tgrad_residual_norm.argtypes = [vp, vp, vp]
+        l.tgrad_residual_norm_backward_bytes.argtypes = [vp, C.POINTER(sz)]
+        l.tgrad_residual_norm_backward.argtypes = [vp, vp, vp, sz, vp]
+        l.tgrad_weight_grad_bytes.argtypes = [vp, C.POINTER(sz)]
+        l.tgrad_weight_grad.argtypes = [vp, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("tgrad_status_string", "tgrad_launch_count"):
                 getattr(l, name).restype = C.c_int
@@ -437,7 +450,7 @@ def _there(index, stream, call, *args, **kw):
         with torch.cuda.stream(stream):
             result = call(*args, **kw)
         for x in args:
-            for t in x.tensors if isinstance(x, TensorList) else (x,):
+            for t in x.tensors if isinstance(x, TensorList) else x if isinstance(x, tuple) else (x,):
                 if isinstance(t, torch.Tensor):
                     t.record_stream(stream)
         return result
@@ -740,3 +753,305 @@ def preference_loss(logits, targets, starts, ref_logp, beta: float = 0.1, label_
         _written(dlogits)
     _, loss, logp, rewards = out.split_with_sizes((ws // 4, 1, rows, 2 * pairs))
     return PreferenceLoss(loss[0], rewards, logp, grad)
+
+
+# --- a trained block: activations kept in 8 bits and what computes from them ---------------------------------------
+#
+# Matrices are [rows, width] CUDA tensors of fp32, fp16 or bfloat16 whose rows may lie apart (the entries of a row are
+# adjacent); devices and streams as above.  Outputs must not overlap inputs.
+
+class Packed(NamedTuple):
+    """A matrix kept in 8.25 bits an entry (act_pack): blocks of 32 entries of a row share a power of two."""
+    data: "torch.Tensor"        # uint8: the codes of all rows, then the blocks' exponents
+    rows: int
+    width: int
+    dtype: "torch.dtype"        # what was packed, and what it is read back as
+
+
+class GatedAct(NamedTuple):
+    y: "torch.Tensor"
+    a8: Optional[Packed]
+    u8: Optional[Packed]
+
+
+class GatedActGrads(NamedTuple):
+    da: "torch.Tensor"
+    du: Optional["torch.Tensor"]
+    y8: Optional[Packed]        # the output as computed from the kept inputs
+
+
+class ResidualNorm(NamedTuple):
+    x: "torch.Tensor"           # the residual stream behind the block
+    h: "torch.Tensor"           # normalised: the next block's input
+    stats: "torch.Tensor"       # what the backward call needs of the forward one
+    x8: Optional[Packed]
+    f8: Optional[Packed]
+    h8: Optional[Packed]
+
+
+class ResidualNormGrads(NamedTuple):
+    x: "torch.Tensor"
+    f: Optional["torch.Tensor"]
+    weight: Optional["torch.Tensor"]
+    bias: Optional["torch.Tensor"]
+    post_weight: Optional["torch.Tensor"]
+    post_bias: Optional["torch.Tensor"]
+    gate: Optional["torch.Tensor"]
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+_pack_rows = struct.Struct("@Pq").pack
+_pack_gated = struct.Struct("@qqiiPqPqPqPPP").pack
+_pack_norm = struct.Struct("@qqiiiiffiiPPPPPPq").pack
+_pack_norm_forward = struct.Struct("@PqPqPqPqPPPP").pack
+_pack_norm_backward = struct.Struct("@PqPqPqPqPPPPqPqPqPPPP").pack
+_pack_weight_grad = struct.Struct("@qqqiiPqPPqii").pack
+_NO_ROWS = (0, 0)
+
+
+def _matrix(name, t):
+    """(tgrad_dtype, rows, width, device index, (address, stride)) of a [rows, width] tensor."""
+    types = _torch()[1]
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} is a CUDA tensor [rows, width]")
+    d = types.get(t.dtype)
+    if d is None or d == C64:
+        raise ValueError(f"{name} is fp32, fp16 or bfloat16")
+    rows, width = t.shape
+    if width < 1:
+        raise ValueError(f"{name} has no columns")
+    stride, inner = t.stride()
+    if inner != 1 and width > 1:
+        raise ValueError(f"the entries of a row of {name} are adjacent")
+    return d, rows, width, t.get_device(), (t.data_ptr(), stride if rows > 1 else width)
+
+
+def _like(name, t, d, rows, width, index):
+    """(address, stride) of a matrix of the given type, shape and device."""
+    m = _matrix(name, t)
+    if m[:4] != (d, rows, width, index):
+        raise ValueError(f"{name} is a matrix of {rows} x {width} entries, of the others' dtype and device")
+    return m[4]
+
+
+def _packed_bytes(rows, width) -> int:
+    blocks = -(-width // 32)
+    return rows * (32 * blocks + -(-blocks // 4) * 4)
+
+
+def _new_packed(rows, width, dtype, index) -> Packed:
+    torch = _torch_types[0]
+    return Packed(torch.empty(_packed_bytes(rows, width), dtype=torch.uint8, device=index), rows, width, dtype)
+
+
+def _packed_ptr(name, p, rows, width, dtype, index) -> int:
+    if not isinstance(p, Packed) or p.rows != rows or p.width != width or p.dtype != dtype:
+        raise ValueError(f"{name} is a packed matrix of {rows} x {width} entries of {dtype}")
+    t = p.data
+    if t.dtype is not _torch_types[0].uint8 or not t.is_contiguous() or t.numel() != _packed_bytes(rows, width) or not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} is not the packed matrix that it says it is, or lives on another device")
+    return t.data_ptr()
+
+
+def act_pack(x, out: Optional[Packed] = None, stream=None) -> Packed:
+    """The matrix x in 8.25 bits an entry: 8-bit codes, and a power of two for each block of 32 entries of a row.  An entry reads back
+    within half a step, a step being 1/64 of the power of two that its block's largest entry reaches (within one step for an entry that
+    near the next power of two).  Zeros and the signs of what does not vanish are kept; a block with an infinity or NaN reads back as NaN.
+    `out`: a packed matrix of the same shape and dtype to write to."""
+    d, rows, width, index, place = _matrix("x", x)
+    if _elsewhere(index, stream):
+        return _there(index, stream, act_pack, x, out)
+    if out is None:
+        out = _new_packed(rows, width, x.dtype, index)
+        to = out.data.data_ptr()
+    else:
+        to = _packed_ptr("out", out, rows, width, x.dtype, index)
+    _check(lib().tgrad_act_pack(_pack_rows(*place), rows, width, d, to, _raw_stream(index)), "tgrad_act_pack")
+    return out
+
+
+def act_unpack(packed: Packed, out=None, stream=None):
+    """The matrix that a packed one reads back as, in the dtype that it was packed from."""
+    torch, types, _ = _torch()
+    index = packed.data.get_device()
+    if _elsewhere(index, stream):
+        return _there(index, stream, act_unpack, packed, out)
+    rows, width = packed.rows, packed.width
+    src, d = _packed_ptr("packed", packed, rows, width, packed.dtype, index), types[packed.dtype]
+    given = out is not None
+    if not given:
+        out = torch.empty((rows, width), dtype=packed.dtype, device=index)
+    _check(lib().tgrad_act_unpack(src, rows, width, d, _pack_rows(*_like("out", out, d, rows, width, index)), _raw_stream(index)), "tgrad_act_unpack")
+    if given:
+        _written(out)
+    return out
+
+
+def gated_act(a, u=None, act: str = "silu", keep: bool = True, stream=None) -> GatedAct:
+    """y = act(a) * u, or act(a) without u, and a and u packed for the backward call (unless keep is False).  act: "silu", "gelu"
+    (with the normal distribution) or "gelu_tanh".  a and u may be the halves of one tensor."""
+    d, rows, width, index, place = _matrix("a", a)
+    if _elsewhere(index, stream):
+        return _there(index, stream, gated_act, a, u, act, keep)
+    kind = ACTIVATIONS[act]
+    other = _like("u", u, d, rows, width, index) if u is not None else _NO_ROWS
+    y = _torch_types[0].empty((rows, width), dtype=a.dtype, device=index)
+    a8 = _new_packed(rows, width, a.dtype, index) if keep else None
+    u8 = _new_packed(rows, width, a.dtype, index) if keep and u is not None else None
+    args = _pack_gated(rows, width, d, kind, *place, *other, y.data_ptr(), width, a8.data.data_ptr() if keep else 0, u8.data.data_ptr() if u8 is not None else 0, 0)
+    _check(lib().tgrad_gated_act(args, _raw_stream(index)), "tgrad_gated_act")
+    return GatedAct(y, a8, u8)
+
+
+def gated_act_backward(a8: Packed, u8: Optional[Packed], dy, act: str = "silu", keep_y: bool = False, da=None, du=None, stream=None) -> GatedActGrads:
+    """Gradients of a gated activation with respect to a and u, from its kept inputs and its output's gradient dy.  keep_y: also the
+    output as computed from the kept inputs, packed, the input of the next layer for weight_grad.  `da`, `du`: where to
+    write the gradients (such as the halves of one tensor)."""
+    d, rows, width, index, place = _matrix("dy", dy)
+    if _elsewhere(index, stream):
+        return _there(index, stream, gated_act_backward, a8, u8, dy, act, keep_y, da, du)
+    kind, given = ACTIVATIONS[act], [t for t in (da, du) if t is not None]
+    a_p = _packed_ptr("a8", a8, rows, width, dy.dtype, index)
+    u_p = _packed_ptr("u8", u8, rows, width, dy.dtype, index) if u8 is not None else 0
+    if u8 is None and du is not None:
+        raise ValueError("without u8 there is no du")
+    if da is None:
+        da = _torch_types[0].empty((rows, width), dtype=dy.dtype, device=index)
+    if du is None and u8 is not None:
+        du = _torch_types[0].empty((rows, width), dtype=dy.dtype, device=index)
+    y8 = _new_packed(rows, width, dy.dtype, index) if keep_y else None
+    args = _pack_gated(rows, width, d, kind, *_like("da", da, d, rows, width, index), *(_like("du", du, d, rows, width, index) if du is not None else _NO_ROWS),
+                       *place, a_p, u_p, y8.data.data_ptr() if keep_y else 0)
+    _check(lib().tgrad_gated_act_backward(args, _raw_stream(index)), "tgrad_gated_act_backward")
+    for t in given:
+        _written(t)
+    return GatedActGrads(da, du, y8)
+
+
+def _norm_config(d, rows, width, index, weight, bias, post_weight, post_bias, gate, starts, scale, kind, post, eps):
+    """(the configuration for the library, tgrad_dtype of the parameters, the gate's rows) after checks of what the library cannot see."""
+    torch, types, _ = _torch_types
+    if kind not in ("rms", "layer"):
+        raise ValueError('kind is "rms" or "layer"')
+    if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
+        raise ValueError("a bias comes with its weight")
+    params = [("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias), ("gate", gate)]
+    pd, pointers = None, []
+    for name, t in params:
+        if t is None:
+            pointers.append(0)
+            continue
+        if pd is None:
+            pd = types.get(t.dtype)
+        if types.get(t.dtype) != pd or (pd != R32 and pd != d) or t.get_device() != index or not t.is_cuda:
+            raise ValueError("parameters are fp32 or of the activations' dtype, all alike, on their device")
+        if name != "gate" and (t.shape != (width,) or (width > 1 and t.stride(0) != 1)):
+            raise ValueError(f"{name} is a contiguous tensor [width]")
+        pointers.append(t.data_ptr())
+    groups, gate_stride = 0, 0
+    if gate is not None:
+        if gate.dim() not in (1, 2) or gate.shape[-1] != width or (width > 1 and gate.stride(-1) != 1) or gate.numel() == 0:
+            raise ValueError("gate is a tensor [width] or [groups, width], the entries of a row adjacent")
+        groups, gate_stride = (1, width) if gate.dim() == 1 else (gate.shape[0], gate.stride(0) if gate.shape[0] > 1 else width)
+    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (groups + 1,) or groups == 0 or not starts.is_cuda or
+                               starts.get_device() != index or not starts.is_contiguous()):
+        raise ValueError("starts is a contiguous int32 tensor [groups + 1] on the activations' device, and comes with a gate [groups, width]")
+    if starts is None and groups and rows % groups:
+        raise ValueError("the gate's groups of rows are of equal size unless starts says where they begin")
+    if pd is None:
+        pd = R32
+    return _pack_norm(rows, width, d, pd, kind == "layer", bool(post), scale, eps, groups, 0, starts.data_ptr() if starts is not None else 0,
+                      *pointers, gate_stride), pd, groups
+
+
+def residual_norm(x, f=None, weight=None, bias=None, post_weight=None, post_bias=None, gate=None, starts=None, scale: float = 1.0,
+                  kind: str = "rms", post: bool = True, eps: float = 1e-6, keep_x: bool = False, keep_f: bool = False, keep_h: bool = False,
+                  stream=None) -> ResidualNorm:
+    """The norms around a block's output f, its gate and the residual stream x in one pass:
+        x' = scale * x + gate * norm(f; post_weight, post_bias),   h = norm(x'; weight, bias)
+    with norm(v) = v / sqrt(mean(v^2) + eps) * weight (kind "rms") or (v - mean) / sqrt(var + eps) * weight + bias ("layer").  post False: f as it is;
+    f None: x' = scale * x.  gate: [width], [groups, width] with groups of equal size or those that `starts` (int32 [groups + 1], device) gives, or
+    [rows, width]; rows of no group have gate 0, whatever stands in f.  Parameters are fp32 or of x's dtype.  keep_*: x', f or h also packed
+    (as rounded), for the backward call or for weight_grad.  Widths up to 16384."""
+    d, rows, width, index, place = _matrix("x", x)
+    if _elsewhere(index, stream):
+        return _there(index, stream, residual_norm, x, f, weight, bias, post_weight, post_bias, gate, starts, scale, kind, post, eps, keep_x, keep_f, keep_h)
+    torch, _, f32 = _torch_types
+    other = _like("f", f, d, rows, width, index) if f is not None else _NO_ROWS
+    if f is None and (gate is not None or post_weight is not None or keep_f):
+        raise ValueError("without f there is no gate, no post_weight and nothing of f to keep")
+    config, _, _ = _norm_config(d, rows, width, index, weight, bias, post_weight, post_bias, gate, starts, scale, kind, post, eps)
+    out, h = (torch.empty((rows, width), dtype=x.dtype, device=index) for _ in range(2))
+    stats = torch.empty((4 if kind == "layer" else 2, rows), dtype=f32, device=index)
+    kept = [_new_packed(rows, width, x.dtype, index) if k else None for k in (keep_x, keep_f, keep_h)]
+    io = _pack_norm_forward(*place, *other, out.data_ptr(), width, h.data_ptr(), width, *(k.data.data_ptr() if k is not None else 0 for k in kept), stats.data_ptr())
+    _check(lib().tgrad_residual_norm(config, io, _raw_stream(index)), "tgrad_residual_norm")
+    return ResidualNorm(out, h, stats, *kept)
+
+
+def residual_norm_backward(grad_h, x, stats, f=None, grad_x=None, weight=None, post_weight=None, post_bias=None, gate=None, starts=None,
+                           scale: float = 1.0, kind: str = "rms", post: bool = True, stream=None) -> ResidualNormGrads:
+    """Gradients of residual_norm from those of h and of x' (grad_x, None: none).  x is the x' that the forward call returned and f its block
+    output, each as a tensor or Packed; stats and the other arguments are the forward call's.  Gradients of the parameters that are given (of
+    both biases where kind is "layer") have their dtype and shape; sums over rows are fp32, of a fixed order."""
+    d, rows, width, index, place = _matrix("grad_h", grad_h)
+    if _elsewhere(index, stream):
+        return _there(index, stream, residual_norm_backward, grad_h, x, stats, f, grad_x, weight, post_weight, post_bias, gate, starts, scale, kind, post)
+    torch, types, f32 = _torch_types
+    layer, dtype = kind == "layer", grad_h.dtype
+
+    def either(name, t):
+        if t is None:
+            return _NO_ROWS, 0
+        if isinstance(t, Packed):
+            return _NO_ROWS, _packed_ptr(name, t, rows, width, dtype, index)
+        return _like(name, t, d, rows, width, index), 0
+
+    (x_m, x_p), (f_m, f_p) = either("x", x), either("f", f)
+    if f is None and (gate is not None or post_weight is not None):
+        raise ValueError("without f there is no gate and no post_weight")
+    g_m = _like("grad_x", grad_x, d, rows, width, index) if grad_x is not None else _NO_ROWS
+    if stats.dtype is not f32 or stats.shape != (4 if layer else 2, rows) or stats.get_device() != index or not stats.is_contiguous():
+        raise ValueError("stats is what the forward call of the same kind returned")
+    config, pd, groups = _norm_config(d, rows, width, index, weight, None, post_weight, post_bias, gate, starts, scale, kind, post, 0.0)
+    dx = torch.empty((rows, width), dtype=dtype, device=index)
+    df = torch.empty((rows, width), dtype=dtype, device=index) if f is not None else None
+    param = dtype if pd == d else f32
+    want = [weight is not None, weight is not None and layer, post_weight is not None, post_weight is not None and layer]
+    vectors = iter(torch.empty((sum(want), width), dtype=param, device=index).unbind(0))
+    dw, db, dpw, dpb = (next(vectors) if k else None for k in want)
+    dgate = torch.empty(gate.shape, dtype=param, device=index) if gate is not None else None
+    n = C.c_size_t(0)
+    _check(lib().tgrad_residual_norm_backward_bytes(config, C.byref(n)), "tgrad_residual_norm_backward_bytes")
+    ws = torch.empty(n.value, dtype=torch.uint8, device=index)
+    io = _pack_norm_backward(*place, *g_m, *x_m, *f_m, x_p, f_p, stats.data_ptr(), dx.data_ptr(), width, df.data_ptr() if df is not None else 0, width,
+                             dgate.data_ptr() if dgate is not None else 0, width, *(t.data_ptr() if t is not None else 0 for t in (dw, db, dpw, dpb)))
+    _check(lib().tgrad_residual_norm_backward(config, io, ws.data_ptr(), n.value, _raw_stream(index)), "tgrad_residual_norm_backward")
+    return ResidualNormGrads(dx, df, dw, db, dpw, dpb, dgate)
+
+
+def weight_grad(dy, x8: Packed, dtype=None, out=None, accumulate: bool = False, stream=None):
+    """Weight gradient dy^T x [out, width] of a linear layer y = x W^T whose input was kept packed, from its output's gradient dy [rows, out],
+    in dy's dtype or fp32 (`dtype`).  `out`: where to write it, or with accumulate what to add it to.  The products are exact and
+    the sums fp32; dy has the dtype that was packed."""
+    d, rows, n, index, place = _matrix("dy", dy)
+    if _elsewhere(index, stream):
+        return _there(index, stream, weight_grad, dy, x8, dtype, out, accumulate)
+    torch, types, f32 = _torch_types
+    src = _packed_ptr("x8", x8, rows, x8.width, dy.dtype, index)
+    given = out is not None
+    if not given:
+        if accumulate:
+            raise ValueError("accumulate adds to out")
+        out = torch.empty((n, x8.width), dtype=dtype or dy.dtype, device=index)
+    to, out_rows, width, where, out_place = _matrix("out", out)
+    if (dtype is not None and out.dtype != dtype) or (to != d and to != R32) or (out_rows, width, where) != (n, x8.width, index):
+        raise ValueError("out is a matrix [columns of dy, columns of x] of dy's dtype or fp32 on its device")
+    args = _pack_weight_grad(rows, n, width, d, to, *place, src, *out_place, accumulate, 0)
+    size = C.c_size_t(0)
+    _check(lib().tgrad_weight_grad_bytes(args, C.byref(size)), "tgrad_weight_grad_bytes")
+    ws = torch.empty(size.value, dtype=torch.uint8, device=index) if size.value else None
+    _check(lib().tgrad_weight_grad(args, ws.data_ptr() if ws is not None else 0, size.value, _raw_stream(index)), "tgrad_weight_grad")
+    if given:
+        _written(out)
+    return out

@@ -1,0 +1,646 @@
+// Norms around a block of a model, with the block's gate and the scale of the residual stream, forward and backward.
+//
+// With n(v) = (v - m) r w + b of a row, r = 1 / sqrt(mean (v - m)^2 + eps), m = mean v (layer norm) or 0 (RMS norm, without b):
+//   x' = scale x + gate * n_post(f),    h = n_pre(x').
+// Backward, with v^ = (v - m) r and J(d, v^, r) = r (d - v^ mean(d v^) - mean d) (the last term for layer norm only):
+//   t = dx' + J(dh w, x'^, r_pre),   dx = scale t,   df = J(gate t w_post, f^, r_post),
+//   dw = sum dh x'^,  db = sum dh,  dw_post = sum gate t f^,  db_post = sum gate t,  dgate = sum t (f^ w_post + b_post),
+// the sums over the rows that share the parameter.  Rows that share a gate need S1 = sum t f^ and S0 = sum t only: the parameters are
+// factors of these, so one pair of sums per column serves dw_post, db_post and dgate.
+//
+// Bound by memory: every input is read once, every output written once.  A row belongs to `tpr` threads of a block, each holding V vectors
+// of 8 entries; the blocks stay, one per SM, and walk over the rows.  What a thread will read it copies itself into places of
+// its own in shared memory (cp.async), some rows ahead, so the copies need no barrier and no registers, and the memory is busy
+// while a row waits in its reductions.  Column sums stay in registers over all rows of a thread's chunk and are added up in a fixed
+// order by a second launch.
+#pragma once
+#include "packed.cuh"
+
+namespace tg {
+
+constexpr int NM_MAX_STAGES = 4;
+enum { NM_NONE = 0, NM_PLAIN = 1, NM_POST = 2 };      // no block, a block's output as it is, the same normalised
+
+struct ResNormArgs {
+  RowsOf x, f;               // forward: stream and block output; backward: x' and f as kept in storage
+  RowsOf dh, dx;             // backward: gradients of h and of x' (p null: none)
+  RowsOf out0, out1;         // forward: x' (p null: not wanted) and h; backward: dx and df
+  PackedRows px, pf, ph;     // forward: kept copies to write (codes null: not wanted); backward: x' and f given packed (codes null: not)
+  RowsOf w, b, pw, gate, pb; // parameters; p null: 1 (weights, gate) or 0 (biases).  gate: a row for each group
+  RowsOf dgate;              // backward, a gate for each row: its gradient
+  const int* starts;         // groups + 1 first rows, or null: groups of rows_per rows
+  int64_t rows, rows_per;
+  int groups;
+  int gate_rows;             // 1: a gate for each row
+  int mode, width, blocks;   // blocks of 32 entries of a row
+  int pf32;                  // parameters are fp32 (else of the storage type)
+  int shared_params;         // weights (with a single gate row folded in) are held in shared memory
+  float scale, eps;
+  float* stats;              // [2 or 4][rows]: 1 / deviation of f and x', then their means
+  int tpr, stages;
+  int64_t chunk;             // backward: rows of a row group
+  float* part;               // backward: column sums
+  int64_t part_stride;       // floats of a slot's row: 32 blocks
+  int combine;               // backward: the row groups of a block are added up first
+};
+
+// ---- parameters ----
+template <int KIND>
+__device__ __forceinline__ void param8(const RowsOf& t, int pf32, int64_t row, int c, int n, float fill, float (&v)[8]) {
+  if (!t.p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fill;
+  } else if (KIND == LS_F32 || pf32) {
+    const float* p = reinterpret_cast<const float*>(t.p) + row * t.ld + c;
+    if (n == 8 && t.al == 16) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < n ? __ldg(p + i) : 0.f;
+    }
+  } else {
+    const char* p = t.p + (row * t.ld + c) * 2;
+    if (n == 8 && t.al == 16) {
+      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+      const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { const float2 d = widen2<KIND>(u[i]); v[2 * i] = d.x; v[2 * i + 1] = d.y; }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < n ? ld_real<KIND>(p + 2 * i) : 0.f;
+    }
+  }
+}
+template <int KIND>
+__device__ __forceinline__ void store_param(const RowsOf& t, int pf32, int64_t row, int c, float v) {
+  if (KIND == LS_F32 || pf32) reinterpret_cast<float*>(t.p)[row * t.ld + c] = v;
+  else st_real<KIND>(t.p + (row * t.ld + c) * 2, v);
+}
+
+// ---- a thread's places in shared memory ----
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async8u(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4u(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t dst, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst), "r"(v) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v; asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory"); return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory"); return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory"); return v; }
+
+// 8 entries, in planes of 16 bytes per thread (fp32: two of them)
+template <int KIND> struct NmPlanes { static constexpr int n = KIND == LS_F32 ? 2 : 1; };
+template <int KIND>
+__device__ __forceinline__ void fetch8(uint32_t dst, uint32_t plane, const RowsOf& t, int64_t row, int c, int n) {
+  constexpr int B = KIND == LS_F32 ? 4 : 2, E = 4 / B;      // entries of a word
+  const char* p = t.p + (row * t.ld + c) * B;
+  if (n == 8 && t.al == 16) {
+#pragma unroll
+    for (int i = 0; i < B / 2; ++i) cp_async16(dst + i * plane, p + 16 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * B; ++i) {
+      const uint32_t at = dst + (i >> 2) * plane + (i & 3) * 4;
+      if (t.al >= 4 && E * i + E <= n) cp_async4u(at, p + 4 * i);
+      else {
+        uint32_t v = 0;
+        if (E == 2) {
+          if (2 * i < n) v = *reinterpret_cast<const unsigned short*>(p + 4 * i);
+          if (2 * i + 1 < n) v |= (uint32_t)*reinterpret_cast<const unsigned short*>(p + 4 * i + 2) << 16;
+        }
+        sts32(at, v);
+      }
+    }
+  }
+}
+template <int KIND>
+__device__ __forceinline__ void take8(uint32_t src, uint32_t plane, float (&v)[8]) {
+  const uint4 a = lds128(src);
+  if (KIND == LS_F32) {
+    const uint4 b = lds128(src + plane);
+    const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+  } else {
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 d = widen2<KIND>(u[i]); v[2 * i] = d.x; v[2 * i + 1] = d.y; }
+  }
+}
+// packed entries: 8 bytes of codes and the word that holds the block's byte
+__device__ __forceinline__ void fetch8_packed(uint32_t dst, const PackedRows& t, int64_t row, int v) {
+  cp_async8u(dst, t.codes + (row * t.blocks * 4 + v) * 8);
+  cp_async4u(dst + 8, t.exps + row * t.exp_stride + ((v >> 2) & ~3));
+}
+__device__ __forceinline__ void take8_packed(uint32_t src, int v, float (&out)[8]) {
+  const uint4 q = lds128(src);
+  unpack8(make_uint2(q.x, q.y), (q.z >> (8 * ((v >> 2) & 3))) & 255u, out);
+}
+
+// ---- sums over a row ----
+struct RowTeam {
+  float2* red;               // two buffers of 32
+  int warps, warp, lane, id, turn;
+  __device__ __forceinline__ void sync() const {
+    if (warps == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
+  }
+  // sums of a and b over the team, the same bits in every thread
+  __device__ __forceinline__ float2 sum(float a, float b) {
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); b += __shfl_xor_sync(0xffffffffu, b, m); }
+    if (warps == 1) return make_float2(a, b);
+    float2* r = red + (turn ^= 32);
+    if (lane == 0) r[warp] = make_float2(a, b);
+    sync();
+    const float2 o = lane < warps ? r[lane] : make_float2(0.f, 0.f);
+    a = o.x; b = o.y;
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); b += __shfl_xor_sync(0xffffffffu, b, m); }
+    return make_float2(a, b);
+  }
+};
+
+// the group that a row belongs to; -1: none
+__device__ __forceinline__ int group_of(const ResNormArgs& A, int64_t row) {
+  if (A.gate_rows) return (int)row;
+  if (!A.starts) return A.groups == 1 ? 0 : (int)(row / A.rows_per);
+  int lo = -1, hi = A.groups;            // starts[lo] <= row < starts[hi]
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (__ldg(A.starts + mid) <= row) lo = mid; else hi = mid; }
+  return lo >= 0 && row < __ldg(A.starts + lo + 1) ? lo : -1;
+}
+
+__device__ __forceinline__ void wait_stages(int ahead) {      // all copies but those of the last `ahead` rows have landed
+  if (ahead <= 0) cp_async_wait<0>();
+  else if (ahead == 1) cp_async_wait<1>();
+  else if (ahead == 2) cp_async_wait<2>();
+  else cp_async_wait<3>();
+}
+
+// weights in shared memory: planes of 4 floats for each half of a vector, w first, then w_post (times the gate where there is one for all rows)
+template <int KIND>
+__device__ __forceinline__ void fill_params(const ResNormArgs& A, float4* ps) {
+  const int nv = 4 * A.blocks;
+  for (int v = threadIdx.x; v < nv; v += blockDim.x) {
+    const int n = max(0, min(8, A.width - 8 * v));
+    float a[8], g[8];
+    param8<KIND>(A.w, A.pf32, 0, 8 * v, n, 1.f, a);
+    ps[v] = make_float4(a[0], a[1], a[2], a[3]); ps[nv + v] = make_float4(a[4], a[5], a[6], a[7]);
+    param8<KIND>(A.pw, A.pf32, 0, 8 * v, n, 1.f, a);
+    if (A.groups == 1 && !A.starts && !A.gate_rows) {
+      param8<KIND>(A.gate, A.pf32, 0, 8 * v, n, 1.f, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] *= g[i];
+    }
+    ps[2 * nv + v] = make_float4(a[0], a[1], a[2], a[3]); ps[3 * nv + v] = make_float4(a[4], a[5], a[6], a[7]);
+  }
+}
+__device__ __forceinline__ void shared8(const float4* ps, int nv, int which, int v, float (&out)[8]) {
+  const float4 a = ps[2 * which * nv + v], b = ps[(2 * which + 1) * nv + v];
+  out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w; out[4] = b.x; out[5] = b.y; out[6] = b.z; out[7] = b.w;
+}
+
+constexpr int NM_RED_BYTES = 32 * 64 * 8;      // 32 teams at most, two buffers of 32 pairs each
+
+// Mean and 1 / deviation of the entries that `take(j, v)` gives.
+template <bool LN, int V, typename Take>
+__device__ __forceinline__ void row_stats(RowTeam& team, const int (&n)[V], float inv, float eps, Take take, float& mean, float& rstd) {
+  mean = 0.f;
+  if (LN) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float v[8]; take(j, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];           // (entries that do not exist are 0)
+    }
+    mean = team.sum(s, 0.f).x * inv;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float v[8]; take(j, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { const float d = LN && i >= n[j] ? 0.f : v[i] - mean; s = fmaf(d, d, s); }
+  }
+  rstd = rsqrtf(fmaf(team.sum(s, 0.f).x, inv, eps));
+}
+
+template <int KIND, bool LN, int V>
+__global__ void __launch_bounds__(1024, 1) norm_forward_kernel(const ResNormArgs A) {
+  extern __shared__ __align__(16) unsigned char nm_smem[];
+  griddep_chain();
+  const int nv = 4 * A.blocks, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
+  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
+  if (A.shared_params) { fill_params<KIND>(A, ps); __syncthreads(); }
+  const uint32_t plane = blockDim.x * 16;
+  constexpr int P = NmPlanes<KIND>::n * V;
+  const uint32_t base = smem_u32(nm_smem) + NM_RED_BYTES + (A.shared_params ? 64 * nv : 0) + threadIdx.x * 16;
+  int at[V], n[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) { at[j] = t + j * A.tpr; n[j] = max(0, min(8, A.width - 8 * at[j])); }
+  const int64_t first = (int64_t)blockIdx.x * teams + mine, step = (int64_t)gridDim.x * teams;
+  const int S = A.stages, per = A.mode == NM_NONE ? 1 : 2;
+  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
+  auto issue = [&](int s, int64_t row) {
+    if (row < A.rows) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        fetch8<KIND>(slot(s, 0, j), plane, A.x, row, 8 * at[j], n[j]);
+        if (A.mode != NM_NONE) fetch8<KIND>(slot(s, 1, j), plane, A.f, row, 8 * at[j], n[j]);
+      }
+    }
+    cp_async_commit();
+  };
+  for (int s = 0; s < S; ++s) issue(s, first + s * step);
+  const float inv = 1.f / (float)A.width;
+  int s = 0;
+  for (int64_t row = first; row < A.rows; row += step) {
+    wait_stages(S - 1);
+    float x[V][8];
+#pragma unroll
+    for (int j = 0; j < V; ++j) take8<KIND>(slot(s, 0, j), plane, x[j]);
+    if (A.mode != NM_NONE) {
+      const int g = group_of(A, row);
+      float m0 = 0.f, r0 = 1.f;
+      if (A.mode == NM_POST)
+        row_stats<LN, V>(team, n, inv, A.eps, [&](int j, float (&v)[8]) { take8<KIND>(slot(s, 1, j), plane, v); }, m0, r0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float f[8], p[8], q[8];
+        take8<KIND>(slot(s, 1, j), plane, f);
+        if (A.pf.codes) {
+          uint32_t byte;
+          const uint2 w = pack8(f, byte);
+          if (at[j] < nv) store_packed(A.pf, row, at[j], row * nv + at[j], w, byte);
+        }
+        const bool folded = A.shared_params && A.groups == 1 && !A.starts && !A.gate_rows;
+        if (A.shared_params && at[j] < nv) shared8(ps, nv, 1, at[j], p); else param8<KIND>(A.pw, A.pf32, 0, 8 * at[j], n[j], 1.f, p);
+        if (!folded) param8<KIND>(A.gate, A.pf32, max(g, 0), 8 * at[j], n[j], 1.f, q);
+        float b[8];
+        if (LN && A.pb.p) {
+          param8<KIND>(A.pb, A.pf32, 0, 8 * at[j], n[j], 0.f, b);
+          if (folded && A.gate.p) param8<KIND>(A.gate, A.pf32, 0, 8 * at[j], n[j], 1.f, q);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float d = (f[i] - m0) * r0 * p[i];
+          if (LN && A.pb.p) d += folded && A.gate.p ? b[i] * q[i] : b[i];
+          if (!folded) d *= q[i];
+          x[j][i] = g >= 0 ? fmaf(A.scale, x[j][i], d) : A.scale * x[j][i];      // (a row of no group: whatever stands in f)
+        }
+      }
+      if (A.stats && t == 0) { A.stats[row] = r0; if (LN) A.stats[2 * A.rows + row] = m0; }
+    } else {
+      if (A.stats && t == 0) { A.stats[row] = 1.f; if (LN) A.stats[2 * A.rows + row] = 0.f; }
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] *= A.scale;
+    }
+    issue(s, row + S * step);                       // the row's places are read: the next one that will stand there
+    s = s + 1 == S ? 0 : s + 1;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (LN || A.b.p || n[j] < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = i < n[j] ? x[j][i] : 0.f;
+      }
+      if (A.out0.p) store8<KIND, false>(A.out0, row, 8 * at[j], n[j], x[j]);
+      if (A.px.codes) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = x[j][i];
+        round8<KIND>(v);
+        uint32_t byte;
+        const uint2 w = pack8(v, byte);
+        if (at[j] < nv) store_packed(A.px, row, at[j], row * nv + at[j], w, byte);
+      }
+    }
+    float m1, r1;
+    row_stats<LN, V>(team, n, inv, A.eps, [&](int j, float (&v)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = x[j][i];
+    }, m1, r1);
+    if (A.stats && t == 0) { A.stats[A.rows + row] = r1; if (LN) A.stats[3 * A.rows + row] = m1; }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float p[8], b[8];
+      if (A.shared_params && at[j] < nv) shared8(ps, nv, 0, at[j], p); else param8<KIND>(A.w, A.pf32, 0, 8 * at[j], n[j], 1.f, p);
+      if (LN) param8<KIND>(A.b, A.pf32, 0, 8 * at[j], n[j], 0.f, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] = (x[j][i] - m1) * r1 * p[i];
+        if (LN) x[j][i] += b[i];
+        if (i >= n[j]) x[j][i] = 0.f;
+      }
+      store8<KIND, false>(A.out1, row, 8 * at[j], n[j], x[j]);
+      if (A.ph.codes) {
+        round8<KIND>(x[j]);
+        uint32_t byte;
+        const uint2 w = pack8(x[j], byte);
+        if (at[j] < nv) store_packed(A.ph, row, at[j], row * nv + at[j], w, byte);
+      }
+    }
+  }
+  cp_async_wait<0>();
+}
+
+// Slot of the column sums: those of dh (and dh x'^) at [slot], those of t (and t f^) at [slots + slot + group], so that row groups
+// that see several sequences, and sequences that several row groups see, have places of their own.
+template <int KIND, bool LN, int V>
+__global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs A) {
+  extern __shared__ __align__(16) unsigned char nm_smem[];
+  griddep_chain();
+  const int nv = 4 * A.blocks, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
+  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
+  if (A.shared_params) { fill_params<KIND>(A, ps); __syncthreads(); }
+  const uint32_t plane = blockDim.x * 16;
+  constexpr int P = NmPlanes<KIND>::n * V;
+  const uint32_t ring = NM_RED_BYTES + (A.shared_params ? 64 * nv : 0);
+  const uint32_t base = smem_u32(nm_smem) + ring + threadIdx.x * 16;
+  int at[V], n[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) { at[j] = t + j * A.tpr; n[j] = max(0, min(8, A.width - 8 * at[j])); }
+  const int64_t team_id = (int64_t)blockIdx.x * teams + mine;
+  const int64_t first = team_id * A.chunk, last = min(first + A.chunk, A.rows);
+  const int S = A.stages;
+  const int per = 2 + (A.dx.p ? 1 : 0) + (A.mode != NM_NONE ? 1 : 0);
+  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
+  const int T_DX = 2, T_F = A.dx.p ? 3 : 2;
+  auto issue = [&](int s, int64_t row) {
+    if (S > 0 && row < last) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        fetch8<KIND>(slot(s, 0, j), plane, A.dh, row, 8 * at[j], n[j]);
+        if (A.px.codes) { if (at[j] < nv) fetch8_packed(slot(s, 1, j), A.px, row, at[j]); }
+        else fetch8<KIND>(slot(s, 1, j), plane, A.x, row, 8 * at[j], n[j]);
+        if (A.dx.p) fetch8<KIND>(slot(s, T_DX, j), plane, A.dx, row, 8 * at[j], n[j]);
+        if (A.mode != NM_NONE) {
+          if (A.pf.codes) { if (at[j] < nv) fetch8_packed(slot(s, T_F, j), A.pf, row, at[j]); }
+          else fetch8<KIND>(slot(s, T_F, j), plane, A.f, row, 8 * at[j], n[j]);
+        }
+      }
+    }
+    cp_async_commit();
+  };
+  // a tensor's entries: from the thread's places, or (no room for a row there) from memory
+  auto dense = [&](int s, int tensor, const RowsOf& m, int64_t row, int j, float (&v)[8]) {
+    if (S > 0) take8<KIND>(slot(s, tensor, j), plane, v); else load8<KIND, false>(m, row, 8 * at[j], n[j], v);
+  };
+  auto kept = [&](int s, int tensor, const PackedRows& p, const RowsOf& m, int64_t row, int j, float (&v)[8]) {
+    if (!p.codes) dense(s, tensor, m, row, j, v);
+    else if (at[j] >= nv) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    } else if (S > 0) take8_packed(slot(s, tensor, j), at[j], v);
+    else unpack8(ld_codes(p.codes + (row * nv + at[j]) * 8), p.exps[row * p.exp_stride + (at[j] >> 2)], v);
+  };
+  float sw[V][8], sb[LN ? V : 1][8], s1[V][8], s0[LN ? V : 1][8];
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { sw[j][i] = s1[j][i] = 0.f; if (LN) sb[j][i] = s0[j][i] = 0.f; }
+  const int nw = LN ? 2 : 1;
+  const int64_t slots = A.combine ? gridDim.x : (int64_t)gridDim.x * teams;
+  auto flush = [&](float* to, float (&a)[V][8], bool clear) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (at[j] < nv) {
+        reinterpret_cast<float4*>(to + 8 * at[j])[0] = make_float4(a[j][0], a[j][1], a[j][2], a[j][3]);
+        reinterpret_cast<float4*>(to + 8 * at[j])[1] = make_float4(a[j][4], a[j][5], a[j][6], a[j][7]);
+        if (clear) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) a[j][i] = 0.f;
+        }
+      }
+  };
+  auto slot_w = [&](int64_t k, int which) { return A.part + (k * nw + which) * A.part_stride; };
+  auto slot_s = [&](int64_t k, int which) { return A.part + ((slots + k) * nw + which) * A.part_stride; };
+  for (int s = 0; s < S; ++s) issue(s, first + s);
+  const float inv = 1.f / (float)A.width;
+  const bool folded = A.shared_params && A.groups == 1 && !A.starts && !A.gate_rows;
+  int s = 0, group = -1;
+  float4 next = make_float4(1.f, 1.f, 0.f, 0.f);       // the statistics of a row, read a row ahead
+  auto read_stats = [&](int64_t row) {
+    if (row >= last) return;
+    next.y = A.stats[A.rows + row];
+    if (LN) next.w = A.stats[3 * A.rows + row];
+    if (A.mode == NM_POST) { next.x = A.stats[row]; if (LN) next.z = A.stats[2 * A.rows + row]; }
+  };
+  read_stats(first);
+  for (int64_t row = first; row < last; ++row) {
+    wait_stages(S - 1);
+    const float r0 = next.x, r1 = next.y, m0 = next.z, m1 = next.w;
+    read_stats(row + 1);
+    float sum_u = 0.f, sum_d = 0.f;
+    float tt[V][8];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float d[8], u[8], p[8];
+      dense(s, 0, A.dh, row, j, d);
+      kept(s, 1, A.px, A.x, row, j, u);
+      if (A.shared_params && at[j] < nv) shared8(ps, nv, 0, at[j], p); else param8<KIND>(A.w, A.pf32, 0, 8 * at[j], n[j], 1.f, p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float xh = (u[i] - m1) * r1;
+        sw[j][i] = fmaf(d[i], xh, sw[j][i]);
+        if (LN) sb[j][i] += d[i];
+        const float e = d[i] * p[i];
+        tt[j][i] = e;
+        sum_u = fmaf(e, xh, sum_u);
+        if (LN) sum_d += e;
+      }
+    }
+    float2 c = team.sum(sum_u, sum_d);
+    c.x *= inv; c.y *= inv;
+    int g = -1;
+    if (A.mode != NM_NONE) {
+      g = group_of(A, row);
+      if (!A.combine && !A.gate_rows && g != group) {            // another sequence: its own column sums
+        if (group >= 0) { flush(slot_s(team_id + group, 0), s1, true); if (LN) flush(slot_s(team_id + group, 1), reinterpret_cast<float (&)[V][8]>(s0), true); }
+        group = g;
+      }
+    }
+    sum_u = sum_d = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float u[8], v[8];
+      kept(s, 1, A.px, A.x, row, j, u);
+      if (A.dx.p) dense(s, T_DX, A.dx, row, j, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float xh = (u[i] - m1) * r1;
+        float e = fmaf(-xh, c.x, tt[j][i]);
+        if (LN) e -= c.y;
+        tt[j][i] = A.dx.p ? fmaf(r1, e, v[i]) : r1 * e;
+        v[i] = A.scale * tt[j][i];
+      }
+      store8<KIND, false>(A.out0, row, 8 * at[j], n[j], v);
+      if (A.mode != NM_NONE && g >= 0) {
+        float f[8], p[8], q[8];
+        kept(s, T_F, A.pf, A.f, row, j, f);
+        if (A.shared_params && at[j] < nv) shared8(ps, nv, 1, at[j], p); else param8<KIND>(A.pw, A.pf32, 0, 8 * at[j], n[j], 1.f, p);
+        if (!folded) param8<KIND>(A.gate, A.pf32, g, 8 * at[j], n[j], 1.f, q);
+        if (A.gate_rows && A.dgate.p) {
+          float b[8];
+          param8<KIND>(A.pw, A.pf32, 0, 8 * at[j], n[j], 1.f, u);
+          param8<KIND>(A.pb, A.pf32, 0, 8 * at[j], n[j], 0.f, b);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < n[j]) store_param<KIND>(A.dgate, A.pf32, row, 8 * at[j] + i, tt[j][i] * fmaf((f[i] - m0) * r0, u[i], b[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float fh = (f[i] - m0) * r0;
+          const float d = folded ? tt[j][i] : tt[j][i] * q[i];
+          const float to = A.gate_rows ? d : tt[j][i];
+          s1[j][i] = fmaf(to, fh, s1[j][i]);
+          if (LN) s0[j][i] += i < n[j] ? to : 0.f;
+          const float e = i < n[j] ? d * p[i] : 0.f;
+          tt[j][i] = e;
+          sum_u = fmaf(e, fh, sum_u);
+          if (LN) sum_d += e;
+        }
+      }
+    }
+    if (A.mode != NM_NONE) {
+      c = make_float2(0.f, 0.f);
+      if (A.mode == NM_POST) { c = team.sum(sum_u, sum_d); c.x *= inv; c.y *= inv; }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float f[8];
+        if (A.mode == NM_POST) kept(s, T_F, A.pf, A.f, row, j, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (A.mode == NM_POST) {
+            const float fh = (f[i] - m0) * r0;
+            float e = fmaf(-fh, c.x, tt[j][i]);
+            if (LN) e -= c.y;
+            tt[j][i] = r0 * e;
+          }
+          if (g < 0) tt[j][i] = 0.f;
+        }
+        store8<KIND, false>(A.out1, row, 8 * at[j], n[j], tt[j]);
+      }
+    }
+    if (S > 0) { issue(s, row + S); s = s + 1 == S ? 0 : s + 1; }
+  }
+  cp_async_wait<0>();
+  if (!A.part) return;
+  if (A.combine) {
+    // the block's teams, one kind of sum after the other, through the ring's memory
+    float* buf = reinterpret_cast<float*>(nm_smem + ring);
+    auto join = [&](float* to, float (&a)[V][8]) {
+      __syncthreads();
+      flush(buf + (int64_t)mine * A.part_stride, a, false);
+      __syncthreads();
+      for (int c = threadIdx.x; c < A.part_stride; c += blockDim.x) {
+        float v = 0.f;
+        for (int k = 0; k < teams; ++k) v += buf[(int64_t)k * A.part_stride + c];
+        to[c] = v;
+      }
+    };
+    join(slot_w(blockIdx.x, 0), sw);
+    if (LN) join(slot_w(blockIdx.x, 1), reinterpret_cast<float (&)[V][8]>(sb));
+    if (A.mode != NM_NONE) {
+      join(slot_s(blockIdx.x, 0), s1);
+      if (LN) join(slot_s(blockIdx.x, 1), reinterpret_cast<float (&)[V][8]>(s0));
+    }
+    return;
+  }
+  flush(slot_w(team_id, 0), sw, false);
+  if (LN) flush(slot_w(team_id, 1), reinterpret_cast<float (&)[V][8]>(sb), false);
+  if (A.mode != NM_NONE && group >= 0) {
+    flush(slot_s(team_id + group, 0), s1, false);
+    if (LN) flush(slot_s(team_id + group, 1), reinterpret_cast<float (&)[V][8]>(s0), false);
+  }
+}
+
+// Column sums of the slots, in a fixed order: 32 columns a block, 32 threads on each.
+constexpr int NF_Y = 32;
+struct NormSums {
+  const float* part;
+  int64_t slots, part_stride, chunk, rows, rows_per;
+  const int* starts;
+  int groups, width, pf32, per_row, post;   // per_row: the sums hold gate * t already; post: the block's output is normalised
+  RowsOf w, b, pw, pb, gate;                // parameters
+  RowsOf dw, db, dpw, dpb, dgate;           // their gradients; p null: not wanted
+};
+
+template <int KIND, bool LN>
+__global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSums A) {
+  __shared__ float2 red[NF_Y][33];
+  griddep_chain();
+  const int x = threadIdx.x, y = threadIdx.y, c = blockIdx.x * 32 + x, nw = LN ? 2 : 1;
+  const bool live = c < A.width;
+  auto join = [&](float2 v) {               // over y, to every thread of the column
+    red[y][x] = v;
+    __syncthreads();
+    float2 s = make_float2(0.f, 0.f);
+    for (int k = 0; k < NF_Y; ++k) { s.x += red[k][x].x; s.y += red[k][x].y; }
+    __syncthreads();
+    return s;
+  };
+  auto over = [&](int64_t at, int64_t k0, int64_t k1, int64_t from, int64_t step) {      // slots at + [k0, k1]
+    float2 v = make_float2(0.f, 0.f);
+    if (live)
+      for (int64_t k = k0 + from; k <= k1; k += step) {
+        const float* p = A.part + (at + k) * nw * A.part_stride + c;
+        v.x += p[0];
+        if (LN) v.y += p[A.part_stride];
+      }
+    return v;
+  };
+  auto param = [&](const RowsOf& t, int64_t row, float fill) {
+    if (!t.p || !live) return fill;
+    return KIND == LS_F32 || A.pf32 ? reinterpret_cast<const float*>(t.p)[row * t.ld + c] : ld_real<KIND>(t.p + (row * t.ld + c) * 2);
+  };
+  if (A.dw.p || A.db.p) {
+    const float2 v = join(over(0, 0, A.slots - 1, y, NF_Y));
+    if (y == 0 && live) {
+      if (A.dw.p) store_param<KIND>(A.dw, A.pf32, 0, c, v.x);
+      if (A.db.p) store_param<KIND>(A.db, A.pf32, 0, c, v.y);
+    }
+  }
+  if (!A.dpw.p && !A.dpb.p && (!A.dgate.p || A.per_row)) return;
+  const float pw = A.post ? param(A.pw, 0, 1.f) : 1.f, pb = LN && A.post ? param(A.pb, 0, 0.f) : 0.f;
+  float2 total = make_float2(0.f, 0.f);
+  if (A.per_row) total = join(over(A.slots, 0, A.slots - 1, y, NF_Y));
+  else {
+    // many groups: a thread takes whole ones; few: all threads on each
+    const bool whole = A.groups >= NF_Y;
+    for (int g = whole ? y : 0; g < A.groups; g += whole ? NF_Y : 1) {
+      int64_t r0 = 0, r1 = A.rows;
+      if (A.starts) { r0 = max((int64_t)A.starts[g], (int64_t)0); r1 = min((int64_t)A.starts[g + 1], A.rows); }
+      else if (A.groups > 1) { r0 = g * A.rows_per; r1 = r0 + A.rows_per; }
+      float2 v = make_float2(0.f, 0.f);
+      if (r0 < r1) {
+        const int64_t k0 = A.chunk ? r0 / A.chunk : 0, k1 = A.chunk ? (r1 - 1) / A.chunk : A.slots - 1;      // chunk 0: combined sums, one group
+        v = over(A.slots + g, k0, k1, whole ? 0 : y, whole ? 1 : NF_Y);
+      }
+      if (!whole) v = join(v);
+      const float gate = param(A.gate, g, 1.f);
+      if (live && A.dgate.p && (whole || y == 0)) store_param<KIND>(A.dgate, A.pf32, g, c, fmaf(v.x, pw, v.y * pb));
+      total.x = fmaf(gate, v.x, total.x); total.y = fmaf(gate, v.y, total.y);
+    }
+    if (whole) total = join(total);
+  }
+  if (y == 0 && live) {
+    if (A.dpw.p) store_param<KIND>(A.dpw, A.pf32, 0, c, total.x);
+    if (A.dpb.p) store_param<KIND>(A.dpb, A.pf32, 0, c, total.y);
+  }
+}
+
+}  // namespace tg

@@ -1,0 +1,320 @@
+// Activations in 8 bits: packing, unpacking, and the gated activation that keeps its inputs packed.
+//
+// Format.  A block of 32 entries of a row shares a power of two: with E = floor(log2 max |x|) over the block and
+// e = max(E - 6, -126),
+//   code = clamp(round(x 2^-e), -127, 127) (round to nearest even),   x^ = code 2^e,
+// and the block's byte is e + 127.  So |x - x^| <= 2^e / 2, half of 1/64 of a power of two that the largest entry reaches (up to
+// 2^e for an entry within 1/256 of the next one, where the code is clamped).  Byte 0: a block of zeros.  Byte 255: a block with an entry
+// that is not finite; its codes are 0 and 0 * 2^128 = 0 * infinity makes every entry read back as NaN, without a test.
+// A power of two and not max / 127: the quotient, the codes and x^ are exact, so the codes do not depend on how they are computed, and
+// x^ (7 bits) is itself a bfloat16, or an fp16 number where x was one: a tensor core multiplies by x^ without a rounding.
+// Memory: rows of 32 B codes each (B blocks, the last one filled with zeros), then rows of B bytes, padded with zeros to a
+// multiple of 4.
+//
+// All kernels here are bound by memory: a thread takes 8 entries at a time (16 bytes of 16-bit storage, 8 bytes of codes), four
+// neighbours a block, and several of them in flight.  The arithmetic is kept below the 16 instructions per entry that the copy rate leaves.
+#pragma once
+#include "lists.cuh"
+
+namespace tg {
+
+// Rows of a dense tensor: `al` bytes (2, 4, 8 or 16) divide the address of every row's first entry.
+struct RowsOf {
+  char* p;
+  int64_t ld;            // entries from one row to the next
+  int al;
+};
+struct PackedRows {
+  unsigned char* codes;  // 32 * blocks bytes a row
+  unsigned char* exps;   // exp_stride bytes a row
+  int blocks, exp_stride;
+};
+
+constexpr int PK_THREADS = 256;
+
+// 8 entries of a row from entry c on, of which n (0..8) exist; the others are 0.  ALIGNED: al is 16 and n is 8 or 0.
+template <int KIND, bool ALIGNED>
+__device__ __forceinline__ void load8(const RowsOf& t, int64_t row, int c, int n, float (&v)[8]) {
+  constexpr int B = KIND == LS_F32 ? 4 : 2;
+  const char* p = t.p + (row * t.ld + c) * B;
+  if (n == 8 && (ALIGNED || t.al >= 4)) {
+    uint32_t w[8];
+    if (ALIGNED || t.al == 16) {
+#pragma unroll
+      for (int i = 0; i < B / 2; ++i) {
+        const uint4 q = ld_stream(reinterpret_cast<const uint4*>(p) + i);
+        w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+      }
+    } else if (t.al == 8) {
+#pragma unroll
+      for (int i = 0; i < B; ++i) { const uint2 q = reinterpret_cast<const uint2*>(p)[i]; w[2 * i] = q.x; w[2 * i + 1] = q.y; }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * B; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (KIND == LS_F32) v[i] = __uint_as_float(w[i]);
+      else if ((i & 1) == 0) { const float2 q = widen2<KIND>(w[i / 2]); v[i] = q.x; v[i + 1] = q.y; }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? ld_real<KIND>(p + i * B) : 0.f;
+  }
+}
+template <int KIND, bool ALIGNED>
+__device__ __forceinline__ void store8(const RowsOf& t, int64_t row, int c, int n, const float (&v)[8]) {
+  constexpr int B = KIND == LS_F32 ? 4 : 2;
+  char* p = t.p + (row * t.ld + c) * B;
+  if (n == 8 && (ALIGNED || t.al >= 4)) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (KIND == LS_F32) w[i] = __float_as_uint(v[i]);
+      else if ((i & 1) == 0) w[i / 2] = narrow2<KIND>(v[i], v[i + 1]);
+    }
+    if (ALIGNED || t.al == 16) {
+#pragma unroll
+      for (int i = 0; i < B / 2; ++i) st_stream(reinterpret_cast<uint4*>(p) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+    } else if (t.al == 8) {
+#pragma unroll
+      for (int i = 0; i < B; ++i) reinterpret_cast<uint2*>(p)[i] = make_uint2(w[2 * i], w[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * B; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) st_real<KIND>(p + i * B, v[i]);
+  }
+}
+// rounded to the storage type and back
+template <int KIND>
+__device__ __forceinline__ void round8(float (&v)[8]) {
+  if (KIND != LS_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) { const float2 q = widen2<KIND>(narrow2<KIND>(v[i], v[i + 1])); v[i] = q.x; v[i + 1] = q.y; }
+  }
+}
+
+// Codes of 8 entries; the four threads of a block of 32 (lanes 4 i to 4 i + 3) call it together, with the whole warp.
+__device__ __forceinline__ uint2 pack8(const float (&v)[8], uint32_t& byte) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);      // as integers: NaN above infinity above the rest
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const int e = (int)(top >> 23);
+  byte = e == 255 ? 255u : (top == 0 ? 0u : (uint32_t)max(e - 6, 1));
+  const float up = __uint_as_float((254u - (e == 255 ? 1u : byte)) << 23);              // 2^(127 - byte)
+  uint32_t q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    q[i] = __float_as_uint(fminf(fmaxf(v[i] * up, -127.f), 127.f) + 12582912.f);        // 1.5 * 2^23: the integer stands in the low bits
+  uint2 w;
+  w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+  w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+  if (e == 255) w = make_uint2(0u, 0u);
+  return w;
+}
+__device__ __forceinline__ void unpack8(uint2 w, uint32_t byte, float (&v)[8]) {
+  const float s = __uint_as_float(byte << 23);
+  const uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;                          // code + 128
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = (__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + i)) - 8388736.f) * s;  // 2^23 + 128
+    v[4 + i] = (__uint_as_float(__byte_perm(y, 0x4b000000u, 0x7440 + i)) - 8388736.f) * s;
+  }
+}
+__device__ __forceinline__ uint2 ld_codes(const unsigned char* p) {
+  uint2 v;
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+
+// An item is 8 entries of a row, numbered through the rows: item i has its codes at byte 8 i.
+struct ItemWalk {
+  int64_t items;         // rows * per_row
+  int64_t rows;
+  int width, per_row;    // items of a row: 4 * blocks
+};
+__device__ __forceinline__ void item_place(const ItemWalk& k, int64_t i, int64_t& row, int& v) {
+  if (k.items <= 0xffffffffll) { const uint32_t r = (uint32_t)i / (uint32_t)k.per_row; row = r; v = (int)((uint32_t)i - r * (uint32_t)k.per_row); }
+  else { row = i / k.per_row; v = (int)(i - row * k.per_row); }
+}
+// entries of item v of a row that exist
+__device__ __forceinline__ int item_count(const ItemWalk& k, int v) { return max(0, min(8, k.width - 8 * v)); }
+
+__device__ __forceinline__ void store_packed(const PackedRows& t, int64_t row, int v, int64_t item, uint2 codes, uint32_t byte) {
+  asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1,%2};" ::"l"(t.codes + item * 8), "r"(codes.x), "r"(codes.y) : "memory");
+  if ((v & 3) == 0) {
+    unsigned char* e = t.exps + row * t.exp_stride;
+    e[v >> 2] = (unsigned char)byte;
+    if ((v >> 2) == t.blocks - 1)
+      for (int k = t.blocks; k < t.exp_stride; ++k) e[k] = 0;
+  }
+}
+
+template <int KIND, bool ALIGNED, int U>
+__global__ void __launch_bounds__(PK_THREADS) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
+  griddep_chain();
+  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
+  float v[U][8];
+  int64_t row[U];
+  int at[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = first + j * PK_THREADS;
+    item_place(k, min(i, k.items - 1), row[j], at[j]);
+    load8<KIND, ALIGNED>(x, row[j], 8 * at[j], i < k.items ? item_count(k, at[j]) : 0, v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = first + j * PK_THREADS;
+    uint32_t byte;
+    const uint2 w = pack8(v[j], byte);
+    if (i < k.items) store_packed(out, row[j], at[j], i, w, byte);
+  }
+}
+
+template <int KIND, bool ALIGNED, int U>
+__global__ void __launch_bounds__(PK_THREADS) unpack_kernel(const PackedRows in, const RowsOf x, const ItemWalk k) {
+  griddep_chain();
+  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
+  uint2 w[U];
+  uint32_t byte[U];
+  int64_t row[U];
+  int at[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = min(first + j * PK_THREADS, k.items - 1);
+    item_place(k, i, row[j], at[j]);
+    w[j] = ld_codes(in.codes + i * 8);
+    byte[j] = in.exps[row[j] * in.exp_stride + (at[j] >> 2)];
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    float v[8];
+    unpack8(w[j], byte[j], v);
+    if (first + j * PK_THREADS < k.items) store8<KIND, ALIGNED>(x, row[j], 8 * at[j], item_count(k, at[j]), v);
+  }
+}
+
+// ---- gated activation ----
+// y = act(a) u.  With p the activation's gate (the logistic function of z(a), or the normal distribution at a for GELU), act(a) = a p and
+//   act'(a) = p + a p (1 - p) z'(a),   act'(a) = p + a exp(-a^2 / 2) / sqrt(2 pi)  for GELU;
+// the tanh form of GELU is a p with z = 2 sqrt(2 / pi) (a + 0.044715 a^3), since (1 + tanh w) / 2 = 1 / (1 + exp(-2 w)).  With
+// t = exp(-|z|) the logistic function is 1 / (1 + t) or t / (1 + t) and p (1 - p) = t / (1 + t)^2: nothing cancels or overflows.
+enum { ACT_SILU = 0, ACT_GELU = 1, ACT_GELU_TANH = 2 };
+
+// p; s: act'(a)
+template <int ACT>
+__device__ __forceinline__ float act_gate(float a, float& s) {
+  if (ACT == ACT_GELU) {
+    const float p = 0.5f * erfcf(a * -0.70710678118654752f);
+    s = fmaf(a * 0.3989422804014327f, __expf(-0.5f * a * a), p);
+    return p;
+  }
+  const float z = ACT == ACT_SILU ? a : 1.5957691216057308f * fmaf(0.044715f * a * a, a, a);
+  const float t = __expf(-fabsf(z)), r = __fdividef(1.f, 1.f + t), tr = t * r, q = tr * r;
+  const float p = z < 0.f ? tr : r;
+  if (ACT == ACT_SILU) s = fmaf(a, q, p);
+  else s = q == 0.f ? p : fmaf(a * q, 1.5957691216057308f * fmaf(0.134145f * a, a, 1.f), p);      // far out z' overflows where q is 0
+  return p;
+}
+
+struct GatedArgs {
+  RowsOf a, u, y;            // forward; u.p null: y = act(a)
+  RowsOf dy, da, du;         // backward
+  PackedRows pa, pu, py;     // kept inputs; py.codes null: not wanted
+};
+
+template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
+__global__ void __launch_bounds__(PK_THREADS) gated_kernel(const GatedArgs g, const ItemWalk k) {
+  griddep_chain();
+  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
+  float a[U][8], u[U][8];
+  int64_t row[U];
+  int at[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = first + j * PK_THREADS;
+    item_place(k, min(i, k.items - 1), row[j], at[j]);
+    const int n = i < k.items ? item_count(k, at[j]) : 0;
+    load8<KIND, ALIGNED>(g.a, row[j], 8 * at[j], n, a[j]);
+    if (GATED) load8<KIND, ALIGNED>(g.u, row[j], 8 * at[j], n, u[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = first + j * PK_THREADS;
+    const int n = i < k.items ? item_count(k, at[j]) : 0;
+    uint32_t byte;
+    uint2 w;
+    if (g.pa.codes) {
+      w = pack8(a[j], byte);
+      if (i < k.items) store_packed(g.pa, row[j], at[j], i, w, byte);
+      if (GATED) {
+        w = pack8(u[j], byte);
+        if (i < k.items) store_packed(g.pu, row[j], at[j], i, w, byte);
+      }
+    }
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float s;
+      y[e] = a[j][e] * act_gate<ACT>(a[j][e], s);
+      if (GATED) y[e] *= u[j][e];
+    }
+    store8<KIND, ALIGNED>(g.y, row[j], 8 * at[j], n, y);
+  }
+}
+
+template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
+__global__ void __launch_bounds__(PK_THREADS) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
+  griddep_chain();
+  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
+  float dy[U][8];
+  uint2 wa[U], wu[U];
+  uint32_t ba[U], bu[U];
+  int64_t row[U];
+  int at[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = min(first + j * PK_THREADS, k.items - 1);
+    item_place(k, i, row[j], at[j]);
+    wa[j] = ld_codes(g.pa.codes + i * 8);
+    ba[j] = g.pa.exps[row[j] * g.pa.exp_stride + (at[j] >> 2)];
+    if (GATED) {
+      wu[j] = ld_codes(g.pu.codes + i * 8);
+      bu[j] = g.pu.exps[row[j] * g.pu.exp_stride + (at[j] >> 2)];
+    }
+    load8<KIND, ALIGNED>(g.dy, row[j], 8 * at[j], item_count(k, at[j]), dy[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t i = first + j * PK_THREADS;
+    const int n = i < k.items ? item_count(k, at[j]) : 0;
+    float a[8], u[8], f[8];
+    unpack8(wa[j], ba[j], a);
+    if (GATED) unpack8(wu[j], bu[j], u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float s;
+      const float p = act_gate<ACT>(a[e], s);
+      f[e] = a[e] * p;
+      a[e] = GATED ? dy[j][e] * u[e] * s : dy[j][e] * s;
+      if (GATED) { dy[j][e] *= f[e]; f[e] *= u[e]; }
+    }
+    store8<KIND, ALIGNED>(g.da, row[j], 8 * at[j], n, a);
+    if (GATED) store8<KIND, ALIGNED>(g.du, row[j], 8 * at[j], n, dy[j]);
+    if (g.py.codes) {
+      round8<KIND>(f);
+      uint32_t byte;
+      const uint2 w = pack8(f, byte);
+      if (i < k.items) store_packed(g.py, row[j], at[j], i, w, byte);
+    }
+  }
+}
+
+}  // namespace tg
