@@ -258,32 +258,43 @@ EncodeTiledFn encode_tiled() {
   return fn;
 }
 
-struct WgradPlan { int terms, tiles_n, tiles_k, splits; int64_t steps, per_split; bool copy; int64_t ld; size_t parts_bytes, partial_bytes; };
+struct WgradPlan { int terms, tn, tiles_n, tiles_k, splits; int64_t steps, per_split; bool copy; int64_t ld; size_t parts_bytes, partial_bytes; };
 WgradPlan wgrad_plan(const tgrad_weight_grad_args* c, int sm) {
   WgradPlan p;
   const int kind = kind_of(c->dtype);
   p.terms = kind == LS_F32 ? 3 : 1;
   p.copy = kind == LS_F32 || misaligned(c->dy.d_data, 16) || (c->rows > 1 && c->dy.row_stride % 8 != 0);
   p.ld = p.copy ? (c->out + 7) / 8 * 8 : c->rows > 1 ? c->dy.row_stride : (c->out + 7) / 8 * 8;
-  p.tiles_n = (int)((c->out + WG_TILE - 1) / WG_TILE); p.tiles_k = (int)((c->width + WG_TILE - 1) / WG_TILE);
+  p.tn = kind_of(c->out_dtype) == LS_F32 ? 128 : 256;      // columns of x of a tile: the sums of fp32 results have to fit in registers
+  p.tiles_n = (int)((c->out + WG_TILE_N - 1) / WG_TILE_N); p.tiles_k = (int)((c->width + p.tn - 1) / p.tn);
   p.steps = (c->rows + WG_TOKENS - 1) / WG_TOKENS * p.terms;
-  // Parts of the tokens: as many as fill the SMs once, of eight steps at least.
+  // Parts of the tokens: as many as fill the SMs (two to a tile) once, of eight steps at least.
   const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-  int64_t splits = sm / tiles;
+  int64_t splits = sm / 2 / tiles;
   if (splits > p.steps / 8) splits = p.steps / 8;
   if (splits < 1) splits = 1;
   p.per_split = (p.steps + splits - 1) / splits;
   p.splits = (int)(p.per_split ? (p.steps + p.per_split - 1) / p.per_split : 1);
   p.parts_bytes = p.copy ? align_up((size_t)p.terms * c->rows * p.ld * 2) : 0;
-  p.partial_bytes = p.splits > 1 ? align_up((size_t)p.splits * tiles * WG_TILE * WG_TILE * 4) : 0;
+  p.partial_bytes = p.splits > 1 ? align_up((size_t)p.splits * tiles * WG_TILE_N * p.tn * 4) : 0;
   return p;
+}
+template <bool F16, int TN>
+tgrad_status wgrad_launch(const WgradPlan& p, int sm, const CUtensorMap& map_dy, const CUtensorMap& map_codes, const WgradArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  TG_TRY(allow_shared(wgrad_kernel<F16, TN>, WgGeom<TN>::SMEM, done));
+  const int64_t units = (int64_t)p.tiles_n * p.tiles_k * p.splits;
+  const int64_t clusters = units < sm / 2 ? units : sm / 2;
+  launch_cluster(wgrad_kernel<F16, TN>, dim3((unsigned)(2 * clusters)), dim3(WgGeom<TN>::THREADS), WgGeom<TN>::SMEM, 2, st, map_dy, map_codes, a);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
 }
 tgrad_status check_wgrad(const tgrad_weight_grad_args* c) {
   if (!c) return TGRAD_ERR_INVALID_ARG;
   const int kind = kind_of(c->dtype), to = kind_of(c->out_dtype);
   if (kind < 0 || (to != kind && to != LS_F32) || c->rows < 0 || c->out < 1 || c->width < 1) return TGRAD_ERR_INVALID_ARG;
   if (c->out > ((int64_t)1 << 24) || c->width > ((int64_t)1 << 24) || c->rows >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
-  if ((c->out + WG_TILE - 1) / WG_TILE * ((c->width + WG_TILE - 1) / WG_TILE) >= ((int64_t)1 << 24)) return TGRAD_ERR_UNSUPPORTED;
+  if ((c->out + 255) / 256 * ((c->width + 127) / 128) >= ((int64_t)1 << 24)) return TGRAD_ERR_UNSUPPORTED;
   if (bad_rows(c->dy, c->rows, c->out, kind, true) || bad_packed(c->d_packed, c->rows, true)) return TGRAD_ERR_INVALID_ARG;
   if (!c->d_weight.d_data || bad_rows(c->d_weight, c->out, c->width, to, true)) return TGRAD_ERR_INVALID_ARG;
   return TGRAD_OK;
@@ -437,8 +448,9 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   const PackedRows x = packed_of(c->d_packed, c->rows, c->width);
   a.exps = x.exps; a.exp_words = x.exp_stride / 4;
   a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
-  // fp32 results leave tensor memory every 16 steps of the tensor core (4 of 64 tokens), 16-bit ones once
-  a.group = to == LS_F32 ? 4 : 0x7fffffff;
+  // fp32 results leave tensor memory after every 32 instructions (8 steps of 64 tokens), 16-bit ones once
+  a.group = to == LS_F32 ? 8 : 0x7fffffff;
+  a.ld_partial = (int64_t)p.tiles_k * p.tn;
   a.partial = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.parts_bytes) : nullptr;
   const bool f16 = kind == LS_F16;
   CUtensorMap map_dy, map_codes;
@@ -453,21 +465,12 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   {
     const cuuint64_t dims[3] = {(cuuint64_t)(32 * x.blocks), (cuuint64_t)c->rows, 1};
     const cuuint64_t strides[2] = {(cuuint64_t)(32 * x.blocks), (cuuint64_t)(32 * x.blocks) * c->rows};
-    const cuuint32_t box[3] = {WG_TILE, WG_TOKENS, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)p.tn / 2, WG_TOKENS, 1};
     if (enc(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, x.codes, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return TGRAD_ERR_CUDA;
   }
-  const int64_t units = (int64_t)p.tiles_n * p.tiles_k * p.splits;
-  const dim3 grid((unsigned)(units < sm ? units : sm));
-  static std::atomic<uint64_t> done[2];
-  if (f16) {
-    TG_TRY(allow_shared(wgrad_kernel<true>, WG_SMEM, done[0]));
-    launch_chained(wgrad_kernel<true>, grid, dim3(WG_THREADS), WG_SMEM, st, map_dy, map_codes, a);
-  } else {
-    TG_TRY(allow_shared(wgrad_kernel<false>, WG_SMEM, done[1]));
-    launch_chained(wgrad_kernel<false>, grid, dim3(WG_THREADS), WG_SMEM, st, map_dy, map_codes, a);
-  }
-  TG_LAUNCH_CHECK();
+  if (f16) TG_TRY(to == LS_F32 ? (wgrad_launch<true, 128>(p, sm, map_dy, map_codes, a, st)) : (wgrad_launch<true, 256>(p, sm, map_dy, map_codes, a, st)));
+  else TG_TRY(to == LS_F32 ? (wgrad_launch<false, 128>(p, sm, map_dy, map_codes, a, st)) : (wgrad_launch<false, 256>(p, sm, map_dy, map_codes, a, st)));
   if (p.splits > 1) {
     const int64_t blocks = ((int64_t)a.N * ((a.K + 7) / 8) + 255) / 256;
     launch_chained(wgrad_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);

@@ -1,17 +1,23 @@
 // Weight gradient of a linear layer whose input was kept in 8 bits:  dW[n][k] = sum over tokens m of dy[m][n] x^[m][k].
 //
-// A matrix product whose contraction runs over the rows of both operands, on the 5th-generation tensor cores: per tile of 128 columns of dy
-// by 128 of x and step of 64 tokens,
-//   * one thread loads dy's box (64 tokens of two times 64 entries, 128-byte swizzle) and the codes' (64 tokens of 128 bytes) by tiled TMA,
-//     a warp the blocks' bytes (a word a token);
-//   * four warps turn the codes into 16-bit numbers in the layout that the tensor core reads: x^ = code 2^e has 7 bits, so it is exact in
-//     bfloat16, and in fp16 for what was packed from fp16; products are exact in fp32;
-//   * one thread issues tcgen05.mma (both operands with the tile's columns contiguous), accumulators in tensor memory;
+// A matrix product whose contraction runs over the rows of both operands, on the 5th-generation tensor cores.  Two blocks on neighbouring SMs
+// (a cluster, tcgen05 with cta_group::2) share a tile of 256 columns of dy by TN of x; each holds 128 of dy's and TN / 2 of x's.  Per
+// step of 64 tokens, in each block:
+//   * one thread loads dy's boxes (64 tokens of 64 entries, 128-byte swizzle) and the codes' (64 tokens) by tiled TMA, a warp the blocks'
+//     bytes (a word a token);
+//   * eight warps (four where TN is 128) turn the codes into 16-bit numbers in the layout that the tensor core reads: x^ = code 2^e has 7 bits, so it is exact in
+//     bfloat16, and in fp16 for what was packed from fp16; products are exact in fp32.  Two such groups take steps in turn, so that one's
+//     latencies are covered by the other's;
+//   * in the first block one thread issues tcgen05.mma for both (operands with the tile's columns contiguous), accumulators in tensor memory;
 //   * eight warps move the sums out.  The tensor core adds with truncation, which would bias a long sum, so where the result is fp32 it leaves
-//     tensor memory after every few steps and is added up in registers; a 16-bit result stays there for the whole sum.
+//     tensor memory after every few steps and is added up in registers (TN = 128: as many as fit); a 16-bit result stays there for the
+//     whole sum (TN = 256), and tensor memory holds a second tile meanwhile.
+// Why the two blocks: turning 64 tokens of 128 columns into numbers takes four warps about as long as the tensor cores take for 64 x 256 x 256
+// on two SMs, and a tile of 128 x 128 on one SM would have to read its operands from shared memory as fast as that allows (measured: 3.57 ms
+// for 16384 x 4096 x 14336 that way).
 // fp32 dy is split beforehand into three bfloat16 parts that add up to it exactly, which are three times as many steps into the same sums;
 // 16-bit dy that TMA cannot address (rows that do not start at multiples of 16 bytes) is copied beforehand.
-// Few tiles and many tokens: the tokens are split between blocks, whose sums a second launch adds in a fixed order.
+// Few tiles and many tokens: the tokens are split between clusters, whose sums a second launch adds in a fixed order.
 // Every wait is bounded; one that ran out leaves NaN in the tiles that its block did not finish.
 #pragma once
 #include <cuda.h>
@@ -19,13 +25,20 @@
 
 namespace tg {
 
-constexpr int WG_THREADS = 512;        // warp 0: TMA, 1: MMA issue, 2: the blocks' bytes, 3: tensor memory, 4-7: codes to numbers, 8-15: sums
-constexpr int WG_TOKENS = 64, WG_TILE = 128;
+// Warp 0: TMA, 1: MMA issue, 2: the blocks' bytes, 3: tensor memory, then two groups of NW that turn codes into numbers, then 8 for the sums.
+constexpr int WG_TOKENS = 64, WG_TILE_N = 256;
 constexpr int WG_BOX = 64 * 128;                                  // bytes of 64 tokens by 64 16-bit entries
-constexpr int WG_A = 0, WG_B = 2 * WG_BOX, WG_CODES = 4 * WG_BOX, WG_EXPS = 5 * WG_BOX, WG_STAGE = 5 * WG_BOX + 1024;
-constexpr int WG_STAGES = 5;
-constexpr int WG_NUMBER_THREADS = 128, WG_SUM_THREADS = 256;
-constexpr size_t WG_SMEM = (size_t)WG_STAGES * WG_STAGE + 1024;
+// Three rings of shared memory, for three lifetimes: dy's boxes from their copy to the end of the instructions that read them, codes from their copy
+// until they are numbers, numbers from then to the end of the instructions.  (One ring of stages that hold all three has five of them, too few
+// to cover the copies' latency: 588 ns a step instead of the 270 that the tensor cores take.)
+template <int TN> struct WgGeom {
+  static constexpr int H = TN / 2;                                // columns of x of a block
+  static constexpr int NW = TN == 256 ? 8 : 4, THREADS = 32 * (4 + 2 * NW + 8);      // (with fp32 sums, 96 registers a thread)
+  static constexpr int SA = TN == 256 ? 6 : 8, SB = 4;      // places for copies (dy's and codes'), for numbers: even, the groups take every second one
+  static constexpr int A_BYTES = 2 * WG_BOX, B_BYTES = H * WG_TOKENS * 2, C_BYTES = H * WG_TOKENS, E_BYTES = WG_TOKENS * 4;
+  static constexpr int B = SA * A_BYTES, C = B + SB * B_BYTES, E = C + SA * C_BYTES;      // dy's ring stands first
+  static constexpr size_t SMEM = (size_t)E + SA * E_BYTES + 1024;
+};
 constexpr uint32_t WG_WAIT_POLLS = 1u << 22;
 constexpr uint64_t WG_WAIT_NS = 500000000ull;
 
@@ -40,14 +53,49 @@ struct WgradArgs {
   int group;                 // steps between two moves of the sums
   RowsOf out;
   int out_kind, accumulate;
-  float* partial;            // [splits][128 tiles_n][128 tiles_k]
+  float* partial;            // [splits][256 tiles_n][ld_partial]
+  int64_t ld_partial;
 };
 
-__device__ __forceinline__ bool wg_wait(uint64_t* bar, uint32_t parity, volatile int* failed) {
+// ---- two blocks as one ----
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// an arrival at the first block's barrier that stands where `bar` stands in this block.  (Without .release.cluster, which would have the
+// thread wait until its writes are visible in the whole cluster: 600 instead of 1,020 TFLOP/s at 8192 x 2048 x 4608.  What the tensor core
+// reads has been written in its own SM's shared memory and passed the proxy fence, which is what orders it.)
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(bar)));
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc2(uint32_t* smem_result, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_result)), "r"(cols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc2(uint32_t taddr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void umma2_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+               : "memory");
+}
+// both blocks' barriers that stand at `bar` get an arrival once every MMA issued so far has completed
+__device__ __forceinline__ void umma2_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+
+// Waits of whole warps: the result is the same in all lanes, and known to be by the compiler.  What one thread does for its block (copies,
+// tensor-core instructions, their commits) stands in loops that whole warps run and is done by an elected lane: these instructions take
+// their operands from registers of the warp, and in code that the compiler holds for divergent it moves each there by a loop of its own
+// (measured with `if (lane == 0)` around the loops: 870 clocks for the instructions of a step, 588 ns a step in all).
+__device__ __noinline__ bool wg_wait_long(uint64_t* bar, uint32_t parity, volatile int* failed) {
   uint64_t start = 0;
   for (uint32_t i = 0; i < WG_WAIT_POLLS; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 63) == 63) {
+    if ((i & 15) == 15) {
       if (*failed) return false;
       uint64_t now;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
@@ -58,6 +106,23 @@ __device__ __forceinline__ bool wg_wait(uint64_t* bar, uint32_t parity, volatile
   *failed = 1;
   return false;
 }
+__device__ __forceinline__ bool wg_wait(uint64_t* bar, uint32_t parity, volatile int* failed) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const bool ok = wg_wait_long(bar, parity, failed);
+  __syncwarp();
+  return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+// Place in a ring of N and the parity of its barriers.
+template <int N>
+struct WgRing {
+  uint32_t at = 0, parity = 0;
+  __device__ __forceinline__ void next(uint32_t by = 1) { if ((at += by) >= N) { at -= N; parity ^= 1; } }
+};
 
 // Descriptor of a tile whose columns are contiguous (128-byte swizzle): groups of 64 columns WG_BOX bytes apart, groups of 8 tokens 1,024.
 __device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr) {
@@ -77,17 +142,17 @@ __device__ __forceinline__ void wg_tile(const WgradArgs& A, int tile, int& tn, i
 }
 
 // 8 codes to 8 numbers, exact.  The low seven bits of a code stand as mantissa behind 128 (bfloat16 0x4300), the sign bit in the number
-// that is taken from it (128, or 256 with the lowest exponent bit set).
+// that is taken from it (128, or 256 with the lowest exponent bit set).  byte: the block's, in both halves of the word.
 template <bool F16>
 __device__ __forceinline__ uint4 wg_numbers(uint2 w, uint32_t byte) {
   uint32_t r[4];
   if (F16) {
     float v[8];
-    unpack8(w, byte, v);
+    unpack8(w, byte & 255u, v);
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = narrow2<LS_F16>(v[2 * i], v[2 * i + 1]);
   } else {
-    const uint32_t s = byte * 0x00800080u;             // 2^e twice
+    const uint32_t s = byte << 7;                      // 2^e, twice
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t t = __byte_perm(i < 2 ? w.x : w.y, 0u, i & 1 ? 0x4342 : 0x4140);
@@ -115,184 +180,243 @@ __device__ __forceinline__ void wg_store(const WgradArgs& A, int64_t n, int k, c
   store8<KIND, false>(A.out, n, k, cnt, o);
 }
 
-template <bool F16>
-__global__ void __launch_bounds__(WG_THREADS, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes, const WgradArgs A) {
+template <bool F16, int TN>
+__global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes, const WgradArgs A) {
+  typedef WgGeom<TN> G;
+  constexpr int SA = G::SA, SB = G::SB, NW = G::NW;
+  constexpr int KIND = TN == 128 ? LS_F32 : F16 ? LS_F16 : LS_BF16;      // of the result
   extern __shared__ unsigned char wg_raw[];
-  __shared__ __align__(8) uint64_t full[WG_STAGES], ready[WG_STAGES], empty[WG_STAGES], acc_full[2], acc_free[2];
+  // (of ready and acc_free the first block's are used)
+  __shared__ __align__(8) uint64_t full[SA], a_empty[SA], c_empty[SA], ready[SB], b_empty[SB], acc_full[2], acc_free[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int failed_s;
   volatile int* failed = &failed_s;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t raw = smem_u32(wg_raw), stage0 = (raw + 1023u) & ~1023u;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  const uint32_t raw = smem_u32(wg_raw), ring = (raw + 1023u) & ~1023u;
 
   if (tid == 0) {
-    for (int s = 0; s < WG_STAGES; ++s) { mbar_init(&full[s], 33); mbar_init(&ready[s], WG_NUMBER_THREADS); mbar_init(&empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_free[b], WG_SUM_THREADS); }
+    for (int s = 0; s < SA; ++s) { mbar_init(&full[s], 33); mbar_init(&a_empty[s], 1); mbar_init(&c_empty[s], NW); }
+    for (int s = 0; s < SB; ++s) { mbar_init(&ready[s], 2 * NW); mbar_init(&b_empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_free[b], 2 * 8); }
     failed_s = 0;
     fence_mbar_init();
   }
-  if (warp == 3) { tmem_alloc(&tmem_slot, 256); tmem_relinquish(); }
+  if (warp == 3) tmem_alloc2(&tmem_slot, 2 * TN);
   tc_fence_before_sync();
   __syncthreads();
+  cluster_sync();
   tc_fence_after_sync();
   const uint32_t tmem = tmem_slot;
   griddep_chain();
 
-  const int tiles = A.tiles_n * A.tiles_k, units = tiles * A.splits;
+  const int tiles = A.tiles_n * A.tiles_k, units = tiles * A.splits, clusters = gridDim.x >> 1, mine = blockIdx.x >> 1;
   // what a unit (a tile and a part of the tokens) is
   auto steps_of = [&](int unit, int64_t& from) {
     const int64_t sp = unit / tiles;
     from = sp * A.per_split;
     return (uint32_t)max((int64_t)0, min(A.per_split, A.steps - from));
   };
+  bool ok = true;
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t g = 0;                                    // steps so far: stage g % STAGES, round g / STAGES
-      for (int unit = blockIdx.x; unit < units && !*failed; unit += gridDim.x) {
-        int tn, tk; wg_tile(A, unit % tiles, tn, tk);
-        int64_t from; const uint32_t n = steps_of(unit, from);
-        for (uint32_t it = 0; it < n; ++it, ++g) {
-          const int s = g % WG_STAGES;
-          if (!wg_wait(&empty[s], ((g / WG_STAGES) & 1) ^ 1, failed)) break;
-          const int64_t step = from + it;
-          const int chunk = (int)(step / A.terms), term = (int)(step - (int64_t)chunk * A.terms);
-          const uint32_t at = stage0 + s * WG_STAGE;
-          mbar_expect_tx(&full[s], 3 * WG_BOX);
-          tma_load_3d(at + WG_A, &map_dy, tn * WG_TILE, chunk * WG_TOKENS, term, &full[s]);
-          tma_load_3d(at + WG_A + WG_BOX, &map_dy, tn * WG_TILE + 64, chunk * WG_TOKENS, term, &full[s]);
-          tma_load_3d(at + WG_CODES, &map_codes, tk * WG_TILE, chunk * WG_TOKENS, 0, &full[s]);
+    WgRing<SA> a;
+    uint32_t g = 0;
+    for (int unit = mine; unit < units && ok; unit += clusters) {
+      int tn, tk; wg_tile(A, unit % tiles, tn, tk);
+      const int n0 = tn * WG_TILE_N + (int)rank * 128, k0 = tk * TN + (int)rank * G::H;
+      int64_t from; const uint32_t n = steps_of(unit, from);
+      int m0 = (int)(from / A.terms) * WG_TOKENS, term = (int)(from % A.terms);
+      for (uint32_t it = 0; it < n; ++it, ++g, a.next()) {
+        ok = wg_wait(&c_empty[a.at], a.parity ^ 1, failed) && wg_wait(&a_empty[a.at], a.parity ^ 1, failed);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t at = ring + a.at * G::A_BYTES;
+          mbar_expect_tx(&full[a.at], 2 * WG_BOX + G::C_BYTES);
+          tma_load_3d(ring + G::C + a.at * G::C_BYTES, &map_codes, k0, m0, 0, &full[a.at]);
+          tma_load_3d(at, &map_dy, n0, m0, term, &full[a.at]);
+          tma_load_3d(at + WG_BOX, &map_dy, n0 + 64, m0, term, &full[a.at]);
         }
+        __syncwarp();
+        if (++term == A.terms) { term = 0; m0 += WG_TOKENS; }
       }
-      // copies still under way must land before the block's shared memory is given up (only after a wait that ran out)
-      if (*failed)
-        for (uint32_t j = g > WG_STAGES ? g - WG_STAGES : 0; j < g; ++j) mbar_wait_bounded(&full[j % WG_STAGES], (j / WG_STAGES) & 1, 1u << 16);
     }
-    __syncwarp();
+    // the tensor core's arrivals from the other block come in before this one ends, and so do copies after a wait that ran out
+    for (uint32_t j = g > SA ? g - SA : 0; j < g && ok; ++j) ok = wg_wait(&a_empty[j % SA], (j / SA) & 1, failed);
+    for (uint32_t j = g > SB ? g - SB : 0; j < g && ok; ++j) ok = wg_wait(&b_empty[j % SB], (j / SB) & 1, failed);
+    if (!ok)
+      for (uint32_t j = g > SA ? g - SA : 0; j < g; ++j) mbar_wait_bounded(&full[j % SA], (j / SA) & 1, 1u << 16);
   } else if (warp == 1) {
-    if (lane == 0) {
-      // fp32 accumulator, both operands with their columns contiguous (bits 15, 16), 128 x 128
-      const uint32_t idesc = umma_idesc(F16 ? 0 : 1, WG_TILE) | (1u << 15) | (1u << 16);
-      uint32_t g = 0, moves = 0;
-      for (int unit = blockIdx.x; unit < units && !*failed; unit += gridDim.x) {
+    if (rank == 0) {
+      // fp32 accumulator, both operands with their columns contiguous (bits 15, 16), 256 rows
+      const uint32_t idesc = (umma_idesc(F16 ? 0 : 1, TN) & 0x00ffffffu) | (16u << 24) | (1u << 15) | (1u << 16);
+      const uint64_t da0 = umma_desc_mn128(ring), db0 = umma_desc_mn128(ring + G::B);
+      WgRing<SA> a;
+      WgRing<SB> b;
+      WgRing<2> acc;
+      for (int unit = mine; unit < units && ok; unit += clusters) {
         int64_t from; const uint32_t n = steps_of(unit, from);
         uint32_t in_group = 0;
-        for (uint32_t it = 0; it < n; ++it, ++g) {
-          const uint32_t b = moves & 1;
-          if (in_group == 0 && !wg_wait(&acc_free[b], ((moves >> 1) & 1) ^ 1, failed)) break;
-          const int s = g % WG_STAGES;
-          if (!wg_wait(&ready[s], (g / WG_STAGES) & 1, failed)) break;
+        for (uint32_t it = 0; it < n; ++it, a.next(), b.next()) {
+          ok = (in_group != 0 || wg_wait(&acc_free[acc.at], acc.parity ^ 1, failed)) && wg_wait(&ready[b.at], b.parity, failed);      // numbers and dy's boxes of both blocks
+          if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t at = stage0 + s * WG_STAGE;
-          const uint64_t da = umma_desc_mn128(at + WG_A), db = umma_desc_mn128(at + WG_B);
+          const bool last = in_group + 1 == (uint32_t)A.group || it + 1 == n;
+          if (elect_one()) {
+            const uint64_t da = da0 + (uint64_t)(a.at * (G::A_BYTES >> 4)), db = db0 + (uint64_t)(b.at * (G::B_BYTES >> 4));
 #pragma unroll
-          for (int ks = 0; ks < WG_TOKENS / 16; ++ks)      // 16 tokens: two groups of 8
-            umma_ss<false>(tmem + b * WG_TILE, da + (uint64_t)(ks * 2048 >> 4), db + (uint64_t)(ks * 2048 >> 4), idesc, in_group != 0 || ks != 0);
-          umma_commit(&empty[s]);
-          if (++in_group == (uint32_t)A.group || it + 1 == n) { umma_commit(&acc_full[b]); in_group = 0; ++moves; }
+            for (int ks = 0; ks < WG_TOKENS / 16; ++ks)      // 16 tokens: two groups of 8
+              umma2_f16(tmem + acc.at * TN, da + (uint64_t)(ks * 2048 >> 4), db + (uint64_t)(ks * 2048 >> 4), idesc, in_group != 0 || ks != 0);
+            umma2_commit(&b_empty[b.at]);
+            umma2_commit(&a_empty[a.at]);
+            if (last) umma2_commit(&acc_full[acc.at]);
+          }
+          __syncwarp();
+          if (last) { in_group = 0; acc.next(); } else ++in_group;
         }
       }
     }
-    __syncwarp();
   } else if (warp == 2) {
-    uint32_t g = 0;
-    for (int unit = blockIdx.x; unit < units && !*failed; unit += gridDim.x) {
+    WgRing<SA> a;
+    for (int unit = mine; unit < units && ok; unit += clusters) {
       int tn, tk; wg_tile(A, unit % tiles, tn, tk);
+      const int word = (tk * TN + (int)rank * G::H) >> 7;
       int64_t from; const uint32_t n = steps_of(unit, from);
-      for (uint32_t it = 0; it < n; ++it, ++g) {
-        const int s = g % WG_STAGES;
-        if (!wg_wait(&empty[s], ((g / WG_STAGES) & 1) ^ 1, failed)) break;
-        const int64_t m0 = (from + it) / A.terms * WG_TOKENS;
-        unsigned char* to = wg_raw + (stage0 - raw) + s * WG_STAGE + WG_EXPS;
+      int m0 = (int)(from / A.terms) * WG_TOKENS, term = (int)(from % A.terms);
+      for (uint32_t it = 0; it < n; ++it, a.next()) {
+        ok = wg_wait(&c_empty[a.at], a.parity ^ 1, failed);
+        if (!ok) break;
+        unsigned char* to = wg_raw + (ring - raw) + G::E + a.at * G::E_BYTES;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int64_t m = m0 + lane + 32 * h;
-          const bool in = m < A.tokens && tk < A.exp_words;
-          cp_async4(to + 4 * (lane + 32 * h), A.exps + (in ? (m * A.exp_words + tk) * 4 : 0), in ? 4 : 0);
+          const int64_t m = (int64_t)m0 + lane + 32 * h;
+          const bool in = m < A.tokens && word < A.exp_words;
+          cp_async4(to + 4 * (lane + 32 * h), A.exps + (in ? (m * A.exp_words + word) * 4 : 0), in ? 4 : 0);
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[a.at])) : "memory");
+        if (++term == A.terms) { term = 0; m0 += WG_TOKENS; }
       }
     }
     cp_async_wait<0>();
-  } else if (warp >= 4 && warp < 8) {
-    const int w = tid - 128;
-    const int q = w & 15, m_first = w >> 4;              // this thread: columns 8 q .. 8 q + 7 of tokens m_first + 8 i
-    uint32_t g = 0;
-    for (int unit = blockIdx.x; unit < units && !*failed; unit += gridDim.x) {
+  } else if (warp >= 4 && warp < 4 + 2 * NW) {
+    constexpr int Q = G::H / 8, T = 32 * NW, PER = WG_TOKENS * Q / T;      // vectors of 8 columns per token; threads of a group; vectors of a thread
+    const int w = (tid - 128) % T, group = (warp - 4) / NW;
+    const int q = w % Q, m_first = w / Q;                       // this thread: columns 8 q .. of tokens m_first + i T / Q
+    const uint32_t pick = 0x4040u + 0x0101u * (uint32_t)((q >> 2) + (TN == 128 ? 2 * (int)rank : 0));      // the block's byte of a token's word
+    // (T / Q is a multiple of 8: the swizzle of a thread's vectors is the same for all its tokens)
+    const uint32_t from_c = ring + G::C + m_first * G::H + q * 8, from_e = ring + G::E + m_first * 4;
+    const uint32_t to_b = ring + G::B + (q >> 3) * WG_BOX + m_first * 128 + (((q & 7) ^ (m_first & 7)) << 4);
+    WgRing<SA> a;
+    WgRing<SB> b;
+    a.at = b.at = group;                                        // this group's steps: every second one through all units
+    uint32_t skip = group;
+    for (int unit = mine; unit < units && ok; unit += clusters) {
       int64_t from; const uint32_t n = steps_of(unit, from);
-      for (uint32_t it = 0; it < n; ++it, ++g) {
-        const int s = g % WG_STAGES;
-        if (!wg_wait(&full[s], (g / WG_STAGES) & 1, failed)) break;
-        const uint32_t at = stage0 + s * WG_STAGE;
-        uint2 c[8];
-        uint32_t e[8];
+      uint32_t it = skip;
+      for (; it < n; it += 2, a.next(2), b.next(2)) {
+        ok = wg_wait(&full[a.at], a.parity, failed);                // dy's boxes too: the arrival below stands for them as well
+        if (!ok) break;
+        uint2 code[PER];
+        uint32_t e[PER];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int m = m_first + 8 * i;
-          c[i] = lds64(at + WG_CODES + m * 128 + q * 8);
-          e[i] = lds32(at + WG_EXPS + m * 4);
+        for (int i = 0; i < PER; ++i) {
+          code[i] = lds64(from_c + a.at * G::C_BYTES + i * (T / Q) * G::H);
+          e[i] = lds32(from_e + a.at * G::E_BYTES + i * (T / Q) * 4);
         }
+        uint4 r[PER];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int m = m_first + 8 * i;
-          const uint4 r = wg_numbers<F16>(c[i], (e[i] >> (8 * (q >> 2))) & 255u);
-          const uint32_t to = at + WG_B + (q >> 3) * WG_BOX + m * 128 + (((q & 7) ^ (m & 7)) << 4);
-          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w) : "memory");
-        }
+        for (int i = 0; i < PER; ++i) r[i] = wg_numbers<F16>(code[i], __byte_perm(e[i], 0u, pick));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c_empty[a.at]);
+        ok = wg_wait(&b_empty[b.at], b.parity ^ 1, failed);
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to_b + b.at * G::B_BYTES + i * (T / Q) * 128), "r"(r[i].x), "r"(r[i].y), "r"(r[i].z), "r"(r[i].w) : "memory");
         fence_async_smem();
-        mbar_arrive(&ready[s]);
+        __syncwarp();
+        if (lane == 0) arrive_first(&ready[b.at]);
       }
+      skip = it - n;
     }
-  } else if (warp >= 8) {
-    const int quarter = warp & 3, half = (warp - 8) >> 2;  // tensor-memory lanes 32 * quarter .., columns 64 * half ..
-    uint32_t moves = 0;
-    for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+  } else if (warp >= 4 + 2 * NW) {
+    constexpr int W = TN / 2;                              // columns of a warp
+    const int quarter = warp & 3, half = (warp - 4 - 2 * NW) >> 2; // tensor-memory lanes 32 * quarter .., columns W * half ..
+    WgRing<2> acc;
+    for (int unit = mine; unit < units; unit += clusters) {
       int tn, tk; wg_tile(A, unit % tiles, tn, tk);
       int64_t from; const uint32_t n = steps_of(unit, from);
-      const uint32_t groups = (n + A.group - 1) / A.group;
-      float sum[64];
+      const int64_t row = (int64_t)tn * WG_TILE_N + rank * 128 + quarter * 32 + lane;
+      const int col = tk * TN + half * W;
+      // 16 sums of a row: to the split's place, or rounded and stored
+      auto put = [&](int c, const float (&v)[16]) {
+        if (A.partial) {
+          float4* p = reinterpret_cast<float4*>(A.partial + ((int64_t)(unit / tiles) * A.tiles_n * WG_TILE_N + row) * A.ld_partial + c);
 #pragma unroll
-      for (int i = 0; i < 64; ++i) sum[i] = 0.f;
-      for (uint32_t k = 0; k < groups; ++k, ++moves) {
-        const uint32_t b = moves & 1;
-        const bool ok = wg_wait(&acc_full[b], (moves >> 1) & 1, failed);
-        if (!__all_sync(0xffffffffu, ok)) {
+          for (int i = 0; i < 4; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else if (row < A.N) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i) sum[i] = __int_as_float(0x7fffffff);
-          break;
+          for (int i = 0; i < 2; ++i) wg_store<KIND>(A, row, c + 8 * i, v + 8 * i);
         }
+      };
+      const uint32_t lanes = tmem + half * W + ((uint32_t)(quarter * 32) << 16);
+      if (TN == 128) {
+        const uint32_t groups = (n + A.group - 1) / A.group;
+        float sum[W / 16][16];
+#pragma unroll
+        for (int p = 0; p < W / 16; ++p)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[p][i] = 0.f;
+        for (uint32_t k = 0; k < groups && ok; ++k, acc.next()) {
+          ok = wg_wait(&acc_full[acc.at], acc.parity, failed);
+          if (!ok) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int p = 0; p < W / 16; ++p) {
+            uint32_t r[16];
+            tmem_ld16(lanes + acc.at * TN + 16 * p, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[p][i] += __uint_as_float(r[i]);
+          }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) arrive_first(&acc_free[acc.at]);
+        }
+#pragma unroll
+        for (int p = 0; p < W / 16; ++p) {
+          if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[p][i] = __int_as_float(0x7fffffff);
+          }
+          put(col + 16 * p, sum[p]);
+        }
+      } else {
+        ok = ok && wg_wait(&acc_full[acc.at], acc.parity, failed);
         tc_fence_after_sync();
-        const uint32_t ta = tmem + b * WG_TILE + half * 64 + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
+        for (int p = 0; p < W / 16; ++p) {
           uint32_t r[16];
-          tmem_ld16(ta + 16 * p, r);
+          tmem_ld16(lanes + acc.at * TN + 16 * p, r);
           tmem_wait_ld();
+          if (p == W / 16 - 1) {                           // all read: the tensor core may have the place back
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0 && ok) arrive_first(&acc_free[acc.at]);
+          }
+          float v[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sum[16 * p + i] += __uint_as_float(r[i]);
+          for (int i = 0; i < 16; ++i) v[i] = ok ? __uint_as_float(r[i]) : __int_as_float(0x7fffffff);
+          put(col + 16 * p, v);
         }
-        tc_fence_before_sync();
-        mbar_arrive(&acc_free[b]);
-      }
-      const int64_t row = (int64_t)tn * WG_TILE + quarter * 32 + lane;
-      const int col = tk * WG_TILE + half * 64;
-      if (A.partial) {
-        float4* p = reinterpret_cast<float4*>(A.partial + (((int64_t)(unit / tiles) * A.tiles_n * WG_TILE + row) * A.tiles_k) * WG_TILE + col);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = make_float4(sum[4 * i], sum[4 * i + 1], sum[4 * i + 2], sum[4 * i + 3]);
-      } else if (row < A.N) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (A.out_kind == LS_F32) wg_store<LS_F32>(A, row, col + 8 * i, sum + 8 * i);
-          else if (A.out_kind == LS_F16) wg_store<LS_F16>(A, row, col + 8 * i, sum + 8 * i);
-          else wg_store<LS_BF16>(A, row, col + 8 * i, sum + 8 * i);
-        }
+        acc.next();
       }
     }
   }
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 3) tmem_dealloc(tmem, 256);
+  cluster_sync();                                          // no block ends while the other may still read from it or arrive at its barriers
+  if (warp == 3) tmem_dealloc2(tmem, 2 * TN);
 }
 
 // dW from the splits' sums: 8 entries a thread, the splits in order.
@@ -303,7 +427,7 @@ __global__ void __launch_bounds__(256) wgrad_sum_kernel(const WgradArgs A) {
   if (i >= (int64_t)A.N * per) return;
   const int64_t n = i / per;
   const int k = (int)(i - n * per) * 8;
-  const int64_t ld = (int64_t)A.tiles_k * WG_TILE, size = (int64_t)A.tiles_n * WG_TILE * ld;
+  const int64_t ld = A.ld_partial, size = (int64_t)A.tiles_n * WG_TILE_N * ld;
   float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int s = 0; s < A.splits; ++s) {
