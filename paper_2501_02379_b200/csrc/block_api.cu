@@ -210,8 +210,33 @@ NormPlan norm_plan(const tgrad_norm_config* c, int tensors, bool backward, int s
   p.smem = NM_RED_BYTES + (p.shared_params ? params : 0) + ring;
   return p;
 }
+// Whether the kernels for aligned rows of whole vectors take a call.
+bool norm_fast(const NormPlan& p, const ResNormArgs& a, bool backward) {
+  if (p.V > 2 || !p.shared_params || p.stages < 1 || a.width % 8 != 0 || a.gate_rows || a.mode == NM_PLAIN) return false;
+  const RowsOf* rows[6] = {&a.x, &a.f, &a.dh, &a.dx, &a.out0, &a.out1};
+  for (const RowsOf* r : rows)
+    if (r->p && r->al != 16) return false;
+  return true;
+}
+template <int KIND, bool LN, int V>
+tgrad_status norm_fast_launch(const NormPlan& p, const ResNormArgs& a, bool backward, cudaStream_t st) {
+  if (backward) {
+    static std::atomic<uint64_t> done{0};
+    TG_TRY(allow_shared(norm_backward_fast_kernel<KIND, LN, V>, kNormShared, done));
+    launch_chained(norm_backward_fast_kernel<KIND, LN, V>, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
+  } else {
+    static std::atomic<uint64_t> done{0};
+    TG_TRY(allow_shared(norm_forward_fast_kernel<KIND, LN, V>, kNormShared, done));
+    launch_chained(norm_forward_fast_kernel<KIND, LN, V>, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
+  }
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
 template <int KIND, bool LN, int V>
 tgrad_status norm_launch(const NormPlan& p, const ResNormArgs& a, bool backward, cudaStream_t st) {
+  if constexpr (V <= 2) {
+    if (norm_fast(p, a, backward)) return norm_fast_launch<KIND, LN, V>(p, a, backward, st);
+  }
   if (backward) {
     static std::atomic<uint64_t> done{0};
     TG_TRY(allow_shared(norm_backward_kernel<KIND, LN, V>, kNormShared, done));

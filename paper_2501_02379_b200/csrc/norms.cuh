@@ -194,8 +194,12 @@ __device__ __forceinline__ void fill_params(const ResNormArgs& A, float4* ps) {
     const int n = max(0, min(8, A.width - 8 * v));
     float a[8], g[8];
     param8<KIND>(A.w, A.pf32, 0, 8 * v, n, 1.f, a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = i < n ? a[i] : 0.f;      // (0 where there is no entry, also without weights)
     ps[v] = make_float4(a[0], a[1], a[2], a[3]); ps[nv + v] = make_float4(a[4], a[5], a[6], a[7]);
     param8<KIND>(A.pw, A.pf32, 0, 8 * v, n, 1.f, a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = i < n ? a[i] : 0.f;
     if (A.groups == 1 && !A.starts && !A.gate_rows) {
       param8<KIND>(A.gate, A.pf32, 0, 8 * v, n, 1.f, g);
 #pragma unroll
@@ -565,6 +569,429 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
   if (A.mode != NM_NONE && group >= 0) {
     flush(slot_s(team_id + group, 0), s1, false);
     if (LN) flush(slot_s(team_id + group, 1), reinterpret_cast<float (&)[V][8]>(s0), false);
+  }
+}
+
+// ---- the same for what large models run: every row at a multiple of 16 bytes, a width of whole vectors of 8, weights in shared memory ----
+// Per entry these take 9 (forward) and 14 (backward) instructions instead of the general kernels' 40 and 97: pairs of fp32 in one instruction, no
+// tests per entry, and what a reduction separates is kept in registers instead of being read and widened again.
+
+// the pair q of a vector of 8 entries held in 16-byte words
+template <int KIND>
+struct Vec8 {
+  uint4 w[NmPlanes<KIND>::n];
+  __device__ __forceinline__ void take(uint32_t src, uint32_t plane) {
+    w[0] = lds128(src);
+    if (KIND == LS_F32) w[NmPlanes<KIND>::n - 1] = lds128(src + plane);
+  }
+  __device__ __forceinline__ uint64_t pair(int q) const {
+    if (KIND == LS_F32) {
+      const uint4& v = w[q >> 1 ? NmPlanes<KIND>::n - 1 : 0];
+      return q & 1 ? pk2(__uint_as_float(v.z), __uint_as_float(v.w)) : pk2(__uint_as_float(v.x), __uint_as_float(v.y));
+    }
+    const float2 f = widen2<KIND>(q == 0 ? w[0].x : q == 1 ? w[0].y : q == 2 ? w[0].z : w[0].w);
+    return pk2(f.x, f.y);
+  }
+};
+// 4 pairs of a packed vector, times r
+__device__ __forceinline__ void packed_pairs(uint32_t src, int v, float r, uint64_t (&out)[4]) {
+  const uint4 q = lds128(src);
+  const float s = __uint_as_float(((q.z >> (8 * ((v >> 2) & 3))) & 255u) << 23) * r;      // (a power of two: no rounding but that of the products)
+  const uint64_t scale = pk2(s, s), off = pk2(-8388736.f, -8388736.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = (i < 2 ? q.x : q.y) ^ 0x80808080u;
+    const uint64_t c = pk2(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + 2 * (i & 1))), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7441 + 2 * (i & 1))));
+    out[i] = mul2(add2(c, off), scale);
+  }
+}
+template <int KIND>
+__device__ __forceinline__ void store_pairs(const RowsOf& t, int64_t row, int c, const uint64_t (&v)[4]) {
+  constexpr int B = KIND == LS_F32 ? 4 : 2;
+  uint4* p = reinterpret_cast<uint4*>(t.p + (row * t.ld + c) * B);
+  const float2 a = upk2(v[0]), b = upk2(v[1]), d = upk2(v[2]), e = upk2(v[3]);
+  if (KIND == LS_F32) {
+    st_stream(p, make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)));
+    st_stream(p + 1, make_uint4(__float_as_uint(d.x), __float_as_uint(d.y), __float_as_uint(e.x), __float_as_uint(e.y)));
+  } else st_stream(p, make_uint4(narrow2<KIND>(a.x, a.y), narrow2<KIND>(b.x, b.y), narrow2<KIND>(d.x, d.y), narrow2<KIND>(e.x, e.y)));
+}
+// kept copy of 4 pairs, as rounded to the storage type; whole warps
+template <int KIND>
+__device__ __forceinline__ void keep_pairs(const PackedRows& t, int64_t row, int v, int nv, const uint64_t (&x)[4], bool rounded) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 q = upk2(x[i]); f[2 * i] = q.x; f[2 * i + 1] = q.y; }
+  if (!rounded) round8<KIND>(f);
+  uint32_t byte;
+  const uint2 w = pack8(f, byte);
+  if (v < nv) store_packed(t, row, v, row * nv + v, w, byte);
+}
+__device__ __forceinline__ void shared_pairs(const float4* ps, int nv, int which, int v, uint64_t (&out)[4]) {
+  const float4 a = ps[2 * which * nv + v], b = ps[(2 * which + 1) * nv + v];
+  out[0] = pk2(a.x, a.y); out[1] = pk2(a.z, a.w); out[2] = pk2(b.x, b.y); out[3] = pk2(b.z, b.w);
+}
+template <int KIND>
+__device__ __forceinline__ void param_pairs(const RowsOf& t, int pf32, int64_t row, int c, int n, float fill, uint64_t (&out)[4]) {
+  float v[8];
+  param8<KIND>(t, pf32, row, c, n, fill, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = pk2(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ float sum_pair(uint64_t v) { const float2 f = upk2(v); return f.x + f.y; }
+
+template <int KIND, bool LN, int V>
+__global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNormArgs A) {
+  extern __shared__ __align__(16) unsigned char nm_smem[];
+  griddep_chain();
+  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
+  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
+  fill_params<KIND>(A, ps);
+  __syncthreads();
+  const uint32_t plane = blockDim.x * 16;
+  constexpr int P = NmPlanes<KIND>::n * V;
+  const uint32_t base = smem_u32(nm_smem) + NM_RED_BYTES + 64 * nv + threadIdx.x * 16;
+  const int64_t first = (int64_t)blockIdx.x * teams + mine, step = (int64_t)gridDim.x * teams;
+  const int S = A.stages, per = A.mode == NM_NONE ? 1 : 2;
+  const bool folded = A.groups == 1 && !A.starts;
+  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
+  auto issue = [&](int s, int64_t row, bool all) {
+    if (row < A.rows) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
+        if (!all && v >= nv) continue;                   // zeros since the first round
+        fetch8<KIND>(slot(s, 0, j), plane, A.x, row, 8 * v, n);
+        if (A.mode != NM_NONE) fetch8<KIND>(slot(s, 1, j), plane, A.f, row, 8 * v, n);
+      }
+    }
+    cp_async_commit();
+  };
+  for (int s = 0; s < S; ++s) issue(s, first + s * step, true);
+  const float inv = 1.f / (float)A.width;
+  const uint64_t zero = pk2(0.f, 0.f), scale = pk2(A.scale, A.scale);
+  // mean and 1 / deviation of V vectors, which leave without the mean
+  auto stats = [&](uint64_t (&v)[V][4], float& mean, float& rstd) {
+    mean = 0.f;
+    if (LN) {
+      uint64_t s = zero;
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = add2(s, v[j][i]);
+      mean = team.sum(sum_pair(s), 0.f).x * inv;
+      const uint64_t m = pk2(-mean, -mean);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (t + j * A.tpr < nd) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[j][i] = add2(v[j][i], m);
+        }
+    }
+    uint64_t s = zero, r = zero;
+#pragma unroll
+    for (int j = 0; j < V; ++j) { s = fma2(v[j][0], v[j][0], s); r = fma2(v[j][1], v[j][1], r); s = fma2(v[j][2], v[j][2], s); r = fma2(v[j][3], v[j][3], r); }
+    rstd = rsqrtf(fmaf(team.sum(sum_pair(add2(s, r)), 0.f).x, inv, A.eps));
+  };
+  int s = 0;
+  for (int64_t row = first; row < A.rows; row += step) {
+    wait_stages(S - 1);
+    uint64_t x[V][4];
+    float mean, rstd;
+    if (A.mode != NM_NONE) {
+      uint64_t f[V][4];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        Vec8<KIND> w;
+        w.take(slot(s, 1, j), plane);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[j][i] = w.pair(i);
+        if (A.pf.codes) keep_pairs<KIND>(A.pf, row, t + j * A.tpr, nv, f[j], true);
+      }
+      stats(f, mean, rstd);
+      if (A.stats && t == 0) { A.stats[row] = rstd; if (LN) A.stats[2 * A.rows + row] = mean; }
+      const int g = folded ? 0 : group_of(A, row);
+      const uint64_t r = pk2(rstd, rstd);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
+        Vec8<KIND> w;
+        w.take(slot(s, 0, j), plane);
+        uint64_t p[4], q[4], b[4];
+        if (n) shared_pairs(ps, nv, 1, v, p);
+        else p[0] = p[1] = p[2] = p[3] = zero;
+        if (LN && A.pb.p) {
+          param_pairs<KIND>(A.pb, A.pf32, 0, 8 * v, n, 0.f, b);
+          if (folded && A.gate.p) {
+            param_pairs<KIND>(A.gate, A.pf32, 0, 8 * v, n, 1.f, q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = mul2(b[i], q[i]);
+          }
+        }
+        if (!folded) param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, n, 1.f, q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint64_t d = mul2(mul2(f[j][i], r), p[i]);
+          if (LN && A.pb.p) d = add2(d, b[i]);
+          if (!folded) d = mul2(d, q[i]);
+          if (!folded && g < 0) d = zero;                // a row of no group: whatever stands in f
+          x[j][i] = fma2(scale, w.pair(i), d);
+        }
+      }
+    } else {
+      if (A.stats && t == 0) { A.stats[row] = 1.f; if (LN) A.stats[2 * A.rows + row] = 0.f; }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        Vec8<KIND> w;
+        w.take(slot(s, 0, j), plane);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j][i] = mul2(scale, w.pair(i));
+      }
+    }
+    issue(s, row + S * step, false);                     // the row's places are read: the next one that will stand there
+    s = s + 1 == S ? 0 : s + 1;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int v = t + j * A.tpr;
+      if (A.out0.p && v < nd) store_pairs<KIND>(A.out0, row, 8 * v, x[j]);
+      if (A.px.codes) keep_pairs<KIND>(A.px, row, v, nv, x[j], false);
+    }
+    stats(x, mean, rstd);
+    if (A.stats && t == 0) { A.stats[A.rows + row] = rstd; if (LN) A.stats[3 * A.rows + row] = mean; }
+    const uint64_t r = pk2(rstd, rstd);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
+      uint64_t p[4], b[4];
+      if (n) shared_pairs(ps, nv, 0, v, p);
+      else p[0] = p[1] = p[2] = p[3] = zero;
+      if (LN && A.b.p) param_pairs<KIND>(A.b, A.pf32, 0, 8 * v, n, 0.f, b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[j][i] = mul2(x[j][i], r);
+        x[j][i] = LN && A.b.p ? fma2(x[j][i], p[i], b[i]) : mul2(x[j][i], p[i]);
+      }
+      if (n) store_pairs<KIND>(A.out1, row, 8 * v, x[j]);
+      if (A.ph.codes) keep_pairs<KIND>(A.ph, row, v, nv, x[j], false);
+    }
+  }
+  cp_async_wait<0>();
+}
+
+template <int KIND, bool LN, int V>
+__global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNormArgs A) {
+  extern __shared__ __align__(16) unsigned char nm_smem[];
+  griddep_chain();
+  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
+  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
+  fill_params<KIND>(A, ps);
+  __syncthreads();
+  const uint32_t plane = blockDim.x * 16;
+  constexpr int P = NmPlanes<KIND>::n * V;
+  const uint32_t ring = NM_RED_BYTES + 64 * nv;
+  const uint32_t base = smem_u32(nm_smem) + ring + threadIdx.x * 16;
+  const int64_t team_id = (int64_t)blockIdx.x * teams + mine;
+  const int64_t first = team_id * A.chunk, last = min(first + A.chunk, A.rows);
+  const int S = A.stages, T_DX = 2, T_F = A.dx.p ? 3 : 2, per = T_F + (A.mode != NM_NONE ? 1 : 0);
+  const bool folded = A.groups == 1 && !A.starts;
+  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
+  auto issue = [&](int s, int64_t row, bool all) {
+    if (row < last) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
+        if (!all && v >= nv) continue;                   // zeros since the first round
+        fetch8<KIND>(slot(s, 0, j), plane, A.dh, row, 8 * v, n);
+        if (A.px.codes) { if (v < nv) fetch8_packed(slot(s, 1, j), A.px, row, v); }
+        else fetch8<KIND>(slot(s, 1, j), plane, A.x, row, 8 * v, n);
+        if (A.dx.p) fetch8<KIND>(slot(s, T_DX, j), plane, A.dx, row, 8 * v, n);
+        if (A.mode != NM_NONE) {
+          if (A.pf.codes) { if (v < nv) fetch8_packed(slot(s, T_F, j), A.pf, row, v); }
+          else fetch8<KIND>(slot(s, T_F, j), plane, A.f, row, 8 * v, n);
+        }
+      }
+    }
+    cp_async_commit();
+  };
+  const uint64_t zero = pk2(0.f, 0.f), scale = pk2(A.scale, A.scale);
+  // (entries - mean) / deviation of a vector
+  auto unit = [&](uint32_t at, const PackedRows& packed, int v, float mean, float rstd, uint64_t (&out)[4]) {
+    if (packed.codes) {
+      if (v < nv) packed_pairs(at, v, LN ? 1.f : rstd, out);
+      else out[0] = out[1] = out[2] = out[3] = zero;
+      if (!LN) return;
+    } else {
+      Vec8<KIND> w;
+      w.take(at, plane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = w.pair(i);
+    }
+    const uint64_t m = pk2(-mean, -mean), r = pk2(rstd, rstd);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = mul2(LN ? add2(out[i], m) : out[i], r);
+  };
+  uint64_t sw[V][4], s1[V][4], sb[LN ? V : 1][4], s0[LN ? V : 1][4];
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { sw[j][i] = s1[j][i] = zero; if (LN) sb[LN ? j : 0][i] = s0[LN ? j : 0][i] = zero; }
+  const int nw = LN ? 2 : 1;
+  const int64_t slots = A.combine ? gridDim.x : (int64_t)gridDim.x * teams;
+  auto flush = [&](float* to, const uint64_t (&a)[4], int j) {
+    const int v = t + j * A.tpr;
+    if (v >= nv) return;
+    const float2 f0 = upk2(a[0]), f1 = upk2(a[1]), f2 = upk2(a[2]), f3 = upk2(a[3]);
+    reinterpret_cast<float4*>(to + 8 * v)[0] = make_float4(f0.x, f0.y, f1.x, f1.y);
+    reinterpret_cast<float4*>(to + 8 * v)[1] = make_float4(f2.x, f2.y, f3.x, f3.y);
+  };
+  auto slot_w = [&](int64_t k, int which) { return A.part + (k * nw + which) * A.part_stride; };
+  auto slot_s = [&](int64_t k, int which) { return A.part + ((slots + k) * nw + which) * A.part_stride; };
+  for (int s = 0; s < S; ++s) issue(s, first + s, true);
+  const float inv = 1.f / (float)A.width;
+  int s = 0, group = -1;
+  float4 next = make_float4(1.f, 1.f, 0.f, 0.f);       // the statistics of a row, read a row ahead
+  auto read_stats = [&](int64_t row) {
+    if (row >= last) return;
+    next.y = A.stats[A.rows + row];
+    if (LN) next.w = A.stats[3 * A.rows + row];
+    if (A.mode == NM_POST) { next.x = A.stats[row]; if (LN) next.z = A.stats[2 * A.rows + row]; }
+  };
+  read_stats(first);
+  for (int64_t row = first; row < last; ++row) {
+    wait_stages(S - 1);
+    const float r0 = next.x, r1 = next.y, m0 = next.z, m1 = next.w;
+    read_stats(row + 1);
+    uint64_t e[V][4], u[V][4], su = zero, sd = zero;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int v = t + j * A.tpr;
+      Vec8<KIND> d;
+      d.take(slot(s, 0, j), plane);
+      unit(slot(s, 1, j), A.px, v, m1, r1, u[j]);
+      uint64_t w[4];
+      if (v < nv) shared_pairs(ps, nv, 0, v, w);
+      else w[0] = w[1] = w[2] = w[3] = zero;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t di = d.pair(i);
+        sw[j][i] = fma2(di, u[j][i], sw[j][i]);
+        if (LN) sb[LN ? j : 0][i] = add2(sb[LN ? j : 0][i], di);
+        e[j][i] = mul2(di, w[i]);
+        su = fma2(e[j][i], u[j][i], su);
+        if (LN) sd = add2(sd, e[j][i]);
+      }
+    }
+    float2 c = team.sum(sum_pair(su), LN ? sum_pair(sd) : 0.f);
+    c.x *= -inv; c.y *= -inv;
+    int g = 0;
+    if (!folded) {
+      g = group_of(A, row);
+      if (g != group) {                                  // another sequence: its own column sums
+        if (group >= 0) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) { flush(slot_s(team_id + group, 0), s1[j], j); if (LN) flush(slot_s(team_id + group, 1), s0[LN ? j : 0], j); }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { s1[j][i] = zero; if (LN) s0[LN ? j : 0][i] = zero; }
+        group = g;
+      }
+    }
+    const uint64_t cu = pk2(c.x, c.x), cd = pk2(c.y, c.y), r = pk2(r1, r1);
+    su = sd = zero;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int v = t + j * A.tpr;
+      Vec8<KIND> x;
+      if (A.dx.p) x.take(slot(s, T_DX, j), plane);
+      uint64_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint64_t k = fma2(u[j][i], cu, e[j][i]);
+        if (LN) k = add2(k, cd);
+        e[j][i] = A.dx.p ? fma2(r, k, x.pair(i)) : mul2(r, k);
+        o[i] = mul2(scale, e[j][i]);
+      }
+      if (v < nd) store_pairs<KIND>(A.out0, row, 8 * v, o);
+      if (A.mode != NM_NONE) {
+        unit(slot(s, T_F, j), A.pf, v, m0, r0, u[j]);
+        uint64_t p[4], q[4];
+        if (v < nv) shared_pairs(ps, nv, 1, v, p);
+        else p[0] = p[1] = p[2] = p[3] = zero;
+        if (!folded) {
+          param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, v < nd ? 8 : 0, 1.f, q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], q[i]);
+          if (g < 0) {                                   // a row of no group: whatever stands in f
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[j][i] = e[j][i] = zero;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s1[j][i] = fma2(e[j][i], u[j][i], s1[j][i]);
+          if (LN) s0[LN ? j : 0][i] = add2(s0[LN ? j : 0][i], e[j][i]);
+          e[j][i] = mul2(e[j][i], p[i]);
+          su = fma2(e[j][i], u[j][i], su);
+          if (LN) sd = add2(sd, e[j][i]);
+        }
+      }
+    }
+    issue(s, row + S, false);
+    s = s + 1 == S ? 0 : s + 1;
+    if (A.mode != NM_NONE) {
+      c = team.sum(sum_pair(su), LN ? sum_pair(sd) : 0.f);
+      c.x *= -inv; c.y *= -inv;
+      const uint64_t fu = pk2(c.x, c.x), fd = pk2(c.y, c.y), f = pk2(r0, r0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr;
+        uint64_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint64_t k = fma2(u[j][i], fu, e[j][i]);
+          if (LN) k = add2(k, fd);
+          o[i] = g < 0 ? zero : mul2(f, k);
+        }
+        if (v < nd) store_pairs<KIND>(A.out1, row, 8 * v, o);
+      }
+    }
+  }
+  cp_async_wait<0>();
+  if (!A.part) return;
+  if (A.combine && teams > 1) {
+    // the block's teams, one kind of sum after the other, through the ring's memory
+    float* buf = reinterpret_cast<float*>(nm_smem + ring);
+    auto join = [&](float* to, const uint64_t (&a)[V][4]) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) flush(buf + (int64_t)mine * A.part_stride, a[j], j);
+      __syncthreads();
+      for (int c = threadIdx.x; c < A.part_stride; c += blockDim.x) {
+        float v = 0.f;
+        for (int k = 0; k < teams; ++k) v += buf[(int64_t)k * A.part_stride + c];
+        to[c] = v;
+      }
+    };
+    join(slot_w(blockIdx.x, 0), sw);
+    if constexpr (LN) join(slot_w(blockIdx.x, 1), sb);
+    if (A.mode != NM_NONE) {
+      join(slot_s(blockIdx.x, 0), s1);
+      if constexpr (LN) join(slot_s(blockIdx.x, 1), s0);
+    }
+    return;
+  }
+  const int at = A.mode == NM_NONE ? -1 : folded ? 0 : group;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    flush(slot_w(team_id, 0), sw[j], j);
+    if (LN) flush(slot_w(team_id, 1), sb[LN ? j : 0], j);
+    if (at >= 0) {
+      flush(slot_s(team_id + at, 0), s1[j], j);
+      if (LN) flush(slot_s(team_id + at, 1), s0[LN ? j : 0], j);
+    }
   }
 }
 
