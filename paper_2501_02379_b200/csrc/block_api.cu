@@ -210,32 +210,42 @@ NormPlan norm_plan(const tgrad_norm_config* c, int tensors, bool backward, int s
   p.smem = NM_RED_BYTES + (p.shared_params ? params : 0) + ring;
   return p;
 }
-// Whether the kernels for aligned rows of whole vectors take a call.
-bool norm_fast(const NormPlan& p, const ResNormArgs& a, bool backward) {
-  if (p.V > 2 || !p.shared_params || p.stages < 1 || a.width % 8 != 0 || a.gate_rows || a.mode == NM_PLAIN) return false;
+// Whether the kernels for aligned rows of whole vectors take a call, and with which ring.
+bool norm_fast(NormPlan& p, const ResNormArgs& a, int kind, bool backward) {
+  if (p.V > 2 || a.width % 8 != 0 || a.gate_rows || a.mode == NM_PLAIN) return false;
+  if (backward && (a.mode != NM_POST || !a.dx.p || a.px.codes)) return false;
   const RowsOf* rows[6] = {&a.x, &a.f, &a.dh, &a.dx, &a.out0, &a.out1};
   for (const RowsOf* r : rows)
     if (r->p && r->al != 16) return false;
-  return true;
+  const int64_t each = backward ? p.chunk : (a.rows + (int64_t)p.grid * p.teams - 1) / ((int64_t)p.grid * p.teams);
+  if (each * p.teams <= 2) return false;             // filling shared memory with the weights would not pay
+  const size_t row = (size_t)a.width * bytes_of(kind), fixed = NM_RED_BYTES + NM_BARS + 256 * (size_t)a.blocks;
+  const size_t stage = p.teams * (backward ? 3 * row + (a.pf.codes ? 32 * (size_t)a.blocks : row) : (a.mode == NM_NONE ? 1 : 2) * row);
+  if (fixed + stage > kNormShared) return false;
+  int64_t stages = (int64_t)((kNormShared - fixed) / stage);
+  if (stages > NM_MAX_STAGES) stages = NM_MAX_STAGES;
+  if (stages > each) stages = each;
+  p.stages = (int)stages;
+  const size_t join = p.combine ? (size_t)p.teams * 128 * a.blocks : 0, ring = stages * stage;
+  p.smem = fixed + (ring < join ? join : ring);
+  return p.smem <= kNormShared;
 }
 template <int KIND, bool LN, int V>
-tgrad_status norm_fast_launch(const NormPlan& p, const ResNormArgs& a, bool backward, cudaStream_t st) {
-  if (backward) {
-    static std::atomic<uint64_t> done{0};
-    TG_TRY(allow_shared(norm_backward_fast_kernel<KIND, LN, V>, kNormShared, done));
-    launch_chained(norm_backward_fast_kernel<KIND, LN, V>, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
-  } else {
-    static std::atomic<uint64_t> done{0};
-    TG_TRY(allow_shared(norm_forward_fast_kernel<KIND, LN, V>, kNormShared, done));
-    launch_chained(norm_forward_fast_kernel<KIND, LN, V>, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
-  }
+tgrad_status norm_fast_launch(const NormPlan& p, ResNormArgs& a, bool backward, cudaStream_t st) {
+  static std::atomic<uint64_t> done[3];
+  const int which = !backward ? 0 : a.pf.codes ? 1 : 2;
+  void (*kern)(ResNormArgs) = which == 0 ? norm_forward_fast_kernel<KIND, LN, V> : which == 1 ? norm_backward_fast_kernel<KIND, LN, V, true> : norm_backward_fast_kernel<KIND, LN, V, false>;
+  TG_TRY(allow_shared(kern, kNormShared, done[which]));
+  a.stages = p.stages;
+  launch_chained(kern, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
 template <int KIND, bool LN, int V>
-tgrad_status norm_launch(const NormPlan& p, const ResNormArgs& a, bool backward, cudaStream_t st) {
+tgrad_status norm_launch(const NormPlan& p, ResNormArgs& a, bool backward, cudaStream_t st) {
   if constexpr (V <= 2) {
-    if (norm_fast(p, a, backward)) return norm_fast_launch<KIND, LN, V>(p, a, backward, st);
+    NormPlan fast = p;
+    if (norm_fast(fast, a, KIND, backward)) return norm_fast_launch<KIND, LN, V>(fast, a, backward, st);
   }
   if (backward) {
     static std::atomic<uint64_t> done{0};
@@ -250,7 +260,7 @@ tgrad_status norm_launch(const NormPlan& p, const ResNormArgs& a, bool backward,
   return TGRAD_OK;
 }
 template <int KIND, bool LN>
-tgrad_status norm_vectors(const NormPlan& p, const ResNormArgs& a, bool backward, cudaStream_t st) {
+tgrad_status norm_vectors(const NormPlan& p, ResNormArgs& a, bool backward, cudaStream_t st) {
   return p.V == 1 ? norm_launch<KIND, LN, 1>(p, a, backward, st) : p.V == 2 ? norm_launch<KIND, LN, 2>(p, a, backward, st) : norm_launch<KIND, LN, 4>(p, a, backward, st);
 }
 tgrad_status norm_kind(int kind, bool layer, const NormPlan& p, ResNormArgs& a, bool backward, cudaStream_t st) {

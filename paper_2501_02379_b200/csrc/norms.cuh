@@ -89,11 +89,17 @@ __device__ __forceinline__ void cp_async4u(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void sts32(uint32_t dst, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts128(uint32_t dst, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v; asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory"); return v;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v; asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory"); return v;
+}
+__device__ __forceinline__ void bulk_g2s_at(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {      // bulk_g2s to a shared address
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory"); return v; }
 
@@ -138,8 +144,9 @@ __device__ __forceinline__ void take8(uint32_t src, uint32_t plane, float (&v)[8
 }
 // packed entries: 8 bytes of codes and the word that holds the block's byte
 __device__ __forceinline__ void fetch8_packed(uint32_t dst, const PackedRows& t, int64_t row, int v) {
-  cp_async8u(dst, t.codes + (row * t.blocks * 4 + v) * 8);
-  cp_async4u(dst + 8, t.exps + row * t.exp_stride + ((v >> 2) & ~3));
+  const unsigned char *codes = t.codes + row * t.blocks * 32, *exps = t.exps + row * t.exp_stride;
+  cp_async8u(dst, codes + (uint32_t)v * 8u);
+  cp_async4u(dst + 8, exps + (uint32_t)((v >> 2) & ~3));
 }
 __device__ __forceinline__ void take8_packed(uint32_t src, int v, float (&out)[8]) {
   const uint4 q = lds128(src);
@@ -154,18 +161,21 @@ struct RowTeam {
     if (warps == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
   }
-  // sums of a and b over the team, the same bits in every thread
+  // sums of a and b (TWO) over the team, the same bits in every thread
+  template <bool TWO>
   __device__ __forceinline__ float2 sum(float a, float b) {
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); b += __shfl_xor_sync(0xffffffffu, b, m); }
+    for (int m = 16; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); if (TWO) b += __shfl_xor_sync(0xffffffffu, b, m); }
     if (warps == 1) return make_float2(a, b);
     float2* r = red + (turn ^= 32);
-    if (lane == 0) r[warp] = make_float2(a, b);
+    if (lane == 0) { if (TWO) r[warp] = make_float2(a, b); else r[warp].x = a; }
     sync();
-    const float2 o = lane < warps ? r[lane] : make_float2(0.f, 0.f);
-    a = o.x; b = o.y;
+    a = lane < warps ? r[lane].x : 0.f;
+    if (TWO) b = lane < warps ? r[lane].y : 0.f;
+    if (warps > 16) { a += __shfl_xor_sync(0xffffffffu, a, 16); if (TWO) b += __shfl_xor_sync(0xffffffffu, b, 16); }
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); b += __shfl_xor_sync(0xffffffffu, b, m); }
+    for (int m = 8; m > 0; m >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, m); if (TWO) b += __shfl_xor_sync(0xffffffffu, b, m); }
+    if (warps <= 16) { a = __shfl_sync(0xffffffffu, a, 0); if (TWO) b = __shfl_sync(0xffffffffu, b, 0); }      // (lanes 16 to 31 have summed zeros)
     return make_float2(a, b);
   }
 };
@@ -227,7 +237,7 @@ __device__ __forceinline__ void row_stats(RowTeam& team, const int (&n)[V], floa
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[i];           // (entries that do not exist are 0)
     }
-    mean = team.sum(s, 0.f).x * inv;
+    mean = team.sum<false>(s, 0.f).x * inv;
   }
   float s = 0.f;
 #pragma unroll
@@ -236,7 +246,7 @@ __device__ __forceinline__ void row_stats(RowTeam& team, const int (&n)[V], floa
 #pragma unroll
     for (int i = 0; i < 8; ++i) { const float d = LN && i >= n[j] ? 0.f : v[i] - mean; s = fmaf(d, d, s); }
   }
-  rstd = rsqrtf(fmaf(team.sum(s, 0.f).x, inv, eps));
+  rstd = rsqrtf(fmaf(team.sum<false>(s, 0.f).x, inv, eps));
 }
 
 template <int KIND, bool LN, int V>
@@ -467,7 +477,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
         if (LN) sum_d += e;
       }
     }
-    float2 c = team.sum(sum_u, sum_d);
+    float2 c = team.sum<LN>(sum_u, sum_d);
     c.x *= inv; c.y *= inv;
     int g = -1;
     if (A.mode != NM_NONE) {
@@ -521,7 +531,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
     }
     if (A.mode != NM_NONE) {
       c = make_float2(0.f, 0.f);
-      if (A.mode == NM_POST) { c = team.sum(sum_u, sum_d); c.x *= inv; c.y *= inv; }
+      if (A.mode == NM_POST) { c = team.sum<LN>(sum_u, sum_d); c.x *= inv; c.y *= inv; }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         float f[8];
@@ -573,30 +583,68 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
 }
 
 // ---- the same for what large models run: every row at a multiple of 16 bytes, a width of whole vectors of 8, weights in shared memory ----
-// Per entry these take 9 (forward) and 14 (backward) instructions instead of the general kernels' 40 and 97: pairs of fp32 in one instruction, no
-// tests per entry, and what a reduction separates is kept in registers instead of being read and widened again.
+// Per entry these take a fraction of the general kernels' instructions (40 forward, 97 backward): rows come by bulk copies that one thread of a row's
+// team issues some rows ahead, into places that are free once the team's next barrier, which the reductions have anyway, is passed; pairs of fp32 in
+// one instruction; no tests per entry; what a reduction separates is kept in registers instead of being read and widened again.
+// A wait for a copy is bounded; one that ran out turns all results of its team's further rows, and the column sums, to NaN.
 
-// the pair q of a vector of 8 entries held in 16-byte words
-template <int KIND>
-struct Vec8 {
-  uint4 w[NmPlanes<KIND>::n];
-  __device__ __forceinline__ void take(uint32_t src, uint32_t plane) {
-    w[0] = lds128(src);
-    if (KIND == LS_F32) w[NmPlanes<KIND>::n - 1] = lds128(src + plane);
-  }
-  __device__ __forceinline__ uint64_t pair(int q) const {
-    if (KIND == LS_F32) {
-      const uint4& v = w[q >> 1 ? NmPlanes<KIND>::n - 1 : 0];
-      return q & 1 ? pk2(__uint_as_float(v.z), __uint_as_float(v.w)) : pk2(__uint_as_float(v.x), __uint_as_float(v.y));
+constexpr uint32_t NM_WAIT_POLLS = 1u << 20;
+constexpr uint64_t NM_WAIT_NS = 500000000ull;
+__device__ __noinline__ bool nm_wait_long(uint64_t* bar, uint32_t parity) {
+  uint64_t start = 0;
+  for (uint32_t i = 0; i < NM_WAIT_POLLS; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 15) == 15) {
+      uint64_t now;
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+      if (start == 0) start = now;
+      else if (now - start > NM_WAIT_NS) break;
     }
-    const float2 f = widen2<KIND>(q == 0 ? w[0].x : q == 1 ? w[0].y : q == 2 ? w[0].z : w[0].w);
-    return pk2(f.x, f.y);
   }
+  return false;
+}
+// A team's places for rows.  poison: NaN once a copy has not come, 0 before.
+struct NmRing {
+  uint64_t* bars;
+  int stages, at = 0;
+  uint32_t parity = 0, failed = 0;      // failed: 1 + the place and parity whose copy did not come
+  float poison = 0.f;
+  __device__ __forceinline__ void wait() {
+    if (failed == 0 && !mbar_try_wait(&bars[at], parity) && !nm_wait_long(&bars[at], parity)) {
+      poison = __int_as_float(0x7fffffff);
+      failed = 1 + 2 * at + parity;
+    }
+  }
+  __device__ __forceinline__ void next() { if (++at == stages) { at = 0; parity ^= 1; } }
 };
-// 4 pairs of a packed vector, times r
-__device__ __forceinline__ void packed_pairs(uint32_t src, int v, float r, uint64_t (&out)[4]) {
-  const uint4 q = lds128(src);
-  const float s = __uint_as_float(((q.z >> (8 * ((v >> 2) & 3))) & 255u) << 23) * r;      // (a power of two: no rounding but that of the products)
+// After a wait that ran out nothing more is copied; what is under way has to land before shared memory is given up.
+__device__ __noinline__ void nm_settle(uint64_t* bars, int stages, uint32_t failed) {
+  for (int k = 0; k < stages; ++k) {
+    const int s = ((int)(failed - 1) >> 1) + k;
+    nm_wait_long(&bars[s % stages], ((failed - 1) ^ (uint32_t)(s >= stages)) & 1u);
+  }
+}
+
+template <int KIND> __device__ __forceinline__ const char* row_of(const RowsOf& t, int64_t row) { return t.p + row * t.ld * (KIND == LS_F32 ? 4 : 2); }
+// the pairs of vector v of a row that starts at `row`
+template <int KIND>
+__device__ __forceinline__ void take_pairs(uint32_t row, uint32_t v, uint64_t (&out)[4]) {
+  if (KIND == LS_F32) {
+    const uint4 a = lds128(row + v * 32), b = lds128(row + v * 32 + 16);
+    out[0] = pk2(__uint_as_float(a.x), __uint_as_float(a.y)); out[1] = pk2(__uint_as_float(a.z), __uint_as_float(a.w));
+    out[2] = pk2(__uint_as_float(b.x), __uint_as_float(b.y)); out[3] = pk2(__uint_as_float(b.z), __uint_as_float(b.w));
+  } else {
+    const uint4 a = lds128(row + v * 16);
+    float2 f = widen2<KIND>(a.x); out[0] = pk2(f.x, f.y);
+    f = widen2<KIND>(a.y); out[1] = pk2(f.x, f.y);
+    f = widen2<KIND>(a.z); out[2] = pk2(f.x, f.y);
+    f = widen2<KIND>(a.w); out[3] = pk2(f.x, f.y);
+  }
+}
+// the same of a packed row, times r
+__device__ __forceinline__ void take_packed(uint32_t row, uint32_t v, uint32_t byte, float r, uint64_t (&out)[4]) {
+  const uint2 q = lds64(row + v * 8);
+  const float s = __uint_as_float(byte << 23) * r;      // (a power of two: no rounding but that of the products)
   const uint64_t scale = pk2(s, s), off = pk2(-8388736.f, -8388736.f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -606,10 +654,9 @@ __device__ __forceinline__ void packed_pairs(uint32_t src, int v, float r, uint6
   }
 }
 template <int KIND>
-__device__ __forceinline__ void store_pairs(const RowsOf& t, int64_t row, int c, const uint64_t (&v)[4]) {
-  constexpr int B = KIND == LS_F32 ? 4 : 2;
-  uint4* p = reinterpret_cast<uint4*>(t.p + (row * t.ld + c) * B);
-  const float2 a = upk2(v[0]), b = upk2(v[1]), d = upk2(v[2]), e = upk2(v[3]);
+__device__ __forceinline__ void store_pairs(const char* row, uint32_t v, const uint64_t (&x)[4]) {
+  const float2 a = upk2(x[0]), b = upk2(x[1]), d = upk2(x[2]), e = upk2(x[3]);
+  uint4* p = reinterpret_cast<uint4*>(const_cast<char*>(row) + v * (KIND == LS_F32 ? 32u : 16u));
   if (KIND == LS_F32) {
     st_stream(p, make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)));
     st_stream(p + 1, make_uint4(__float_as_uint(d.x), __float_as_uint(d.y), __float_as_uint(e.x), __float_as_uint(e.y)));
@@ -626,9 +673,10 @@ __device__ __forceinline__ void keep_pairs(const PackedRows& t, int64_t row, int
   const uint2 w = pack8(f, byte);
   if (v < nv) store_packed(t, row, v, row * nv + v, w, byte);
 }
-__device__ __forceinline__ void shared_pairs(const float4* ps, int nv, int which, int v, uint64_t (&out)[4]) {
-  const float4 a = ps[2 * which * nv + v], b = ps[(2 * which + 1) * nv + v];
-  out[0] = pk2(a.x, a.y); out[1] = pk2(a.z, a.w); out[2] = pk2(b.x, b.y); out[3] = pk2(b.z, b.w);
+__device__ __forceinline__ void shared_pairs(uint32_t ps, uint32_t nv, int which, uint32_t v, uint64_t (&out)[4]) {
+  const uint4 a = lds128(ps + (2 * which * nv + v) * 16), b = lds128(ps + ((2 * which + 1) * nv + v) * 16);
+  out[0] = pk2(__uint_as_float(a.x), __uint_as_float(a.y)); out[1] = pk2(__uint_as_float(a.z), __uint_as_float(a.w));
+  out[2] = pk2(__uint_as_float(b.x), __uint_as_float(b.y)); out[3] = pk2(__uint_as_float(b.z), __uint_as_float(b.w));
 }
 template <int KIND>
 __device__ __forceinline__ void param_pairs(const RowsOf& t, int pf32, int64_t row, int c, int n, float fill, uint64_t (&out)[4]) {
@@ -638,36 +686,40 @@ __device__ __forceinline__ void param_pairs(const RowsOf& t, int pf32, int64_t r
   for (int i = 0; i < 4; ++i) out[i] = pk2(v[2 * i], v[2 * i + 1]);
 }
 __device__ __forceinline__ float sum_pair(uint64_t v) { const float2 f = upk2(v); return f.x + f.y; }
+__device__ __forceinline__ void zero_pairs(uint64_t (&v)[4]) { v[0] = v[1] = v[2] = v[3] = pk2(0.f, 0.f); }
+
+// Shared memory of a team: NM_MAX_STAGES barriers; then, behind all teams' and the weights, its ring of rows.
+constexpr int NM_BARS = 32 * NM_MAX_STAGES * 8;
 
 template <int KIND, bool LN, int V>
 __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNormArgs A) {
   extern __shared__ __align__(16) unsigned char nm_smem[];
-  griddep_chain();
-  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr;
+  const int mine = __shfl_sync(0xffffffffu, threadIdx.x / A.tpr, 0), t = threadIdx.x - mine * A.tpr;      // (known to the compiler as the warp's: rows' addresses are)
   RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
-  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
-  fill_params<KIND>(A, ps);
-  __syncthreads();
-  const uint32_t plane = blockDim.x * 16;
-  constexpr int P = NmPlanes<KIND>::n * V;
-  const uint32_t base = smem_u32(nm_smem) + NM_RED_BYTES + 64 * nv + threadIdx.x * 16;
-  const int64_t first = (int64_t)blockIdx.x * teams + mine, step = (int64_t)gridDim.x * teams;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(nm_smem + NM_RED_BYTES) + mine * NM_MAX_STAGES;
   const int S = A.stages, per = A.mode == NM_NONE ? 1 : 2;
+  if (t == 0) {
+    for (int s = 0; s < S; ++s) mbar_init(&bars[s], 1);
+    fence_mbar_init();
+  }
+  griddep_chain();
+  fill_params<KIND>(A, reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES + NM_BARS));
+  __syncthreads();
+  const uint32_t bytes = (uint32_t)A.width * (KIND == LS_F32 ? 4 : 2), ps = smem_u32(nm_smem) + NM_RED_BYTES + NM_BARS;
+  const uint32_t places = ps + 64 * nv + (uint32_t)(mine * S * per) * bytes;
+  NmRing ring{bars, S};
+  const int64_t first = (int64_t)blockIdx.x * teams + mine, step = (int64_t)gridDim.x * teams;
   const bool folded = A.groups == 1 && !A.starts;
-  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
-  auto issue = [&](int s, int64_t row, bool all) {
-    if (row < A.rows) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
-        if (!all && v >= nv) continue;                   // zeros since the first round
-        fetch8<KIND>(slot(s, 0, j), plane, A.x, row, 8 * v, n);
-        if (A.mode != NM_NONE) fetch8<KIND>(slot(s, 1, j), plane, A.f, row, 8 * v, n);
-      }
-    }
-    cp_async_commit();
+  auto issue = [&](int s, int64_t row) {                 // one thread
+    if (row >= A.rows || ring.failed) return;
+    mbar_expect_tx(&bars[s], bytes * per);
+    const uint32_t to = places + (uint32_t)(s * per) * bytes;
+    bulk_g2s_at(to, row_of<KIND>(A.x, row), bytes, &bars[s]);
+    if (A.mode != NM_NONE) bulk_g2s_at(to + bytes, row_of<KIND>(A.f, row), bytes, &bars[s]);
   };
-  for (int s = 0; s < S; ++s) issue(s, first + s * step, true);
+  if (t == 0)
+    for (int s = 0; s < S; ++s) issue(s, first + s * step);
   const float inv = 1.f / (float)A.width;
   const uint64_t zero = pk2(0.f, 0.f), scale = pk2(A.scale, A.scale);
   // mean and 1 / deviation of V vectors, which leave without the mean
@@ -679,7 +731,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
       for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) s = add2(s, v[j][i]);
-      mean = team.sum(sum_pair(s), 0.f).x * inv;
+      mean = team.sum<false>(sum_pair(s), 0.f).x * inv;
       const uint64_t m = pk2(-mean, -mean);
 #pragma unroll
       for (int j = 0; j < V; ++j)
@@ -691,151 +743,157 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
     uint64_t s = zero, r = zero;
 #pragma unroll
     for (int j = 0; j < V; ++j) { s = fma2(v[j][0], v[j][0], s); r = fma2(v[j][1], v[j][1], r); s = fma2(v[j][2], v[j][2], s); r = fma2(v[j][3], v[j][3], r); }
-    rstd = rsqrtf(fmaf(team.sum(sum_pair(add2(s, r)), 0.f).x, inv, A.eps));
+    rstd = rsqrtf(fmaf(team.sum<false>(sum_pair(add2(s, r)), 0.f).x, inv, A.eps));
   };
-  int s = 0;
   for (int64_t row = first; row < A.rows; row += step) {
-    wait_stages(S - 1);
+    ring.wait();
+    const uint32_t from = places + (uint32_t)(ring.at * per) * bytes;
     uint64_t x[V][4];
     float mean, rstd;
     if (A.mode != NM_NONE) {
       uint64_t f[V][4];
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        Vec8<KIND> w;
-        w.take(slot(s, 1, j), plane);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[j][i] = w.pair(i);
-        if (A.pf.codes) keep_pairs<KIND>(A.pf, row, t + j * A.tpr, nv, f[j], true);
+        const int v = t + j * A.tpr;
+        if (v < nd) take_pairs<KIND>(from + bytes, v, f[j]); else zero_pairs(f[j]);
+        if (A.pf.codes) keep_pairs<KIND>(A.pf, row, v, nv, f[j], true);
       }
       stats(f, mean, rstd);
+      rstd += ring.poison;
       if (A.stats && t == 0) { A.stats[row] = rstd; if (LN) A.stats[2 * A.rows + row] = mean; }
       const int g = folded ? 0 : group_of(A, row);
       const uint64_t r = pk2(rstd, rstd);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
-        Vec8<KIND> w;
-        w.take(slot(s, 0, j), plane);
+        const int v = t + j * A.tpr;
+        if (v >= nd) { zero_pairs(x[j]); continue; }
         uint64_t p[4], q[4], b[4];
-        if (n) shared_pairs(ps, nv, 1, v, p);
-        else p[0] = p[1] = p[2] = p[3] = zero;
+        take_pairs<KIND>(from, v, x[j]);
+        shared_pairs(ps, nv, 1, v, p);
         if (LN && A.pb.p) {
-          param_pairs<KIND>(A.pb, A.pf32, 0, 8 * v, n, 0.f, b);
+          param_pairs<KIND>(A.pb, A.pf32, 0, 8 * v, 8, 0.f, b);
           if (folded && A.gate.p) {
-            param_pairs<KIND>(A.gate, A.pf32, 0, 8 * v, n, 1.f, q);
+            param_pairs<KIND>(A.gate, A.pf32, 0, 8 * v, 8, 1.f, q);
 #pragma unroll
             for (int i = 0; i < 4; ++i) b[i] = mul2(b[i], q[i]);
           }
         }
-        if (!folded) param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, n, 1.f, q);
+        if (folded) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint64_t d = mul2(mul2(f[j][i], r), p[i]);
-          if (LN && A.pb.p) d = add2(d, b[i]);
-          if (!folded) d = mul2(d, q[i]);
-          if (!folded && g < 0) d = zero;                // a row of no group: whatever stands in f
-          x[j][i] = fma2(scale, w.pair(i), d);
+          for (int i = 0; i < 4; ++i) {
+            const uint64_t d = mul2(f[j][i], r);
+            x[j][i] = fma2(scale, x[j][i], LN && A.pb.p ? fma2(d, p[i], b[i]) : mul2(d, p[i]));
+          }
+        } else {
+          param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, 8, 1.f, q);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint64_t d = mul2(mul2(f[j][i], r), p[i]);
+            if (LN && A.pb.p) d = add2(d, b[i]);
+            x[j][i] = g < 0 ? mul2(scale, x[j][i]) : fma2(scale, x[j][i], mul2(d, q[i]));      // (a row of no group: whatever stands in f)
+          }
         }
       }
     } else {
       if (A.stats && t == 0) { A.stats[row] = 1.f; if (LN) A.stats[2 * A.rows + row] = 0.f; }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        Vec8<KIND> w;
-        w.take(slot(s, 0, j), plane);
+        const int v = t + j * A.tpr;
+        if (v >= nd) { zero_pairs(x[j]); continue; }
+        take_pairs<KIND>(from, v, x[j]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[j][i] = mul2(scale, w.pair(i));
+        for (int i = 0; i < 4; ++i) x[j][i] = mul2(scale, x[j][i]);
       }
     }
-    issue(s, row + S * step, false);                     // the row's places are read: the next one that will stand there
-    s = s + 1 == S ? 0 : s + 1;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int v = t + j * A.tpr;
-      if (A.out0.p && v < nd) store_pairs<KIND>(A.out0, row, 8 * v, x[j]);
+      if (A.out0.p && v < nd) store_pairs<KIND>(row_of<KIND>(A.out0, row), v, x[j]);
       if (A.px.codes) keep_pairs<KIND>(A.px, row, v, nv, x[j], false);
     }
     stats(x, mean, rstd);
+    rstd += ring.poison;
+    if (A.tpr == 32) __syncwarp();                         // (a team of several warps has passed a barrier in the sum above)
+    if (t == 0) issue(ring.at, row + S * step);                  // the row's places have been read: the next one that will stand there
+    ring.next();
     if (A.stats && t == 0) { A.stats[A.rows + row] = rstd; if (LN) A.stats[3 * A.rows + row] = mean; }
     const uint64_t r = pk2(rstd, rstd);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
-      uint64_t p[4], b[4];
-      if (n) shared_pairs(ps, nv, 0, v, p);
-      else p[0] = p[1] = p[2] = p[3] = zero;
-      if (LN && A.b.p) param_pairs<KIND>(A.b, A.pf32, 0, 8 * v, n, 0.f, b);
+      const int v = t + j * A.tpr;
+      if (v < nd) {
+        uint64_t p[4], b[4];
+        shared_pairs(ps, nv, 0, v, p);
+        if (LN && A.b.p) {
+          param_pairs<KIND>(A.b, A.pf32, 0, 8 * v, 8, 0.f, b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[j][i] = mul2(x[j][i], r);
-        x[j][i] = LN && A.b.p ? fma2(x[j][i], p[i], b[i]) : mul2(x[j][i], p[i]);
+          for (int i = 0; i < 4; ++i) x[j][i] = fma2(mul2(x[j][i], r), p[i], b[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[j][i] = mul2(mul2(x[j][i], r), p[i]);
+        }
+        store_pairs<KIND>(row_of<KIND>(A.out1, row), v, x[j]);
       }
-      if (n) store_pairs<KIND>(A.out1, row, 8 * v, x[j]);
       if (A.ph.codes) keep_pairs<KIND>(A.ph, row, v, nv, x[j], false);
     }
   }
-  cp_async_wait<0>();
+  if (t == 0 && ring.failed) nm_settle(ring.bars, S, ring.failed);
 }
 
-template <int KIND, bool LN, int V>
+// Backward with a normalised block and a gradient of x'; x' in storage, f packed (PF) or in storage.
+template <int KIND, bool LN, int V, bool PF>
 __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNormArgs A) {
   extern __shared__ __align__(16) unsigned char nm_smem[];
-  griddep_chain();
-  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr, mine = threadIdx.x / A.tpr, t = threadIdx.x - mine * A.tpr;
+  const int nv = 4 * A.blocks, nd = A.width >> 3, teams = blockDim.x / A.tpr;
+  const int mine = __shfl_sync(0xffffffffu, threadIdx.x / A.tpr, 0), t = threadIdx.x - mine * A.tpr;
   RowTeam team{reinterpret_cast<float2*>(nm_smem) + mine * 64, A.tpr >> 5, t >> 5, (int)(threadIdx.x & 31), mine + 1, 0};
-  float4* ps = reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES);
-  fill_params<KIND>(A, ps);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(nm_smem + NM_RED_BYTES) + mine * NM_MAX_STAGES;
+  const int S = A.stages;
+  if (t == 0) {
+    for (int s = 0; s < S; ++s) mbar_init(&bars[s], 1);
+    fence_mbar_init();
+  }
+  griddep_chain();
+  fill_params<KIND>(A, reinterpret_cast<float4*>(nm_smem + NM_RED_BYTES + NM_BARS));
   __syncthreads();
-  const uint32_t plane = blockDim.x * 16;
-  constexpr int P = NmPlanes<KIND>::n * V;
-  const uint32_t ring = NM_RED_BYTES + 64 * nv;
-  const uint32_t base = smem_u32(nm_smem) + ring + threadIdx.x * 16;
+  const uint32_t bytes = (uint32_t)A.width * (KIND == LS_F32 ? 4 : 2), f_bytes = PF ? 32u * A.blocks : bytes, stage = 3 * bytes + f_bytes;
+  const uint32_t ps = smem_u32(nm_smem) + NM_RED_BYTES + NM_BARS, places = ps + 64 * nv + (uint32_t)(mine * S) * stage;
+  NmRing ring{bars, S};
   const int64_t team_id = (int64_t)blockIdx.x * teams + mine;
   const int64_t first = team_id * A.chunk, last = min(first + A.chunk, A.rows);
-  const int S = A.stages, T_DX = 2, T_F = A.dx.p ? 3 : 2, per = T_F + (A.mode != NM_NONE ? 1 : 0);
   const bool folded = A.groups == 1 && !A.starts;
-  auto slot = [&](int s, int tensor, int j) { return base + (uint32_t)((s * per + tensor) * P + j * NmPlanes<KIND>::n) * plane; };
-  auto issue = [&](int s, int64_t row, bool all) {
-    if (row < last) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int v = t + j * A.tpr, n = v < nd ? 8 : 0;
-        if (!all && v >= nv) continue;                   // zeros since the first round
-        fetch8<KIND>(slot(s, 0, j), plane, A.dh, row, 8 * v, n);
-        if (A.px.codes) { if (v < nv) fetch8_packed(slot(s, 1, j), A.px, row, v); }
-        else fetch8<KIND>(slot(s, 1, j), plane, A.x, row, 8 * v, n);
-        if (A.dx.p) fetch8<KIND>(slot(s, T_DX, j), plane, A.dx, row, 8 * v, n);
-        if (A.mode != NM_NONE) {
-          if (A.pf.codes) { if (v < nv) fetch8_packed(slot(s, T_F, j), A.pf, row, v); }
-          else fetch8<KIND>(slot(s, T_F, j), plane, A.f, row, 8 * v, n);
-        }
-      }
-    }
-    cp_async_commit();
+  auto issue = [&](int s, int64_t row) {                 // one thread
+    if (row >= last || ring.failed) return;
+    mbar_expect_tx(&bars[s], stage);
+    const uint32_t to = places + (uint32_t)s * stage;
+    bulk_g2s_at(to, row_of<KIND>(A.dh, row), bytes, &bars[s]);
+    bulk_g2s_at(to + bytes, row_of<KIND>(A.x, row), bytes, &bars[s]);
+    bulk_g2s_at(to + 2 * bytes, row_of<KIND>(A.dx, row), bytes, &bars[s]);
+    bulk_g2s_at(to + 3 * bytes, PF ? reinterpret_cast<const char*>(A.pf.codes) + row * f_bytes : row_of<KIND>(A.f, row), f_bytes, &bars[s]);
   };
+  if (t == 0)
+    for (int s = 0; s < S; ++s) issue(s, first + s);
+  // what comes by plain loads, a row ahead: the statistics and (PF) the bytes of this thread's blocks
+  float4 next = make_float4(1.f, 1.f, 0.f, 0.f);
+  uint32_t next_byte[V];
+  auto ahead = [&](int64_t row) {
+    if (row >= last) return;
+    next.x = A.stats[row]; next.y = A.stats[A.rows + row];
+    if (LN) { next.z = A.stats[2 * A.rows + row]; next.w = A.stats[3 * A.rows + row]; }
+    if (PF) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (t + j * A.tpr < nd) next_byte[j] = A.pf.exps[row * A.pf.exp_stride + ((t + j * A.tpr) >> 2)];
+    }
+  };
+  ahead(first);
   const uint64_t zero = pk2(0.f, 0.f), scale = pk2(A.scale, A.scale);
-  // (entries - mean) / deviation of a vector
-  auto unit = [&](uint32_t at, const PackedRows& packed, int v, float mean, float rstd, uint64_t (&out)[4]) {
-    if (packed.codes) {
-      if (v < nv) packed_pairs(at, v, LN ? 1.f : rstd, out);
-      else out[0] = out[1] = out[2] = out[3] = zero;
-      if (!LN) return;
-    } else {
-      Vec8<KIND> w;
-      w.take(at, plane);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = w.pair(i);
-    }
-    const uint64_t m = pk2(-mean, -mean), r = pk2(rstd, rstd);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = mul2(LN ? add2(out[i], m) : out[i], r);
-  };
   uint64_t sw[V][4], s1[V][4], sb[LN ? V : 1][4], s0[LN ? V : 1][4];
 #pragma unroll
-  for (int j = 0; j < V; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { sw[j][i] = s1[j][i] = zero; if (LN) sb[LN ? j : 0][i] = s0[LN ? j : 0][i] = zero; }
+  for (int j = 0; j < V; ++j) {
+    zero_pairs(sw[j]); zero_pairs(s1[j]);
+    if (LN) { zero_pairs(sb[LN ? j : 0]); zero_pairs(s0[LN ? j : 0]); }
+  }
   const int nw = LN ? 2 : 1;
   const int64_t slots = A.combine ? gridDim.x : (int64_t)gridDim.x * teams;
   auto flush = [&](float* to, const uint64_t (&a)[4], int j) {
@@ -847,87 +905,85 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
   };
   auto slot_w = [&](int64_t k, int which) { return A.part + (k * nw + which) * A.part_stride; };
   auto slot_s = [&](int64_t k, int which) { return A.part + ((slots + k) * nw + which) * A.part_stride; };
-  for (int s = 0; s < S; ++s) issue(s, first + s, true);
   const float inv = 1.f / (float)A.width;
-  int s = 0, group = -1;
-  float4 next = make_float4(1.f, 1.f, 0.f, 0.f);       // the statistics of a row, read a row ahead
-  auto read_stats = [&](int64_t row) {
-    if (row >= last) return;
-    next.y = A.stats[A.rows + row];
-    if (LN) next.w = A.stats[3 * A.rows + row];
-    if (A.mode == NM_POST) { next.x = A.stats[row]; if (LN) next.z = A.stats[2 * A.rows + row]; }
-  };
-  read_stats(first);
+  int group = folded ? 0 : -1;
   for (int64_t row = first; row < last; ++row) {
-    wait_stages(S - 1);
-    const float r0 = next.x, r1 = next.y, m0 = next.z, m1 = next.w;
-    read_stats(row + 1);
+    const float r0 = next.x, m0 = next.z, m1 = next.w;
+    float r1 = next.y;
+    uint32_t byte[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) byte[j] = next_byte[j];
+    ahead(row + 1);
+    ring.wait();
+    r1 += ring.poison;
+    const uint32_t from = places + (uint32_t)ring.at * stage;
     uint64_t e[V][4], u[V][4], su = zero, sd = zero;
+    {
+      const uint64_t m = pk2(-m1, -m1), r = pk2(r1, r1);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int v = t + j * A.tpr;
-      Vec8<KIND> d;
-      d.take(slot(s, 0, j), plane);
-      unit(slot(s, 1, j), A.px, v, m1, r1, u[j]);
-      uint64_t w[4];
-      if (v < nv) shared_pairs(ps, nv, 0, v, w);
-      else w[0] = w[1] = w[2] = w[3] = zero;
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr;
+        if (v >= nd) { zero_pairs(e[j]); zero_pairs(u[j]); continue; }
+        uint64_t d[4], w[4];
+        take_pairs<KIND>(from, v, d);
+        take_pairs<KIND>(from + bytes, v, u[j]);
+        shared_pairs(ps, nv, 0, v, w);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint64_t di = d.pair(i);
-        sw[j][i] = fma2(di, u[j][i], sw[j][i]);
-        if (LN) sb[LN ? j : 0][i] = add2(sb[LN ? j : 0][i], di);
-        e[j][i] = mul2(di, w[i]);
-        su = fma2(e[j][i], u[j][i], su);
-        if (LN) sd = add2(sd, e[j][i]);
+        for (int i = 0; i < 4; ++i) {
+          u[j][i] = mul2(LN ? add2(u[j][i], m) : u[j][i], r);
+          sw[j][i] = fma2(d[i], u[j][i], sw[j][i]);
+          if (LN) sb[LN ? j : 0][i] = add2(sb[LN ? j : 0][i], d[i]);
+          e[j][i] = mul2(d[i], w[i]);
+          su = fma2(e[j][i], u[j][i], su);
+          if (LN) sd = add2(sd, e[j][i]);
+        }
       }
     }
-    float2 c = team.sum(sum_pair(su), LN ? sum_pair(sd) : 0.f);
-    c.x *= -inv; c.y *= -inv;
+    float2 c = team.sum<LN>(sum_pair(su), LN ? sum_pair(sd) : 0.f);
     int g = 0;
     if (!folded) {
       g = group_of(A, row);
       if (g != group) {                                  // another sequence: its own column sums
-        if (group >= 0) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) { flush(slot_s(team_id + group, 0), s1[j], j); if (LN) flush(slot_s(team_id + group, 1), s0[LN ? j : 0], j); }
+        for (int j = 0; j < V; ++j) {
+          if (group >= 0) { flush(slot_s(team_id + group, 0), s1[j], j); if (LN) flush(slot_s(team_id + group, 1), s0[LN ? j : 0], j); }
+          zero_pairs(s1[j]);
+          if (LN) zero_pairs(s0[LN ? j : 0]);
         }
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { s1[j][i] = zero; if (LN) s0[LN ? j : 0][i] = zero; }
         group = g;
       }
     }
-    const uint64_t cu = pk2(c.x, c.x), cd = pk2(c.y, c.y), r = pk2(r1, r1);
-    su = sd = zero;
+    {
+      // t = dx' + r1 (e - u mean(e u) - mean e)
+      const uint64_t cu = pk2(-inv * c.x, -inv * c.x), cd = pk2(-inv * c.y, -inv * c.y), r = pk2(r1, r1), m = pk2(-m0, -m0), q0 = pk2(r0, r0);
+      su = sd = zero;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int v = t + j * A.tpr;
-      Vec8<KIND> x;
-      if (A.dx.p) x.take(slot(s, T_DX, j), plane);
-      uint64_t o[4];
+      for (int j = 0; j < V; ++j) {
+        const int v = t + j * A.tpr;
+        if (v >= nd) continue;
+        uint64_t x[4], p[4];
+        take_pairs<KIND>(from + 2 * bytes, v, x);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint64_t k = fma2(u[j][i], cu, e[j][i]);
-        if (LN) k = add2(k, cd);
-        e[j][i] = A.dx.p ? fma2(r, k, x.pair(i)) : mul2(r, k);
-        o[i] = mul2(scale, e[j][i]);
-      }
-      if (v < nd) store_pairs<KIND>(A.out0, row, 8 * v, o);
-      if (A.mode != NM_NONE) {
-        unit(slot(s, T_F, j), A.pf, v, m0, r0, u[j]);
-        uint64_t p[4], q[4];
-        if (v < nv) shared_pairs(ps, nv, 1, v, p);
-        else p[0] = p[1] = p[2] = p[3] = zero;
+        for (int i = 0; i < 4; ++i) {
+          uint64_t k = fma2(u[j][i], cu, e[j][i]);
+          if (LN) k = add2(k, cd);
+          e[j][i] = fma2(r, k, x[i]);
+          x[i] = mul2(scale, e[j][i]);
+        }
+        store_pairs<KIND>(row_of<KIND>(A.out0, row), v, x);
+        if (PF) take_packed(from + 3 * bytes, v, byte[j], LN ? 1.f : r0, u[j]);
+        else take_pairs<KIND>(from + 3 * bytes, v, u[j]);
+        if (LN || !PF) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[j][i] = mul2(LN ? add2(u[j][i], m) : u[j][i], q0);
+        }
+        shared_pairs(ps, nv, 1, v, p);
         if (!folded) {
-          param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, v < nd ? 8 : 0, 1.f, q);
+          uint64_t q[4];
+          param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, 8, 1.f, q);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], q[i]);
-          if (g < 0) {                                   // a row of no group: whatever stands in f
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u[j][i] = e[j][i] = zero;
-          }
+          if (g < 0) { zero_pairs(u[j]); zero_pairs(e[j]); }      // a row of no group: whatever stands in f
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -939,31 +995,32 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
         }
       }
     }
-    issue(s, row + S, false);
-    s = s + 1 == S ? 0 : s + 1;
-    if (A.mode != NM_NONE) {
-      c = team.sum(sum_pair(su), LN ? sum_pair(sd) : 0.f);
-      c.x *= -inv; c.y *= -inv;
-      const uint64_t fu = pk2(c.x, c.x), fd = pk2(c.y, c.y), f = pk2(r0, r0);
+    c = team.sum<LN>(sum_pair(su), LN ? sum_pair(sd) : 0.f);
+    if (A.tpr == 32) __syncwarp();
+    if (t == 0) issue(ring.at, row + S);                         // the row's places have been read
+    ring.next();
+    {
+      const float r = g < 0 ? 0.f : r0;
+      const uint64_t fu = pk2(-inv * c.x, -inv * c.x), fd = pk2(-inv * c.y, -inv * c.y), f = pk2(r, r);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = t + j * A.tpr;
-        uint64_t o[4];
+        if (v >= nd) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint64_t k = fma2(u[j][i], fu, e[j][i]);
           if (LN) k = add2(k, fd);
-          o[i] = g < 0 ? zero : mul2(f, k);
+          e[j][i] = mul2(f, k);
         }
-        if (v < nd) store_pairs<KIND>(A.out1, row, 8 * v, o);
+        store_pairs<KIND>(row_of<KIND>(A.out1, row), v, e[j]);
       }
     }
   }
-  cp_async_wait<0>();
+  if (t == 0 && ring.failed) nm_settle(ring.bars, S, ring.failed);
   if (!A.part) return;
   if (A.combine && teams > 1) {
     // the block's teams, one kind of sum after the other, through the ring's memory
-    float* buf = reinterpret_cast<float*>(nm_smem + ring);
+    float* buf = reinterpret_cast<float*>(nm_smem + NM_RED_BYTES + NM_BARS + 64 * nv);
     auto join = [&](float* to, const uint64_t (&a)[V][4]) {
       __syncthreads();
 #pragma unroll
@@ -977,20 +1034,17 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
     };
     join(slot_w(blockIdx.x, 0), sw);
     if constexpr (LN) join(slot_w(blockIdx.x, 1), sb);
-    if (A.mode != NM_NONE) {
-      join(slot_s(blockIdx.x, 0), s1);
-      if constexpr (LN) join(slot_s(blockIdx.x, 1), s0);
-    }
+    join(slot_s(blockIdx.x, 0), s1);
+    if constexpr (LN) join(slot_s(blockIdx.x, 1), s0);
     return;
   }
-  const int at = A.mode == NM_NONE ? -1 : folded ? 0 : group;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     flush(slot_w(team_id, 0), sw[j], j);
     if (LN) flush(slot_w(team_id, 1), sb[LN ? j : 0], j);
-    if (at >= 0) {
-      flush(slot_s(team_id + at, 0), s1[j], j);
-      if (LN) flush(slot_s(team_id + at, 1), s0[LN ? j : 0], j);
+    if (group >= 0) {
+      flush(slot_s(team_id + group, 0), s1[j], j);
+      if (LN) flush(slot_s(team_id + group, 1), s0[LN ? j : 0], j);
     }
   }
 }
