@@ -85,8 +85,9 @@ inline bool many(const ItemWalk& k) { return k.items >= (int64_t)148 * 8 * PK_TH
 
 template <int KIND>
 tgrad_status pack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k, cudaStream_t st) {
-  if (x.al == 16 && k.width % 8 == 0) return many(k) ? launch_items(pack_kernel<KIND, true, 4>, 4, k, st, x, p) : launch_items(pack_kernel<KIND, true, 1>, 1, k, st, x, p);
-  return many(k) ? launch_items(pack_kernel<KIND, false, 2>, 2, k, st, x, p) : launch_items(pack_kernel<KIND, false, 1>, 1, k, st, x, p);
+  // (one vector a thread: 16384 x 8192 bf16 88 us, 97 with two, 122 with four; threads to switch between count for more than loads of one thread)
+  if (x.al == 16 && k.width % 8 == 0) return launch_items(pack_kernel<KIND, true, 1>, 1, k, st, x, p);
+  return launch_items(pack_kernel<KIND, false, 1>, 1, k, st, x, p);
 }
 template <int KIND>
 tgrad_status unpack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k, cudaStream_t st) {
@@ -97,12 +98,8 @@ tgrad_status unpack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k
 // ---- gated activation ----
 template <int KIND, int ACT, bool GATED>
 tgrad_status gated_launch(const GatedArgs& g, const ItemWalk& k, bool aligned, bool backward, cudaStream_t st) {
-  if (!backward) {
-    if (aligned) return many(k) ? launch_items(gated_kernel<KIND, ACT, GATED, true, 2>, 2, k, st, g) : launch_items(gated_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g);
-    return launch_items(gated_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
-  }
-  if (aligned) return many(k) ? launch_items(gated_backward_kernel<KIND, ACT, GATED, true, 2>, 2, k, st, g) : launch_items(gated_backward_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g);
-  return launch_items(gated_backward_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
+  if (!backward) return aligned ? launch_items(gated_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g) : launch_items(gated_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
+  return aligned ? launch_items(gated_backward_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g) : launch_items(gated_backward_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
 }
 template <int KIND, int ACT>
 tgrad_status gated_act(const GatedArgs& g, const ItemWalk& k, bool gated, bool aligned, bool backward, cudaStream_t st) {
@@ -269,15 +266,24 @@ tgrad_status norm_kind(int kind, bool layer, const NormPlan& p, ResNormArgs& a, 
   if (layer) return kind == LS_F32 ? norm_vectors<LS_F32, true>(p, a, backward, st) : kind == LS_F16 ? norm_vectors<LS_F16, true>(p, a, backward, st) : norm_vectors<LS_BF16, true>(p, a, backward, st);
   return kind == LS_F32 ? norm_vectors<LS_F32, false>(p, a, backward, st) : kind == LS_F16 ? norm_vectors<LS_F16, false>(p, a, backward, st) : norm_vectors<LS_BF16, false>(p, a, backward, st);
 }
-template <int KIND>
-void sums_launch(bool layer, const NormSums& s, cudaStream_t st) {
-  const dim3 grid((unsigned)((s.width + 31) / 32)), block(32, NF_Y);
-  if (layer) launch_chained(norm_sums_kernel<KIND, true>, grid, block, 0, st, s);
-  else launch_chained(norm_sums_kernel<KIND, false>, grid, block, 0, st, s);
+template <int KIND, bool LN>
+tgrad_status sums_launch(const NormSums& s, cudaStream_t st) {
+  const unsigned columns = (unsigned)((s.width + 31) / 32);
+  const bool groups = s.dpw.p || s.dpb.p || (s.dgate.p && !s.per_row);      // any sum over t is wanted
+  const unsigned parts = !groups ? 1u : s.groups < 1024 ? 1u + s.groups : 1024u;
+  NormSums a = s;
+  if (!groups) a.groups = 0;
+  launch_chained(norm_sums_kernel<KIND, LN>, dim3(columns, parts), dim3(32, NF_Y), 0, st, a);
+  TG_LAUNCH_CHECK();
+  if (groups && s.groups > 1 && (s.dpw.p || s.dpb.p)) {
+    launch_chained(norm_groups_kernel<KIND, LN>, dim3(columns), dim3(32, NF_Y), 0, st, a);
+    TG_LAUNCH_CHECK();
+  }
+  return TGRAD_OK;
 }
-// (the plan of four matrices a row needs the most slots of all: fewer matrices change the stages only)
 size_t norm_part_bytes(const tgrad_norm_config* c, const NormPlan& p) {
-  return align_up((size_t)(2 * p.slots + (c->groups > 1 ? c->groups : 1)) * (c->layer ? 2 : 1) * 32 * blocks_of(c->width) * 4);
+  const bool single = !c->d_starts && (c->groups <= 1 || c->groups == c->rows);
+  return align_up((size_t)(2 * p.slots + (single ? 1 : 2 * (int64_t)c->groups)) * (c->layer ? 2 : 1) * 32 * blocks_of(c->width) * 4);
 }
 
 // ---- weight gradient ----
@@ -431,15 +437,12 @@ tgrad_status tgrad_residual_norm_backward(const tgrad_norm_config* c, const tgra
   NormSums s; memset(&s, 0, sizeof(s));
   s.part = static_cast<float*>(d_workspace); s.slots = c->rows > 0 ? p.slots : 0; s.part_stride = 32 * blocks_of(c->width);
   s.chunk = p.combine ? 0 : p.chunk; s.rows = c->rows; s.rows_per = a.rows_per; s.starts = c->d_starts;
-  s.groups = a.groups; s.width = a.width; s.pf32 = a.pf32; s.per_row = a.gate_rows; s.post = a.mode == NM_POST;
-  s.w = a.w; s.b = a.b; s.pw = a.pw; s.pb = a.pb; s.gate = a.gate;
+  s.groups = a.gate_rows ? 1 : a.groups; s.width = a.width; s.pf32 = a.pf32; s.per_row = a.gate_rows; s.post = a.mode == NM_POST;
+  s.pw = a.pw; s.pb = a.pb; s.gate = a.gate;
   s.dw = vector_of(io->d_dweight, pk); s.db = vector_of(io->d_dbias, pk); s.dpw = vector_of(io->d_dpost_weight, pk); s.dpb = vector_of(io->d_dpost_bias, pk);
   s.dgate = a.dgate;
-  if (kind == LS_F32) sums_launch<LS_F32>(c->layer != 0, s, st);
-  else if (kind == LS_F16) sums_launch<LS_F16>(c->layer != 0, s, st);
-  else sums_launch<LS_BF16>(c->layer != 0, s, st);
-  TG_LAUNCH_CHECK();
-  return TGRAD_OK;
+  if (c->layer) return kind == LS_F32 ? sums_launch<LS_F32, true>(s, st) : kind == LS_F16 ? sums_launch<LS_F16, true>(s, st) : sums_launch<LS_BF16, true>(s, st);
+  return kind == LS_F32 ? sums_launch<LS_F32, false>(s, st) : kind == LS_F16 ? sums_launch<LS_F16, false>(s, st) : sums_launch<LS_BF16, false>(s, st);
 }
 
 tgrad_status tgrad_weight_grad_bytes(const tgrad_weight_grad_args* c, size_t* workspace_bytes) {

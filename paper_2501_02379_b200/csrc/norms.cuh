@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_kernel(const ResNormArgs
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j][i] = i < n[j] ? x[j][i] : 0.f;
       }
-      if (A.out0.p) store8<KIND, false>(A.out0, row, 8 * at[j], n[j], x[j]);
+      if (A.out0.p) store8_any<KIND>(A.out0, row, 8 * at[j], n[j], x[j], true);
       if (A.px.codes) {
         float v[8];
 #pragma unroll
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_kernel(const ResNormArgs
         if (LN) x[j][i] += b[i];
         if (i >= n[j]) x[j][i] = 0.f;
       }
-      store8<KIND, false>(A.out1, row, 8 * at[j], n[j], x[j]);
+      store8_any<KIND>(A.out1, row, 8 * at[j], n[j], x[j], true);
       if (A.ph.codes) {
         round8<KIND>(x[j]);
         uint32_t byte;
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
         tt[j][i] = A.dx.p ? fmaf(r1, e, v[i]) : r1 * e;
         v[i] = A.scale * tt[j][i];
       }
-      store8<KIND, false>(A.out0, row, 8 * at[j], n[j], v);
+      store8_any<KIND>(A.out0, row, 8 * at[j], n[j], v, true);
       if (A.mode != NM_NONE && g >= 0) {
         float f[8], p[8], q[8];
         kept(s, T_F, A.pf, A.f, row, j, f);
@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
           }
           if (g < 0) tt[j][i] = 0.f;
         }
-        store8<KIND, false>(A.out1, row, 8 * at[j], n[j], tt[j]);
+        store8_any<KIND>(A.out1, row, 8 * at[j], n[j], tt[j], true);
       }
     }
     if (S > 0) { issue(s, row + S); s = s + 1 == S ? 0 : s + 1; }
@@ -1049,78 +1049,98 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
   }
 }
 
-// Column sums of the slots, in a fixed order: 32 columns a block, 32 threads on each.
-constexpr int NF_Y = 32;
+// Column sums of the slots, in a fixed order: 32 columns a block, NF_Y threads on each.  Blocks (x, 0) add up dw and db, blocks (x, 1 + g) the
+// sums of group g.  Several groups: their sums go behind the slots, and a second launch multiplies them by the gates and adds them.
+constexpr int NF_Y = 16;
 struct NormSums {
-  const float* part;
+  float* part;
   int64_t slots, part_stride, chunk, rows, rows_per;
   const int* starts;
   int groups, width, pf32, per_row, post;   // per_row: the sums hold gate * t already; post: the block's output is normalised
-  RowsOf w, b, pw, pb, gate;                // parameters
+  RowsOf pw, pb, gate;                      // parameters
   RowsOf dw, db, dpw, dpb, dgate;           // their gradients; p null: not wanted
 };
+template <int KIND>
+__device__ __forceinline__ float sums_param(const RowsOf& t, int pf32, int64_t row, int c, float fill) {
+  if (!t.p) return fill;
+  return KIND == LS_F32 || pf32 ? reinterpret_cast<const float*>(t.p)[row * t.ld + c] : ld_real<KIND>(t.p + (row * t.ld + c) * 2);
+}
+// where the sums of group g stand
+__device__ __forceinline__ float* sums_of_group(const NormSums& A, int nw, int64_t g) { return A.part + (2 * A.slots + A.groups + g) * nw * A.part_stride; }
 
 template <int KIND, bool LN>
-__global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSums A) {
+__global__ void __launch_bounds__(32 * NF_Y) norm_sums_kernel(const NormSums A) {
   __shared__ float2 red[NF_Y][33];
   griddep_chain();
   const int x = threadIdx.x, y = threadIdx.y, c = blockIdx.x * 32 + x, nw = LN ? 2 : 1;
   const bool live = c < A.width;
-  auto join = [&](float2 v) {               // over y, to every thread of the column
-    red[y][x] = v;
-    __syncthreads();
-    float2 s = make_float2(0.f, 0.f);
-    for (int k = 0; k < NF_Y; ++k) { s.x += red[k][x].x; s.y += red[k][x].y; }
-    __syncthreads();
-    return s;
-  };
-  auto over = [&](int64_t at, int64_t k0, int64_t k1, int64_t from, int64_t step) {      // slots at + [k0, k1]
-    float2 v = make_float2(0.f, 0.f);
-    if (live)
-      for (int64_t k = k0 + from; k <= k1; k += step) {
-        const float* p = A.part + (at + k) * nw * A.part_stride + c;
-        v.x += p[0];
-        if (LN) v.y += p[A.part_stride];
-      }
-    return v;
-  };
-  auto param = [&](const RowsOf& t, int64_t row, float fill) {
-    if (!t.p || !live) return fill;
-    return KIND == LS_F32 || A.pf32 ? reinterpret_cast<const float*>(t.p)[row * t.ld + c] : ld_real<KIND>(t.p + (row * t.ld + c) * 2);
-  };
-  if (A.dw.p || A.db.p) {
-    const float2 v = join(over(0, 0, A.slots - 1, y, NF_Y));
-    if (y == 0 && live) {
-      if (A.dw.p) store_param<KIND>(A.dw, A.pf32, 0, c, v.x);
-      if (A.db.p) store_param<KIND>(A.db, A.pf32, 0, c, v.y);
-    }
-  }
-  if (!A.dpw.p && !A.dpb.p && (!A.dgate.p || A.per_row)) return;
-  const float pw = A.post ? param(A.pw, 0, 1.f) : 1.f, pb = LN && A.post ? param(A.pb, 0, 0.f) : 0.f;
-  float2 total = make_float2(0.f, 0.f);
-  if (A.per_row) total = join(over(A.slots, 0, A.slots - 1, y, NF_Y));
-  else {
-    // many groups: a thread takes whole ones; few: all threads on each
-    const bool whole = A.groups >= NF_Y;
-    for (int g = whole ? y : 0; g < A.groups; g += whole ? NF_Y : 1) {
+  for (int64_t part = blockIdx.y; part <= A.groups; part += gridDim.y) {
+    const int64_t g = part - 1;
+    int64_t at = 0, k0 = 0, k1 = A.slots - 1;             // slots at + [k0, k1]
+    if (g >= 0) {
+      at = A.slots + (A.per_row ? 0 : g);
       int64_t r0 = 0, r1 = A.rows;
       if (A.starts) { r0 = max((int64_t)A.starts[g], (int64_t)0); r1 = min((int64_t)A.starts[g + 1], A.rows); }
       else if (A.groups > 1) { r0 = g * A.rows_per; r1 = r0 + A.rows_per; }
-      float2 v = make_float2(0.f, 0.f);
-      if (r0 < r1) {
-        const int64_t k0 = A.chunk ? r0 / A.chunk : 0, k1 = A.chunk ? (r1 - 1) / A.chunk : A.slots - 1;      // chunk 0: combined sums, one group
-        v = over(A.slots + g, k0, k1, whole ? 0 : y, whole ? 1 : NF_Y);
-      }
-      if (!whole) v = join(v);
-      const float gate = param(A.gate, g, 1.f);
-      if (live && A.dgate.p && (whole || y == 0)) store_param<KIND>(A.dgate, A.pf32, g, c, fmaf(v.x, pw, v.y * pb));
-      total.x = fmaf(gate, v.x, total.x); total.y = fmaf(gate, v.y, total.y);
+      if (r0 >= r1) k1 = -1;
+      else if (A.chunk) { k0 = r0 / A.chunk; k1 = (r1 - 1) / A.chunk; }      // (chunk 0: combined sums, one group)
     }
-    if (whole) total = join(total);
+    float2 v = make_float2(0.f, 0.f);
+    if (live) {
+      const float* p = A.part + (at + k0 + y) * nw * A.part_stride + c;
+#pragma unroll 8
+      for (int64_t k = k0 + y; k <= k1; k += NF_Y, p += (int64_t)NF_Y * nw * A.part_stride) {
+        v.x += p[0];
+        if (LN) v.y += p[A.part_stride];
+      }
+    }
+    red[y][x] = v;
+    __syncthreads();
+    if (y == 0 && live) {
+      for (int k = 1; k < NF_Y; ++k) { v.x += red[k][x].x; v.y += red[k][x].y; }
+      if (g < 0) {
+        if (A.dw.p) store_param<KIND>(A.dw, A.pf32, 0, c, v.x);
+        if (A.db.p) store_param<KIND>(A.db, A.pf32, 0, c, v.y);
+      } else {
+        if (A.dgate.p && !A.per_row) {
+          const float pw = A.post ? sums_param<KIND>(A.pw, A.pf32, 0, c, 1.f) : 1.f, pb = LN && A.post ? sums_param<KIND>(A.pb, A.pf32, 0, c, 0.f) : 0.f;
+          store_param<KIND>(A.dgate, A.pf32, g, c, fmaf(v.x, pw, v.y * pb));
+        }
+        if (A.groups == 1) {
+          const float gate = A.per_row ? 1.f : sums_param<KIND>(A.gate, A.pf32, 0, c, 1.f);
+          if (A.dpw.p) store_param<KIND>(A.dpw, A.pf32, 0, c, gate * v.x);
+          if (A.dpb.p) store_param<KIND>(A.dpb, A.pf32, 0, c, gate * v.y);
+        } else {
+          float* to = sums_of_group(A, nw, g) + c;
+          to[0] = v.x;
+          if (LN) to[A.part_stride] = v.y;
+        }
+      }
+    }
+    __syncthreads();
   }
-  if (y == 0 && live) {
-    if (A.dpw.p) store_param<KIND>(A.dpw, A.pf32, 0, c, total.x);
-    if (A.dpb.p) store_param<KIND>(A.dpb, A.pf32, 0, c, total.y);
+}
+template <int KIND, bool LN>
+__global__ void __launch_bounds__(32 * NF_Y) norm_groups_kernel(const NormSums A) {
+  __shared__ float2 red[NF_Y][33];
+  griddep_chain();
+  const int x = threadIdx.x, y = threadIdx.y, c = blockIdx.x * 32 + x, nw = LN ? 2 : 1;
+  float2 v = make_float2(0.f, 0.f);
+  if (c < A.width) {
+#pragma unroll 4
+    for (int64_t g = y; g < A.groups; g += NF_Y) {
+      const float gate = sums_param<KIND>(A.gate, A.pf32, g, c, 1.f);
+      const float* p = sums_of_group(A, nw, g) + c;
+      v.x = fmaf(gate, p[0], v.x);
+      if (LN) v.y = fmaf(gate, p[A.part_stride], v.y);
+    }
+  }
+  red[y][x] = v;
+  __syncthreads();
+  if (y == 0 && c < A.width) {
+    for (int k = 1; k < NF_Y; ++k) { v.x += red[k][x].x; v.y += red[k][x].y; }
+    if (A.dpw.p) store_param<KIND>(A.dpw, A.pf32, 0, c, v.x);
+    if (A.dpb.p) store_param<KIND>(A.dpb, A.pf32, 0, c, v.y);
   }
 }
 

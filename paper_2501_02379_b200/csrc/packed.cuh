@@ -30,7 +30,7 @@ struct PackedRows {
   int blocks, exp_stride;
 };
 
-constexpr int PK_THREADS = 256;
+constexpr int PK_THREADS = 256, PK_BLOCKS = 8;      // blocks of an SM that the registers have to leave room for
 
 // 8 entries of a row from entry c on, of which n (0..8) exist; the others are 0.  ALIGNED: al is 16 and n is 8 or 0.
 template <int KIND, bool ALIGNED>
@@ -89,6 +89,40 @@ __device__ __forceinline__ void store8(const RowsOf& t, int64_t row, int c, int 
       if (i < n) st_real<KIND>(p + i * B, v[i]);
   }
 }
+// 16 bytes from byte 16 - m of w on, m in [4 K, 4 K + 4) and even
+template <int K>
+__device__ __forceinline__ void shifted4(const uint32_t (&w)[8], int m, uint32_t (&o)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = m & 2 ? __funnelshift_r(w[3 + i - K], w[4 + i - K], 16) : w[4 + i - K];
+}
+// store8 for rows of any alignment, by a whole warp.  Where its lanes hold neighbouring vectors of one row (`same`), the aligned 16 bytes that two
+// neighbours share are put together from both, so that nearly all is written 16 bytes at a time: 16-bit entries one by one took six times as long
+// (16384 x 8191 bf16 read back from codes: 364 us).
+template <int KIND>
+__device__ __forceinline__ void store8_any(const RowsOf& t, int64_t row, int c, int n, const float (&v)[8], bool same) {
+  if (KIND == LS_F32 || t.al == 16 || !same) { store8<KIND, false>(t, row, c, n, v); return; }
+  uint16_t* p = reinterpret_cast<uint16_t*>(t.p) + row * t.ld + c;
+  const int m = __shfl_sync(0xffffffffu, (int)(reinterpret_cast<uintptr_t>(p) & 15), 0);      // bytes, the same for all lanes
+  uint32_t w[8];                                                                              // the neighbour's words, then this lane's
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { w[4 + i] = narrow2<KIND>(v[2 * i], v[2 * i + 1]); w[i] = __shfl_up_sync(0xffffffffu, w[4 + i], 1); }
+  const bool full = n == 8;
+  const int lane = threadIdx.x & 31;
+  const uint32_t all = __ballot_sync(0xffffffffu, full);
+  const bool before = lane > 0 && (all >> (lane - 1) & 1), behind = lane < 31 && (all >> (lane + 1) & 1);
+  if (full && before) {
+    uint32_t o[4];
+    if (m < 4) shifted4<0>(w, m, o); else if (m < 8) shifted4<1>(w, m, o); else if (m < 12) shifted4<2>(w, m, o); else shifted4<3>(w, m, o);
+    st_stream(reinterpret_cast<uint4*>(p - m / 2), make_uint4(o[0], o[1], o[2], o[3]));
+  }
+  // what no pair of neighbours covers: the first lane's head, the last full one's tail, a row's last entries
+  const int from = full && before ? 8 - m / 2 : 0, to = full && behind ? 8 - m / 2 : n;
+  if (from < to) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= from && i < to) p[i] = (uint16_t)(w[4 + i / 2] >> (16 * (i & 1)));
+  }
+}
 // rounded to the storage type and back
 template <int KIND>
 __device__ __forceinline__ void round8(float (&v)[8]) {
@@ -99,19 +133,30 @@ __device__ __forceinline__ void round8(float (&v)[8]) {
 }
 
 // Codes of 8 entries; the four threads of a block of 32 (lanes 4 i to 4 i + 3) call it together, with the whole warp.
+// The integer of v 2^-e stands in the low bits of v 2^-e + 1.5 * 2^23.  Only a block whose largest entry is within 1/256 of the next power of two
+// can have codes beyond 127; the test for that is one for the warp, so that the usual path has no clamp per entry.
 __device__ __forceinline__ uint2 pack8(const float (&v)[8], uint32_t& byte) {
-  uint32_t top = 0;
+  float m = fabsf(v[0]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);      // as integers: NaN above infinity above the rest
+  for (int i = 1; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(v[i])));
+  uint32_t top = __float_as_uint(m);                     // as integers from here: NaN above infinity above the rest
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const int e = (int)(top >> 23);
   byte = e == 255 ? 255u : (top == 0 ? 0u : (uint32_t)max(e - 6, 1));
   const float up = __uint_as_float((254u - (e == 255 ? 1u : byte)) << 23);              // 2^(127 - byte)
   uint32_t q[8];
+  if (__any_sync(0xffffffffu, (top & 0x7fffffu) >= 0x7f0000u)) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    q[i] = __float_as_uint(fminf(fmaxf(v[i] * up, -127.f), 127.f) + 12582912.f);        // 1.5 * 2^23: the integer stands in the low bits
+    for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(fminf(fmaxf(v[i] * up, -127.f), 127.f) + 12582912.f);
+  } else {
+    const uint64_t u2 = pk2(up, up), magic = pk2(12582912.f, 12582912.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = upk2(fma2(pk2(v[2 * i], v[2 * i + 1]), u2, magic));
+      q[2 * i] = __float_as_uint(f.x); q[2 * i + 1] = __float_as_uint(f.y);
+    }
+  }
   uint2 w;
   w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
   w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
@@ -120,11 +165,13 @@ __device__ __forceinline__ uint2 pack8(const float (&v)[8], uint32_t& byte) {
 }
 __device__ __forceinline__ void unpack8(uint2 w, uint32_t byte, float (&v)[8]) {
   const float s = __uint_as_float(byte << 23);
-  const uint32_t x = w.x ^ 0x80808080u, y = w.y ^ 0x80808080u;                          // code + 128
+  const uint64_t scale = pk2(s, s), off = pk2(-8388736.f, -8388736.f);                  // 2^23 + 128
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[i] = (__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + i)) - 8388736.f) * s;  // 2^23 + 128
-    v[4 + i] = (__uint_as_float(__byte_perm(y, 0x4b000000u, 0x7440 + i)) - 8388736.f) * s;
+    const uint32_t x = (i < 2 ? w.x : w.y) ^ 0x80808080u;                               // code + 128
+    const uint64_t c = pk2(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + 2 * (i & 1))), __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7441 + 2 * (i & 1))));
+    const float2 f = upk2(mul2(add2(c, off), scale));
+    v[2 * i] = f.x; v[2 * i + 1] = f.y;
   }
 }
 __device__ __forceinline__ uint2 ld_codes(const unsigned char* p) {
@@ -143,6 +190,7 @@ __device__ __forceinline__ void item_place(const ItemWalk& k, int64_t i, int64_t
   if (k.items <= 0xffffffffll) { const uint32_t r = (uint32_t)i / (uint32_t)k.per_row; row = r; v = (int)((uint32_t)i - r * (uint32_t)k.per_row); }
   else { row = i / k.per_row; v = (int)(i - row * k.per_row); }
 }
+__device__ __forceinline__ bool one_row(int64_t row) { return __all_sync(0xffffffffu, row == __shfl_sync(0xffffffffu, row, 0)); }
 // entries of item v of a row that exist
 __device__ __forceinline__ int item_count(const ItemWalk& k, int v) { return max(0, min(8, k.width - 8 * v)); }
 
@@ -157,7 +205,7 @@ __device__ __forceinline__ void store_packed(const PackedRows& t, int64_t row, i
 }
 
 template <int KIND, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float v[U][8];
@@ -197,7 +245,9 @@ __global__ void __launch_bounds__(PK_THREADS) unpack_kernel(const PackedRows in,
   for (int j = 0; j < U; ++j) {
     float v[8];
     unpack8(w[j], byte[j], v);
-    if (first + j * PK_THREADS < k.items) store8<KIND, ALIGNED>(x, row[j], 8 * at[j], item_count(k, at[j]), v);
+    const int n = first + j * PK_THREADS < k.items ? item_count(k, at[j]) : 0;
+    if (ALIGNED) store8<KIND, true>(x, row[j], 8 * at[j], n, v);
+    else store8_any<KIND>(x, row[j], 8 * at[j], n, v, one_row(row[j]));
   }
 }
 
@@ -217,7 +267,10 @@ __device__ __forceinline__ float act_gate(float a, float& s) {
     return p;
   }
   const float z = ACT == ACT_SILU ? a : 1.5957691216057308f * fmaf(0.044715f * a * a, a, a);
-  const float t = __expf(-fabsf(z)), r = __fdividef(1.f, 1.f + t), tr = t * r, q = tr * r;
+  float r;
+  const float t = __expf(-fabsf(z));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));      // of a number from 1 to 2
+  const float tr = t * r, q = tr * r;
   const float p = z < 0.f ? tr : r;
   if (ACT == ACT_SILU) s = fmaf(a, q, p);
   else s = q == 0.f ? p : fmaf(a * q, 1.5957691216057308f * fmaf(0.134145f * a, a, 1.f), p);      // far out z' overflows where q is 0
@@ -231,7 +284,7 @@ struct GatedArgs {
 };
 
 template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS) gated_kernel(const GatedArgs g, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) gated_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float a[U][8], u[U][8];
@@ -266,12 +319,13 @@ __global__ void __launch_bounds__(PK_THREADS) gated_kernel(const GatedArgs g, co
       y[e] = a[j][e] * act_gate<ACT>(a[j][e], s);
       if (GATED) y[e] *= u[j][e];
     }
-    store8<KIND, ALIGNED>(g.y, row[j], 8 * at[j], n, y);
+    if (ALIGNED) store8<KIND, true>(g.y, row[j], 8 * at[j], n, y);
+    else store8_any<KIND>(g.y, row[j], 8 * at[j], n, y, one_row(row[j]));
   }
 }
 
 template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float dy[U][8];
@@ -306,8 +360,14 @@ __global__ void __launch_bounds__(PK_THREADS) gated_backward_kernel(const GatedA
       a[e] = GATED ? dy[j][e] * u[e] * s : dy[j][e] * s;
       if (GATED) { dy[j][e] *= f[e]; f[e] *= u[e]; }
     }
-    store8<KIND, ALIGNED>(g.da, row[j], 8 * at[j], n, a);
-    if (GATED) store8<KIND, ALIGNED>(g.du, row[j], 8 * at[j], n, dy[j]);
+    if (ALIGNED) {
+      store8<KIND, true>(g.da, row[j], 8 * at[j], n, a);
+      if (GATED) store8<KIND, true>(g.du, row[j], 8 * at[j], n, dy[j]);
+    } else {
+      const bool same = one_row(row[j]);
+      store8_any<KIND>(g.da, row[j], 8 * at[j], n, a, same);
+      if (GATED) store8_any<KIND>(g.du, row[j], 8 * at[j], n, dy[j], same);
+    }
     if (g.py.codes) {
       round8<KIND>(f);
       uint32_t byte;
