@@ -70,6 +70,9 @@ PackedRows packed_of(const void* p, int64_t rows, int64_t width) {
 ItemWalk walk_of(int64_t rows, int64_t width) {
   ItemWalk k;
   k.per_row = (int)(4 * blocks_of(width)); k.items = rows * k.per_row; k.rows = rows; k.width = (int)width;
+  uint32_t l = 2;
+  while (((int64_t)1 << l) < k.per_row) ++l;
+  k.magic = (uint32_t)((((uint64_t)1 << (31 + l)) + k.per_row - 1) / k.per_row); k.shift = l - 1;
   return k;
 }
 // Entries per thread: several vectors in flight where there is enough work for that.

@@ -185,9 +185,10 @@ struct ItemWalk {
   int64_t items;         // rows * per_row
   int64_t rows;
   int width, per_row;    // items of a row: 4 * blocks
+  uint32_t magic, shift; // i / per_row = (i magic) >> (32 + shift) for i < 2^31: with l = ceil(log2 per_row), magic = ceil(2^(31 + l) / per_row), shift = l - 1
 };
 __device__ __forceinline__ void item_place(const ItemWalk& k, int64_t i, int64_t& row, int& v) {
-  if (k.items <= 0xffffffffll) { const uint32_t r = (uint32_t)i / (uint32_t)k.per_row; row = r; v = (int)((uint32_t)i - r * (uint32_t)k.per_row); }
+  if (k.items <= 0x7fffffffll) { const uint32_t r = __umulhi((uint32_t)i, k.magic) >> k.shift; row = r; v = (int)((uint32_t)i - r * (uint32_t)k.per_row); }
   else { row = i / k.per_row; v = (int)(i - row * k.per_row); }
 }
 __device__ __forceinline__ bool one_row(int64_t row) { return __all_sync(0xffffffffu, row == __shfl_sync(0xffffffffu, row, 0)); }
