@@ -5,7 +5,11 @@ Everything between the logits and the updated weights is this package's: referen
 the step: the spectral weight goes through the sparse + low-rank optimizer, the dense ones through AdamW, both scaled by the
 clipping coefficient, which never leaves the device.
 
-    python examples/spectral_lm.py [--steps 60]
+With --blocks n, n gated feed-forward blocks stand behind the Fourier layer.  They keep for their backward pass 8 bits an entry: the
+normalised input, both halves of the first layer's output and the block's output; norms, gate, activation and weight
+gradients are this package's.
+
+    python examples/spectral_lm.py [--steps 60] [--blocks 2]
 """
 import argparse
 import os
@@ -17,17 +21,64 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2501_02379_b200 import binding as B  # noqa: E402
 
 VOCAB, WIDTH, LENGTH, PROMPT = 1000, 64, 64, 16
+HIDDEN = 160
+
+
+class FirstNorm(torch.autograd.Function):
+    """x -> (x, h = norm(x), h packed)."""
+
+    @staticmethod
+    def forward(ctx, x, weight):
+        r = B.residual_norm(x, weight=weight, keep_h=True)
+        ctx.save_for_backward(r.x, r.stats, weight)
+        ctx.mark_non_differentiable(r.h8.data)
+        return r.x, r.h, r.h8.data
+
+    @staticmethod
+    def backward(ctx, grad_x, grad_h, _):
+        x, stats, weight = ctx.saved_tensors
+        g = B.residual_norm_backward(grad_h.contiguous(), x, stats, grad_x=grad_x.contiguous(), weight=weight)
+        return g.x, g.weight
+
+
+class FeedForward(torch.autograd.Function):
+    """(x, h, h packed) -> (x' = x + gate * norm(f), h' = norm(x'), h' packed) with f = w_out (silu(a) u), (a, u) = w_in h."""
+
+    @staticmethod
+    def forward(ctx, x, h, h8, w_in, w_out, post_weight, gate, weight):
+        a, u = (h @ w_in.T).split(HIDDEN, 1)
+        y, a8, u8 = B.gated_act(a, u)
+        r = B.residual_norm(x, y @ w_out.T, weight=weight, post_weight=post_weight, gate=gate, keep_f=True, keep_h=True)
+        ctx.save_for_backward(h8, a8.data, u8.data, r.f8.data, r.x, r.stats, w_in, w_out, post_weight, gate, weight)
+        ctx.mark_non_differentiable(r.h8.data)
+        return r.x, r.h, r.h8.data
+
+    @staticmethod
+    def backward(ctx, grad_x, grad_h, _):
+        h8, a8, u8, f8, x, stats, w_in, w_out, post_weight, gate, weight = ctx.saved_tensors
+        rows, width = x.shape
+        kept = lambda data, n: B.Packed(data, rows, n, x.dtype)  # noqa: E731
+        n = B.residual_norm_backward(grad_h.contiguous(), x, stats, kept(f8, width), grad_x=grad_x.contiguous(), weight=weight, post_weight=post_weight, gate=gate)
+        d = x.new_empty(rows, 2 * HIDDEN)
+        g = B.gated_act_backward(kept(a8, HIDDEN), kept(u8, HIDDEN), n.f @ w_out, keep_y=True, da=d[:, :HIDDEN], du=d[:, HIDDEN:])
+        return n.x, d @ w_in, None, B.weight_grad(d, kept(h8, width)), B.weight_grad(n.f, g.y8), n.post_weight, n.gate, n.weight
 
 
 class SpectralLM(torch.nn.Module):
-    """Embedding, one causal spectral convolution over the sequence (complex weight WIDTH x WIDTH x modes), head."""
+    """Embedding, one causal spectral convolution over the sequence (complex weight WIDTH x WIDTH x modes), feed-forward blocks, head."""
 
-    def __init__(self, modes=32):
+    def __init__(self, modes=32, blocks=0):
         super().__init__()
         self.embedding = torch.nn.Parameter(torch.randn(VOCAB, WIDTH) * 0.3)
         self.spectral = torch.nn.Parameter(torch.randn(WIDTH, WIDTH, modes, dtype=torch.complex64) * 0.02)
         self.bias = torch.nn.Parameter(torch.zeros(WIDTH))
         self.head = torch.nn.Parameter(torch.randn(WIDTH, VOCAB) * 0.05)
+        self.blocks = torch.nn.ModuleList()
+        if blocks:
+            self.norm = torch.nn.Parameter(torch.ones(WIDTH))
+        for _ in range(blocks):
+            self.blocks.append(torch.nn.ParameterDict({"w_in": torch.randn(2 * HIDDEN, WIDTH) * WIDTH ** -0.5, "w_out": torch.randn(WIDTH, HIDDEN) * HIDDEN ** -0.5,
+                                                       "post_weight": torch.ones(WIDTH), "gate": torch.full((WIDTH,), 0.1), "weight": torch.ones(WIDTH)}))
 
     def forward(self, tokens):
         x = self.embedding[tokens]                                              # [batch, length, width]
@@ -36,6 +87,11 @@ class SpectralLM(torch.nn.Module):
         spectrum = torch.einsum("bif,iof->bof", torch.fft.rfft(x.transpose(1, 2), n=n), torch.fft.rfft(kernel, n=n))
         mixed = torch.fft.irfft(spectrum, n=n)[..., :tokens.shape[1]].transpose(1, 2)
         x = x + torch.nn.functional.gelu(mixed + self.bias)
+        if self.blocks:
+            x, h, h8 = FirstNorm.apply(x.flatten(0, 1), self.norm)
+            for b in self.blocks:
+                x, h, h8 = FeedForward.apply(x, h, h8, b["w_in"], b["w_out"], b["post_weight"], b["gate"], b["weight"])
+            return h @ self.head
         return (x @ self.head).flatten(0, 1)                                    # [batch * length, vocab]
 
 
@@ -79,7 +135,7 @@ def pairs_batch(pairs, gen):
 
 def train_preference(model, trainer, steps, pairs=16, seed=0):
     gen = torch.Generator("cuda").manual_seed(seed)
-    reference = SpectralLM().cuda()
+    reference = SpectralLM(blocks=len(model.blocks)).cuda()
     reference.load_state_dict(model.state_dict())
     log = []
     for _ in range(steps):
@@ -114,9 +170,9 @@ def train_policy(model, trainer, steps, batch=64, updates=2, seed=1):
     return torch.stack(log).cpu()
 
 
-def main(steps=60):
+def main(steps=60, blocks=0):
     torch.manual_seed(0)
-    model = SpectralLM().cuda()
+    model = SpectralLM(blocks=blocks).cuda()
     trainer = Trainer(model)
     pref = train_preference(model, trainer, steps)
     print("preference loss %.4f -> %.4f, chosen preferred %.2f -> %.2f" % (pref[0, 0], pref[-1, 0], pref[0, 1], pref[-5:, 1].mean()))
@@ -130,4 +186,6 @@ def main(steps=60):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=60)
-    main(ap.parse_args().steps)
+    ap.add_argument("--blocks", type=int, default=0)
+    args = ap.parse_args()
+    main(args.steps, args.blocks)
