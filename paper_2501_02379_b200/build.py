@@ -3,12 +3,14 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtgrad.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC"]
+              "-Xcompiler", "-fPIC"]
 
 
 def sources():
@@ -29,12 +31,21 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources()
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+
+    def run(args):
+        res = subprocess.run([nvcc] + args, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        return res.stderr
+
+    with tempfile.TemporaryDirectory() as tmp:      # the sources side by side, then the library
+        objects = [os.path.join(tmp, os.path.basename(f) + ".o") for f in sources()]
+        compile_flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
+        with ThreadPoolExecutor(len(objects)) as pool:
+            logs = list(pool.map(lambda fo: run(compile_flags + ["-c", "-o", fo[1], fo[0]]), zip(sources(), objects)))
+        run(NVCC_FLAGS + ["-shared", "-o", LIB] + objects)
     if verbose:
-        print(res.stderr)
+        print("".join(logs))
     return LIB
 
 
