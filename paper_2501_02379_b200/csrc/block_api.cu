@@ -302,7 +302,7 @@ EncodeTiledFn encode_tiled() {
   return fn;
 }
 
-struct WgradPlan { int terms, tn, tiles_n, tiles_k, splits; int64_t steps, per_split; bool copy; int64_t ld; size_t parts_bytes, partial_bytes; };
+struct WgradPlan { int terms, tn, tiles_n, tiles_k, whole, splits, clusters; int64_t steps, per_split; bool copy; int64_t ld; size_t parts_bytes, partial_bytes; };
 WgradPlan wgrad_plan(const tgrad_weight_grad_args* c, int sm) {
   WgradPlan p;
   const int kind = kind_of(c->dtype);
@@ -311,26 +311,35 @@ WgradPlan wgrad_plan(const tgrad_weight_grad_args* c, int sm) {
   p.ld = p.copy ? (c->out + 7) / 8 * 8 : c->rows > 1 ? c->dy.row_stride : (c->out + 7) / 8 * 8;
   p.tn = kind_of(c->out_dtype) == LS_F32 ? 128 : 256;      // columns of x of a tile: the sums of fp32 results have to fit in registers
   p.tiles_n = (int)((c->out + WG_TILE_N - 1) / WG_TILE_N); p.tiles_k = (int)((c->width + p.tn - 1) / p.tn);
-  p.steps = (c->rows + WG_TOKENS - 1) / WG_TOKENS * p.terms;
-  // Parts of the tokens: as many as fill the SMs (two to a tile) once, of eight steps at least.
-  const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-  int64_t splits = sm / 2 / tiles;
-  if (splits > p.steps / 8) splits = p.steps / 8;
-  if (splits < 1) splits = 1;
+  const int tokens = p.tn == 128 ? WgGeom<128>::TOKENS : WgGeom<256>::TOKENS;
+  p.steps = (c->rows + tokens - 1) / tokens * p.terms;
+  // Whole tiles for all full rounds of the clusters (two SMs each); what is left is split along the tokens, in parts of 512 at least, as many as
+  // keep the clusters busy for one round.
+  const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k, clusters = sm / 2 < 1 ? 1 : sm / 2;
+  int64_t rest = tiles % clusters, splits = rest ? clusters / rest : 1;
+  if (splits > p.steps * tokens / 512) splits = p.steps * tokens / 512;
+  if (splits < 2) { splits = 1; rest = 0; }
   p.per_split = (p.steps + splits - 1) / splits;
   p.splits = (int)(p.per_split ? (p.steps + p.per_split - 1) / p.per_split : 1);
+  if (p.splits < 2) { p.splits = 1; rest = 0; }
+  p.whole = (int)(tiles - rest);
+  const int64_t units = p.whole + rest * p.splits;
+  p.clusters = (int)(units < clusters ? units : clusters);
   p.parts_bytes = p.copy ? align_up((size_t)p.terms * c->rows * p.ld * 2) : 0;
-  p.partial_bytes = p.splits > 1 ? align_up((size_t)p.splits * tiles * WG_TILE_N * p.tn * 4) : 0;
+  p.partial_bytes = p.splits > 1 ? align_up((size_t)p.splits * rest * WG_TILE_N * p.tn * 4) : 0;
   return p;
 }
 template <bool F16, int TN>
-tgrad_status wgrad_launch(const WgradPlan& p, int sm, const CUtensorMap& map_dy, const CUtensorMap& map_codes, const WgradArgs& a, cudaStream_t st) {
+tgrad_status wgrad_launch(const WgradPlan& p, const CUtensorMap& map_dy, const CUtensorMap& map_codes, const WgradArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
   TG_TRY(allow_shared(wgrad_kernel<F16, TN>, WgGeom<TN>::SMEM, done));
-  const int64_t units = (int64_t)p.tiles_n * p.tiles_k * p.splits;
-  const int64_t clusters = units < sm / 2 ? units : sm / 2;
-  launch_cluster(wgrad_kernel<F16, TN>, dim3((unsigned)(2 * clusters)), dim3(WgGeom<TN>::THREADS), WgGeom<TN>::SMEM, 2, st, map_dy, map_codes, a);
+  launch_cluster(wgrad_kernel<F16, TN>, dim3((unsigned)(2 * p.clusters)), dim3(WgGeom<TN>::THREADS), WgGeom<TN>::SMEM, 2, st, map_dy, map_codes, a);
   TG_LAUNCH_CHECK();
+  if (p.splits > 1) {
+    const int64_t threads = ((int64_t)p.tiles_n * p.tiles_k - p.whole) * WG_TILE_N * (TN / 8);
+    launch_chained(wgrad_sum_kernel<TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a);
+    TG_LAUNCH_CHECK();
+  }
   return TGRAD_OK;
 }
 tgrad_status check_wgrad(const tgrad_weight_grad_args* c) {
@@ -488,35 +497,29 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   }
   const PackedRows x = packed_of(c->d_packed, c->rows, c->width);
   a.exps = x.exps; a.exp_words = x.exp_stride / 4;
-  a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
-  // fp32 results leave tensor memory after every 32 instructions (8 steps of 64 tokens), 16-bit ones once
-  a.group = to == LS_F32 ? 8 : 0x7fffffff;
-  a.ld_partial = (int64_t)p.tiles_k * p.tn;
+  a.whole = p.whole; a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
+  // fp32 results leave tensor memory after every 32 instructions (4 steps of 128 tokens), 16-bit ones once
+  a.group = to == LS_F32 ? 4 : 0x7fffffff;
   a.partial = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.parts_bytes) : nullptr;
   const bool f16 = kind == LS_F16;
   CUtensorMap map_dy, map_codes;
-  const cuuint32_t one[3] = {1, 1, 1};
+  const cuuint32_t one[3] = {1, 1, 1}, tokens = p.tn == 128 ? WgGeom<128>::TOKENS : WgGeom<256>::TOKENS;
   {
     const cuuint64_t dims[3] = {(cuuint64_t)(p.copy ? p.ld : c->out), (cuuint64_t)c->rows, (cuuint64_t)p.terms};
     const cuuint64_t strides[2] = {(cuuint64_t)p.ld * 2, (cuuint64_t)p.ld * 2 * c->rows};
-    const cuuint32_t box[3] = {64, WG_TOKENS, 1};
+    const cuuint32_t box[3] = {64, tokens, 1};
     if (enc(&map_dy, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(dy), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return TGRAD_ERR_CUDA;
   }
   {
     const cuuint64_t dims[3] = {(cuuint64_t)(32 * x.blocks), (cuuint64_t)c->rows, 1};
     const cuuint64_t strides[2] = {(cuuint64_t)(32 * x.blocks), (cuuint64_t)(32 * x.blocks) * c->rows};
-    const cuuint32_t box[3] = {(cuuint32_t)p.tn / 2, WG_TOKENS, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)p.tn / 2, tokens, 1};
     if (enc(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, x.codes, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) return TGRAD_ERR_CUDA;
   }
-  if (f16) TG_TRY(to == LS_F32 ? (wgrad_launch<true, 128>(p, sm, map_dy, map_codes, a, st)) : (wgrad_launch<true, 256>(p, sm, map_dy, map_codes, a, st)));
-  else TG_TRY(to == LS_F32 ? (wgrad_launch<false, 128>(p, sm, map_dy, map_codes, a, st)) : (wgrad_launch<false, 256>(p, sm, map_dy, map_codes, a, st)));
-  if (p.splits > 1) {
-    const int64_t blocks = ((int64_t)a.N * ((a.K + 7) / 8) + 255) / 256;
-    launch_chained(wgrad_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
-    TG_LAUNCH_CHECK();
-  }
+  if (f16) TG_TRY(to == LS_F32 ? (wgrad_launch<true, 128>(p, map_dy, map_codes, a, st)) : (wgrad_launch<true, 256>(p, map_dy, map_codes, a, st)));
+  else TG_TRY(to == LS_F32 ? (wgrad_launch<false, 128>(p, map_dy, map_codes, a, st)) : (wgrad_launch<false, 256>(p, map_dy, map_codes, a, st)));
   return TGRAD_OK;
 }
 

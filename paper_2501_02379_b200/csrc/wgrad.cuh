@@ -2,7 +2,7 @@
 //
 // A matrix product whose contraction runs over the rows of both operands, on the 5th-generation tensor cores.  Two blocks on neighbouring SMs
 // (a cluster, tcgen05 with cta_group::2) share a tile of 256 columns of dy by TN of x; each holds 128 of dy's and TN / 2 of x's.  Per
-// step of 64 tokens, in each block:
+// step of 64 tokens (128 where TN is 128), in each block:
 //   * one thread loads dy's boxes (64 tokens of 64 entries, 128-byte swizzle) and the codes' (64 tokens) by tiled TMA, a warp the blocks'
 //     bytes (a word a token);
 //   * eight warps (four where TN is 128) turn the codes into 16-bit numbers in the layout that the tensor core reads: x^ = code 2^e has 7 bits, so it is exact in
@@ -17,7 +17,8 @@
 // for 16384 x 4096 x 14336 that way).
 // fp32 dy is split beforehand into three bfloat16 parts that add up to it exactly, which are three times as many steps into the same sums;
 // 16-bit dy that TMA cannot address (rows that do not start at multiples of 16 bytes) is copied beforehand.
-// Few tiles and many tokens: the tokens are split between clusters, whose sums a second launch adds in a fixed order.
+// The tiles behind the last full round of the clusters (all, where there are few): their tokens are split between clusters, whose sums a second
+// launch adds in a fixed order.  (16384 x 4096 x 14336 has 896 tiles for 74 clusters: 12 rounds and 8 tiles.)
 // Every wait is bounded; one that ran out leaves NaN in the tiles that its block did not finish.
 #pragma once
 #include <cuda.h>
@@ -26,16 +27,17 @@
 namespace tg {
 
 // Warp 0: TMA, 1: MMA issue, 2: the blocks' bytes, 3: tensor memory, then two groups of NW that turn codes into numbers, then 8 for the sums.
-constexpr int WG_TOKENS = 64, WG_TILE_N = 256;
-constexpr int WG_BOX = 64 * 128;                                  // bytes of 64 tokens by 64 16-bit entries
+constexpr int WG_TILE_N = 256;
 // Three rings of shared memory, for three lifetimes: dy's boxes from their copy to the end of the instructions that read them, codes from their copy
 // until they are numbers, numbers from then to the end of the instructions.  (One ring of stages that hold all three has five of them, too few
 // to cover the copies' latency: 588 ns a step instead of the 270 that the tensor cores take.)
 template <int TN> struct WgGeom {
+  static constexpr int TOKENS = TN == 256 ? 64 : 128;             // of a step: 16 KB of numbers for a block either way
+  static constexpr int BOX = TOKENS * 128;                        // bytes of a step's tokens by 64 16-bit entries
   static constexpr int H = TN / 2;                                // columns of x of a block
   static constexpr int NW = TN == 256 ? 8 : 4, THREADS = 32 * (4 + 2 * NW + 8);      // (with fp32 sums, 96 registers a thread)
-  static constexpr int SA = TN == 256 ? 6 : 8, SB = 4;      // places for copies (dy's and codes'), for numbers: even, the groups take every second one
-  static constexpr int A_BYTES = 2 * WG_BOX, B_BYTES = H * WG_TOKENS * 2, C_BYTES = H * WG_TOKENS, E_BYTES = WG_TOKENS * 4;
+  static constexpr int SA = TN == 256 ? 6 : 4, SB = TN == 256 ? 4 : 3;      // places for copies (dy's and codes'), for numbers
+  static constexpr int A_BYTES = 2 * BOX, B_BYTES = H * TOKENS * 2, C_BYTES = H * TOKENS, E_BYTES = TOKENS * 4;
   static constexpr int B = SA * A_BYTES, C = B + SB * B_BYTES, E = C + SA * C_BYTES;      // dy's ring stands first
   static constexpr size_t SMEM = (size_t)E + SA * E_BYTES + 1024;
 };
@@ -48,13 +50,13 @@ struct WgradArgs {
   int64_t tokens;
   int terms;                 // parts of dy (3 for fp32)
   int N, K;
-  int tiles_n, tiles_k, splits;
-  int64_t steps, per_split;  // steps of the whole contraction and of a split
+  int tiles_n, tiles_k;
+  int whole, splits;         // tiles whose sums one cluster forms; parts of the tokens of the others
+  int64_t steps, per_split;  // steps of the whole contraction and of a part
   int group;                 // steps between two moves of the sums
   RowsOf out;
   int out_kind, accumulate;
-  float* partial;            // [splits][256 tiles_n][ld_partial]
-  int64_t ld_partial;
+  float* partial;            // [splits][tiles - whole][256][TN]
 };
 
 // ---- two blocks as one ----
@@ -124,10 +126,10 @@ struct WgRing {
   __device__ __forceinline__ void next(uint32_t by = 1) { if ((at += by) >= N) { at -= N; parity ^= 1; } }
 };
 
-// Descriptor of a tile whose columns are contiguous (128-byte swizzle): groups of 64 columns WG_BOX bytes apart, groups of 8 tokens 1,024.
-__device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr) {
+// Descriptor of a tile whose columns are contiguous (128-byte swizzle): groups of 64 columns `box` bytes apart, groups of 8 tokens 1,024.
+__device__ __forceinline__ uint64_t umma_desc_mn128(uint32_t smem_addr, uint32_t box) {
   uint64_t d = (uint64_t)((smem_addr & 0x3ffffu) >> 4);
-  d |= (uint64_t)(WG_BOX >> 4) << 16;
+  d |= (uint64_t)(box >> 4) << 16;
   d |= (uint64_t)(1024 >> 4) << 32;
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
@@ -210,12 +212,13 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
   const uint32_t tmem = tmem_slot;
   griddep_chain();
 
-  const int tiles = A.tiles_n * A.tiles_k, units = tiles * A.splits, clusters = gridDim.x >> 1, mine = blockIdx.x >> 1;
-  // what a unit (a tile and a part of the tokens) is
+  // A unit is a tile, or a part of the tokens of one of the tiles behind the last full round of the clusters.
+  const int rest = A.tiles_n * A.tiles_k - A.whole, units = A.whole + rest * A.splits, clusters = gridDim.x >> 1, mine = blockIdx.x >> 1;
+  auto tile_of = [&](int unit) { return unit < A.whole ? unit : A.whole + (unit - A.whole) % rest; };
+  auto part_of = [&](int unit) { return unit < A.whole ? 0 : (unit - A.whole) / rest; };
   auto steps_of = [&](int unit, int64_t& from) {
-    const int64_t sp = unit / tiles;
-    from = sp * A.per_split;
-    return (uint32_t)max((int64_t)0, min(A.per_split, A.steps - from));
+    from = part_of(unit) * A.per_split;
+    return (uint32_t)(unit < A.whole ? A.steps : max((int64_t)0, min(A.per_split, A.steps - from)));
   };
   bool ok = true;
 
@@ -223,22 +226,22 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
     WgRing<SA> a;
     uint32_t g = 0;
     for (int unit = mine; unit < units && ok; unit += clusters) {
-      int tn, tk; wg_tile(A, unit % tiles, tn, tk);
+      int tn, tk; wg_tile(A, tile_of(unit), tn, tk);
       const int n0 = tn * WG_TILE_N + (int)rank * 128, k0 = tk * TN + (int)rank * G::H;
       int64_t from; const uint32_t n = steps_of(unit, from);
-      int m0 = (int)(from / A.terms) * WG_TOKENS, term = (int)(from % A.terms);
+      int m0 = (int)(from / A.terms) * G::TOKENS, term = (int)(from % A.terms);
       for (uint32_t it = 0; it < n; ++it, ++g, a.next()) {
         ok = wg_wait(&c_empty[a.at], a.parity ^ 1, failed) && wg_wait(&a_empty[a.at], a.parity ^ 1, failed);
         if (!ok) break;
         if (elect_one()) {
           const uint32_t at = ring + a.at * G::A_BYTES;
-          mbar_expect_tx(&full[a.at], 2 * WG_BOX + G::C_BYTES);
+          mbar_expect_tx(&full[a.at], 2 * G::BOX + G::C_BYTES);
           tma_load_3d(ring + G::C + a.at * G::C_BYTES, &map_codes, k0, m0, 0, &full[a.at]);
           tma_load_3d(at, &map_dy, n0, m0, term, &full[a.at]);
-          tma_load_3d(at + WG_BOX, &map_dy, n0 + 64, m0, term, &full[a.at]);
+          tma_load_3d(at + G::BOX, &map_dy, n0 + 64, m0, term, &full[a.at]);
         }
         __syncwarp();
-        if (++term == A.terms) { term = 0; m0 += WG_TOKENS; }
+        if (++term == A.terms) { term = 0; m0 += G::TOKENS; }
       }
     }
     // the tensor core's arrivals from the other block come in before this one ends, and so do copies after a wait that ran out
@@ -250,7 +253,7 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
     if (rank == 0) {
       // fp32 accumulator, both operands with their columns contiguous (bits 15, 16), 256 rows
       const uint32_t idesc = (umma_idesc(F16 ? 0 : 1, TN) & 0x00ffffffu) | (16u << 24) | (1u << 15) | (1u << 16);
-      const uint64_t da0 = umma_desc_mn128(ring), db0 = umma_desc_mn128(ring + G::B);
+      const uint64_t da0 = umma_desc_mn128(ring, G::BOX), db0 = umma_desc_mn128(ring + G::B, G::BOX);
       WgRing<SA> a;
       WgRing<SB> b;
       WgRing<2> acc;
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
           if (elect_one()) {
             const uint64_t da = da0 + (uint64_t)(a.at * (G::A_BYTES >> 4)), db = db0 + (uint64_t)(b.at * (G::B_BYTES >> 4));
 #pragma unroll
-            for (int ks = 0; ks < WG_TOKENS / 16; ++ks)      // 16 tokens: two groups of 8
+            for (int ks = 0; ks < G::TOKENS / 16; ++ks)      // 16 tokens: two groups of 8
               umma2_f16(tmem + acc.at * TN, da + (uint64_t)(ks * 2048 >> 4), db + (uint64_t)(ks * 2048 >> 4), idesc, in_group != 0 || ks != 0);
             umma2_commit(&b_empty[b.at]);
             umma2_commit(&a_empty[a.at]);
@@ -279,33 +282,33 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
   } else if (warp == 2) {
     WgRing<SA> a;
     for (int unit = mine; unit < units && ok; unit += clusters) {
-      int tn, tk; wg_tile(A, unit % tiles, tn, tk);
+      int tn, tk; wg_tile(A, tile_of(unit), tn, tk);
       const int word = (tk * TN + (int)rank * G::H) >> 7;
       int64_t from; const uint32_t n = steps_of(unit, from);
-      int m0 = (int)(from / A.terms) * WG_TOKENS, term = (int)(from % A.terms);
+      int m0 = (int)(from / A.terms) * G::TOKENS, term = (int)(from % A.terms);
       for (uint32_t it = 0; it < n; ++it, a.next()) {
         ok = wg_wait(&c_empty[a.at], a.parity ^ 1, failed);
         if (!ok) break;
         unsigned char* to = wg_raw + (ring - raw) + G::E + a.at * G::E_BYTES;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < G::TOKENS / 32; ++h) {
           const int64_t m = (int64_t)m0 + lane + 32 * h;
           const bool in = m < A.tokens && word < A.exp_words;
           cp_async4(to + 4 * (lane + 32 * h), A.exps + (in ? (m * A.exp_words + word) * 4 : 0), in ? 4 : 0);
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[a.at])) : "memory");
-        if (++term == A.terms) { term = 0; m0 += WG_TOKENS; }
+        if (++term == A.terms) { term = 0; m0 += G::TOKENS; }
       }
     }
     cp_async_wait<0>();
   } else if (warp >= 4 && warp < 4 + 2 * NW) {
-    constexpr int Q = G::H / 8, T = 32 * NW, PER = WG_TOKENS * Q / T;      // vectors of 8 columns per token; threads of a group; vectors of a thread
+    constexpr int Q = G::H / 8, T = 32 * NW, PER = G::TOKENS * Q / T;      // vectors of 8 columns per token; threads of a group; vectors of a thread
     const int w = (tid - 128) % T, group = (warp - 4) / NW;
     const int q = w % Q, m_first = w / Q;                       // this thread: columns 8 q .. of tokens m_first + i T / Q
     const uint32_t pick = 0x4040u + 0x0101u * (uint32_t)((q >> 2) + (TN == 128 ? 2 * (int)rank : 0));      // the block's byte of a token's word
     // (T / Q is a multiple of 8: the swizzle of a thread's vectors is the same for all its tokens)
     const uint32_t from_c = ring + G::C + m_first * G::H + q * 8, from_e = ring + G::E + m_first * 4;
-    const uint32_t to_b = ring + G::B + (q >> 3) * WG_BOX + m_first * 128 + (((q & 7) ^ (m_first & 7)) << 4);
+    const uint32_t to_b = ring + G::B + (q >> 3) * G::BOX + m_first * 128 + (((q & 7) ^ (m_first & 7)) << 4);
     WgRing<SA> a;
     WgRing<SB> b;
     a.at = b.at = group;                                        // this group's steps: every second one through all units
@@ -344,14 +347,14 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
     const int quarter = warp & 3, half = (warp - 4 - 2 * NW) >> 2; // tensor-memory lanes 32 * quarter .., columns W * half ..
     WgRing<2> acc;
     for (int unit = mine; unit < units; unit += clusters) {
-      int tn, tk; wg_tile(A, unit % tiles, tn, tk);
+      int tn, tk; wg_tile(A, tile_of(unit), tn, tk);
       int64_t from; const uint32_t n = steps_of(unit, from);
       const int64_t row = (int64_t)tn * WG_TILE_N + rank * 128 + quarter * 32 + lane;
       const int col = tk * TN + half * W;
       // 16 sums of a row: to the split's place, or rounded and stored
       auto put = [&](int c, const float (&v)[16]) {
-        if (A.partial) {
-          float4* p = reinterpret_cast<float4*>(A.partial + ((int64_t)(unit / tiles) * A.tiles_n * WG_TILE_N + row) * A.ld_partial + c);
+        if (unit >= A.whole && A.splits > 1) {
+          float4* p = reinterpret_cast<float4*>(A.partial + ((int64_t)(unit - A.whole) * WG_TILE_N + rank * 128 + quarter * 32 + lane) * TN + c - tk * TN);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         } else if (row < A.N) {
@@ -419,19 +422,22 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
   if (warp == 3) tmem_dealloc2(tmem, 2 * TN);
 }
 
-// dW from the splits' sums: 8 entries a thread, the splits in order.
+// The tiles whose tokens were split: 8 entries a thread, the parts in order.
+template <int TN>
 __global__ void __launch_bounds__(256) wgrad_sum_kernel(const WgradArgs A) {
   griddep_chain();
-  const int per = (A.K + 7) / 8;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)A.N * per) return;
-  const int64_t n = i / per;
-  const int k = (int)(i - n * per) * 8;
-  const int64_t ld = A.ld_partial, size = (int64_t)A.tiles_n * WG_TILE_N * ld;
+  constexpr int per = TN / 8;
+  const int rest = A.tiles_n * A.tiles_k - A.whole, t = (int)(i / (WG_TILE_N * per)), in = (int)(i - (int64_t)t * WG_TILE_N * per), r = in / per, c = (in - r * per) * 8;
+  if (t >= rest) return;
+  int tn, tk; wg_tile(A, A.whole + t, tn, tk);
+  const int64_t n = (int64_t)tn * WG_TILE_N + r;
+  const int k = tk * TN + c;
+  if (n >= A.N || k >= A.K) return;
   float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int s = 0; s < A.splits; ++s) {
-    const float4* p = reinterpret_cast<const float4*>(A.partial + s * size + n * ld + k);
+    const float4* p = reinterpret_cast<const float4*>(A.partial + (((int64_t)s * rest + t) * WG_TILE_N + r) * TN + c);
     const float4 a = p[0], b = p[1];
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
