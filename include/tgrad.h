@@ -440,7 +440,8 @@ tgrad_status tgrad_preference_loss(const tgrad_logits* logits, const tgrad_prefe
                                    size_t workspace_bytes, void* cuda_stream);
 
 /* For tests of that reporting: the kernels that stream rows of logits through shared memory stop within the first row that takes
- * more than so many copies (0: before any row), and the waits for further ones run out, after half a second.  Negative: never,
+ * more than so many copies (0: before any row), and the waits for further ones run out, after half a second.  The kernels of a trained
+ * block that copy ahead (norms of aligned rows, weight gradients) stop after so many rows or steps.  Negative: never,
  * the default.  For the whole process; the calls after this one take it. */
 tgrad_status tgrad_set_copy_limit(int32_t copies);
 
@@ -455,7 +456,7 @@ tgrad_status tgrad_set_copy_limit(int32_t copies);
  * block filled with zeros), then rows of B bytes, each padded to a multiple of 4.
  *
  * As above: nothing is kept between calls, everything is enqueued on the stream, sums have a fixed order and are fp32, results are rounded
- * to the storage type once.  Pointers need the alignment of their element type (packed ones 16 bytes).  A call's outputs must not overlap each other or
+ * to the storage type once, every wait of a kernel is bounded, and one that ran out leaves NaN (in the rows, column sums or tiles that were not finished).  Pointers need the alignment of their element type (packed ones 16 bytes).  A call's outputs must not overlap each other or
  * its inputs. */
 
 typedef struct {

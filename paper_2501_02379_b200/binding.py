@@ -680,8 +680,8 @@ def token_logprob_backward(logits, targets, lse, grad_logp, entropy=None, grad_e
 
 def set_copy_limit(copies: int = -1) -> None:
     """For tests: the kernels that stream rows of logits through shared memory stop within the first row that takes more than so
-    many copies (0: before any row, -1: never).  The waits for further ones run out, which leaves NaN in the rows that were not
-    finished.  For the whole process."""
+    many copies (0: before any row, -1: never), those of a trained block after so many rows or steps.  The waits for further ones run
+    out, which leaves NaN in the rows (tiles, sums) that were not finished.  For the whole process."""
     _check(lib().tgrad_set_copy_limit(int(copies)), "tgrad_set_copy_limit")
 
 
@@ -821,8 +821,8 @@ def _matrix(name, t):
     if width < 1:
         raise ValueError(f"{name} has no columns")
     stride, inner = t.stride()
-    if inner != 1 and width > 1:
-        raise ValueError(f"the entries of a row of {name} are adjacent")
+    if (inner != 1 and width > 1) or t.is_neg():
+        raise ValueError(f"the entries of a row of {name} are adjacent (and stand there as they are: resolve lazy negations)")
     return d, rows, width, t.get_device(), (t.data_ptr(), stride if rows > 1 else width)
 
 

@@ -236,7 +236,7 @@ tgrad_status norm_fast_launch(const NormPlan& p, ResNormArgs& a, bool backward, 
   const int which = !backward ? 0 : a.pf.codes ? 1 : 2;
   void (*kern)(ResNormArgs) = which == 0 ? norm_forward_fast_kernel<KIND, LN, V> : which == 1 ? norm_backward_fast_kernel<KIND, LN, V, true> : norm_backward_fast_kernel<KIND, LN, V, false>;
   TG_TRY(allow_shared(kern, kNormShared, done[which]));
-  a.stages = p.stages;
+  a.stages = p.stages; a.copies = g_copy_limit.load(std::memory_order_relaxed);
   launch_chained(kern, dim3(p.grid), dim3(p.tpr * p.teams), p.smem, st, a);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
@@ -500,6 +500,7 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   a.whole = p.whole; a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
   // fp32 results leave tensor memory after every 32 instructions (4 steps of 128 tokens), 16-bit ones once
   a.group = to == LS_F32 ? 4 : 0x7fffffff;
+  a.copies = g_copy_limit.load(std::memory_order_relaxed);
   a.partial = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.parts_bytes) : nullptr;
   const bool f16 = kind == LS_F16;
   CUtensorMap map_dy, map_codes;

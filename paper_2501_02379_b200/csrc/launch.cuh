@@ -9,6 +9,8 @@
 
 namespace tg {
 
+constexpr int kNoCopyLimit = 0x7fffffff;
+extern std::atomic<int> g_copy_limit;     // for tests: copies after which the streaming kernels stop (defined in train_api.cu)
 extern std::atomic<int64_t> g_launches;   // kernels launched since the library was loaded (defined in tgrad_api.cu)
 
 #define TG_LAUNCH_CHECK()                                  \

@@ -38,6 +38,7 @@ struct ResNormArgs {
   float scale, eps;
   float* stats;              // [2 or 4][rows]: 1 / deviation of f and x', then their means
   int tpr, stages;
+  int copies;                // for tests: rows that a team copies at most
   int64_t chunk;             // backward: rows of a row group
   float* part;               // backward: column sums
   int64_t part_stride;       // floats of a slot's row: 32 blocks
@@ -607,6 +608,7 @@ __device__ __noinline__ bool nm_wait_long(uint64_t* bar, uint32_t parity) {
 struct NmRing {
   uint64_t* bars;
   int stages, at = 0;
+  int copied = 0;
   uint32_t parity = 0, failed = 0;      // failed: 1 + the place and parity whose copy did not come
   float poison = 0.f;
   __device__ __forceinline__ void wait() {
@@ -712,7 +714,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
   const int64_t first = (int64_t)blockIdx.x * teams + mine, step = (int64_t)gridDim.x * teams;
   const bool folded = A.groups == 1 && !A.starts;
   auto issue = [&](int s, int64_t row) {                 // one thread
-    if (row >= A.rows || ring.failed) return;
+    if (row >= A.rows || ring.failed || ring.copied++ >= A.copies) return;
     mbar_expect_tx(&bars[s], bytes * per);
     const uint32_t to = places + (uint32_t)(s * per) * bytes;
     bulk_g2s_at(to, row_of<KIND>(A.x, row), bytes, &bars[s]);
@@ -863,7 +865,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
   const int64_t first = team_id * A.chunk, last = min(first + A.chunk, A.rows);
   const bool folded = A.groups == 1 && !A.starts;
   auto issue = [&](int s, int64_t row) {                 // one thread
-    if (row >= last || ring.failed) return;
+    if (row >= last || ring.failed || ring.copied++ >= A.copies) return;
     mbar_expect_tx(&bars[s], stage);
     const uint32_t to = places + (uint32_t)s * stage;
     bulk_g2s_at(to, row_of<KIND>(A.dh, row), bytes, &bars[s]);

@@ -54,6 +54,7 @@ struct WgradArgs {
   int whole, splits;         // tiles whose sums one cluster forms; parts of the tokens of the others
   int64_t steps, per_split;  // steps of the whole contraction and of a part
   int group;                 // steps between two moves of the sums
+  int copies;                // for tests: steps that a block copies at most
   RowsOf out;
   int out_kind, accumulate;
   float* partial;            // [splits][tiles - whole][256][TN]
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
       for (uint32_t it = 0; it < n; ++it, ++g, a.next()) {
         ok = wg_wait(&c_empty[a.at], a.parity ^ 1, failed) && wg_wait(&a_empty[a.at], a.parity ^ 1, failed);
         if (!ok) break;
-        if (elect_one()) {
+        if (g < (uint32_t)A.copies && elect_one()) {
           const uint32_t at = ring + a.at * G::A_BYTES;
           mbar_expect_tx(&full[a.at], 2 * G::BOX + G::C_BYTES);
           tma_load_3d(ring + G::C + a.at * G::C_BYTES, &map_codes, k0, m0, 0, &full[a.at]);

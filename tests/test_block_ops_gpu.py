@@ -465,6 +465,59 @@ def test_on_another_stream_and_captured():
         assert all(torch.equal(a, b) for a, b in zip(out, _chain(x, f, dh, w, gate)))
 
 
+def test_rows_far_apart():
+    """Rows whose distance passes 32 bits, in entries and in bytes."""
+    far, rows, width = (1 << 31) + 8, 3, 200
+    buf = torch.zeros(2 * far + 300, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((rows, width), (far, 1))
+    near = torch.randn(rows, width, generator=gen(1), device="cuda").bfloat16()
+    x.copy_(near)
+    p = B.act_pack(x)
+    assert torch.equal(p.data, B.act_pack(near).data)
+    r, q = B.gated_act(x, x), B.gated_act(near, near)
+    assert torch.equal(r.y, q.y) and torch.equal(r.u8.data, q.u8.data)
+    n, m = B.residual_norm(x, x, scale=0.5), B.residual_norm(near, near, scale=0.5)
+    assert torch.equal(n.x, m.x) and torch.equal(n.h, m.h)
+    assert all(torch.equal(a, b) for a, b in zip(B.residual_norm_backward(x, x, n.stats, x, grad_x=x)[:2], B.residual_norm_backward(near, near, n.stats, near, grad_x=near)[:2]))
+    assert torch.equal(B.weight_grad(x, p), B.weight_grad(near, p))
+    B.gated_act_backward(r.a8, r.u8, near, da=x)
+    assert torch.equal(x, B.gated_act_backward(r.a8, r.u8, near).da)
+    B.act_unpack(p, out=x)
+    assert torch.equal(x, B.act_unpack(p)) and float(buf.abs().max()) == float(x.abs().max())
+    del buf, x
+    torch.cuda.empty_cache()
+
+
+def test_waits_that_run_out_are_reported():
+    """The copies stop early: what was not finished is NaN, the calls return, and the next ones are right."""
+    x, f, dh, dx = (torch.randn(600, 8192, generator=gen(i), device="cuda").bfloat16() for i in range(4))
+    w = torch.ones(8192, device="cuda")
+    p = B.act_pack(x)
+    forward = lambda: B.residual_norm(x, f, weight=w, post_weight=w)  # noqa: E731
+    stats = forward().stats
+    backward = lambda: B.residual_norm_backward(dh, x, stats, f, grad_x=dx, weight=w, post_weight=w)  # noqa: E731
+    grads = [lambda: B.weight_grad(dh, p), lambda: B.weight_grad(dh, p, dtype=torch.float32)]
+    want = [forward(), backward(), [c() for c in grads]]
+    for limit in (0, 1, 2):
+        B.set_copy_limit(limit)
+        try:
+            r, g, dw = forward(), backward(), [c() for c in grads]
+            torch.cuda.synchronize()
+        finally:
+            B.set_copy_limit(-1)
+        for got, right in ((r.x, want[0].x), (r.h, want[0].h), (g.x, want[1].x), (g.f, want[1].f)):
+            bad = torch.isnan(got).all(1)
+            assert bool((bad | (got == right).all(1)).all()) and bool(bad.any() if limit < 2 else True)      # whole rows, or right ones
+        if limit == 0:
+            assert bool(torch.isnan(r.h).all()) and bool(torch.isnan(g.x).all()) and all(bool(torch.isnan(t).all()) for t in dw)
+        if bool(torch.isnan(g.x).any()):
+            assert bool(torch.isnan(g.weight).all()) and bool(torch.isnan(g.post_weight).all())
+        assert all(bool(torch.isnan(t).all()) or torch.equal(t, u) for t, u in zip(dw, want[2]))
+    again = [forward(), backward(), [c() for c in grads]]
+    assert all(a is b or torch.equal(a, b) for a, b in zip(again[0], want[0])) and all(a is b or torch.equal(a, b) for a, b in zip(again[1], want[1]))
+    assert all(torch.equal(a, b) for a, b in zip(again[2], want[2]))
+
+
 def test_two_streams_at_once():
     ins = [[torch.randn(3000, 512, generator=gen(10 * k + i), device="cuda").bfloat16() for i in range(3)] for k in range(2)]
     w, gate = torch.randn(512, generator=gen(4), device="cuda"), torch.randn(512, generator=gen(5), device="cuda")
@@ -500,7 +553,7 @@ def test_binding_refuses():
     p = B.act_pack(x)
     w = torch.ones(64, device="cuda")
     r = B.residual_norm(x, x, weight=w)
-    bad = [lambda: B.act_pack(x[0]), lambda: B.act_pack(x.T), lambda: B.act_pack(x.double()), lambda: B.act_pack(x[:, :0]), lambda: B.act_pack(x, out=B.act_pack(x[:2])),
+    bad = [lambda: B.act_pack(x[0]), lambda: B.act_pack(torch.complex(x, x).conj().imag), lambda: B.act_pack(x.T), lambda: B.act_pack(x.double()), lambda: B.act_pack(x[:, :0]), lambda: B.act_pack(x, out=B.act_pack(x[:2])),
            lambda: B.act_unpack(p._replace(rows=5)), lambda: B.act_unpack(p._replace(data=p.data[1:])), lambda: B.act_unpack(p, out=torch.zeros(4, 63, device="cuda")),
            lambda: B.act_unpack(p, out=x.half()), lambda: B.gated_act(x, x[:2]), lambda: B.gated_act(x, x.half()), lambda: B.gated_act_backward(p, None, x, du=x.clone()),
            lambda: B.gated_act_backward(p, p, x.half()), lambda: B.gated_act_backward(p, x, x), lambda: B.residual_norm(x, x, weight=w[:5]), lambda: B.residual_norm(x, x, weight=w.half()),
