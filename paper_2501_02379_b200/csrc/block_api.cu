@@ -498,8 +498,8 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   const PackedRows x = packed_of(c->d_packed, c->rows, c->width);
   a.exps = x.exps; a.exp_words = x.exp_stride / 4;
   a.whole = p.whole; a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
-  // fp32 results leave tensor memory after every 32 instructions (4 steps of 128 tokens), 16-bit ones once
-  a.group = to == LS_F32 ? 4 : 0x7fffffff;
+  // fp32 results leave tensor memory after every 32 instructions (4 steps of 128 tokens; 16 where the entries are fp32), 16-bit ones once
+  a.group = kind == LS_F32 ? 2 : to == LS_F32 ? 4 : 0x7fffffff;
   a.copies = g_copy_limit.load(std::memory_order_relaxed);
   a.partial = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.parts_bytes) : nullptr;
   const bool f16 = kind == LS_F16;

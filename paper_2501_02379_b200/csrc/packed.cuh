@@ -30,7 +30,9 @@ struct PackedRows {
   int blocks, exp_stride;
 };
 
-constexpr int PK_THREADS = 256, PK_BLOCKS = 8;      // blocks of an SM that the registers have to leave room for
+// Blocks of an SM that the registers of the 16-bit kernels have to leave room for: threads to switch between are worth a few spilled registers
+// (12000 x 2730 fp16, rows at odd words: gated activation 67 us, 81 without the bound; backward 60 and 79).
+constexpr int PK_THREADS = 256, PK_BLOCKS = 8, PK_BLOCKS_ODD = 6;
 
 // 8 entries of a row from entry c on, of which n (0..8) exist; the others are 0.  ALIGNED: al is 16 and n is 8 or 0.
 template <int KIND, bool ALIGNED>
@@ -100,7 +102,7 @@ __device__ __forceinline__ void shifted4(const uint32_t (&w)[8], int m, uint32_t
 // (16384 x 8191 bf16 read back from codes: 364 us).
 template <int KIND>
 __device__ __forceinline__ void store8_any(const RowsOf& t, int64_t row, int c, int n, const float (&v)[8], bool same) {
-  if (KIND == LS_F32 || t.al == 16 || !same) { store8<KIND, false>(t, row, c, n, v); return; }
+  if (KIND == LS_F32 || t.al >= 4 || !same) { store8<KIND, false>(t, row, c, n, v); return; }
   uint16_t* p = reinterpret_cast<uint16_t*>(t.p) + row * t.ld + c;
   const int m = __shfl_sync(0xffffffffu, (int)(reinterpret_cast<uintptr_t>(p) & 15), 0);      // bytes, the same for all lanes
   uint32_t w[8];                                                                              // the neighbour's words, then this lane's
@@ -206,7 +208,7 @@ __device__ __forceinline__ void store_packed(const PackedRows& t, int64_t row, i
 }
 
 template <int KIND, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float v[U][8];
@@ -285,7 +287,7 @@ struct GatedArgs {
 };
 
 template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) gated_kernel(const GatedArgs g, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float a[U][8], u[U][8];
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F3
 }
 
 template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, ALIGNED && U == 1 && KIND != LS_F32 ? PK_BLOCKS : 1) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
+__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
   const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
   float dy[U][8];
