@@ -1021,12 +1021,18 @@ def residual_norm_backward(grad_h, x, stats, f=None, grad_x=None, weight=None, p
     vectors = iter(torch.empty((sum(want), width), dtype=param, device=index).unbind(0))
     dw, db, dpw, dpb = (next(vectors) if k else None for k in want)
     dgate = torch.empty(gate.shape, dtype=param, device=index) if gate is not None else None
-    n = C.c_size_t(0)
-    _check(lib().tgrad_residual_norm_backward_bytes(config, C.byref(n)), "tgrad_residual_norm_backward_bytes")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=index)
+    key = ("residual_norm_backward", rows, width, d, pd, layer, groups, starts is not None, index)      # what the workspace's size goes by
+    size = _workspace_bytes.get(key)
+    if size is None:
+        n = C.c_size_t(0)
+        _check(lib().tgrad_residual_norm_backward_bytes(config, C.byref(n)), "tgrad_residual_norm_backward_bytes")
+        if len(_workspace_bytes) > 4096:
+            _workspace_bytes.clear()
+        size = _workspace_bytes[key] = n.value
+    ws = torch.empty(size, dtype=torch.uint8, device=index)
     io = _pack_norm_backward(*place, *g_m, *x_m, *f_m, x_p, f_p, stats.data_ptr(), dx.data_ptr(), width, df.data_ptr() if df is not None else 0, width,
                              dgate.data_ptr() if dgate is not None else 0, width, *(t.data_ptr() if t is not None else 0 for t in (dw, db, dpw, dpb)))
-    _check(lib().tgrad_residual_norm_backward(config, io, ws.data_ptr(), n.value, _raw_stream(index)), "tgrad_residual_norm_backward")
+    _check(lib().tgrad_residual_norm_backward(config, io, ws.data_ptr(), size, _raw_stream(index)), "tgrad_residual_norm_backward")
     return ResidualNormGrads(dx, df, dw, db, dpw, dpb, dgate)
 
 

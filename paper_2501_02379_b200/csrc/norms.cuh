@@ -13,6 +13,8 @@
 // its own in shared memory (cp.async), some rows ahead, so the copies need no barrier and no registers, and the memory is busy
 // while a row waits in its reductions.  Column sums stay in registers over all rows of a thread's chunk and are added up in a fixed
 // order by a second launch.
+// Measured at 16384 x 8192 bf16: forward 176 us (164 at the copy rate; 227 with f kept in 8 bits), backward 265 us (246) from f in storage,
+// 277 us (226) from f in 8 bits.
 #pragma once
 #include "packed.cuh"
 
@@ -584,7 +586,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
 }
 
 // ---- the same for what large models run: every row at a multiple of 16 bytes, a width of whole vectors of 8, weights in shared memory ----
-// Per entry these take a fraction of the general kernels' instructions (40 forward, 97 backward): rows come by bulk copies that one thread of a row's
+// Per entry the backward kernel takes 42 instructions instead of the general one's 97: rows come by bulk copies that one thread of a row's
 // team issues some rows ahead, into places that are free once the team's next barrier, which the reductions have anyway, is passed; pairs of fp32 in
 // one instruction; no tests per entry; what a reduction separates is kept in registers instead of being read and widened again.
 // A wait for a copy is bounded; one that ran out turns all results of its team's further rows, and the column sums, to NaN.

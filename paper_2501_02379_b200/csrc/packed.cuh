@@ -11,8 +11,9 @@
 // Memory: rows of 32 B codes each (B blocks, the last one filled with zeros), then rows of B bytes, padded with zeros to a
 // multiple of 4.
 //
-// All kernels here are bound by memory: a thread takes 8 entries at a time (16 bytes of 16-bit storage, 8 bytes of codes), four
-// neighbours a block, and several of them in flight.  The arithmetic is kept below the 16 instructions per entry that the copy rate leaves.
+// A thread takes 8 entries (16 bytes of 16-bit storage, 8 bytes of codes), four neighbours a block.  Reading back is bound by memory
+// (16384 x 8192 bf16: 62 us, 62 at the copy rate); packing by issue slots, 73 % busy, beside memory (84 us for 62), and so is the gated
+// activation (16384 x 14336 bf16 silu: forward 394 us for 290, backward 324 us for 290).
 #pragma once
 #include "lists.cuh"
 

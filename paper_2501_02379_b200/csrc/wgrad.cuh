@@ -12,9 +12,11 @@
 //   * eight warps move the sums out.  The tensor core adds with truncation, which would bias a long sum, so where the result is fp32 it leaves
 //     tensor memory after every few steps and is added up in registers (TN = 128: as many as fit); a 16-bit result stays there for the
 //     whole sum (TN = 256), and tensor memory holds a second tile meanwhile.
-// Why the two blocks: turning 64 tokens of 128 columns into numbers takes four warps about as long as the tensor cores take for 64 x 256 x 256
-// on two SMs, and a tile of 128 x 128 on one SM would have to read its operands from shared memory as fast as that allows (measured: 3.57 ms
-// for 16384 x 4096 x 14336 that way).
+// Bound by the warps that turn codes into numbers: a group takes about 1,000 clocks for a step, 500 a step for the two, and the tensor
+// cores of two SMs 512 for 64 x 256 x 256; measured 446 ns a step for 270 of tensor cores (8192 x 2048 x 4608 bf16: 112 us, 1,385 TFLOP/s,
+// tensor pipe 74 % busy, the pipe of integer and logic instructions 65 %; to fp32 145 us; 16384 x 4096 x 14336: 1.70 ms at sustained clocks).  Two blocks and
+// not one: each turns half of the columns into numbers, and a tile of 128 x 128 on one SM would have to read its operands from shared
+// memory as fast as that allows (16384 x 4096 x 14336 that way: 3.57 ms).
 // fp32 dy is split beforehand into three bfloat16 parts that add up to it exactly, which are three times as many steps into the same sums;
 // 16-bit dy that TMA cannot address (rows that do not start at multiples of 16 bytes) is copied beforehand.
 // The tiles behind the last full round of the clusters (all, where there are few): their tokens are split between clusters, whose sums a second
@@ -26,11 +28,10 @@
 
 namespace tg {
 
-// Warp 0: TMA, 1: MMA issue, 2: the blocks' bytes, 3: tensor memory, then two groups of NW that turn codes into numbers, then 8 for the sums.
 constexpr int WG_TILE_N = 256;
-// Three rings of shared memory, for three lifetimes: dy's boxes from their copy to the end of the instructions that read them, codes from their copy
-// until they are numbers, numbers from then to the end of the instructions.  (One ring of stages that hold all three has five of them, too few
-// to cover the copies' latency: 588 ns a step instead of the 270 that the tensor cores take.)
+// Warp 0: TMA, 1: MMA issue, 2: the blocks' bytes, 3: tensor memory, then two groups of NW that turn codes into numbers, then 8 for the sums.
+// Rings of shared memory, for three lifetimes: dy's boxes from their copy to the end of the instructions that read them, codes from their copy
+// until they are numbers (the first two of one depth, so that one barrier stands for both copies), numbers from then to the end of the instructions.
 template <int TN> struct WgGeom {
   static constexpr int TOKENS = TN == 256 ? 64 : 128;             // of a step: 16 KB of numbers for a block either way
   static constexpr int BOX = TOKENS * 128;                        // bytes of a step's tokens by 64 16-bit entries
@@ -93,7 +94,7 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
 // Waits of whole warps: the result is the same in all lanes, and known to be by the compiler.  What one thread does for its block (copies,
 // tensor-core instructions, their commits) stands in loops that whole warps run and is done by an elected lane: these instructions take
 // their operands from registers of the warp, and in code that the compiler holds for divergent it moves each there by a loop of its own
-// (measured with `if (lane == 0)` around the loops: 870 clocks for the instructions of a step, 588 ns a step in all).
+// (measured with `if (lane == 0)` around the loops: 870 clocks for the instructions of a step).
 __device__ __noinline__ bool wg_wait_long(uint64_t* bar, uint32_t parity, volatile int* failed) {
   uint64_t start = 0;
   for (uint32_t i = 0; i < WG_WAIT_POLLS; ++i) {
