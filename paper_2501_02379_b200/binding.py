@@ -877,7 +877,9 @@ def act_unpack(packed: Packed, out=None, stream=None):
     if _elsewhere(index, stream):
         return _there(index, stream, act_unpack, packed, out)
     rows, width = packed.rows, packed.width
-    src, d = _packed_ptr("packed", packed, rows, width, packed.dtype, index), types[packed.dtype]
+    src, d = _packed_ptr("packed", packed, rows, width, packed.dtype, index), types.get(packed.dtype)
+    if d is None or d == C64:
+        raise ValueError("packed is of fp32, fp16 or bfloat16")
     given = out is not None
     if not given:
         out = torch.empty((rows, width), dtype=packed.dtype, device=index)

@@ -987,7 +987,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
           param_pairs<KIND>(A.gate, A.pf32, max(g, 0), 8 * v, 8, 1.f, q);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[i] = mul2(p[i], q[i]);
-          if (g < 0) { zero_pairs(u[j]); zero_pairs(e[j]); }      // a row of no group: whatever stands in f
+          if (g < 0) { zero_pairs(u[j]); zero_pairs(e[j]); zero_pairs(p); }      // a row of no group: whatever stands in f
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

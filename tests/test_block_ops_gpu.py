@@ -349,6 +349,40 @@ def test_rows_of_no_sequence_do_not_see_the_block():
     assert all(torch.equal(a, b) for a, b in zip(out, same))
 
 
+@pytest.mark.parametrize("keep_f", [False, True])
+def test_rows_of_no_sequence_among_many(keep_f):
+    """The same on the kernels for many aligned rows; a gate that is not finite stays with its own sequence."""
+    rows, width = 2000, 512
+    x, f, dh, dx, how, _ = norm_case(rows, width, "bf16", "f32", False, True, "ragged", 6)
+    how["starts"] = torch.tensor([100, 500, 500, 900, 1900], dtype=torch.int32, device="cuda")
+    how["gate"][0] = math.nan
+    f[:100], f[1900:] = math.nan, math.inf
+    r = B.residual_norm(x, f, scale=0.5, keep_f=keep_f, **how)
+    none = torch.cat([torch.arange(100), torch.arange(1900, 2000)]).cuda()
+    assert torch.equal(r.x[none], (x[none].float() * 0.5).bfloat16()) and bool(torch.isfinite(r.h[none]).all()) and bool(torch.isnan(r.x[100:500]).all())
+    out = B.residual_norm_backward(dh, r.x.nan_to_num(1.0), r.stats.nan_to_num(1.0), r.f8 if keep_f else f, grad_x=dx, scale=0.5, **how)
+    assert bool((out.f[none] == 0).all()) and bool(torch.isfinite(out.x).all()) and bool(torch.isnan(out.f[100:500]).all())
+    assert bool(torch.isfinite(out.gate[1:]).all()) and bool(torch.isfinite(out.f[500:]).all())
+
+
+def test_norm_calls_of_other_kinds():
+    """One sequence with rows outside of it, more sequences than blocks on them, no gradient of x', everything kept, on either kernels."""
+    for rows, width in ((70, 99), (900, 1024)):
+        x, f, dh, dx, how, _ = norm_case(rows, width, "bf16", "f32", True, True, "one", 7)
+        how["starts"] = torch.tensor([5, rows - 7], dtype=torch.int32, device="cuda")
+        check_norm(x, f, dh, dx, how, [5, rows - 7], "bf16", "f32", True, True)
+        x, f, dh, dx, how, _ = norm_case(rows, width, "f16", "f16", False, True, "one", 8)
+        check_norm(x, f, dh, None, how, None, "f16", "f16", False, True, kept=(False, True))
+        check_norm(x, f, dh, dx, how, None, "f16", "f16", False, True, kept=(True, True))
+    rows, width, groups = 3000, 40, 1500
+    x, f, dh, dx, how, _ = norm_case(rows, width, "f32", "f32", True, True, "none", 9)
+    how["gate"] = torch.randn(groups, width, generator=gen(3), device="cuda")
+    check_norm(x, f, dh, dx, how, None, "f32", "f32", True, True)
+    starts = sorted([0, rows] + [int(k) for k in torch.randint(0, rows, (groups - 1,), generator=gen(4), device="cuda").tolist()])
+    how["starts"] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    check_norm(x, f, dh, dx, how, starts, "f32", "f32", True, True)
+
+
 def test_norm_of_rows_of_zeros_and_of_equal_entries():
     x = torch.zeros(4, 200, device="cuda")
     x[1] = 3.0
@@ -394,6 +428,19 @@ def test_weight_grad(dt, to):
 def test_weight_grad_of_many_tiles():
     check_weight_grad(700, 2100, 1500, "bf16", "bf16")
     check_weight_grad(333, 1800, 2222, "f16", "f32", pad=1)
+
+
+def test_weight_grad_of_full_rounds_and_a_rest():
+    """More tiles than clusters, and tokens enough to split the tiles of the last round."""
+    for n, width, dt, to in ((4096, 5120, "bf16", "bf16"), (2048, 2600, "f16", "f32")):
+        rows = 1200
+        x, dy = matrix(rows, width, dt, 1), matrix(rows, n, dt, 3, size=0.3)
+        p = B.act_pack(x)
+        xk = B.act_unpack(p).double()
+        want, mag = dy.double().T @ xk, dy.double().abs().T @ xk.abs()
+        steps = -(-rows // 16)
+        tol = mag * ((min(steps, 16) if to == "f32" else steps) * 2 * 2.0 ** -22 + (steps / 16 + 150) * U) + HALF_ULP[to] * 1.01 * want.abs() + TINY[to]
+        assert bool(((B.weight_grad(dy, p, dtype=DT[to]).double() - want).abs() <= tol).all())
 
 
 def test_weight_grad_of_wide_ranges():
@@ -554,7 +601,7 @@ def test_binding_refuses():
     w = torch.ones(64, device="cuda")
     r = B.residual_norm(x, x, weight=w)
     bad = [lambda: B.act_pack(x[0]), lambda: B.act_pack(torch.complex(x, x).conj().imag), lambda: B.act_pack(x.T), lambda: B.act_pack(x.double()), lambda: B.act_pack(x[:, :0]), lambda: B.act_pack(x, out=B.act_pack(x[:2])),
-           lambda: B.act_unpack(p._replace(rows=5)), lambda: B.act_unpack(p._replace(data=p.data[1:])), lambda: B.act_unpack(p, out=torch.zeros(4, 63, device="cuda")),
+           lambda: B.act_unpack(p._replace(rows=5)), lambda: B.act_unpack(p._replace(dtype=torch.float64)), lambda: B.act_unpack(p._replace(data=p.data[1:])), lambda: B.act_unpack(p, out=torch.zeros(4, 63, device="cuda")),
            lambda: B.act_unpack(p, out=x.half()), lambda: B.gated_act(x, x[:2]), lambda: B.gated_act(x, x.half()), lambda: B.gated_act_backward(p, None, x, du=x.clone()),
            lambda: B.gated_act_backward(p, p, x.half()), lambda: B.gated_act_backward(p, x, x), lambda: B.residual_norm(x, x, weight=w[:5]), lambda: B.residual_norm(x, x, weight=w.half()),
            lambda: B.residual_norm(x, x, weight=w, gate=w.bfloat16()), lambda: B.residual_norm(x, x, bias=w), lambda: B.residual_norm(x, gate=w), lambda: B.residual_norm(x, keep_f=True),
