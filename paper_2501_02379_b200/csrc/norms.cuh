@@ -593,7 +593,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
 
 constexpr uint32_t NM_WAIT_POLLS = 1u << 20;
 constexpr uint64_t NM_WAIT_NS = 500000000ull;
-__device__ __noinline__ bool nm_wait_long(uint64_t* bar, uint32_t parity) {
+static __device__ __noinline__ bool nm_wait_long(uint64_t* bar, uint32_t parity) {
   uint64_t start = 0;
   for (uint32_t i = 0; i < NM_WAIT_POLLS; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -622,7 +622,7 @@ struct NmRing {
   __device__ __forceinline__ void next() { if (++at == stages) { at = 0; parity ^= 1; } }
 };
 // After a wait that ran out nothing more is copied; what is under way has to land before shared memory is given up.
-__device__ __noinline__ void nm_settle(uint64_t* bars, int stages, uint32_t failed) {
+static __device__ __noinline__ void nm_settle(uint64_t* bars, int stages, uint32_t failed) {
   for (int k = 0; k < stages; ++k) {
     const int s = ((int)(failed - 1) >> 1) + k;
     nm_wait_long(&bars[s % stages], ((failed - 1) ^ (uint32_t)(s >= stages)) & 1u);

@@ -95,7 +95,7 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
 // tensor-core instructions, their commits) stands in loops that whole warps run and is done by an elected lane: these instructions take
 // their operands from registers of the warp, and in code that the compiler holds for divergent it moves each there by a loop of its own
 // (measured with `if (lane == 0)` around the loops: 870 clocks for the instructions of a step).
-__device__ __noinline__ bool wg_wait_long(uint64_t* bar, uint32_t parity, volatile int* failed) {
+static __device__ __noinline__ bool wg_wait_long(uint64_t* bar, uint32_t parity, volatile int* failed) {
   uint64_t start = 0;
   for (uint32_t i = 0; i < WG_WAIT_POLLS; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
