@@ -8,7 +8,7 @@ namespace {
 
 ItemWalk walk_of(int64_t rows, int64_t width) {
   ItemWalk k;
-  k.per_row = (int)(4 * blocks_of(width)); k.items = rows * k.per_row; k.rows = rows; k.width = (int)width;
+  k.per_row = (int)(4 * blocks_of(width)); k.items = rows * k.per_row; k.width = (int)width;
   uint32_t l = 2;
   while (((int64_t)1 << l) < k.per_row) ++l;
   k.magic = (uint32_t)((((uint64_t)1 << (31 + l)) + k.per_row - 1) / k.per_row); k.shift = l - 1;

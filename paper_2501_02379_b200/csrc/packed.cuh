@@ -186,7 +186,6 @@ __device__ __forceinline__ uint2 ld_codes(const unsigned char* p) {
 // An item is 8 entries of a row, numbered through the rows: item i has its codes at byte 8 i.
 struct ItemWalk {
   int64_t items;         // rows * per_row
-  int64_t rows;
   int width, per_row;    // items of a row: 4 * blocks
   uint32_t magic, shift; // i / per_row = (i magic) >> (32 + shift) for i < 2^31: with l = ceil(log2 per_row), magic = ceil(2^(31 + l) / per_row), shift = l - 1
 };
