@@ -1040,8 +1040,9 @@ def residual_norm_backward(grad_h, x, stats, f=None, grad_x=None, weight=None, p
 
 def weight_grad(dy, x8: Packed, dtype=None, out=None, accumulate: bool = False, stream=None):
     """Weight gradient dy^T x [out, width] of a linear layer y = x W^T whose input was kept packed, from its output's gradient dy [rows, out],
-    in dy's dtype or fp32 (`dtype`).  `out`: where to write it, or with accumulate what to add it to.  The products are exact and
-    the sums fp32; dy has the dtype that was packed."""
+    in dy's dtype or fp32 (`dtype`).  `out`: where to write it, or with accumulate what to add it to.  The products are exact;
+    sums over 512 tokens (4096 where the result has 16 bits) are the tensor core's, off by at most 2^-17 (2^-14) of the sum of magnitudes, and are
+    added in fp32.  dy has the dtype that was packed."""
     d, rows, n, index, place = _matrix("dy", dy)
     if _elsewhere(index, stream):
         return _there(index, stream, weight_grad, dy, x8, dtype, out, accumulate)

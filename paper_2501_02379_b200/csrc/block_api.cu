@@ -113,12 +113,19 @@ WgradPlan wgrad_plan(const tgrad_weight_grad_args* c, int sm) {
   p.partial_bytes = p.splits > 1 ? align_up((size_t)p.splits * rest * WG_TILE_N * p.tn * 4) : 0;
   return p;
 }
+template <bool F16, int TN, bool RUNNING>
+tgrad_status wgrad_product(const WgradPlan& p, const CUtensorMap& map_dy, const CUtensorMap& map_codes, const WgradArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  TG_TRY(allow_shared(wgrad_kernel<F16, TN, RUNNING>, WgGeom<TN>::SMEM, done));
+  launch_cluster(wgrad_kernel<F16, TN, RUNNING>, dim3((unsigned)(2 * p.clusters)), dim3(WgGeom<TN>::THREADS), WgGeom<TN>::SMEM, 2, st, map_dy, map_codes, a);
+  TG_LAUNCH_CHECK();
+  return TGRAD_OK;
+}
 template <bool F16, int TN>
 tgrad_status wgrad_launch(const WgradPlan& p, const CUtensorMap& map_dy, const CUtensorMap& map_codes, const WgradArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> done{0};
-  TG_TRY(allow_shared(wgrad_kernel<F16, TN>, WgGeom<TN>::SMEM, done));
-  launch_cluster(wgrad_kernel<F16, TN>, dim3((unsigned)(2 * p.clusters)), dim3(WgGeom<TN>::THREADS), WgGeom<TN>::SMEM, 2, st, map_dy, map_codes, a);
-  TG_LAUNCH_CHECK();
+  // running sums where some unit has more steps than a group
+  if (TN == 256 && (p.whole > 0 ? p.steps : p.per_split) > a.group) TG_TRY((wgrad_product<F16, TN, TN == 256>(p, map_dy, map_codes, a, st)));
+  else TG_TRY((wgrad_product<F16, TN, false>(p, map_dy, map_codes, a, st)));
   if (p.splits > 1) {
     const int64_t threads = ((int64_t)p.tiles_n * p.tiles_k - p.whole) * WG_TILE_N * (TN / 8);
     launch_chained(wgrad_sum_kernel<TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a);
@@ -216,8 +223,9 @@ tgrad_status tgrad_weight_grad(const tgrad_weight_grad_args* c, void* d_workspac
   const PackedRows x = packed_of(c->d_packed, c->rows, c->width);
   a.exps = x.exps; a.exp_words = x.exp_stride / 4;
   a.whole = p.whole; a.splits = p.splits; a.steps = p.steps; a.per_split = p.per_split;
-  // fp32 results leave tensor memory after every 32 instructions (4 steps of 128 tokens; 16 where the entries are fp32), 16-bit ones once
-  a.group = kind == LS_F32 ? 2 : to == LS_F32 ? 4 : 0x7fffffff;
+  // Instructions of 16 tokens whose sums the tensor core forms, cutting off at most 2^-22 at each: 32 for fp32 results (4 steps of 128 tokens; 16
+  // where the entries are fp32), 256 for 16-bit ones (64 steps of 64), an eighth of half an ulp of fp16.
+  a.group = kind == LS_F32 ? 2 : p.tn == 128 ? 4 : 64;
   a.copies = g_copy_limit.load(std::memory_order_relaxed);
   a.partial = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + p.parts_bytes) : nullptr;
   const bool f16 = kind == LS_F16;

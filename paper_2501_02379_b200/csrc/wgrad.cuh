@@ -9,9 +9,10 @@
 //     bfloat16, and in fp16 for what was packed from fp16; products are exact in fp32.  Two such groups take steps in turn, so that one's
 //     latencies are covered by the other's;
 //   * in the first block one thread issues tcgen05.mma for both (operands with the tile's columns contiguous), accumulators in tensor memory;
-//   * eight warps move the sums out.  The tensor core adds with truncation, which would bias a long sum, so where the result is fp32 it leaves
-//     tensor memory after every few steps and is added up in registers (TN = 128: as many as fit); a 16-bit result stays there for the
-//     whole sum (TN = 256), and tensor memory holds a second tile meanwhile.
+//   * eight warps move the sums out.  The tensor core adds with truncation, which biases a long sum (by 1e-7 an instruction where the terms have one
+//     sign: 7.8e-4 after 7500, more than half an ulp of fp16), so sums of a few steps leave it and are added in fp32: for an fp32 result after 32
+//     instructions (16 where the entries are fp32), into registers (TN = 128: as many as fit); for a 16-bit result (TN = 256) after 256, into the
+//     other half of tensor memory (1.7e-5 at most).  A 16-bit sum of 64 steps or fewer stays, and tensor memory holds a second tile meanwhile.
 // Bound by the warps that turn codes into numbers: a group takes about 1,000 clocks for a step, 500 a step for the two, and the tensor
 // cores of two SMs 512 for 64 x 256 x 256; measured 446 ns a step for 270 of tensor cores (8192 x 2048 x 4608 bf16: 112 us, 1,385 TFLOP/s,
 // tensor pipe 74 % busy, the pipe of integer and logic instructions 65 %; to fp32 145 us; 16384 x 4096 x 14336: 1.70 ms at sustained clocks).  Two blocks and
@@ -86,6 +87,14 @@ __device__ __forceinline__ void umma2_f16(uint32_t d_tmem, uint64_t adesc, uint6
                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
                : "memory");
 }
+// 16 consecutive columns of this thread's lane from registers.  Whole warp.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+      "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // both blocks' barriers that stand at `bar` get an arrival once every MMA issued so far has completed
 __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
@@ -184,14 +193,15 @@ __device__ __forceinline__ void wg_store(const WgradArgs& A, int64_t n, int k, c
   store8<KIND, false>(A.out, n, k, cnt, o);
 }
 
-template <bool F16, int TN>
+// RUNNING (TN = 256): a unit has more than one group, and half of tensor memory holds the running sums instead of a second accumulator.
+template <bool F16, int TN, bool RUNNING>
 __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes, const WgradArgs A) {
   typedef WgGeom<TN> G;
-  constexpr int SA = G::SA, SB = G::SB, NW = G::NW;
+  constexpr int SA = G::SA, SB = G::SB, NW = G::NW, ACC = RUNNING ? 1 : 2;      // ACC: accumulators in tensor memory
   constexpr int KIND = TN == 128 ? LS_F32 : F16 ? LS_F16 : LS_BF16;      // of the result
   extern __shared__ unsigned char wg_raw[];
   // (of ready and acc_free the first block's are used)
-  __shared__ __align__(8) uint64_t full[SA], a_empty[SA], c_empty[SA], ready[SB], b_empty[SB], acc_full[2], acc_free[2];
+  __shared__ __align__(8) uint64_t full[SA], a_empty[SA], c_empty[SA], ready[SB], b_empty[SB], acc_full[ACC], acc_free[ACC];
   __shared__ uint32_t tmem_slot;
   __shared__ int failed_s;
   volatile int* failed = &failed_s;
@@ -202,11 +212,11 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
   if (tid == 0) {
     for (int s = 0; s < SA; ++s) { mbar_init(&full[s], 33); mbar_init(&a_empty[s], 1); mbar_init(&c_empty[s], NW); }
     for (int s = 0; s < SB; ++s) { mbar_init(&ready[s], 2 * NW); mbar_init(&b_empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_free[b], 2 * 8); }
+    for (int b = 0; b < ACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_free[b], 2 * 8); }
     failed_s = 0;
     fence_mbar_init();
   }
-  if (warp == 3) tmem_alloc2(&tmem_slot, 2 * TN);
+  if (warp == 3) tmem_alloc2(&tmem_slot, 2 * TN);          // two accumulators, or one and the running sums
   tc_fence_before_sync();
   __syncthreads();
   cluster_sync();
@@ -258,7 +268,7 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
       const uint64_t da0 = umma_desc_mn128(ring, G::BOX), db0 = umma_desc_mn128(ring + G::B, G::BOX);
       WgRing<SA> a;
       WgRing<SB> b;
-      WgRing<2> acc;
+      WgRing<ACC> acc;
       for (int unit = mine; unit < units && ok; unit += clusters) {
         int64_t from; const uint32_t n = steps_of(unit, from);
         uint32_t in_group = 0;
@@ -347,7 +357,7 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
   } else if (warp >= 4 + 2 * NW) {
     constexpr int W = TN / 2;                              // columns of a warp
     const int quarter = warp & 3, half = (warp - 4 - 2 * NW) >> 2; // tensor-memory lanes 32 * quarter .., columns W * half ..
-    WgRing<2> acc;
+    WgRing<ACC> acc;
     for (int unit = mine; unit < units; unit += clusters) {
       int tn, tk; wg_tile(A, tile_of(unit), tn, tk);
       int64_t from; const uint32_t n = steps_of(unit, from);
@@ -395,6 +405,39 @@ __global__ void __launch_bounds__(WgGeom<TN>::THREADS, 1) wgrad_kernel(const __g
             for (int i = 0; i < 16; ++i) sum[p][i] = __int_as_float(0x7fffffff);
           }
           put(col + 16 * p, sum[p]);
+        }
+      } else if (RUNNING) {
+        // (the tensor core waits until a group's sums are added: at 8192 x 2048 x 4608 1.3 % of the time with 64 steps a group, 3 % with 32, 6 % with 16)
+        const uint32_t groups = (n + A.group - 1) / A.group, sums = lanes + TN;      // these warps' alone
+        for (uint32_t k = 0; k < groups && ok; ++k, acc.next()) {
+          ok = wg_wait(&acc_full[acc.at], acc.parity, failed);
+          if (!ok) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int p = 0; p < W / 16; ++p) {
+            uint32_t r[16], s[16];
+            float v[16];
+            tmem_ld16(lanes + 16 * p, r);
+            if (k != 0) tmem_ld16(sums + 16 * p, s);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = k != 0 ? __uint_as_float(s[i]) + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+            tmem_st16(sums + 16 * p, v);
+          }
+          tmem_wait_st();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) arrive_first(&acc_free[acc.at]);
+        }
+#pragma unroll
+        for (int p = 0; p < W / 16; ++p) {
+          uint32_t r[16];
+          tmem_ld16(sums + 16 * p, r);
+          tmem_wait_ld();
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = ok ? __uint_as_float(r[i]) : __int_as_float(0x7fffffff);
+          put(col + 16 * p, v);
         }
       } else {
         ok = ok && wg_wait(&acc_full[acc.at], acc.parity, failed);

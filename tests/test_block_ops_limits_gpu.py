@@ -1,0 +1,23 @@
+"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens.  u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
+import pytest
+import torch
+
+from paper_2501_02379_b200 import binding as B
+from tests.test_block_ops_gpu import DT, U, gen
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ weight gradient
+@pytest.mark.parametrize("dt,digits", [("f16", 11), ("bf16", 8)])
+def test_weight_grad_of_many_tokens_is_off_by_its_rounding(dt, digits):
+    """Terms of one sign, whole tiles.  The tensor core cuts off at most 2^-22 of a sum per instruction, and 256 instructions
+    of 16 tokens form a sum; these are added in fp32, u each; the stored result is off by half a step, 2^-digits of its power of two."""
+    rows, clusters = 120000, torch.cuda.get_device_properties(0).multi_processor_count // 2
+    n, width = 512, 256 * (clusters // 2)                     # two tiles by as many as make one full round
+    dy = (0.125 + 0.125 * torch.rand(rows, n, generator=gen(1), device="cuda")).to(DT[dt])
+    x8 = B.act_pack((0.5 + torch.rand(rows, width, generator=gen(2), device="cuda")).to(DT[dt]))
+    got = B.weight_grad(dy, x8).double()
+    want = dy.double().T @ B.act_unpack(x8).double()
+    half = torch.exp2(torch.floor(torch.log2(want)) - digits)
+    assert bool(((got - want).abs() <= half + want * (256 * 2.0 ** -22 + rows / 4096 * U)).all())
