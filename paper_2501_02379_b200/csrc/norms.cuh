@@ -1082,7 +1082,7 @@ __global__ void __launch_bounds__(32 * NF_Y) norm_sums_kernel(const NormSums A) 
       at = A.slots + (A.per_row ? 0 : g);
       int64_t r0 = 0, r1 = A.rows;
       if (A.starts) { r0 = max((int64_t)A.starts[g], (int64_t)0); r1 = min((int64_t)A.starts[g + 1], A.rows); }
-      else if (A.groups > 1) { r0 = g * A.rows_per; r1 = r0 + A.rows_per; }
+      else if (A.groups > 1) { r0 = g * A.rows_per; r1 = min(r0 + A.rows_per, A.rows); }      // (no rows at all: no group has any)
       if (r0 >= r1) k1 = -1;
       else if (A.chunk) { k0 = r0 / A.chunk; k1 = (r1 - 1) / A.chunk; }      // (chunk 0: combined sums, one group)
     }

@@ -1,4 +1,7 @@
-"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens.  u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
+"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, batches without rows.
+u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
+import math
+
 import pytest
 import torch
 
@@ -21,3 +24,31 @@ def test_weight_grad_of_many_tokens_is_off_by_its_rounding(dt, digits):
     want = dy.double().T @ B.act_unpack(x8).double()
     half = torch.exp2(torch.floor(torch.log2(want)) - digits)
     assert bool(((got - want).abs() <= half + want * (256 * 2.0 ** -22 + rows / 4096 * U)).all())
+
+
+# ------------------------------------------------------------------------------------------------ norms: nothing there
+def _dirty():
+    """Memory that a workspace may be given holds NaN."""
+    for n in (1 << 12, 1 << 16, 1 << 20, 1 << 24):
+        torch.full((n,), math.nan, device="cuda")
+
+
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("gate", [(3, 64), (1, 64), (64,)])
+def test_no_rows_give_gradients_of_zero(layer, gate):
+    empty, one = torch.zeros(0, 64, device="cuda"), torch.ones(64, device="cuda")
+    how = {"weight": one, "post_weight": one, "gate": torch.full(gate, 0.5, device="cuda"), "kind": "layer" if layer else "rms"}
+    if layer:
+        how["post_bias"] = one
+    for starts in (None, [0] * (gate[0] + 1) if len(gate) == 2 else [0, 0]):
+        if starts is not None:
+            how["starts"] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        r = B.residual_norm(empty, empty, **how)
+        assert r.x.shape == r.h.shape == (0, 64)
+        for grad_x in (empty, None):
+            _dirty()
+            g = B.residual_norm_backward(empty, r.x, r.stats, empty, grad_x=grad_x, **how)
+            assert g.x.shape == g.f.shape == (0, 64) and g.gate.shape == gate
+            for name in ("weight", "bias", "post_weight", "post_bias", "gate"):
+                t = getattr(g, name)
+                assert t is None or bool((t == 0).all()), name
