@@ -952,17 +952,17 @@ def _norm_config(d, rows, width, index, weight, bias, post_weight, post_bias, ga
         pointers.append(t.data_ptr())
     groups, gate_stride = 0, 0
     if gate is not None:
-        if gate.dim() not in (1, 2) or gate.shape[-1] != width or (width > 1 and gate.stride(-1) != 1) or gate.numel() == 0:
+        if gate.dim() not in (1, 2) or gate.shape[-1] != width or (width > 1 and gate.stride(-1) != 1) or (gate.numel() == 0 and rows > 0):
             raise ValueError("gate is a tensor [width] or [groups, width], the entries of a row adjacent")
         groups, gate_stride = (1, width) if gate.dim() == 1 else (gate.shape[0], gate.stride(0) if gate.shape[0] > 1 else width)
-    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (groups + 1,) or groups == 0 or not starts.is_cuda or
+    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (groups + 1,) or gate is None or not starts.is_cuda or
                                starts.get_device() != index or not starts.is_contiguous()):
         raise ValueError("starts is a contiguous int32 tensor [groups + 1] on the activations' device, and comes with a gate [groups, width]")
     if starts is None and groups and rows % groups:
         raise ValueError("the gate's groups of rows are of equal size unless starts says where they begin")
     if pd is None:
         pd = R32
-    return _pack_norm(rows, width, d, pd, kind == "layer", bool(post), scale, eps, groups, 0, starts.data_ptr() if starts is not None else 0,
+    return _pack_norm(rows, width, d, pd, kind == "layer", bool(post), scale, eps, groups, 0, starts.data_ptr() if starts is not None and groups else 0,
                       *pointers, gate_stride), pd, groups
 
 

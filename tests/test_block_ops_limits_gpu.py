@@ -52,3 +52,15 @@ def test_no_rows_give_gradients_of_zero(layer, gate):
             for name in ("weight", "bias", "post_weight", "post_bias", "gate"):
                 t = getattr(g, name)
                 assert t is None or bool((t == 0).all()), name
+
+
+def test_no_rows_with_a_gate_for_each():
+    empty, one = torch.zeros(0, 64, device="cuda"), torch.ones(64, device="cuda")
+    for starts in (None, torch.zeros(1, dtype=torch.int32, device="cuda")):
+        r = B.residual_norm(empty, empty, weight=one, post_weight=one, gate=empty, starts=starts, keep_f=True, keep_h=True)
+        assert r.h.shape == (0, 64)
+        _dirty()
+        g = B.residual_norm_backward(empty, r.x, r.stats, r.f8, grad_x=empty, weight=one, post_weight=one, gate=empty, starts=starts)
+        assert g.gate.shape == (0, 64) and bool((g.weight == 0).all()) and bool((g.post_weight == 0).all())
+    with pytest.raises(ValueError):
+        B.residual_norm(torch.zeros(2, 64, device="cuda"), torch.zeros(2, 64, device="cuda"), gate=empty)
