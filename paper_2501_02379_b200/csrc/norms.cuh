@@ -1069,6 +1069,13 @@ __device__ __forceinline__ float sums_param(const RowsOf& t, int pf32, int64_t r
 // where the sums of group g stand
 __device__ __forceinline__ float* sums_of_group(const NormSums& A, int nw, int64_t g) { return A.part + (2 * A.slots + A.groups + g) * nw * A.part_stride; }
 
+// the rows of group g: [r0, r1), none where r0 >= r1
+__device__ __forceinline__ void rows_of_group(const NormSums& A, int64_t g, int64_t& r0, int64_t& r1) {
+  r0 = 0; r1 = A.rows;
+  if (A.starts) { r0 = max((int64_t)A.starts[g], (int64_t)0); r1 = min((int64_t)A.starts[g + 1], A.rows); }
+  else if (A.groups > 1) { r0 = g * A.rows_per; r1 = min(r0 + A.rows_per, A.rows); }      // (no rows at all: no group has any)
+}
+
 template <int KIND, bool LN>
 __global__ void __launch_bounds__(32 * NF_Y) norm_sums_kernel(const NormSums A) {
   __shared__ float2 red[NF_Y][33];
@@ -1078,12 +1085,13 @@ __global__ void __launch_bounds__(32 * NF_Y) norm_sums_kernel(const NormSums A) 
   for (int64_t part = blockIdx.y; part <= A.groups; part += gridDim.y) {
     const int64_t g = part - 1;
     int64_t at = 0, k0 = 0, k1 = A.slots - 1;             // slots at + [k0, k1]
+    bool none = false;                                    // a group without rows
     if (g >= 0) {
       at = A.slots + (A.per_row ? 0 : g);
-      int64_t r0 = 0, r1 = A.rows;
-      if (A.starts) { r0 = max((int64_t)A.starts[g], (int64_t)0); r1 = min((int64_t)A.starts[g + 1], A.rows); }
-      else if (A.groups > 1) { r0 = g * A.rows_per; r1 = min(r0 + A.rows_per, A.rows); }      // (no rows at all: no group has any)
-      if (r0 >= r1) k1 = -1;
+      int64_t r0, r1;
+      rows_of_group(A, g, r0, r1);
+      none = r0 >= r1;
+      if (none) k1 = -1;
       else if (A.chunk) { k0 = r0 / A.chunk; k1 = (r1 - 1) / A.chunk; }      // (chunk 0: combined sums, one group)
     }
     float2 v = make_float2(0.f, 0.f);
@@ -1105,10 +1113,10 @@ __global__ void __launch_bounds__(32 * NF_Y) norm_sums_kernel(const NormSums A) 
       } else {
         if (A.dgate.p && !A.per_row) {
           const float pw = A.post ? sums_param<KIND>(A.pw, A.pf32, 0, c, 1.f) : 1.f, pb = LN && A.post ? sums_param<KIND>(A.pb, A.pf32, 0, c, 0.f) : 0.f;
-          store_param<KIND>(A.dgate, A.pf32, g, c, fmaf(v.x, pw, v.y * pb));
+          store_param<KIND>(A.dgate, A.pf32, g, c, none ? 0.f : fmaf(v.x, pw, v.y * pb));
         }
         if (A.groups == 1) {
-          const float gate = A.per_row ? 1.f : sums_param<KIND>(A.gate, A.pf32, 0, c, 1.f);
+          const float gate = A.per_row || none ? 1.f : sums_param<KIND>(A.gate, A.pf32, 0, c, 1.f);
           if (A.dpw.p) store_param<KIND>(A.dpw, A.pf32, 0, c, gate * v.x);
           if (A.dpb.p) store_param<KIND>(A.dpb, A.pf32, 0, c, gate * v.y);
         } else {
@@ -1130,7 +1138,9 @@ __global__ void __launch_bounds__(32 * NF_Y) norm_groups_kernel(const NormSums A
   if (c < A.width) {
 #pragma unroll 4
     for (int64_t g = y; g < A.groups; g += NF_Y) {
-      const float gate = sums_param<KIND>(A.gate, A.pf32, g, c, 1.f);
+      int64_t r0, r1;
+      rows_of_group(A, g, r0, r1);
+      const float gate = r0 < r1 ? sums_param<KIND>(A.gate, A.pf32, g, c, 1.f) : 0.f;      // (one that no row has may be anything)
       const float* p = sums_of_group(A, nw, g) + c;
       v.x = fmaf(gate, p[0], v.x);
       if (LN) v.y = fmaf(gate, p[A.part_stride], v.y);

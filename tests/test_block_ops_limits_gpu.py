@@ -1,4 +1,4 @@
-"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, batches without rows.
+"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, sequences and batches without rows.
 u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
 import math
 
@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2501_02379_b200 import binding as B
-from tests.test_block_ops_gpu import DT, U, gen
+from tests.test_block_ops_gpu import DT, U, gen, norm_case
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,36 @@ def test_no_rows_with_a_gate_for_each():
         assert g.gate.shape == (0, 64) and bool((g.weight == 0).all()) and bool((g.post_weight == 0).all())
     with pytest.raises(ValueError):
         B.residual_norm(torch.zeros(2, 64, device="cuda"), torch.zeros(2, 64, device="cuda"), gate=empty)
+
+
+@pytest.mark.parametrize("rows,width", [(90, 99), (2000, 512)])      # the general kernels; those for aligned rows
+@pytest.mark.parametrize("layer", [False, True])
+def test_gate_of_an_empty_sequence_has_no_part(rows, width, layer):
+    x, f, dh, dx, how, _ = norm_case(rows, width, "bf16", "f32", layer, True, "ragged", 5)
+    f = f.contiguous()
+    kind = "layer" if layer else "rms"
+    how.pop("bias", None)
+    cases = [([3, 3, rows // 2, rows // 2, rows], (0, 2)), ([rows + 7, rows + 9, rows + 9, rows + 12, rows + 15], (0, 1, 2, 3)), ([0, 1, 2, rows, rows], (3,))]
+    for starts, empty in cases:
+        how["starts"] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        r = B.residual_norm(x, f, kind=kind, **how)
+        out = []
+        for fill in (0.0, math.nan, -math.inf):
+            gate = how["gate"].clone()
+            gate[list(empty)] = fill
+            out.append(B.residual_norm_backward(dh, r.x, r.stats, f, grad_x=dx, kind=kind, **{**how, "gate": gate}))
+        for got in out:
+            assert all(t is None or (bool(torch.isfinite(t).all()) and torch.equal(t, u)) for t, u in zip(got, out[0]))
+            assert bool((got.gate[list(empty)] == 0).all())
+    # no post_weight that is not finite gets into the gradient of a gate without rows
+    how["post_weight"][0] = math.inf
+    assert bool((B.residual_norm_backward(dh, r.x, r.stats, f, grad_x=dx, kind=kind, **how).gate[3] == 0).all())
+    how["post_weight"][0] = 1.0
+    # one sequence, and it has no rows
+    gate, starts = torch.full((1, width), math.nan, device="cuda"), torch.tensor([5, 5], dtype=torch.int32, device="cuda")
+    got = B.residual_norm_backward(dh, r.x, r.stats, f, grad_x=dx, kind=kind, **{**how, "gate": gate, "starts": starts})
+    assert bool((got.gate == 0).all()) and bool((got.post_weight == 0).all()) and (not layer or bool((got.post_bias == 0).all()))
+    # no rows at all
+    for gate in (gate, gate[0], gate.expand(3, width).contiguous()):
+        got = B.residual_norm_backward(dh[:0], x[:0], r.stats[:, :0].contiguous(), f[:0], grad_x=dx[:0], kind=kind, **{**how, "gate": gate, "starts": None})
+        assert bool((got.gate == 0).all()) and bool((got.post_weight == 0).all()) and (not layer or bool((got.post_bias == 0).all()))
