@@ -586,7 +586,8 @@ __global__ void __launch_bounds__(512, 1) norm_backward_kernel(const ResNormArgs
 // Per entry the backward kernel takes 42 instructions instead of the general one's 97: rows come by bulk copies that one thread of a row's
 // team issues some rows ahead, into places that are free once the team's next barrier, which the reductions have anyway, is passed; pairs of fp32 in
 // one instruction; no tests per entry; what a reduction separates is kept in registers instead of being read and widened again.
-// A wait for a copy is bounded; one that ran out turns all results of its team's further rows, and the column sums, to NaN.
+// A wait for a copy is bounded; one that ran out turns what its warp makes of the team's further rows to NaN (x', means, kept copies, gradients and
+// column sums), and by the sums over a row all that follows from these.
 
 constexpr uint32_t NM_WAIT_POLLS = 1u << 20;
 constexpr uint64_t NM_WAIT_NS = 500000000ull;
@@ -603,18 +604,20 @@ static __device__ __noinline__ bool nm_wait_long(uint64_t* bar, uint32_t parity)
   }
   return false;
 }
-// A team's places for rows.  poison: NaN once a copy has not come, 0 before.
+// A team's places for rows.  poison: NaN once a copy has not come, -0 before, which changes nothing that it is added to.
 struct NmRing {
   uint64_t* bars;
   int stages, at = 0;
   int copied = 0;
   uint32_t parity = 0, failed = 0;      // failed: 1 + the place and parity whose copy did not come
-  float poison = 0.f;
-  __device__ __forceinline__ void wait() {
-    if (failed == 0 && !mbar_try_wait(&bars[at], parity) && !nm_wait_long(&bars[at], parity)) {
-      poison = __int_as_float(0x7fffffff);
-      failed = 1 + 2 * at + parity;
-    }
+  float poison = -0.f;
+  __device__ __forceinline__ void wait() {                 // whole warps, which give up together
+    if (failed != 0 || __all_sync(0xffffffffu, mbar_try_wait(&bars[at], parity))) return;
+    const bool ok = nm_wait_long(&bars[at], parity);
+    __syncwarp();
+    if (__all_sync(0xffffffffu, ok)) return;
+    poison = __int_as_float(0x7fffffff);
+    failed = 1 + 2 * at + parity;
   }
   __device__ __forceinline__ void next() { if (++at == stages) { at = 0; parity ^= 1; } }
 };
@@ -722,7 +725,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
   if (t == 0)
     for (int s = 0; s < S; ++s) issue(s, first + s * step);
   const float inv = 1.f / (float)A.width;
-  const uint64_t zero = pk2(0.f, 0.f), scale = pk2(A.scale, A.scale);
+  const uint64_t zero = pk2(0.f, 0.f);
   // mean and 1 / deviation of V vectors, which leave without the mean
   auto stats = [&](uint64_t (&v)[V][4], float& mean, float& rstd) {
     mean = 0.f;
@@ -749,6 +752,7 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
   for (int64_t row = first; row < A.rows; row += step) {
     ring.wait();
     const uint32_t from = places + (uint32_t)(ring.at * per) * bytes;
+    const uint64_t scale = pk2(A.scale + ring.poison, A.scale + ring.poison), lost = pk2(ring.poison, ring.poison);      // (a scale that is NaN makes x' so)
     uint64_t x[V][4];
     float mean, rstd;
     if (A.mode != NM_NONE) {
@@ -757,10 +761,10 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
       for (int j = 0; j < V; ++j) {
         const int v = t + j * A.tpr;
         if (v < nd) take_pairs<KIND>(from + bytes, v, f[j]); else zero_pairs(f[j]);
+        f[j][0] = add2(f[j][0], lost);                     // one NaN: the whole kept block, and by the sums the row
         if (A.pf.codes) keep_pairs<KIND>(A.pf, row, v, nv, f[j], true);
       }
       stats(f, mean, rstd);
-      rstd += ring.poison;
       if (A.stats && t == 0) { A.stats[row] = rstd; if (LN) A.stats[2 * A.rows + row] = mean; }
       const int g = folded ? 0 : group_of(A, row);
       const uint64_t r = pk2(rstd, rstd);
@@ -813,7 +817,6 @@ __global__ void __launch_bounds__(1024, 1) norm_forward_fast_kernel(const ResNor
       if (A.px.codes) keep_pairs<KIND>(A.px, row, v, nv, x[j], false);
     }
     stats(x, mean, rstd);
-    rstd += ring.poison;
     if (A.tpr == 32) __syncwarp();                         // (a team of several warps has passed a barrier in the sum above)
     if (t == 0) issue(ring.at, row + S * step);                  // the row's places have been read: the next one that will stand there
     ring.next();
@@ -1019,6 +1022,13 @@ __global__ void __launch_bounds__(512, 1) norm_backward_fast_kernel(const ResNor
   }
   if (t == 0 && ring.failed) nm_settle(ring.bars, S, ring.failed);
   if (!A.part) return;
+  if (LN) {                                              // (of the column sums only these have been formed without 1 / deviation)
+    const uint64_t p = pk2(ring.poison, ring.poison);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sb[LN ? j : 0][i] = add2(sb[LN ? j : 0][i], p);
+  }
   if (A.combine && teams > 1) {
     // the block's teams, one kind of sum after the other, through the ring's memory
     float* buf = reinterpret_cast<float*>(nm_smem + NM_RED_BYTES + NM_BARS + 64 * nv);

@@ -1,4 +1,5 @@
-"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, sequences and batches without rows.
+"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, sequences and batches without rows, waits
+that run out.
 u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
 import math
 
@@ -97,3 +98,54 @@ def test_gate_of_an_empty_sequence_has_no_part(rows, width, layer):
     for gate in (gate, gate[0], gate.expand(3, width).contiguous()):
         got = B.residual_norm_backward(dh[:0], x[:0], r.stats[:, :0].contiguous(), f[:0], grad_x=dx[:0], kind=kind, **{**how, "gate": gate, "starts": None})
         assert bool((got.gate == 0).all()) and bool((got.post_weight == 0).all()) and (not layer or bool((got.post_bias == 0).all()))
+
+
+# ------------------------------------------------------------------------------------------------ waits that run out
+def _nan(t):
+    return bool(torch.isnan(t).all())
+
+
+@pytest.mark.parametrize("layer", [False, True])
+def test_waits_that_run_out_leave_nothing_finite(layer):
+    """No copy comes: all that was made from rows is NaN, kept copies, means and sums among them.  Some come: the same or right, entry by entry."""
+    rows, width = 3000, 1024                                   # two rows a team and more
+    x, f, dh, dx, how, _ = norm_case(rows, width, "bf16", "f32", layer, True, "one", 3)
+    f = f.contiguous()                                         # rows that are copied ahead
+    kind = "layer" if layer else "rms"
+    alone = {k: how[k] for k in ("weight", "bias") if k in how}
+    among = {**how, "gate": how["gate"].repeat(2, 1), "starts": torch.tensor([40, 300, rows - 60], dtype=torch.int32, device="cuda")}
+    back = lambda h: {k: v for k, v in h.items() if k != "bias"}  # noqa: E731
+    stats = B.residual_norm(x, f, kind=kind, **how).stats
+
+    def calls():
+        out = [B.residual_norm(x, f, kind=kind, keep_x=True, keep_f=True, keep_h=True, **h) for h in (how, among)]
+        out.append(B.residual_norm(x, kind=kind, keep_x=True, keep_h=True, **alone))
+        out += [B.residual_norm_backward(dh, x, stats, f, grad_x=dx, kind=kind, **back(h)) for h in (how, among)]
+        flat = []
+        for k, r in enumerate(out):
+            for name, t in r._asdict().items():
+                if t is not None:
+                    flat.append((k, name, B.act_unpack(t) if isinstance(t, B.Packed) else t))
+        return flat
+
+    want = calls()
+    for limit in (0, 1):
+        B.set_copy_limit(limit)
+        try:
+            got = calls()
+            torch.cuda.synchronize()
+        finally:
+            B.set_copy_limit(-1)
+        outside = torch.cat([torch.arange(40), torch.arange(rows - 60, rows)]).cuda()
+        for (k, name, t), (_, _, right) in zip(got, want):
+            if limit == 0:
+                if k == 2 and name == "stats":
+                    t = t[[1, 3] if layer else [1]]           # (of a block that is not there: 1 and 0)
+                if k == 4 and name == "f":
+                    assert bool((t[outside] == 0).all())      # rows of no sequence: 0 whatever is there
+                    t = t[40:rows - 60]
+                assert _nan(t), (k, name)
+            elif k < 3:
+                bad = torch.isnan(t)
+                assert bool((bad | (t == right)).all()) and (name == "stats" or bool(bad.any())), (k, name)
+    assert all(torch.equal(t, right) for (_, _, t), (_, _, right) in zip(calls(), want))
