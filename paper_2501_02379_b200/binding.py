@@ -845,10 +845,11 @@ def _new_packed(rows, width, dtype, index) -> Packed:
 
 
 def _packed_ptr(name, p, rows, width, dtype, index) -> int:
-    if not isinstance(p, Packed) or p.rows != rows or p.width != width or p.dtype != dtype:
-        raise ValueError(f"{name} is a packed matrix of {rows} x {width} entries of {dtype}")
+    """The address of a packed matrix of the given rows, width (None: any), dtype and device."""
+    if not isinstance(p, Packed) or p.rows != rows or (width is not None and p.width != width) or p.dtype != dtype:
+        raise ValueError(f"{name} is a packed matrix of {rows} x {'any' if width is None else width} entries of {dtype}")
     t = p.data
-    if t.dtype is not _torch_types[0].uint8 or not t.is_contiguous() or t.numel() != _packed_bytes(rows, width) or not t.is_cuda or t.get_device() != index:
+    if t.dtype is not _torch_types[0].uint8 or not t.is_contiguous() or t.numel() != _packed_bytes(rows, p.width) or not t.is_cuda or t.get_device() != index:
         raise ValueError(f"{name} is not the packed matrix that it says it is, or lives on another device")
     return t.data_ptr()
 
@@ -873,6 +874,8 @@ def act_pack(x, out: Optional[Packed] = None, stream=None) -> Packed:
 def act_unpack(packed: Packed, out=None, stream=None):
     """The matrix that a packed one reads back as, in the dtype that it was packed from."""
     torch, types, _ = _torch()
+    if not isinstance(packed, Packed) or not packed.data.is_cuda:
+        raise ValueError("packed is a packed matrix on a GPU")
     index = packed.data.get_device()
     if _elsewhere(index, stream):
         return _there(index, stream, act_unpack, packed, out)
@@ -1047,7 +1050,7 @@ def weight_grad(dy, x8: Packed, dtype=None, out=None, accumulate: bool = False, 
     if _elsewhere(index, stream):
         return _there(index, stream, weight_grad, dy, x8, dtype, out, accumulate)
     torch, types, f32 = _torch_types
-    src = _packed_ptr("x8", x8, rows, x8.width, dy.dtype, index)
+    src = _packed_ptr("x8", x8, rows, None, dy.dtype, index)
     given = out is not None
     if not given:
         if accumulate:

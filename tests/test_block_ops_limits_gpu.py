@@ -1,5 +1,5 @@
 """The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, sequences and batches without rows, waits
-that run out.
+that run out, arguments of other kinds.
 u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
 import math
 
@@ -149,3 +149,15 @@ def test_waits_that_run_out_leave_nothing_finite(layer):
                 bad = torch.isnan(t)
                 assert bool((bad | (t == right)).all()) and (name == "stats" or bool(bad.any())), (k, name)
     assert all(torch.equal(t, right) for (_, _, t), (_, _, right) in zip(calls(), want))
+
+
+# ------------------------------------------------------------------------------------------------ arguments
+def test_packed_matrices_are_checked():
+    x = torch.randn(4, 64, device="cuda")
+    p = B.act_pack(x)
+    host = p._replace(data=p.data.cpu())
+    for call in (lambda: B.act_unpack(host), lambda: B.act_unpack(host, out=x),
+                 lambda: B.act_unpack(x), lambda: B.act_unpack(p.data), lambda: B.weight_grad(x, None), lambda: B.weight_grad(x, x), lambda: B.weight_grad(x, host),
+                 lambda: B.gated_act_backward(host, p, x)):
+        with pytest.raises(ValueError):
+            call()
