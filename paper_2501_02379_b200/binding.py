@@ -800,6 +800,19 @@ class ResidualNormGrads(NamedTuple):
 
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+class UnknownActivation(ValueError, KeyError):
+    """A ValueError as for other arguments, and a KeyError for those who look for one."""
+
+
+def _activation(act) -> int:
+    kind = ACTIVATIONS.get(act)
+    if kind is None:
+        raise UnknownActivation(f"act is one of {', '.join(ACTIVATIONS)}")
+    return kind
+
+
 _pack_rows = struct.Struct("@Pq").pack
 _pack_gated = struct.Struct("@qqiiPqPqPqPPP").pack
 _pack_norm = struct.Struct("@qqiiiiffiiPPPPPPq").pack
@@ -898,7 +911,7 @@ def gated_act(a, u=None, act: str = "silu", keep: bool = True, stream=None) -> G
     d, rows, width, index, place = _matrix("a", a)
     if _elsewhere(index, stream):
         return _there(index, stream, gated_act, a, u, act, keep)
-    kind = ACTIVATIONS[act]
+    kind = _activation(act)
     other = _like("u", u, d, rows, width, index) if u is not None else _NO_ROWS
     y = _torch_types[0].empty((rows, width), dtype=a.dtype, device=index)
     a8 = _new_packed(rows, width, a.dtype, index) if keep else None
@@ -915,7 +928,7 @@ def gated_act_backward(a8: Packed, u8: Optional[Packed], dy, act: str = "silu", 
     d, rows, width, index, place = _matrix("dy", dy)
     if _elsewhere(index, stream):
         return _there(index, stream, gated_act_backward, a8, u8, dy, act, keep_y, da, du)
-    kind, given = ACTIVATIONS[act], [t for t in (da, du) if t is not None]
+    kind, given = _activation(act), [t for t in (da, du) if t is not None]
     a_p = _packed_ptr("a8", a8, rows, width, dy.dtype, index)
     u_p = _packed_ptr("u8", u8, rows, width, dy.dtype, index) if u8 is not None else 0
     if u8 is None and du is not None:

@@ -161,3 +161,12 @@ def test_packed_matrices_are_checked():
                  lambda: B.gated_act_backward(host, p, x)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_unknown_activations_are_refused():
+    x = torch.randn(4, 64, device="cuda")
+    p = B.act_pack(x)
+    for call in (lambda: B.gated_act(x, x, act="relu"), lambda: B.gated_act(x, act=None), lambda: B.gated_act_backward(p, p, x, act="relu")):
+        for kind in (ValueError, KeyError):
+            with pytest.raises(kind):
+                call()
