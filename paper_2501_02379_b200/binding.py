@@ -875,12 +875,13 @@ def act_pack(x, out: Optional[Packed] = None, stream=None) -> Packed:
     d, rows, width, index, place = _matrix("x", x)
     if _elsewhere(index, stream):
         return _there(index, stream, act_pack, x, out)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _new_packed(rows, width, x.dtype, index)
-        to = out.data.data_ptr()
-    else:
-        to = _packed_ptr("out", out, rows, width, x.dtype, index)
+    to = _packed_ptr("out", out, rows, width, x.dtype, index) if given else out.data.data_ptr()
     _check(lib().tgrad_act_pack(_pack_rows(*place), rows, width, d, to, _raw_stream(index)), "tgrad_act_pack")
+    if given:
+        _written(out.data)
     return out
 
 

@@ -170,3 +170,11 @@ def test_unknown_activations_are_refused():
         for kind in (ValueError, KeyError):
             with pytest.raises(kind):
                 call()
+
+
+def test_packing_in_place_counts_as_a_change():
+    x = torch.randn(4, 64, device="cuda")
+    p = B.act_pack(x)
+    before = p.data._version
+    assert B.act_pack(2 * x, out=p) is p and p.data._version > before
+    assert torch.equal(B.act_unpack(p), 2 * B.act_unpack(B.act_pack(x)))
