@@ -964,6 +964,8 @@ def _norm_config(d, rows, width, index, weight, bias, post_weight, post_bias, ga
             pd = types.get(t.dtype)
         if types.get(t.dtype) != pd or (pd != R32 and pd != d) or t.get_device() != index or not t.is_cuda:
             raise ValueError("parameters are fp32 or of the activations' dtype, all alike, on their device")
+        if t.is_neg():
+            raise ValueError(f"{name} stands negated: resolve lazy negations")
         if name != "gate" and (t.shape != (width,) or (width > 1 and t.stride(0) != 1)):
             raise ValueError(f"{name} is a contiguous tensor [width]")
         pointers.append(t.data_ptr())
@@ -1030,7 +1032,7 @@ def residual_norm_backward(grad_h, x, stats, f=None, grad_x=None, weight=None, p
     if f is None and (gate is not None or post_weight is not None):
         raise ValueError("without f there is no gate and no post_weight")
     g_m = _like("grad_x", grad_x, d, rows, width, index) if grad_x is not None else _NO_ROWS
-    if stats.dtype is not f32 or stats.shape != (4 if layer else 2, rows) or stats.get_device() != index or not stats.is_contiguous():
+    if stats.dtype is not f32 or stats.shape != (4 if layer else 2, rows) or stats.get_device() != index or not stats.is_contiguous() or stats.is_neg():
         raise ValueError("stats is what the forward call of the same kind returned")
     config, pd, groups = _norm_config(d, rows, width, index, weight, None, post_weight, post_bias, gate, starts, scale, kind, post, 0.0)
     dx = torch.empty((rows, width), dtype=dtype, device=index)

@@ -178,3 +178,18 @@ def test_packing_in_place_counts_as_a_change():
     before = p.data._version
     assert B.act_pack(2 * x, out=p) is p and p.data._version > before
     assert torch.equal(B.act_unpack(p), 2 * B.act_unpack(B.act_pack(x)))
+
+
+def test_parameters_that_stand_negated_are_refused():
+    x, w = torch.randn(4, 64, device="cuda"), torch.rand(64, device="cuda")
+    minus = torch._neg_view(w)
+    r = B.residual_norm(x, x, weight=w, post_weight=w, gate=w)
+    for name in ("weight", "post_weight", "gate"):
+        how = {"weight": w, "post_weight": w, "gate": w, name: minus}
+        for call in (lambda: B.residual_norm(x, x, **how), lambda: B.residual_norm_backward(x, r.x, r.stats, x, **how)):
+            with pytest.raises(ValueError):
+                call()
+    with pytest.raises(ValueError):
+        B.residual_norm(x, x, weight=w, bias=minus, kind="layer")
+    with pytest.raises(ValueError):
+        B.residual_norm_backward(x, r.x, torch._neg_view(r.stats), x, weight=w)
