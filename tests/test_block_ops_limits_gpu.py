@@ -1,5 +1,5 @@
-"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, sequences and batches without rows, waits
-that run out, arguments of other kinds.
+"""The operators of a trained block at the ends of their ranges (run with -m gpu): sums over many tokens, rows as the fast kernels
+take them, sequences and batches without rows, waits that run out, arguments of other kinds.
 u = 2^-24 is half an fp32 ulp, bounds are those of test_block_ops_gpu."""
 import math
 
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2501_02379_b200 import binding as B
-from tests.test_block_ops_gpu import DT, U, gen, norm_case
+from tests.test_block_ops_gpu import DT, U, check_norm, gen, norm_case
 
 pytestmark = pytest.mark.gpu
 
@@ -25,6 +25,25 @@ def test_weight_grad_of_many_tokens_is_off_by_its_rounding(dt, digits):
     want = dy.double().T @ B.act_unpack(x8).double()
     half = torch.exp2(torch.floor(torch.log2(want)) - digits)
     assert bool(((got - want).abs() <= half + want * (256 * 2.0 ** -22 + rows / 4096 * U)).all())
+
+
+# ------------------------------------------------------------------------------------------------ norms of aligned rows
+@pytest.mark.parametrize("dt,pdt", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("gate", ["none", "one", "equal", "ragged", "many"])
+def test_residual_norm_of_aligned_rows(gate, layer, dt, pdt):
+    """Every row at a multiple of 16 bytes, whole vectors, several rows a team: the kernels that copy rows ahead, in both directions."""
+    shapes = [(603, 64), (3000, 40), (600, 512), (450, 1024), (303, 2008), (300, 4096), (300, 8192)]
+    for i in range(len(gate) % 3, len(shapes), 3):
+        x, f, dh, dx, how, starts = norm_case(*shapes[i], dt, pdt, layer, True, gate, 20 * i)
+        check_norm(x, f.contiguous(), dh, dx, how, starts, dt, pdt, layer, True, kept=(False, i % 2 == 0))
+
+
+@pytest.mark.parametrize("layer", [False, True])
+def test_norm_before_a_block_of_aligned_rows(layer):
+    for i, (rows, width, dt) in enumerate([(3000, 40, "bf16"), (450, 1024, "f32"), (300, 8192, "f16"), (300, 16384, "bf16")]):
+        x, _, dh, dx, how, _ = norm_case(rows, width, dt, "f32", layer, False, "none", 30 * i)
+        check_norm(x, None, dh, dx, how, None, dt, "f32", layer, False, scale=0.7, kept=(i % 2 == 0, False))
 
 
 # ------------------------------------------------------------------------------------------------ norms: nothing there
