@@ -14,22 +14,21 @@ ItemWalk walk_of(int64_t rows, int64_t width) {
   k.magic = (uint32_t)((((uint64_t)1 << (31 + l)) + k.per_row - 1) / k.per_row); k.shift = l - 1;
   return k;
 }
-// Entries per thread: several vectors in flight where there is enough work for that.
 template <typename... KA, typename... AA>
-tgrad_status launch_items(void (*kern)(KA...), int per_thread, const ItemWalk& k, cudaStream_t st, AA&&... args) {
+tgrad_status launch_items(void (*kern)(KA...), int per_thread, const ItemWalk& k, cudaStream_t st, AA&&... args) {      // per_thread: vectors
   const int64_t grid = (k.items + PK_THREADS * per_thread - 1) / (PK_THREADS * per_thread);
   if (grid >= ((int64_t)1 << 31)) return TGRAD_ERR_UNSUPPORTED;
   launch_chained(kern, dim3((unsigned)grid), dim3(PK_THREADS), 0, st, static_cast<AA&&>(args)..., k);
   TG_LAUNCH_CHECK();
   return TGRAD_OK;
 }
-inline bool many(const ItemWalk& k) { return k.items >= (int64_t)148 * 8 * PK_THREADS; }
+// Reading back: several vectors a thread in flight where every SM has its threads all the same.
+inline bool many(const ItemWalk& k) { return k.items >= (int64_t)sm_count() * 8 * PK_THREADS; }
 
 template <int KIND>
 tgrad_status pack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k, cudaStream_t st) {
-  // (one vector a thread: 16384 x 8192 bf16 88 us, 97 with two, 122 with four; threads to switch between count for more than loads of one thread)
-  if (x.al == 16 && k.width % 8 == 0) return launch_items(pack_kernel<KIND, true, 1>, 1, k, st, x, p);
-  return launch_items(pack_kernel<KIND, false, 1>, 1, k, st, x, p);
+  if (x.al == 16 && k.width % 8 == 0) return launch_items(pack_kernel<KIND, true>, 1, k, st, x, p);
+  return launch_items(pack_kernel<KIND, false>, 1, k, st, x, p);
 }
 template <int KIND>
 tgrad_status unpack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k, cudaStream_t st) {
@@ -40,8 +39,8 @@ tgrad_status unpack_kind(const RowsOf& x, const PackedRows& p, const ItemWalk& k
 // ---- gated activation ----
 template <int KIND, int ACT, bool GATED>
 tgrad_status gated_launch(const GatedArgs& g, const ItemWalk& k, bool aligned, bool backward, cudaStream_t st) {
-  if (!backward) return aligned ? launch_items(gated_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g) : launch_items(gated_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
-  return aligned ? launch_items(gated_backward_kernel<KIND, ACT, GATED, true, 1>, 1, k, st, g) : launch_items(gated_backward_kernel<KIND, ACT, GATED, false, 1>, 1, k, st, g);
+  if (!backward) return aligned ? launch_items(gated_kernel<KIND, ACT, GATED, true>, 1, k, st, g) : launch_items(gated_kernel<KIND, ACT, GATED, false>, 1, k, st, g);
+  return aligned ? launch_items(gated_backward_kernel<KIND, ACT, GATED, true>, 1, k, st, g) : launch_items(gated_backward_kernel<KIND, ACT, GATED, false>, 1, k, st, g);
 }
 template <int KIND, int ACT>
 tgrad_status gated_act(const GatedArgs& g, const ItemWalk& k, bool gated, bool aligned, bool backward, cudaStream_t st) {

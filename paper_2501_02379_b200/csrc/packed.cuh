@@ -207,26 +207,19 @@ __device__ __forceinline__ void store_packed(const PackedRows& t, int64_t row, i
   }
 }
 
-template <int KIND, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
+// (one vector a thread: 16384 x 8192 bf16 88 us, 97 with two, 122 with four; threads to switch between count for more than loads of one thread)
+template <int KIND, bool ALIGNED>
+__global__ void __launch_bounds__(PK_THREADS, KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) pack_kernel(const RowsOf x, const PackedRows out, const ItemWalk k) {
   griddep_chain();
-  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
-  float v[U][8];
-  int64_t row[U];
-  int at[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = first + j * PK_THREADS;
-    item_place(k, min(i, k.items - 1), row[j], at[j]);
-    load8<KIND, ALIGNED>(x, row[j], 8 * at[j], i < k.items ? item_count(k, at[j]) : 0, v[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = first + j * PK_THREADS;
-    uint32_t byte;
-    const uint2 w = pack8(v[j], byte);
-    if (i < k.items) store_packed(out, row[j], at[j], i, w, byte);
-  }
+  const int64_t i = (int64_t)blockIdx.x * PK_THREADS + threadIdx.x;
+  float v[8];
+  int64_t row;
+  int at;
+  item_place(k, min(i, k.items - 1), row, at);
+  load8<KIND, ALIGNED>(x, row, 8 * at, i < k.items ? item_count(k, at) : 0, v);
+  uint32_t byte;
+  const uint2 w = pack8(v, byte);
+  if (i < k.items) store_packed(out, row, at, i, w, byte);
 }
 
 template <int KIND, bool ALIGNED, int U>
@@ -286,97 +279,78 @@ struct GatedArgs {
   PackedRows pa, pu, py;     // kept inputs; py.codes null: not wanted
 };
 
-template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_kernel(const GatedArgs g, const ItemWalk k) {
+template <int KIND, int ACT, bool GATED, bool ALIGNED>
+__global__ void __launch_bounds__(PK_THREADS, KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
-  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
-  float a[U][8], u[U][8];
-  int64_t row[U];
-  int at[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = first + j * PK_THREADS;
-    item_place(k, min(i, k.items - 1), row[j], at[j]);
-    const int n = i < k.items ? item_count(k, at[j]) : 0;
-    load8<KIND, ALIGNED>(g.a, row[j], 8 * at[j], n, a[j]);
-    if (GATED) load8<KIND, ALIGNED>(g.u, row[j], 8 * at[j], n, u[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = first + j * PK_THREADS;
-    const int n = i < k.items ? item_count(k, at[j]) : 0;
+  const int64_t i = (int64_t)blockIdx.x * PK_THREADS + threadIdx.x;
+  float a[8], u[8];
+  int64_t row;
+  int at;
+  item_place(k, min(i, k.items - 1), row, at);
+  const int n = i < k.items ? item_count(k, at) : 0;
+  load8<KIND, ALIGNED>(g.a, row, 8 * at, n, a);
+  if (GATED) load8<KIND, ALIGNED>(g.u, row, 8 * at, n, u);
+  if (g.pa.codes) {
     uint32_t byte;
-    uint2 w;
-    if (g.pa.codes) {
-      w = pack8(a[j], byte);
-      if (i < k.items) store_packed(g.pa, row[j], at[j], i, w, byte);
-      if (GATED) {
-        w = pack8(u[j], byte);
-        if (i < k.items) store_packed(g.pu, row[j], at[j], i, w, byte);
-      }
+    uint2 w = pack8(a, byte);
+    if (i < k.items) store_packed(g.pa, row, at, i, w, byte);
+    if (GATED) {
+      w = pack8(u, byte);
+      if (i < k.items) store_packed(g.pu, row, at, i, w, byte);
     }
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float s;
-      y[e] = a[j][e] * act_gate<ACT>(a[j][e], s);
-      if (GATED) y[e] *= u[j][e];
-    }
-    if (ALIGNED) store8<KIND, true>(g.y, row[j], 8 * at[j], n, y);
-    else store8_any<KIND>(g.y, row[j], 8 * at[j], n, y, one_row(row[j]));
   }
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float s;
+    y[e] = a[e] * act_gate<ACT>(a[e], s);
+    if (GATED) y[e] *= u[e];
+  }
+  if (ALIGNED) store8<KIND, true>(g.y, row, 8 * at, n, y);
+  else store8_any<KIND>(g.y, row, 8 * at, n, y, one_row(row));
 }
 
-template <int KIND, int ACT, bool GATED, bool ALIGNED, int U>
-__global__ void __launch_bounds__(PK_THREADS, U == 1 && KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
+template <int KIND, int ACT, bool GATED, bool ALIGNED>
+__global__ void __launch_bounds__(PK_THREADS, KIND != LS_F32 ? (ALIGNED ? PK_BLOCKS : PK_BLOCKS_ODD) : 1) gated_backward_kernel(const GatedArgs g, const ItemWalk k) {
   griddep_chain();
-  const int64_t first = (int64_t)blockIdx.x * (PK_THREADS * U) + threadIdx.x;
-  float dy[U][8];
-  uint2 wa[U], wu[U];
-  uint32_t ba[U], bu[U];
-  int64_t row[U];
-  int at[U];
-#pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = min(first + j * PK_THREADS, k.items - 1);
-    item_place(k, i, row[j], at[j]);
-    wa[j] = ld_codes(g.pa.codes + i * 8);
-    ba[j] = g.pa.exps[row[j] * g.pa.exp_stride + (at[j] >> 2)];
-    if (GATED) {
-      wu[j] = ld_codes(g.pu.codes + i * 8);
-      bu[j] = g.pu.exps[row[j] * g.pu.exp_stride + (at[j] >> 2)];
-    }
-    load8<KIND, ALIGNED>(g.dy, row[j], 8 * at[j], item_count(k, at[j]), dy[j]);
+  const int64_t item = (int64_t)blockIdx.x * PK_THREADS + threadIdx.x, i = min(item, k.items - 1);
+  float dy[8], a[8], u[8], f[8];
+  int64_t row;
+  int at;
+  item_place(k, i, row, at);
+  const uint2 wa = ld_codes(g.pa.codes + i * 8);
+  const uint32_t ba = g.pa.exps[row * g.pa.exp_stride + (at >> 2)];
+  uint2 wu;
+  uint32_t bu;
+  if (GATED) {
+    wu = ld_codes(g.pu.codes + i * 8);
+    bu = g.pu.exps[row * g.pu.exp_stride + (at >> 2)];
   }
+  load8<KIND, ALIGNED>(g.dy, row, 8 * at, item_count(k, at), dy);
+  const int n = item < k.items ? item_count(k, at) : 0;
+  unpack8(wa, ba, a);
+  if (GATED) unpack8(wu, bu, u);
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int64_t i = first + j * PK_THREADS;
-    const int n = i < k.items ? item_count(k, at[j]) : 0;
-    float a[8], u[8], f[8];
-    unpack8(wa[j], ba[j], a);
-    if (GATED) unpack8(wu[j], bu[j], u);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float s;
-      const float p = act_gate<ACT>(a[e], s);
-      f[e] = a[e] * p;
-      a[e] = GATED ? dy[j][e] * u[e] * s : dy[j][e] * s;
-      if (GATED) { dy[j][e] *= f[e]; f[e] *= u[e]; }
-    }
-    if (ALIGNED) {
-      store8<KIND, true>(g.da, row[j], 8 * at[j], n, a);
-      if (GATED) store8<KIND, true>(g.du, row[j], 8 * at[j], n, dy[j]);
-    } else {
-      const bool same = one_row(row[j]);
-      store8_any<KIND>(g.da, row[j], 8 * at[j], n, a, same);
-      if (GATED) store8_any<KIND>(g.du, row[j], 8 * at[j], n, dy[j], same);
-    }
-    if (g.py.codes) {
-      round8<KIND>(f);
-      uint32_t byte;
-      const uint2 w = pack8(f, byte);
-      if (i < k.items) store_packed(g.py, row[j], at[j], i, w, byte);
-    }
+  for (int e = 0; e < 8; ++e) {
+    float s;
+    const float p = act_gate<ACT>(a[e], s);
+    f[e] = a[e] * p;
+    a[e] = GATED ? dy[e] * u[e] * s : dy[e] * s;
+    if (GATED) { dy[e] *= f[e]; f[e] *= u[e]; }
+  }
+  if (ALIGNED) {
+    store8<KIND, true>(g.da, row, 8 * at, n, a);
+    if (GATED) store8<KIND, true>(g.du, row, 8 * at, n, dy);
+  } else {
+    const bool same = one_row(row);
+    store8_any<KIND>(g.da, row, 8 * at, n, a, same);
+    if (GATED) store8_any<KIND>(g.du, row, 8 * at, n, dy, same);
+  }
+  if (g.py.codes) {
+    round8<KIND>(f);
+    uint32_t byte;
+    const uint2 w = pack8(f, byte);
+    if (item < k.items) store_packed(g.py, row, at, item, w, byte);
   }
 }
 
