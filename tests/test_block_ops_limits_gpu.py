@@ -170,6 +170,24 @@ def test_waits_that_run_out_leave_nothing_finite(layer):
     assert all(torch.equal(t, right) for (_, _, t), (_, _, right) in zip(calls(), want))
 
 
+def test_waits_that_run_out_within_long_sums():
+    """A weight gradient whose sums leave the tensor core several times: tiles are NaN or right."""
+    dy, x = (torch.randn(8192, n, generator=gen(n), device="cuda").bfloat16() for n in (2048, 2560))
+    x8 = B.act_pack(x)
+    want = B.weight_grad(dy, x8)
+    for limit in (0, 70, 135):                                # of 139 steps of a block on 148 SMs: a tile of 128, which leaves twice, and a part of another
+        B.set_copy_limit(limit)
+        try:
+            got = B.weight_grad(dy, x8)
+            torch.cuda.synchronize()
+        finally:
+            B.set_copy_limit(-1)
+        tiles = torch.isnan(got).view(8, 256, 10, 256).transpose(1, 2).flatten(2)
+        assert bool((tiles.all(2) | ~tiles.any(2)).all()) and bool(tiles.any()) and (limit > 128 or bool(tiles.all()))
+        assert bool((torch.isnan(got) | (got == want)).all())
+    assert torch.equal(B.weight_grad(dy, x8), want)
+
+
 # ------------------------------------------------------------------------------------------------ arguments
 def test_packed_matrices_are_checked():
     x = torch.randn(4, 64, device="cuda")
