@@ -495,7 +495,8 @@ tgrad_status tgrad_gated_act_backward(const tgrad_gated_args* args, void* cuda_s
  *   x' = scale x + gate * n_post(f),   h = n_pre(x').
  * Without a block (f.d_data NULL) x' = scale x; with post = 0 the block's output is taken as it is.
  * The gate (groups >= 1) has a row for each group of rows: groups of equal size, or with d_starts the rows [starts[g], starts[g + 1]) of group g,
- * groups + 1 device numbers that do not decrease.  A row of no group has gate 0, whatever stands in f.  groups = rows: a gate for each row.
+ * groups + 1 device numbers that do not decrease.  A row of no group has gate 0, whatever stands in f, and a group
+ * without rows has no part in any gradient, whatever stands in its gate.  groups = rows: a gate for each row.
  * Parameters are fp32 or of the activations' type, NULL: ones and zeros.  Sums of squares are fp32: entries above 1e18 overflow them.
  * 1 <= width <= 16384 and rows < 2^31 (TGRAD_ERR_UNSUPPORTED otherwise). */
 typedef struct {

@@ -13,8 +13,8 @@
 // its own in shared memory (cp.async), some rows ahead, so the copies need no barrier and no registers, and the memory is busy
 // while a row waits in its reductions.  Column sums stay in registers over all rows of a thread's chunk and are added up in a fixed
 // order by a second launch.
-// Measured at 16384 x 8192 bf16: forward 176 us (164 at the copy rate; 227 with f kept in 8 bits), backward 265 us (246) from f in storage,
-// 277 us (226) from f in 8 bits.
+// Measured at 16384 x 8192 bf16 at burst clocks: forward 176 us (164 at the copy rate; 204 with f kept in 8 bits, 185), backward 265 us (246) from f in
+// storage, 272 us (226) from f in 8 bits.
 #pragma once
 #include "packed.cuh"
 

@@ -13,7 +13,7 @@
 //
 // A thread takes 8 entries (16 bytes of 16-bit storage, 8 bytes of codes), four neighbours a block.  Reading back is bound by memory
 // (16384 x 8192 bf16: 62 us, 62 at the copy rate); packing by issue slots, 73 % busy, beside memory (84 us for 62), and so is the gated
-// activation (16384 x 14336 bf16 silu: forward 394 us for 290, backward 324 us for 290).
+// activation (16384 x 14336 bf16 silu at burst clocks: forward 394 us for 290, backward 330 us for 290; 781 us for both at sustained ones).
 #pragma once
 #include "lists.cuh"
 
