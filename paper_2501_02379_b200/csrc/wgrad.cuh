@@ -15,7 +15,7 @@
 //     other half of tensor memory (1.7e-5 at most).  A 16-bit sum of 64 steps or fewer stays, and tensor memory holds a second tile meanwhile.
 // Bound by the warps that turn codes into numbers: a group takes about 1,000 clocks for a step, 500 a step for the two, and the tensor
 // cores of two SMs 512 for 64 x 256 x 256; measured 450 ns a step for 270 of tensor cores (8192 x 2048 x 4608 bf16: 116 us, 1,335 TFLOP/s,
-// tensor pipe 73 % busy, the pipe of integer and logic instructions 65 %; to fp32 148 us; 16384 x 4096 x 14336: 1.75 ms at sustained clocks).  Two blocks and
+// tensor pipe 73 % busy, the pipe of integer and logic instructions 65 %; to fp32 148 us; 16384 x 4096 x 14336: 1.72 ms at sustained clocks).  Two blocks and
 // not one: each turns half of the columns into numbers, and a tile of 128 x 128 on one SM would have to read its operands from shared
 // memory as fast as that allows (16384 x 4096 x 14336 that way: 3.57 ms).
 // fp32 dy is split beforehand into three bfloat16 parts that add up to it exactly, which are three times as many steps into the same sums;
